@@ -190,9 +190,10 @@ def prepare(case, seed):
         free = torch.cat([spare, live[-1], more])
         t["tables"] = live[:-1].contiguous()
         t["num_blocks"] = held + more.numel()
-        t["ring"] = torch.full((t["num_blocks"],), -1, dtype=torch.int32, device="cuda")
+        # (twice the pool's blocks: room for what a turn longer than the window takes and gives at once)
+        t["ring"] = torch.full((2 * t["num_blocks"],), -1, dtype=torch.int32, device="cuda")
         start = (1 << 33) + int(seed) % 1000              # a ring in use for long
-        at = (torch.arange(free.numel(), device="cuda") + start) % t["num_blocks"]
+        at = (torch.arange(free.numel(), device="cuda") + start) % t["ring"].numel()
         t["ring"][at] = free
         t["counts"] = torch.tensor([start, start + free.numel()], dtype=torch.int64, device="cuda")
         t["lens"], t["new"] = int32(ctx), int32(n)
