@@ -76,6 +76,8 @@ typedef enum {
                                        decode context, a context past its block table, a
                                        turn longer than max_new_len); see each call */
 #define LS_DEVERR_INTERNAL 0x4u     /* an internal bounded wait expired (a library bug) */
+#define LS_DEVERR_FREE_LIST 0x8u    /* kv_tables_update: too few free blocks, no room to give
+                                       blocks back, or counters that cannot be */
 
 typedef struct ls_kv_pool ls_kv_pool;
 
@@ -255,6 +257,145 @@ ls_status paged_attn_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
                              const int32_t *block_tables, int32_t max_blocks_per_session,
                              float scale, void *out, void *workspace, size_t workspace_bytes,
                              hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Sliding-window attention over the same cache, and the bookkeeping that goes
+ * with it on the GPU.  A multi-turn speech session's history grows without end
+ * (§2.1, §5); a windowed layer reads only its last `window` tokens and its first
+ * `sinks` ones, and blocks behind the window can be used again.  All entry
+ * points of this section refuse (LS_EINVAL) a call made while another device
+ * than the pool's is current, q, out, k_new, v_new or a workspace that is not
+ * 16-byte aligned, and index arrays that are not aligned to their type.
+ * ---------------------------------------------------------------------- */
+
+/* Largest window and most first tokens. */
+#define LS_MAX_WINDOW_TOKENS (1 << 29)
+
+/*
+ * paged_attn_decode_window — paged_attn_decode in which the query, at position p
+ * (context_lens[s] with append, else context_lens[s] - 1), sees key t when t <= p
+ * and either t < sinks or t > p - window.
+ *
+ *   window   1 .. LS_MAX_WINDOW_TOKENS: keys seen up to and including position p
+ *   sinks    0 .. LS_MAX_WINDOW_TOKENS: first tokens that stay visible
+ *   workspace  device, >= ls_decode_window_workspace_bytes(...) bytes, 16-byte aligned
+ *
+ * Only table entries of blocks with a seen key (and of the appended token) are
+ * read: others may hold anything, such as ids given back by kv_tables_update.
+ * K and V values of keys that are not seen do not reach the output, NaN and
+ * infinities included.  Other arguments as paged_attn_decode; a host-planned
+ * schedule counts the keys that are seen.  At most 2048 sessions, and 16384
+ * blocks with seen keys per session (LS_EUNSUPPORTED); the table itself may be
+ * wider.  Errors as paged_attn_decode, and LS_EINVAL for a window or sinks out of
+ * range and a table of more than 2^27 - 1 blocks.
+ */
+size_t ls_decode_window_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                        int32_t max_blocks_per_session, int32_t window, int32_t sinks);
+ls_status paged_attn_decode_window(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                   const void *q, const void *k_new, const void *v_new,
+                                   const int32_t *block_tables, int32_t max_blocks_per_session,
+                                   const int32_t *context_lens, const int32_t *context_lens_host,
+                                   int32_t window, int32_t sinks, float scale, void *out, void *workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * paged_attn_prefill_window — paged_attn_prefill with the same mask: new row j of
+ * session s, at position p = reused_lens[s] + j, sees key t when t <= p and
+ * either t < sinks or t > p - window.  The turn's own K/V may be appended by the
+ * call (k_new, v_new) or be in the pool already (NULL, after kv_append).
+ *
+ * Only table entries of blocks that some row of the turn sees (and, with k_new,
+ * of the turn's own tokens) are read.  K and V values of keys that no row of a
+ * query tile (256 / (num_q_heads / num_kv_heads) consecutive new tokens) sees do
+ * not reach its rows; a NaN or infinite V that one row of a tile sees may make
+ * its other rows NaN, as in paged_attn_prefill.  Other arguments, the workspace and errors
+ * as paged_attn_prefill; window, sinks and tables as paged_attn_decode_window.
+ */
+ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                    const void *q, const void *k_new, const void *v_new,
+                                    const int32_t *cu_new_lens, const int32_t *reused_lens,
+                                    const int32_t *lens_host, int32_t total_new_tokens, int32_t max_new_len,
+                                    const int32_t *block_tables, int32_t max_blocks_per_session,
+                                    int32_t window, int32_t sinks, float scale, void *out, void *workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * kv_tables_update — a step's block tables, slot map and lengths, built on the GPU
+ * from the sessions' lengths (block-level allocation, §5.1; the paged block pool
+ * of §6), so that a step needs nothing from the host and can be captured in a
+ * graph.  Session s has seq_lens[s] tokens in the pool and brings new_lens[s].
+ *
+ *   seq_lens, new_lens   device int32 [num_sessions], >= 0
+ *   block_tables  device int32 [num_sessions][max_blocks_per_session]; entries of
+ *                 the blocks that the new tokens open are written, from
+ *                 ceil(seq_lens[s] / 16) on
+ *   free_ring     device int32 [ring_size]: ids of free blocks.  With free_counts =
+ *                 (taken, given), entries taken .. given - 1, modulo ring_size, are
+ *                 free.  Sessions take the blocks they need in session order.  Blocks
+ *                 go back to entries given, given + 1, .., which must not be among the
+ *                 free ones on entry: a ring as large as the pool has that room unless
+ *                 a turn is longer than the window, one of twice that always.  NULL
+ *                 (and ring_size 0, free_counts and next_counts NULL, window 0): the
+ *                 tables already hold every block (for instance the KV manager's)
+ *   free_counts, next_counts   device int64 [2]: counters before and after
+ *   window, sinks  with a window >= 1, blocks that become invisible to every later
+ *                 step (of queries at positions >= seq_lens[s] + new_lens[s], in layers
+ *                 with at most this window and at most these first tokens) and were
+ *                 visible to this step's first query go back to the ring, in
+ *                 session order.  Their table entries stay, since this step's
+ *                 attention still reads them: enqueue it before the next
+ *                 kv_tables_update on the same ring.  Blocks behind the window of
+ *                 seq_lens[s] count as given back before.  0: none are given back
+ *   total_new_tokens   host int: slots in slot_map, >= the sum of new_lens
+ *   max_new_len        host int: no new_lens[s] is larger
+ *   next_lens     device int32 [num_sessions]: seq_lens[s] + new_lens[s]
+ *   cu_new_lens   device int32 [num_sessions + 1]: prefix sums of new_lens
+ *   reused_lens   device int32 [num_sessions] or NULL: seq_lens[s], the lengths this
+ *                 step's attention takes (kept where next_lens is seq_lens itself)
+ *   slot_map      device int64 [total_new_tokens]: block * 16 + offset of each new
+ *                 token, sessions back to back; -1 behind the last
+ *
+ * Inputs and outputs are apart, so a call can be made again with the same
+ * result; next_lens may be seq_lens and next_counts free_counts, for a loop that
+ * advances itself.  All sessions are served or none: a length out of range, one
+ * that does not fit its table, or more rows than total_new_tokens is flagged
+ * LS_DEVERR_LENGTH, and too few free blocks or no room in the ring
+ * LS_DEVERR_FREE_LIST; then tables, ring and counters stay as they are (next_counts =
+ * free_counts, next_lens = seq_lens), cu_new_lens is all 0 and slot_map all -1.  An id
+ * outside the pool is copied as it stands and flagged (LS_DEVERR_BLOCK_ID), its
+ * tokens' slots are -1.  The pool gives the range of ids; its memory is not touched.
+ * Errors: LS_EINVAL (NULL or misaligned pointers, negative sizes, free_ring without
+ * counters or the other way round, a window without free_ring, a window or sinks out
+ * of range, more than 2^27 - 1 blocks per session), LS_EHIP.
+ */
+ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t *seq_lens,
+                           const int32_t *new_lens, int32_t *block_tables, int32_t max_blocks_per_session,
+                           int32_t *free_ring, int32_t ring_size, const int64_t *free_counts,
+                           int64_t *next_counts, int32_t window, int32_t sinks, int32_t total_new_tokens,
+                           int32_t max_new_len, int32_t *next_lens, int32_t *cu_new_lens,
+                           int32_t *reused_lens, int64_t *slot_map, hipStream_t stream);
+
+/*
+ * kv_append — write K/V rows into the pool slots that a slot map names.
+ *
+ *   k_new, v_new   device bf16: row i of total_tokens starts at k_new + i * k_stride
+ *                  (v_stride) elements and holds [num_kv_heads][head_dim]; strides are
+ *                  multiples of 8 and at least num_kv_heads * head_dim (a view of a
+ *                  fused projection needs no copy)
+ *   slot_map       device int64 [total_tokens]: block * 16 + offset; rows with a negative
+ *                  slot are left out; one past the pool is skipped and flagged
+ *                  (LS_DEVERR_BLOCK_ID).  Slots are distinct; one that appears twice
+ *                  holds, value by value, either row
+ *   slot_map_host  optional host copy of slot_map; when given, range and distinctness
+ *                  are checked on the host (LS_EINVAL)
+ *
+ * Other slots of the blocks are left as they are, so calls on different streams
+ * may write different slots of one block.  Errors: LS_EINVAL, LS_ENOMEM (host
+ * memory for that check), LS_EHIP.
+ */
+ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const void *k_new, const void *v_new,
+                    int64_t k_stride, int64_t v_stride, const int64_t *slot_map, const int64_t *slot_map_host,
+                    hipStream_t stream);
 
 /*
  * Arguments shared by the three block-copy calls below.

@@ -11,6 +11,8 @@ Entry points (numpy in, numpy out; bf16 arrays are ``uint16`` bit patterns):
 * :func:`append`  — write new tokens' K/V rows into their pool slots.
 * :func:`stash` / :func:`restore` — block-granular byte copies between the pool
   and a contiguous staging array (the offload / reload of §5 and §5.2).
+* :func:`attend_window`, :func:`append_slots`, :func:`tables_step` — attention rows with a sliding
+  window and first tokens, rows written by a slot map, and a step's block tables and slots.
 * :func:`decode` / :func:`prefill` — the two attention calls of the hot path,
   composed as "append into a private copy of the pool, then attend".
 """
@@ -48,10 +50,12 @@ def _load():
         p, i32, i64, dbl = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_double
         lib.oracle_attend.argtypes = [p, i32, i64, i32, i32, i32, i32, i32, p, i32, i32, p, p, p, p,
                                       dbl, p]
+        lib.oracle_attend_window.argtypes = [p, i32, i64, i32, i32, i32, i32, i32, p, i32, i32, p, p,
+                                             p, p, dbl, i32, i32, p, p, p]
         lib.oracle_append.argtypes = [p, i32, i64, i32, i32, i32, i32, p, i32, i32, p, p, p, p]
         lib.oracle_stash.argtypes = [p, i32, i64, i32, i32, i32, i32, p, p]
         lib.oracle_restore.argtypes = [p, i32, i64, i32, i32, i32, i32, p, p]
-        for f in (lib.oracle_attend, lib.oracle_append, lib.oracle_stash, lib.oracle_restore):
+        for f in (lib.oracle_attend, lib.oracle_attend_window, lib.oracle_append, lib.oracle_stash, lib.oracle_restore):
             f.restype = ctypes.c_int
         _lib = lib
     return _lib
@@ -91,6 +95,30 @@ def attend(pool, block_size, head_dim, layer, q, block_tables, row_session, row_
     if rc != 0:
         raise ValueError("oracle_attend: empty row or block id outside the pool")
     return out
+
+
+def attend_window(pool, block_size, head_dim, layer, q, block_tables, row_session, row_pos,
+                  row_q_index, scale, window, sinks):
+    """Row r, at position row_pos[r], over the keys t <= row_pos[r] with t < sinks or
+    t > row_pos[r] - window.  Returns fp64 (out, mass [rows][Hq][D], score [rows][Hq]): the
+    result, the softmax-weighted mean of |v|, and the largest scale * sum |q_d k_d|."""
+    nl, nb, hkv, tile = _geometry(pool)
+    assert tile == block_size * head_dim
+    q = np.ascontiguousarray(q, dtype=np.uint16)
+    hq = q.shape[1]
+    bt = np.ascontiguousarray(block_tables, dtype=np.int32)
+    rs = np.ascontiguousarray(row_session, dtype=np.int32)
+    rp = np.ascontiguousarray(row_pos, dtype=np.int32)
+    rq = np.ascontiguousarray(row_q_index, dtype=np.int64)
+    out = np.zeros((len(rs), hq, head_dim), dtype=np.float64)
+    mass, score = np.zeros_like(out), np.zeros((len(rs), hq), dtype=np.float64)
+    rc = _load().oracle_attend_window(_ptr(pool), nl, nb, hkv, head_dim, block_size, layer, hq, _ptr(bt),
+                                      bt.shape[1], len(rs), _ptr(rs), _ptr(rp), _ptr(rq), _ptr(q),
+                                      float(scale), int(window), int(sinks), _ptr(out), _ptr(mass),
+                                      _ptr(score))
+    if rc != 0:
+        raise ValueError("oracle_attend_window: position outside the table or block id outside the pool")
+    return out, mass, score
 
 
 def append(pool, block_size, head_dim, layer, block_tables, tok_session, tok_pos, k_new, v_new):
@@ -174,6 +202,50 @@ def prefill(pool, block_size, head_dim, layer, q, k_new, v_new, cu_new_lens, reu
     out = attend(work, block_size, head_dim, layer, q, block_tables, tok_session[sel],
                  tok_pos[sel] + 1, sel, scale)
     return (out, work) if pool_out else out
+
+
+def append_slots(pool, block_size, head_dim, layer, k_new, v_new, slots):
+    """Write row i of k_new/v_new [T][Hkv][D] into slot slots[i] = block * block_size + offset, in
+    place; rows with a negative slot are left out."""
+    slots = np.asarray(slots, dtype=np.int64)
+    keep = slots >= 0
+    blocks = np.arange(pool.shape[1], dtype=np.int32)[None]        # one session that holds the whole pool
+    return append(pool, block_size, head_dim, layer, blocks, np.zeros(int(keep.sum()), dtype=np.int32),
+                  slots[keep].astype(np.int32), k_new[keep], v_new[keep])
+
+
+def tables_step(seq_lens, new_lens, tables, ring=None, counts=None, window=0, sinks=0, total=None,
+                block_size=16):
+    """A step's tables, ring, counters, slots, prefix sums and next lengths, session by session and
+    token by token: token p of a session opens a block when p is a multiple of block_size, and takes
+    the ring's next id; a block is given back when the step's first query could see a key of it (or
+    of a later one), no first token lies in it, and the next step's first query sees none of it.
+    Returns a dict of new arrays (lists that fit the call's outputs)."""
+    tables = np.array(tables, dtype=np.int32)
+    ring = None if ring is None else np.array(ring, dtype=np.int32)
+    taken, given = (0, 0) if counts is None else (int(counts[0]), int(counts[1]))
+    total = int(np.sum(new_lens)) if total is None else total
+    slots = np.full(total, -1, dtype=np.int64)
+    cu, gone = [0], []
+    for s, (have, new) in enumerate(zip(map(int, seq_lens), map(int, new_lens))):
+        for p in range(have, have + new):
+            if p % block_size == 0 and ring is not None:
+                tables[s, p // block_size] = ring[taken % len(ring)]
+                taken += 1
+            slots[cu[-1] + p - have] = int(tables[s, p // block_size]) * block_size + p % block_size
+        cu.append(cu[-1] + new)
+        for b in range(tables.shape[1] if window and ring is not None else 0):
+            end = (b + 1) * block_size                             # position behind its last token
+            visible_before = end > have - window + 1
+            visible_after = end > have + new - window + 1
+            if b * block_size >= sinks and visible_before and not visible_after:
+                gone.append(tables[s, b])
+    for b in gone:
+        ring[given % len(ring)] = b
+        given += 1
+    return {"tables": tables, "ring": ring, "counts": np.array([taken, given], dtype=np.int64),
+            "slots": slots, "cu": np.array(cu, dtype=np.int32),
+            "next": (np.asarray(seq_lens) + np.asarray(new_lens)).astype(np.int32)}
 
 
 def timed(fn, *args, **kwargs):

@@ -18,6 +18,8 @@
  *            does not restate attention itself; the operation is the textbook
  *            scaled dot-product softmax attention, with grouped query heads
  *            (query head h reads KV head h / (Hq/Hkv)).
+ *   window   the same attention over a sliding window of keys and a few first
+ *            tokens, which is what a windowed layer of a long session computes.
  *   append   write new tokens' K and V rows into their pool slots: the slot of
  *            logical token t of session s is (block_table[s][t / B], t % B).
  *   stash    gather whole blocks (every layer, K and V) into a contiguous
@@ -126,6 +128,84 @@ int oracle_attend(const uint16_t *pool, int num_layers, int64_t num_blocks, int 
                                                     layer, b, g, t % block_size, d)]);
         }
         for (int d = 0; d < head_dim; ++d) o[d] /= wsum;
+        free(x);
+    }
+    return bad ? -1 : 0;
+}
+
+/*
+ * Windowed attention rows: row r, at position row_pos[r] of session
+ * row_session[r], sees key t when t <= row_pos[r] and either t < sinks or
+ * t > row_pos[r] - window.  Keys that are not seen are not looked at, nor are
+ * their block ids.  Beside the result, what its error bounds are made of:
+ * mass[r][h][:] = sum_t w_t |v_t| (w: the softmax weights) and
+ * score[r][h] = scale * max_t sum_d |q_d k_td|.
+ */
+int oracle_attend_window(const uint16_t *pool, int num_layers, int64_t num_blocks, int num_kv_heads,
+                         int head_dim, int block_size, int layer, int num_q_heads,
+                         const int32_t *block_tables, int max_blocks_per_session,
+                         int num_rows, const int32_t *row_session, const int32_t *row_pos,
+                         const int64_t *row_q_index, const uint16_t *q, double scale, int window,
+                         int sinks, double *out, double *mass, double *score)
+{
+    if (layer < 0 || layer >= num_layers) return -1;
+    int group = num_q_heads / num_kv_heads;
+    int bad = 0;
+#pragma omp parallel for schedule(dynamic, 1) reduction(| : bad)
+    for (int64_t job = 0; job < (int64_t)num_rows * num_q_heads; ++job) {
+        int r = (int)(job / num_q_heads);
+        int h = (int)(job % num_q_heads);
+        int s = row_session[r];
+        int p = row_pos[r];
+        int g = h / group;
+        const uint16_t *qrow = q + (row_q_index[r] * num_q_heads + h) * head_dim;
+        double *o = out + ((int64_t)r * num_q_heads + h) * head_dim;
+        double *a = mass + ((int64_t)r * num_q_heads + h) * head_dim;
+        for (int d = 0; d < head_dim; ++d) o[d] = a[d] = 0.0;
+        score[(int64_t)r * num_q_heads + h] = 0.0;
+        if (p < 0 || p / block_size >= max_blocks_per_session) {
+            bad = 1;
+            continue;
+        }
+        double *x = (double *)malloc(sizeof(double) * ((size_t)p + 1));
+        if (!x) { bad = 1; continue; }
+        double mu = -INFINITY, most = 0.0;
+        int wrong = 0;
+        for (int t = 0; t <= p && !wrong; ++t) {
+            if (t >= sinks && (int64_t)t <= (int64_t)p - window) continue;
+            int64_t b = block_tables[(int64_t)s * max_blocks_per_session + t / block_size];
+            if (b < 0 || b >= num_blocks) { wrong = 1; break; }
+            double dot = 0.0, size = 0.0;
+            for (int d = 0; d < head_dim; ++d) {
+                double y = widen_bf16(qrow[d]) *
+                           widen_bf16(pool[k_index(num_blocks, num_kv_heads, head_dim, block_size,
+                                                   layer, b, g, t % block_size, d)]);
+                dot += y;
+                size += fabs(y);
+            }
+            x[t] = scale * dot;
+            if (x[t] > mu) mu = x[t];
+            if (scale * size > most) most = scale * size;
+        }
+        if (wrong) { bad = 1; free(x); continue; }
+        double wsum = 0.0;
+        for (int t = 0; t <= p; ++t) {
+            if (t >= sinks && (int64_t)t <= (int64_t)p - window) continue;
+            int64_t b = block_tables[(int64_t)s * max_blocks_per_session + t / block_size];
+            double w = exp(x[t] - mu);
+            wsum += w;
+            for (int d = 0; d < head_dim; ++d) {
+                double v = widen_bf16(pool[v_index(num_blocks, num_kv_heads, head_dim, block_size,
+                                                   layer, b, g, t % block_size, d)]);
+                o[d] += w * v;
+                a[d] += w * fabs(v);
+            }
+        }
+        for (int d = 0; d < head_dim; ++d) {
+            o[d] /= wsum;
+            a[d] /= wsum;
+        }
+        score[(int64_t)r * num_q_heads + h] = most;
         free(x);
     }
     return bad ? -1 : 0;

@@ -5,6 +5,8 @@
 #include <cstdio>
 #include <algorithm>
 #include <cstring>
+#include <initializer_list>
+#include <memory>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -143,6 +145,23 @@ ls_status check_ids_host(const PoolGeom &p, int32_t n, const int32_t *ids) {
     return LS_OK;
 }
 
+// Host check of a slot map: range and distinctness (negative slots are left out).
+ls_status check_slots_host(const PoolGeom &p, int32_t n, const int64_t *slots) {
+    std::unique_ptr<int64_t[]> seen(new (std::nothrow) int64_t[(size_t)n]);
+    if (!seen) return fail(LS_ENOMEM, "out of host memory");
+    int64_t m = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (slots[i] < 0) continue;
+        if (slots[i] / kBlock >= p.num_blocks)
+            return fail(LS_EINVAL, "slot %lld of row %d is past the pool", (long long)slots[i], i);
+        seen[m++] = slots[i];
+    }
+    std::sort(seen.get(), seen.get() + m);
+    const int64_t *twice = std::adjacent_find(seen.get(), seen.get() + m);
+    if (twice != seen.get() + m) return fail(LS_EINVAL, "slot %lld appears twice", (long long)*twice);
+    return LS_OK;
+}
+
 // Copy the slabs of layers [lb, lb + lc) of n blocks between the pool and a
 // block-major all-layer staging array (device, or pinned host through the
 // caller's ring).
@@ -246,6 +265,143 @@ ls_status check_prefill_lens_host(int32_t S, const int32_t *lens, int32_t total,
     return LS_OK;
 }
 
+bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// The current device is the pool's (its error word and stream are what a call uses).
+ls_status check_device(const PoolGeom &p) {
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) {
+        (void)hipGetLastError();
+        dev = -1;
+    }
+    if (dev != p.device) return fail(LS_EINVAL, "the current device (%d) is not the pool's (%d)", dev, p.device);
+    return LS_OK;
+}
+
+ls_status check_window(int32_t window, int32_t sinks, int32_t max_blocks) {
+    if (window < 1 || window > kMaxWindowTokens)
+        return fail(LS_EINVAL, "window (%d) must be in [1, %d]", window, kMaxWindowTokens);
+    if (sinks < 0 || sinks > kMaxWindowTokens)
+        return fail(LS_EINVAL, "sinks (%d) must be in [0, %d]", sinks, kMaxWindowTokens);
+    if (max_blocks > INT32_MAX / kBlock)
+        return fail(LS_EINVAL, "max_blocks_per_session (%d) must be at most %d", max_blocks, INT32_MAX / kBlock);
+    return LS_OK;
+}
+
+// paged_attn_decode, or with windowed paged_attn_decode_window.
+ls_status decode_call(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads, const void *q,
+                      const void *k_new, const void *v_new, const int32_t *block_tables,
+                      int32_t max_blocks_per_session, const int32_t *context_lens, const int32_t *context_lens_host,
+                      bool windowed, int32_t window, int32_t sinks, float scale, void *out, void *workspace,
+                      size_t workspace_bytes, hipStream_t stream) {
+    if (ls_status st = check_pool(pool)) return st;
+    const PoolGeom &p = pool->geom;
+    if (layer < 0 || layer >= p.num_layers)
+        return fail(LS_EINVAL, "layer %d outside [0, %d)", layer, p.num_layers);
+    if (num_sessions < 0) return fail(LS_EINVAL, "num_sessions must be >= 0");
+    if (ls_status st = check_heads(p, num_q_heads)) return st;
+    if (windowed)
+        if (ls_status st = check_window(window, sinks, max_blocks_per_session)) return st;
+    if (num_sessions == 0) return LS_OK;
+    if (!q || !block_tables || !context_lens || !out || !workspace)
+        return fail(LS_EINVAL, "q, block_tables, context_lens, out and workspace must not be NULL");
+    if ((k_new == nullptr) != (v_new == nullptr))
+        return fail(LS_EINVAL, "k_new and v_new must both be given or both be NULL");
+    if (max_blocks_per_session <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
+    if (!(scale > 0.f) || scale != scale) return fail(LS_EINVAL, "scale must be a positive number");
+    if (windowed) {
+        if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(workspace, 16))
+            return fail(LS_EINVAL, "q, out, k_new, v_new and workspace must be 16-byte aligned");
+        if (!aligned(block_tables, 4) || !aligned(context_lens, 4))
+            return fail(LS_EINVAL, "block_tables and context_lens must be 4-byte aligned");
+        if (ls_status st = check_device(p)) return st;
+    } else {
+        window = sinks = 0;
+    }
+    if (context_lens_host)
+        if (ls_status st = check_decode_lens_host(num_sessions, context_lens_host, k_new ? 1 : 0,
+                                                  max_blocks_per_session))
+            return st;
+    const DecodePlan plan = plan_decode(p, num_sessions, num_q_heads,
+                                        windowed ? window_blocks(max_blocks_per_session, window, sinks) : max_blocks_per_session);
+    if (!plan.supported)
+        return fail(LS_EUNSUPPORTED, "batch of %d sessions with %d blocks each exceeds the decode "
+                    "limits (2048 sessions, 16384 blocks per session)", num_sessions, max_blocks_per_session);
+    if (workspace_bytes < plan.total())
+        return fail(LS_ENOMEM, "workspace_bytes (%zu) < required (%zu)", workspace_bytes, plan.total());
+    unsigned int *err = device_error_word();
+    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
+    // The step's own K/V row is written by the decode kernel (no separate append launch).
+    hipError_t e = launch_decode(p, layer, num_sessions, num_q_heads, static_cast<const uint16_t *>(q),
+                                 static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new),
+                                 block_tables, max_blocks_per_session, context_lens, context_lens_host,
+                                 scale, static_cast<uint16_t *>(out), workspace, workspace_bytes, plan, window, sinks,
+                                 err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "decode launch");
+}
+
+// paged_attn_prefill, or with windowed paged_attn_prefill_window.
+ls_status prefill_call(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads, const void *q,
+                       const void *k_new, const void *v_new, const int32_t *cu_new_lens, const int32_t *reused_lens,
+                       const int32_t *lens_host, int32_t total_new_tokens, int32_t max_new_len,
+                       const int32_t *block_tables, int32_t max_blocks_per_session, bool windowed, int32_t window,
+                       int32_t sinks, float scale, void *out, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream) {
+    if (ls_status st = check_pool(pool)) return st;
+    const PoolGeom &p = pool->geom;
+    if (layer < 0 || layer >= p.num_layers)
+        return fail(LS_EINVAL, "layer %d outside [0, %d)", layer, p.num_layers);
+    if (num_sessions < 0 || total_new_tokens < 0 || max_new_len < 0)
+        return fail(LS_EINVAL, "num_sessions, total_new_tokens and max_new_len must be >= 0");
+    if (ls_status st = check_heads(p, num_q_heads)) return st;
+    if (windowed)
+        if (ls_status st = check_window(window, sinks, max_blocks_per_session)) return st;
+    if (num_sessions == 0 || total_new_tokens == 0) return LS_OK;
+    if (!q || !cu_new_lens || !reused_lens || !block_tables || !out)
+        return fail(LS_EINVAL, "q, cu_new_lens, reused_lens, block_tables and out must not be NULL");
+    if ((k_new == nullptr) != (v_new == nullptr))
+        return fail(LS_EINVAL, "k_new and v_new must both be given or both be NULL");
+    if (max_blocks_per_session <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
+    if (max_new_len > total_new_tokens)
+        return fail(LS_EINVAL, "max_new_len (%d) exceeds total_new_tokens (%d)", max_new_len,
+                    total_new_tokens);
+    if (!(scale > 0.f) || scale != scale) return fail(LS_EINVAL, "scale must be a positive number");
+    if (workspace && workspace_bytes < LS_PREFILL_COUNTER_BYTES)
+        return fail(LS_ENOMEM, "prefill workspace of %zu bytes, %zu needed", workspace_bytes,
+                    LS_PREFILL_COUNTER_BYTES);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16)
+        return fail(LS_EINVAL, "prefill workspace must be 16-byte aligned");
+    if (windowed) {
+        if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_new, 16) || !aligned(v_new, 16))
+            return fail(LS_EINVAL, "q, out, k_new and v_new must be 16-byte aligned");
+        if (!aligned(cu_new_lens, 4) || !aligned(reused_lens, 4) || !aligned(block_tables, 4))
+            return fail(LS_EINVAL, "cu_new_lens, reused_lens and block_tables must be 4-byte aligned");
+        if (ls_status st = check_device(p)) return st;
+    } else {
+        window = sinks = 0;
+    }
+    if (lens_host)
+        if (ls_status st = check_prefill_lens_host(num_sessions, lens_host, total_new_tokens, max_new_len,
+                                                   max_blocks_per_session))
+            return st;
+    unsigned int *err = device_error_word();
+    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
+    if (k_new) {
+        hipError_t e = launch_append_prefill(p, layer, num_sessions, total_new_tokens, max_new_len,
+                                             static_cast<const uint16_t *>(k_new),
+                                             static_cast<const uint16_t *>(v_new), cu_new_lens,
+                                             reused_lens, block_tables, max_blocks_per_session,
+                                             lens_host ? static_cast<uint32_t *>(workspace) : nullptr, err,
+                                             stream);
+        if (e != hipSuccess) return hip_fail(e, "append launch");
+    }
+    hipError_t e = launch_prefill(p, layer, num_sessions, num_q_heads, static_cast<const uint16_t *>(q),
+                                  cu_new_lens, reused_lens, lens_host, total_new_tokens, max_new_len, block_tables,
+                                  max_blocks_per_session, scale, static_cast<uint16_t *>(out),
+                                  workspace, workspace_bytes, k_new != nullptr, window, sinks, err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "prefill launch");
+}
+
 }  // namespace
 
 // Message for ls_last_error() from code outside this file (the KV manager).
@@ -331,37 +487,8 @@ ls_status paged_attn_decode(ls_kv_pool *pool, int32_t layer, int32_t num_session
                             int32_t max_blocks_per_session, const int32_t *context_lens,
                             const int32_t *context_lens_host, float scale, void *out,
                             void *workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (ls_status st = check_pool(pool)) return st;
-    const PoolGeom &p = pool->geom;
-    if (layer < 0 || layer >= p.num_layers)
-        return fail(LS_EINVAL, "layer %d outside [0, %d)", layer, p.num_layers);
-    if (num_sessions < 0) return fail(LS_EINVAL, "num_sessions must be >= 0");
-    if (ls_status st = check_heads(p, num_q_heads)) return st;
-    if (num_sessions == 0) return LS_OK;
-    if (!q || !block_tables || !context_lens || !out || !workspace)
-        return fail(LS_EINVAL, "q, block_tables, context_lens, out and workspace must not be NULL");
-    if ((k_new == nullptr) != (v_new == nullptr))
-        return fail(LS_EINVAL, "k_new and v_new must both be given or both be NULL");
-    if (max_blocks_per_session <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
-    if (!(scale > 0.f) || scale != scale) return fail(LS_EINVAL, "scale must be a positive number");
-    if (context_lens_host)
-        if (ls_status st = check_decode_lens_host(num_sessions, context_lens_host, k_new ? 1 : 0,
-                                                  max_blocks_per_session))
-            return st;
-    const DecodePlan plan = plan_decode(p, num_sessions, num_q_heads, max_blocks_per_session);
-    if (!plan.supported)
-        return fail(LS_EUNSUPPORTED, "batch of %d sessions with %d blocks each exceeds the decode "
-                    "limits (2048 sessions, 16384 blocks per session)", num_sessions, max_blocks_per_session);
-    if (workspace_bytes < plan.total())
-        return fail(LS_ENOMEM, "workspace_bytes (%zu) < required (%zu)", workspace_bytes, plan.total());
-    unsigned int *err = device_error_word();
-    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
-    // The step's own K/V row is written by the decode kernel (no separate append launch).
-    hipError_t e = launch_decode(p, layer, num_sessions, num_q_heads, static_cast<const uint16_t *>(q),
-                                 static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new),
-                                 block_tables, max_blocks_per_session, context_lens, context_lens_host,
-                                 scale, static_cast<uint16_t *>(out), workspace, workspace_bytes, plan, err, stream);
-    return e == hipSuccess ? LS_OK : hip_fail(e, "decode launch");
+    return decode_call(pool, layer, num_sessions, num_q_heads, q, k_new, v_new, block_tables, max_blocks_per_session,
+                       context_lens, context_lens_host, false, 0, 0, scale, out, workspace, workspace_bytes, stream);
 }
 
 ls_status ls_decode_schedule(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
@@ -414,48 +541,102 @@ ls_status paged_attn_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
                              const int32_t *block_tables, int32_t max_blocks_per_session,
                              float scale, void *out, void *workspace, size_t workspace_bytes,
                              hipStream_t stream) {
+    return prefill_call(pool, layer, num_sessions, num_q_heads, q, k_new, v_new, cu_new_lens, reused_lens, lens_host,
+                        total_new_tokens, max_new_len, block_tables, max_blocks_per_session, false, 0, 0, scale, out,
+                        workspace, workspace_bytes, stream);
+}
+
+size_t ls_decode_window_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                        int32_t max_blocks_per_session, int32_t window, int32_t sinks) {
+    if (!pool || max_blocks_per_session <= 0 || check_window(window, sinks, max_blocks_per_session) != LS_OK) return 0;
+    return ls_decode_workspace_bytes(pool, num_sessions, num_q_heads, window_blocks(max_blocks_per_session, window, sinks));
+}
+
+ls_status paged_attn_decode_window(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                   const void *q, const void *k_new, const void *v_new,
+                                   const int32_t *block_tables, int32_t max_blocks_per_session,
+                                   const int32_t *context_lens, const int32_t *context_lens_host,
+                                   int32_t window, int32_t sinks, float scale, void *out, void *workspace,
+                                   size_t workspace_bytes, hipStream_t stream) {
+    return decode_call(pool, layer, num_sessions, num_q_heads, q, k_new, v_new, block_tables, max_blocks_per_session,
+                       context_lens, context_lens_host, true, window, sinks, scale, out, workspace, workspace_bytes,
+                       stream);
+}
+
+ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                    const void *q, const void *k_new, const void *v_new,
+                                    const int32_t *cu_new_lens, const int32_t *reused_lens,
+                                    const int32_t *lens_host, int32_t total_new_tokens, int32_t max_new_len,
+                                    const int32_t *block_tables, int32_t max_blocks_per_session,
+                                    int32_t window, int32_t sinks, float scale, void *out, void *workspace,
+                                    size_t workspace_bytes, hipStream_t stream) {
+    return prefill_call(pool, layer, num_sessions, num_q_heads, q, k_new, v_new, cu_new_lens, reused_lens, lens_host,
+                        total_new_tokens, max_new_len, block_tables, max_blocks_per_session, true, window, sinks, scale,
+                        out, workspace, workspace_bytes, stream);
+}
+
+ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t *seq_lens,
+                           const int32_t *new_lens, int32_t *block_tables, int32_t max_blocks_per_session,
+                           int32_t *free_ring, int32_t ring_size, const int64_t *free_counts,
+                           int64_t *next_counts, int32_t window, int32_t sinks, int32_t total_new_tokens,
+                           int32_t max_new_len, int32_t *next_lens, int32_t *cu_new_lens,
+                           int32_t *reused_lens, int64_t *slot_map, hipStream_t stream) {
+    if (ls_status st = check_pool(pool)) return st;
+    if (num_sessions < 0 || total_new_tokens < 0 || max_new_len < 0)
+        return fail(LS_EINVAL, "num_sessions, total_new_tokens and max_new_len must be >= 0");
+    if (max_blocks_per_session <= 0 || max_blocks_per_session > INT32_MAX / kBlock)
+        return fail(LS_EINVAL, "max_blocks_per_session (%d) must be in [1, %d]", max_blocks_per_session, INT32_MAX / kBlock);
+    if (!cu_new_lens || (total_new_tokens > 0 && !slot_map))
+        return fail(LS_EINVAL, "cu_new_lens and slot_map must not be NULL");
+    if (num_sessions > 0 && (!seq_lens || !new_lens || !block_tables || !next_lens))
+        return fail(LS_EINVAL, "seq_lens, new_lens, block_tables and next_lens must not be NULL");
+    if (free_ring) {
+        if (ring_size < 1 || !free_counts || !next_counts)
+            return fail(LS_EINVAL, "a free ring comes with its size (%d) and counters", ring_size);
+        if (window)
+            if (ls_status st = check_window(window, sinks, max_blocks_per_session)) return st;
+    } else if (ring_size || free_counts || next_counts || window) {
+        return fail(LS_EINVAL, "ring_size, counters and a window need a free ring");
+    }
+    for (const void *ptr : {(const void *)seq_lens, (const void *)new_lens, (const void *)block_tables, (const void *)free_ring,
+                            (const void *)next_lens, (const void *)cu_new_lens, (const void *)reused_lens})
+        if (!aligned(ptr, 4)) return fail(LS_EINVAL, "int32 arrays must be 4-byte aligned");
+    if (!aligned(slot_map, 8) || !aligned(free_counts, 8) || !aligned(next_counts, 8))
+        return fail(LS_EINVAL, "slot_map and the counters must be 8-byte aligned");
+    if (ls_status st = check_device(pool->geom)) return st;
+    unsigned int *err = device_error_word();
+    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
+    hipError_t e = launch_tables(pool->geom, num_sessions, seq_lens, new_lens, block_tables, max_blocks_per_session, free_ring,
+                                 ring_size, free_counts, next_counts, window, window ? sinks : 0, total_new_tokens,
+                                 max_new_len, next_lens, cu_new_lens, reused_lens, slot_map, err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "tables launch");
+}
+
+ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const void *k_new, const void *v_new,
+                    int64_t k_stride, int64_t v_stride, const int64_t *slot_map, const int64_t *slot_map_host,
+                    hipStream_t stream) {
     if (ls_status st = check_pool(pool)) return st;
     const PoolGeom &p = pool->geom;
     if (layer < 0 || layer >= p.num_layers)
         return fail(LS_EINVAL, "layer %d outside [0, %d)", layer, p.num_layers);
-    if (num_sessions < 0 || total_new_tokens < 0 || max_new_len < 0)
-        return fail(LS_EINVAL, "num_sessions, total_new_tokens and max_new_len must be >= 0");
-    if (ls_status st = check_heads(p, num_q_heads)) return st;
-    if (num_sessions == 0 || total_new_tokens == 0) return LS_OK;
-    if (!q || !cu_new_lens || !reused_lens || !block_tables || !out)
-        return fail(LS_EINVAL, "q, cu_new_lens, reused_lens, block_tables and out must not be NULL");
-    if ((k_new == nullptr) != (v_new == nullptr))
-        return fail(LS_EINVAL, "k_new and v_new must both be given or both be NULL");
-    if (max_blocks_per_session <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
-    if (max_new_len > total_new_tokens)
-        return fail(LS_EINVAL, "max_new_len (%d) exceeds total_new_tokens (%d)", max_new_len,
-                    total_new_tokens);
-    if (!(scale > 0.f) || scale != scale) return fail(LS_EINVAL, "scale must be a positive number");
-    if (workspace && workspace_bytes < LS_PREFILL_COUNTER_BYTES)
-        return fail(LS_ENOMEM, "prefill workspace of %zu bytes, %zu needed", workspace_bytes,
-                    LS_PREFILL_COUNTER_BYTES);
-    if (reinterpret_cast<uintptr_t>(workspace) % 16)
-        return fail(LS_EINVAL, "prefill workspace must be 16-byte aligned");
-    if (lens_host)
-        if (ls_status st = check_prefill_lens_host(num_sessions, lens_host, total_new_tokens, max_new_len,
-                                                   max_blocks_per_session))
-            return st;
+    if (total_tokens < 0) return fail(LS_EINVAL, "total_tokens must be >= 0");
+    if (total_tokens == 0) return LS_OK;
+    if (!k_new || !v_new || !slot_map) return fail(LS_EINVAL, "k_new, v_new and slot_map must not be NULL");
+    const int64_t row = (int64_t)p.num_kv_heads * p.head_dim, most = INT64_MAX / sizeof(uint16_t) / total_tokens;
+    for (int64_t stride : {k_stride, v_stride})
+        if (stride < row || stride % 8 || stride > most)
+            return fail(LS_EINVAL, "a row stride (%lld) must be a multiple of 8 and at least %lld", (long long)stride,
+                        (long long)row);
+    if (!aligned(k_new, 16) || !aligned(v_new, 16)) return fail(LS_EINVAL, "k_new and v_new must be 16-byte aligned");
+    if (!aligned(slot_map, 8)) return fail(LS_EINVAL, "slot_map must be 8-byte aligned");
+    if (slot_map_host)
+        if (ls_status st = check_slots_host(p, total_tokens, slot_map_host)) return st;
+    if (ls_status st = check_device(p)) return st;
     unsigned int *err = device_error_word();
     if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
-    if (k_new) {
-        hipError_t e = launch_append_prefill(p, layer, num_sessions, total_new_tokens, max_new_len,
-                                             static_cast<const uint16_t *>(k_new),
-                                             static_cast<const uint16_t *>(v_new), cu_new_lens,
-                                             reused_lens, block_tables, max_blocks_per_session,
-                                             lens_host ? static_cast<uint32_t *>(workspace) : nullptr, err,
-                                             stream);
-        if (e != hipSuccess) return hip_fail(e, "append launch");
-    }
-    hipError_t e = launch_prefill(p, layer, num_sessions, num_q_heads, static_cast<const uint16_t *>(q),
-                                  cu_new_lens, reused_lens, lens_host, total_new_tokens, max_new_len, block_tables,
-                                  max_blocks_per_session, scale, static_cast<uint16_t *>(out),
-                                  workspace, workspace_bytes, k_new != nullptr, err, stream);
-    return e == hipSuccess ? LS_OK : hip_fail(e, "prefill launch");
+    hipError_t e = launch_append_slots(p, layer, total_tokens, static_cast<const uint16_t *>(k_new),
+                                       static_cast<const uint16_t *>(v_new), k_stride, v_stride, slot_map, err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "append launch");
 }
 
 ls_status kv_blocks_stash(ls_kv_pool *pool, int32_t n, const int32_t *block_ids,

@@ -4,6 +4,9 @@
 // t % 16; K tiles are chunk-major ([D/8][16 tokens][8 dims]), V tiles
 // dim-major ([D][16 tokens]).  (The decode step's own token is written by the
 // decode kernel.)
+//
+// And the append of rows by a slot map (kv_append): row i goes to slot
+// slots[i] = block * 16 + offset, wherever the map says.
 #include "common.h"
 
 namespace ls {
@@ -95,7 +98,45 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(
     }
 }
 
+// Thread = 8 dims of one row of one KV head: a 16-byte chunk of the K tile, and
+// 8 values, 32 bytes apart, of the V tile.
+__global__ __launch_bounds__(kAppendThreads) void append_slots_kernel(
+    uint16_t *__restrict__ layer_pool, int64_t num_blocks, int32_t num_kv_heads, int32_t head_dim,
+    const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int64_t k_stride, int64_t v_stride,
+    const int64_t *__restrict__ slots, int64_t chunks, unsigned int *err) {
+    const int per_head = head_dim / 8, per_row = num_kv_heads * per_head;
+    for (int64_t c = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * kAppendThreads) {
+        const int64_t row = c / per_row;
+        const int in_row = (int)(c % per_row), g = in_row / per_head, d8 = in_row % per_head;
+        const int64_t slot = slots[row];
+        if (slot < 0) continue;
+        if (slot >= num_blocks * kBlock) {
+            flag_error(err, LS_DEVERR_BLOCK_ID);
+            continue;
+        }
+        const int t = (int)(slot % kBlock);
+        uint16_t *ktile = layer_pool + ((slot / kBlock) * 2 * num_kv_heads + g) * (kBlock * head_dim);
+        uint16_t *vtile = ktile + (int64_t)num_kv_heads * (kBlock * head_dim);
+        *reinterpret_cast<u32x4 *>(ktile + (d8 * kBlock + t) * 8) =
+            *reinterpret_cast<const u32x4 *>(k_new + row * k_stride + in_row * 8);
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(v_new + row * v_stride + in_row * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vtile[(d8 * 8 + e) * kBlock + t] = (uint16_t)(v[e / 2] >> (16 * (e % 2)));
+    }
+}
+
 }  // namespace
+
+hipError_t launch_append_slots(const PoolGeom &p, int layer, int32_t total_tokens, const uint16_t *k_new,
+                               const uint16_t *v_new, int64_t k_stride, int64_t v_stride, const int64_t *slot_map,
+                               unsigned int *err, hipStream_t stream) {
+    const int64_t chunks = (int64_t)total_tokens * p.num_kv_heads * (p.head_dim / 8);
+    const int64_t grid = (chunks + kAppendThreads - 1) / kAppendThreads;
+    hipLaunchKernelGGL(append_slots_kernel, dim3((unsigned)(grid < 65536 ? grid : 65536)), dim3(kAppendThreads), 0, stream,
+                       p.layer_base(layer), p.num_blocks, p.num_kv_heads, p.head_dim, k_new, v_new, k_stride, v_stride,
+                       slot_map, chunks, err);
+    return hipGetLastError();
+}
 
 hipError_t launch_append_prefill(const PoolGeom &p, int layer, int32_t num_sessions, int32_t total_tokens,
                                  int32_t max_new_len, const uint16_t *k_new, const uint16_t *v_new,

@@ -120,6 +120,16 @@ hipError_t launch_append_prefill(const PoolGeom &p, int layer, int32_t num_sessi
                                  const int32_t *cu_new_lens, const int32_t *reused_lens,
                                  const int32_t *block_tables, int32_t max_blocks, uint32_t *counters,
                                  unsigned int *err, hipStream_t stream);
+// Rows of k_new / v_new (k_stride, v_stride elements apart) to the slots of the map.
+hipError_t launch_append_slots(const PoolGeom &p, int layer, int32_t total_tokens, const uint16_t *k_new,
+                               const uint16_t *v_new, int64_t k_stride, int64_t v_stride, const int64_t *slot_map,
+                               unsigned int *err, hipStream_t stream);
+// A step's tables, slots and prefix sums (free_ring null: the tables hold every block).
+hipError_t launch_tables(const PoolGeom &p, int32_t num_sessions, const int32_t *seq_lens, const int32_t *new_lens,
+                         int32_t *block_tables, int32_t max_blocks, int32_t *free_ring, int32_t ring_size,
+                         const int64_t *free_counts, int64_t *next_counts, int32_t window, int32_t sinks,
+                         int32_t total_tokens, int32_t max_new_len, int32_t *next_lens, int32_t *cu_new_lens,
+                         int32_t *reused_lens, int64_t *slot_map, unsigned int *err, hipStream_t stream);
 // With k_new / v_new (both non-null) the step's own token is attended from
 // them and written to its pool slot by the decode kernel itself.
 // The schedule paged_attn_decode runs for a batch: tokens per split, planned
@@ -133,21 +143,29 @@ DecodeSchedule decode_schedule(const PoolGeom &p, int32_t num_sessions, int32_t 
                                const int32_t *context_lens_host, int32_t appended, const DecodePlan &plan,
                                hipStream_t stream);
 
+// Longest window and most first tokens (the kernels add them to positions in 32 bits).
+constexpr int32_t kMaxWindowTokens = LS_MAX_WINDOW_TOKENS;
+// Most blocks of a session that a query with this window reads, of max_blocks
+// in its table: those of the first tokens, and those of `window` tokens at any
+// offset.  A windowed decode is planned (plan_decode) for tables this wide.
+int32_t window_blocks(int32_t max_blocks, int32_t window, int32_t sinks);
+
 // With context_lens_host (the same lengths on the host) the split-K schedule
 // is planned on the host; the split merge is launched only if some session is
-// split.
+// split.  window 0: every key is seen (sinks unused).
 hipError_t launch_decode(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads,
                          const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
                          const int32_t *block_tables,
                          int32_t max_blocks, const int32_t *context_lens, const int32_t *context_lens_host,
                          float scale, uint16_t *out, void *workspace, size_t workspace_bytes,
-                         const DecodePlan &plan, unsigned int *err, hipStream_t stream);
+                         const DecodePlan &plan, int32_t window, int32_t sinks, unsigned int *err,
+                         hipStream_t stream);
 hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads,
                           const uint16_t *q, const int32_t *cu_new_lens,
                           const int32_t *reused_lens, const int32_t *lens_host, int32_t total_tokens,
                           int32_t max_new_len, const int32_t *block_tables, int32_t max_blocks,
                           float scale, uint16_t *out, void *workspace, size_t workspace_bytes, bool counters_cleared,
-                          unsigned int *err, hipStream_t stream);
+                          int32_t window, int32_t sinks, unsigned int *err, hipStream_t stream);
 
 // ---------------------------------------------------------------------------
 // Device helpers

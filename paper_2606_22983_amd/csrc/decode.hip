@@ -97,6 +97,30 @@ struct DecodeArgs {
     uint64_t *arrived;             // decode_small_kernel: [S][Hkv] arrival counts (arrived_word)
 };
 
+// Sliding window: the query at position L - 1 (L keys, its own included) sees
+// key t when t < sinks or t >= L - window.  The kernels walk the blocks that
+// hold such keys as if they were one shorter session: the ceil(sinks / 16)
+// blocks of the first tokens, then the blocks from that of key L - window on.
+// `skip` blocks between the two are left out, so position v of the walk is token
+// v (v < 16 ceil(sinks / 16)) or v + 16 skip.  Below, lengths, splits and blocks
+// are counted on the walk; only table columns are not.  In it the keys not seen
+// are v in [sinks, L_walk - window): at most 15 in the last block of the first
+// tokens and 15 in the window's first block, or, where the two overlap
+// (skip = 0), any number of keys between them.
+struct DecodeWindowArgs : DecodeArgs {
+    int32_t window;                // >= 1
+    int32_t sinks;                 // >= 0
+};
+template <bool kWin>
+using DecodeArgsT = typename std::conditional<kWin, DecodeWindowArgs, DecodeArgs>::type;
+
+// Blocks that a walk of L keys leaves out.  (window and sinks are at most
+// kMaxWindowTokens, so that nothing here overflows.)
+__host__ __device__ __forceinline__ int window_skip(int L, int window, int sinks) {
+    const int gap = (L - window) / kBlock - (sinks + kBlock - 1) / kBlock;
+    return L > window && gap > 0 ? gap : 0;
+}
+
 // A schedule planned on the host (paged_attn_decode with host lengths),
 // passed by value in the kernel arguments: workgroup w runs items
 // start[w] .. start[w + 1] - 1.  Items are 32-bit words (session in bits
@@ -184,6 +208,28 @@ __device__ __forceinline__ int attended_len(const DecodeArgs &a, int s, bool may
     return max(min(raw, cap), 0);
 }
 
+// The length of a session's walk, and the blocks it leaves out.
+__device__ __forceinline__ int walk_len(const DecodeArgs &a, int s, bool may_flag, int &skip) {
+    skip = 0;
+    return attended_len(a, s, may_flag);
+}
+__device__ __forceinline__ int walk_len(const DecodeWindowArgs &a, int s, bool may_flag, int &skip) {
+    const int L = attended_len(a, s, may_flag);
+    skip = window_skip(L, a.window, a.sinks);
+    return L - skip * kBlock;
+}
+// Table column of block j of a walk.
+__device__ __forceinline__ int walk_column(const DecodeArgs &, int j, int) { return j; }
+__device__ __forceinline__ int walk_column(const DecodeWindowArgs &a, int j, int skip) {
+    return j + (j * kBlock >= a.sinks ? skip : 0);
+}
+// Keys [hole_lo, hole_hi) of a walk of L keys are not seen.
+__device__ __forceinline__ void walk_hole(const DecodeArgs &, int, int &lo, int &hi) { lo = hi = 0; }
+__device__ __forceinline__ void walk_hole(const DecodeWindowArgs &a, int L, int &lo, int &hi) {
+    lo = a.sinks;
+    hi = L - a.window;
+}
+
 // Issue the loads of one block (blk < 0: a zero-size descriptor, nothing fetched).
 // koff, voff: this lane's byte offsets, of every k-step and dim tile (arrays
 // of D / 32 and D / 16), or of the first ones alone, the others being constants
@@ -211,22 +257,26 @@ __device__ __forceinline__ void load_block(BlockRegs<D> &r, const uint16_t *pool
         r.v[dt] = __builtin_amdgcn_raw_buffer_load_b64(rv, voff[kAll ? dt : 0], kAll ? 0 : dt * 16 * kBlock * 2, kStreamLoad);
 }
 
-// Online-softmax update with one 16-token block held in registers.
-template <int D>
+// Online-softmax update with one 16-token block held in registers: its keys
+// below L and, with a window, outside [hole_lo, hole_hi).
+template <int D, bool kWin = false>
 __device__ __forceinline__ void process_block(BlockRegs<D> &r, const bf16x8 (&qop)[D / 32],
                                               int tok_base, int L, float scale_log2, int g4,
-                                              float &m, float &lsum, f32x4 (&o)[D / 16]) {
+                                              float &m, float &lsum, f32x4 (&o)[D / 16], int hole_lo = 0,
+                                              int hole_hi = 0) {
     f32x4 sacc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < D / 32; ++ks)
         sacc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r.k[ks]),
                                                        qop[ks], sacc, 0, 0, 0);
-    const bool partial = tok_base + kBlock > L;     // some slot of this block is not a key
+    bool partial = tok_base + kBlock > L;           // some slot of this block is not a key
+    if (kWin) partial = partial || (tok_base + kBlock > hole_lo && tok_base < hole_hi);
+    auto seen = [&](int t) { return t < L && !(kWin && t >= hole_lo && t < hole_hi); };
     float x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[i] = sacc[i] * scale_log2;
-        if (partial && tok_base + 4 * g4 + i >= L) x[i] = -INFINITY;
+        if (partial && !seen(tok_base + 4 * g4 + i)) x[i] = -INFINITY;
     }
     float bm = wave_max_xor_16_32(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
     const float m_new = fmaxf(m, bm);
@@ -245,11 +295,18 @@ __device__ __forceinline__ void process_block(BlockRegs<D> &r, const bf16x8 (&qo
     const uint32_t p23 = pack_bf16x2(p[2], p[3]);
     const s16x4 pb = __builtin_bit_cast(s16x4, make_uint2(p01, p23));
     if (partial) {
-        // Slots at or past L may hold anything (NaN included): zero them so that
-        // 0 * V cannot turn into NaN.
-        const int valid = L - tok_base - 4 * g4;      // tokens of this lane's 4 that exist
-        const uint32_t lo = valid >= 2 ? 0xFFFFFFFFu : (valid == 1 ? 0x0000FFFFu : 0u);
-        const uint32_t hi = valid >= 4 ? 0xFFFFFFFFu : (valid == 3 ? 0x0000FFFFu : 0u);
+        // Slots at or past L may hold anything (NaN included), and so may keys
+        // behind the window: zero them so that 0 * V cannot turn into NaN.
+        uint32_t lo, hi;
+        if constexpr (kWin) {
+            const int t = tok_base + 4 * g4;
+            lo = (seen(t) ? 0x0000FFFFu : 0u) | (seen(t + 1) ? 0xFFFF0000u : 0u);
+            hi = (seen(t + 2) ? 0x0000FFFFu : 0u) | (seen(t + 3) ? 0xFFFF0000u : 0u);
+        } else {
+            const int valid = L - tok_base - 4 * g4;  // tokens of this lane's 4 that exist
+            lo = valid >= 2 ? 0xFFFFFFFFu : (valid == 1 ? 0x0000FFFFu : 0u);
+            hi = valid >= 4 ? 0xFFFFFFFFu : (valid == 3 ? 0x0000FFFFu : 0u);
+        }
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
             r.v[dt].x &= lo;
@@ -341,11 +398,12 @@ __device__ __forceinline__ unsigned block_exclusive_scan(unsigned v, unsigned *s
 //
 // Either way each workgroup fetches the next chunk's block ids while it works
 // on the current one, and requests its first blocks before merging.
-template <int D, int kDepth, int kMaxPerWave, bool kHost, int kItems = kPlanItemsSmall>
-__global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanArg<kHost, kItems> plan) {
+template <int D, int kDepth, int kMaxPerWave, bool kHost, int kItems = kPlanItemsSmall, bool kWin = false>
+__global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a, PlanArg<kHost, kItems> plan) {
     constexpr int kChunk = kMaxPerWave * kDecWaves * kBlock;   // tokens per chunk
     __shared__ int sm_cum[kMaxBatch + 1];       // first full-split row of each session
-    __shared__ int sm_len[kMaxBatch];           // attended length of each session
+    __shared__ int sm_len[kMaxBatch];           // attended length of each session (with a window: of its walk)
+    __shared__ int sm_skip[kWin ? kMaxBatch : 1];   // blocks its walk leaves out
     __shared__ int sm_porder[kMaxBatch];        // sessions of the short-split rows, in row order
     __shared__ int sm_key[kDecThreads];         // block count of a session's short split (-1: none)
     __shared__ unsigned long long sm_kmask[kKeyBins][kDecThreads / 64];  // sessions per short-split key
@@ -384,8 +442,10 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanA
         auto has_short = [&](int L) { return L == 0 || L % T != 0; };   // an empty session still owns one row
         unsigned mine = 0;
         for (int s = s_begin; s < s_end; ++s) {
-            const int L = attended_len(a, s, blockIdx.x == 0);
+            int skip;
+            const int L = walk_len(a, s, blockIdx.x == 0, skip);
             sm_len[s] = L;
+            if constexpr (kWin) sm_skip[s] = skip;
             sm_own[s] = a.appended && a.lens[s] >= 0 && a.lens[s] + 1 <= a.max_blocks * kBlock;
             mine += (unsigned)(L / T) + (has_short(L) ? 1u << 20 : 0u);
         }
@@ -510,10 +570,11 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanA
     // unconditional (its index clamped into the table row) and the id is
     // validated only when it is used, so nothing waits for this load until the
     // chunk is processed.
-    auto fetch_ids = [&](int s_, int split_, int c_) -> int {
-        const int j = min(split_ * (T / kBlock) + c_ * (kChunk / kBlock) + lane, a.max_blocks - 1);
-        return a.block_tables[(int64_t)s_ * a.max_blocks + j];
+    auto fetch_ids = [&](int s_, int split_, int c_, int skip_) -> int {
+        const int j = split_ * (T / kBlock) + c_ * (kChunk / kBlock) + lane;
+        return a.block_tables[(int64_t)s_ * a.max_blocks + min(walk_column(a, j, skip_), a.max_blocks - 1)];
     };
+    auto skip_of = [&](int s_) -> int { return kWin ? sm_skip[kWin ? s_ : 0] : 0; };
     // Validated id (or -1) of entry idx of a fetched id register.
     auto checked_id = [&](int ids, int idx, int nb) -> int {
         const int b = __builtin_amdgcn_readlane(ids, min(idx, kWave - 1));
@@ -556,14 +617,23 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanA
     int s = 0, g = 0, split = 0;
     bool last_planned = false;
     bool have = item_at(0, s, g, split, last_planned);
-    int ids_pre = have ? fetch_ids(s, split, 0) : -1;
+    // (With a window the table columns hang on the length, which is not in LDS
+    // yet when the host planned.)
+    int first_skip = 0;
+    if (have) {
+        if constexpr (kHost && kWin) walk_len(a, s, false, first_skip);
+        else first_skip = skip_of(s);
+    }
+    int ids_pre = have ? fetch_ids(s, split, 0, first_skip) : -1;
     if (have) load_q(s, g, qop);
     if constexpr (kHost) {
         // The schedule came with the arguments, so only the lengths are needed.
         // They are loaded after the first item's block ids and q, whose loads
         // are then already in flight.
         for (int i = tid; i < S; i += kDecThreads) {
-            sm_len[i] = attended_len(a, i, blockIdx.x == 0);
+            int skip;
+            sm_len[i] = walk_len(a, i, blockIdx.x == 0, skip);
+            if constexpr (kWin) sm_skip[i] = skip;
             sm_own[i] = a.appended && a.lens[i] >= 0 && a.lens[i] + 1 <= a.max_blocks * kBlock;
         }
         __syncthreads();
@@ -584,6 +654,8 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanA
         const int L = sm_len[s];
         const int own = sm_own[s];
         const int Lp = L - own;            // keys read from the pool; the own token comes from k_new
+        int hole_lo, hole_hi;
+        walk_hole(a, L, hole_lo, hole_hi);
         const int cur_s = s, cur_g = g, cur_split = split, cur_c = c;
         const bool cur_last_planned = last_planned;
         const int cur_ids = lane < kMaxSplitTokens / kBlock ? sm_ids[wave][u & 1][lane] : -1;
@@ -599,7 +671,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanA
         } else {
             ++c;
         }
-        if (have) next_ids = fetch_ids(s, split, c);
+        if (have) next_ids = fetch_ids(s, split, c, skip_of(s));
         const int nsplit = L > 0 ? (L + T - 1) / T : 1;
         const int blk0 = t0 / kBlock;
         const int nblk = chunk_blocks(L, cur_split, cur_c);
@@ -624,7 +696,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgs a, PlanA
             if (i >= my_n) break;
             const int j = i % kDepth;
             const int tb = (blk0 + wave + i * kDecWaves) * kBlock;
-            process_block<D>(r[j], qop, tb, bb[j] >= 0 ? Lp : 0, a.scale_log2, g4, m, lsum, o);
+            process_block<D, kWin>(r[j], qop, tb, bb[j] >= 0 ? Lp : 0, a.scale_log2, g4, m, lsum, o, hole_lo, hole_hi);
             if (i + kDepth < kMaxPerWave) {
                 bb[j] = bid(i + kDepth);
                 load_block<D>(r[j], a.pool, a.num_kv_heads, cur_g, bb[j], koff, voff);
@@ -824,8 +896,8 @@ struct SmallRows {
 template <bool kHost>
 using SmallRowsArg = typename std::conditional<kHost, SmallRows, NoPlan>::type;
 
-template <int D, int kDepth, bool kLoop, bool kHost>
-__global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgs a, SmallRowsArg<kHost> rows) {
+template <int D, int kDepth, bool kLoop, bool kHost, bool kWin = false>
+__global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<kWin> a, SmallRowsArg<kHost> rows) {
     __shared__ float sm_m[kDecWaves][kMaxGroup];
     __shared__ float sm_l[kDecWaves][kMaxGroup];
     __shared__ __attribute__((aligned(16))) float sm_o[kDecWaves][kMaxGroup][D];
@@ -851,7 +923,8 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgs a,
         bool found = false;
         for (int s0 = 0; s0 < a.num_sessions && !found; s0 += kWave) {
             const int sl = min(s0 + lane, a.num_sessions - 1);
-            const int Ls = attended_len(a, sl, false);
+            int skip_unused;
+            const int Ls = walk_len(a, sl, false, skip_unused);
             const int n = s0 + lane < a.num_sessions ? max((Ls + T - 1) / T, 1) : 0;
             int incl = n;
 #pragma unroll
@@ -873,7 +946,10 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgs a,
     }
 
     // Block ids of the split (one per lane), q and the length, all in flight at once.
-    const int id_at = min(split * (T / kBlock) + lane, a.max_blocks - 1);
+    // (With a window the table columns hang on the length.)
+    int skip = 0;
+    if constexpr (kWin) walk_len(a, s, false, skip);
+    const int id_at = min(walk_column(a, split * (T / kBlock) + lane, skip), a.max_blocks - 1);
     const int ids = a.block_tables[(int64_t)s * a.max_blocks + id_at];
     bf16x8 qop[D / 32];
     {
@@ -886,7 +962,9 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgs a,
         }
     }
     const bool first = split == 0 && g == 0 && tid == 0;
-    const int L = attended_len(a, s, first);
+    const int L = walk_len(a, s, first, skip);
+    int hole_lo, hole_hi;
+    walk_hole(a, L, hole_lo, hole_hi);
     const int own = a.appended && a.lens[s] >= 0 && a.lens[s] + 1 <= a.max_blocks * kBlock;
     // A device length past the host's rows: flagged, and attended as far as the
     // rows go.
@@ -936,8 +1014,8 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgs a,
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) {
             if (i + j < my_n)
-                process_block<D>(r[j], qop, (blk0 + wave + (i + j) * kDecWaves) * kBlock, bb[j] >= 0 ? Lp : 0,
-                                 a.scale_log2, g4, m, lsum, o);
+                process_block<D, kWin>(r[j], qop, (blk0 + wave + (i + j) * kDecWaves) * kBlock, bb[j] >= 0 ? Lp : 0,
+                                       a.scale_log2, g4, m, lsum, o, hole_lo, hole_hi);
             if (kLoop) {
                 bb[j] = bid(wave + (i + j + kDepth) * kDecWaves);
                 load_block<D>(r[j], a.pool, Hkv, g, bb[j], koff, voff);
@@ -1049,14 +1127,15 @@ constexpr int kCombThreads = 1024;
 constexpr int kCombParts = kCombThreads / 256;
 constexpr int kCombPre = 8;                  // splits per thread loaded up front (32 per row)
 
-template <int D>
-__global__ __launch_bounds__(kCombThreads) void decode_combine_kernel(DecodeArgs a) {
+template <int D, bool kWin = false>
+__global__ __launch_bounds__(kCombThreads) void decode_combine_kernel(DecodeArgsT<kWin> a) {
     __shared__ float sm_e[kMaxSplits][kMaxGroup];          // exp2(m_k - M) per split and head
     __shared__ float sm_inv[kMaxGroup];                     // 1 / sum_k exp2(m_k - M) l_k
     __shared__ __attribute__((aligned(16))) float sm_acc[kCombParts - 1][256][4];
     const int g = blockIdx.x;
     const int s = blockIdx.y;
-    const int L = attended_len(a, s, false);
+    int skip_unused;
+    const int L = walk_len(a, s, false, skip_unused);
     if (L <= 0) return;
     const int nsplit = (L + a.split_tokens - 1) / a.split_tokens;
     if (nsplit <= 1) return;
@@ -1593,13 +1672,125 @@ DecodeSchedule decode_schedule(const PoolGeom &p, int32_t num_sessions, int32_t 
     return sc;
 }
 
+int32_t window_blocks(int32_t max_blocks, int32_t window, int32_t sinks) {
+    const int64_t most = ((int64_t)sinks + kBlock - 1) / kBlock + ((int64_t)window + 2 * kBlock - 2) / kBlock;
+    return (int32_t)std::min<int64_t>(max_blocks, most);
+}
+
+namespace {
+
+template <bool kWin>
+hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk_blocks, const int32_t *walk_lens_host,
+                           void *workspace, size_t workspace_bytes, const DecodePlan &plan, DecodeArgsT<kWin> &a,
+                           hipStream_t stream) {
+    const int32_t num_q_heads = a.group * p.num_kv_heads;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    a.split_tokens = plan.split_tokens;
+    a.max_splits = plan.max_splits;
+    a.part_ml = reinterpret_cast<float *>(ws);
+    a.part_acc = reinterpret_cast<float *>(ws + plan.ml_bytes);
+    a.arrived = nullptr;
+    // Small batches.
+    const int64_t resident = (int64_t)stream_cus(p, stream);
+    const SmallDecodePlan sp = choose_small(p, resident, num_sessions, num_q_heads, walk_blocks, walk_lens_host,
+                                            a.appended, workspace, workspace_bytes, plan);
+    if (sp.split_tokens) {
+        a.split_tokens = sp.split_tokens;
+        a.max_splits = sp.single ? 1 : 0;
+        a.arrived = reinterpret_cast<uint64_t *>(ws);
+        a.part_ml = reinterpret_cast<float *>(ws + sp.count_bytes);
+        a.part_acc = reinterpret_cast<float *>(ws + sp.count_bytes + sp.ml_bytes);
+        const dim3 grid((unsigned)(sp.rows * p.num_kv_heads));
+        const int per_wave = sp.split_tokens / (kDecWaves * kBlock);
+#define LS_SMALL(DD, DEPTH, LOOP) \
+    hipLaunchKernelGGL((decode_small_kernel<DD, DEPTH, LOOP, decltype(rows)::value, kWin>), grid, dim3(kDecThreads), 0, stream, a, arg)
+        auto launch = [&](auto rows, const auto &arg) {
+            if (p.head_dim == 128) {
+                if (per_wave <= 2) LS_SMALL(128, 2, false);
+                else if (per_wave <= 4) LS_SMALL(128, 4, false);
+                else LS_SMALL(128, 2, true);
+            } else {
+                if (per_wave <= 4) LS_SMALL(64, 4, false);
+                else LS_SMALL(64, 4, true);
+            }
+        };
+        if (walk_lens_host && !sp.single) {
+            SmallRows list;
+            int n = 0;
+            for (int32_t s = 0; s < num_sessions; ++s) {
+                const int64_t L = (int64_t)walk_lens_host[s] + a.appended;
+                const int ns = (int)std::max<int64_t>(1, (L + sp.split_tokens - 1) / sp.split_tokens);
+                for (int k = 0; k < ns; ++k) list.row[n++] = (uint32_t)s | ((uint32_t)k << 12) | ((uint32_t)ns << 22);
+            }
+            launch(std::true_type{}, list);
+        } else {
+            launch(std::false_type{}, NoPlan{0});
+        }
+#undef LS_SMALL
+        return hipGetLastError();
+    }
+    auto combine = [&]() {
+        const dim3 grid(p.num_kv_heads, num_sessions);
+        if (p.head_dim == 128)
+            hipLaunchKernelGGL((decode_combine_kernel<128, kWin>), grid, dim3(kCombThreads), 0, stream, a);
+        else
+            hipLaunchKernelGGL((decode_combine_kernel<64, kWin>), grid, dim3(kCombThreads), 0, stream, a);
+        return hipGetLastError();
+    };
+    // Host lengths: the schedule is planned here and passed with the arguments.
+    if (walk_lens_host) {
+        const CachedPlan *c = cached_decode_plan(num_sessions, p.num_kv_heads, walk_lens_host, a.appended,
+                                                 (int)resident, std::max(plan.split_tokens, 1024),
+                                                 plan.split_tokens, plan.max_splits > 1);
+        if (c->host) {
+            const bool split = c->split;
+            a.split_tokens = c->T;
+            const dim3 grid((unsigned)resident);
+#define LS_DECODE(DD, ITEMS, PLAN) \
+    hipLaunchKernelGGL((decode_kernel<DD, 2, 8, true, ITEMS, kWin>), grid, dim3(kDecThreads), 0, stream, a, PLAN)
+            if (!c->large) {
+                if (p.head_dim == 128) LS_DECODE(128, kPlanItemsSmall, c->small);
+                else LS_DECODE(64, kPlanItemsSmall, c->small);
+            } else if (p.head_dim == 128) {
+                LS_DECODE(128, kPlanItemsLarge, c->plan);
+            } else {
+                LS_DECODE(64, kPlanItemsLarge, c->plan);
+            }
+#undef LS_DECODE
+            hipError_t e = hipGetLastError();
+            return e != hipSuccess || !split ? e : combine();
+        }
+    }
+    const int64_t upper = (int64_t)num_sessions * p.num_kv_heads * plan.max_splits;
+    // Persistent grid: one 512-thread workgroup (8 waves, this kernel's
+    // occupancy) on every CU the stream may use.
+    dim3 grid((unsigned)std::min<int64_t>(upper, resident));
+    const NoPlan none{0};
+#define LS_DECODE(DD, PW) \
+    hipLaunchKernelGGL((decode_kernel<DD, 2, PW, false, kPlanItemsSmall, kWin>), grid, dim3(kDecThreads), 0, stream, a, none)
+    const int per_wave = plan.split_tokens / (kDecWaves * kBlock);
+    if (p.head_dim == 128) {
+        if (per_wave == 4) LS_DECODE(128, 4);
+        else LS_DECODE(128, 8);
+    } else {
+        if (per_wave == 4) LS_DECODE(64, 4);
+        else LS_DECODE(64, 8);
+    }
+#undef LS_DECODE
+    hipError_t e = hipGetLastError();
+    return e != hipSuccess || plan.max_splits == 1 ? e : combine();
+}
+
+}  // namespace
+
 hipError_t launch_decode(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads,
                          const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
                          const int32_t *block_tables,
                          int32_t max_blocks, const int32_t *context_lens, const int32_t *context_lens_host,
                          float scale, uint16_t *out, void *workspace, size_t workspace_bytes,
-                         const DecodePlan &plan, unsigned int *err, hipStream_t stream) {
-    DecodeArgs a;
+                         const DecodePlan &plan, int32_t window, int32_t sinks, unsigned int *err,
+                         hipStream_t stream) {
+    DecodeWindowArgs a;
     a.pool = p.layer_base(layer);
     a.num_blocks = p.num_blocks;
     a.num_kv_heads = p.num_kv_heads;
@@ -1614,106 +1805,22 @@ hipError_t launch_decode(const PoolGeom &p, int layer, int32_t num_sessions, int
     a.v_new = v_new;
     a.scale_log2 = scale * kLog2e;
     a.err = err;
-    a.split_tokens = plan.split_tokens;
-    a.max_splits = plan.max_splits;
-    uint8_t *ws = static_cast<uint8_t *>(workspace);
-    a.part_ml = reinterpret_cast<float *>(ws);
-    a.part_acc = reinterpret_cast<float *>(ws + plan.ml_bytes);
     a.num_sessions = num_sessions;
-    a.arrived = nullptr;
-    // Small batches.
-    const int64_t resident = (int64_t)stream_cus(p, stream);
-    const SmallDecodePlan sp = choose_small(p, resident, num_sessions, num_q_heads, max_blocks, context_lens_host,
-                                            a.appended, workspace, workspace_bytes, plan);
-    if (sp.split_tokens) {
-        a.split_tokens = sp.split_tokens;
-        a.max_splits = sp.single ? 1 : 0;
-        a.arrived = reinterpret_cast<uint64_t *>(ws);
-        a.part_ml = reinterpret_cast<float *>(ws + sp.count_bytes);
-        a.part_acc = reinterpret_cast<float *>(ws + sp.count_bytes + sp.ml_bytes);
-        const dim3 grid((unsigned)(sp.rows * p.num_kv_heads));
-        const int per_wave = sp.split_tokens / (kDecWaves * kBlock);
-#define LS_SMALL(DD, DEPTH, LOOP) \
-    hipLaunchKernelGGL((decode_small_kernel<DD, DEPTH, LOOP, decltype(rows)::value>), grid, dim3(kDecThreads), 0, stream, a, arg)
-        auto launch = [&](auto rows, const auto &arg) {
-            if (p.head_dim == 128) {
-                if (per_wave <= 2) LS_SMALL(128, 2, false);
-                else if (per_wave <= 4) LS_SMALL(128, 4, false);
-                else LS_SMALL(128, 2, true);
-            } else {
-                if (per_wave <= 4) LS_SMALL(64, 4, false);
-                else LS_SMALL(64, 4, true);
-            }
-        };
-        if (context_lens_host && !sp.single) {
-            SmallRows list;
-            int n = 0;
-            for (int32_t s = 0; s < num_sessions; ++s) {
-                const int64_t L = (int64_t)context_lens_host[s] + a.appended;
-                const int ns = (int)std::max<int64_t>(1, (L + sp.split_tokens - 1) / sp.split_tokens);
-                for (int k = 0; k < ns; ++k) list.row[n++] = (uint32_t)s | ((uint32_t)k << 12) | ((uint32_t)ns << 22);
-            }
-            launch(std::true_type{}, list);
-        } else {
-            launch(std::false_type{}, NoPlan{0});
+    a.window = window;
+    a.sinks = sinks;
+    if (!window)
+        return launch_decode_t<false>(p, num_sessions, max_blocks, context_lens_host, workspace, workspace_bytes, plan,
+                                      a, stream);
+    // The planners see the walks: their lengths (without the appended token, as
+    // those of whole sessions) and the most blocks one has.
+    int32_t walk[kMaxBatch];
+    if (context_lens_host)
+        for (int32_t s = 0; s < num_sessions; ++s) {
+            const int32_t L = context_lens_host[s] + a.appended;
+            walk[s] = context_lens_host[s] - window_skip(L, window, sinks) * kBlock;
         }
-#undef LS_SMALL
-        return hipGetLastError();
-    }
-    dim3 cgrid(p.num_kv_heads, num_sessions);
-    // Host lengths: the schedule is planned here and passed with the arguments.
-    if (context_lens_host) {
-        const CachedPlan *c = cached_decode_plan(num_sessions, p.num_kv_heads, context_lens_host, a.appended,
-                                                 (int)resident, std::max(plan.split_tokens, 1024),
-                                                 plan.split_tokens, plan.max_splits > 1);
-        if (c->host) {
-            const bool split = c->split;
-            a.split_tokens = c->T;
-            const dim3 grid((unsigned)resident);
-            if (!c->large) {
-                if (p.head_dim == 128)
-                    hipLaunchKernelGGL((decode_kernel<128, 2, 8, true>), grid, dim3(kDecThreads), 0, stream, a, c->small);
-                else
-                    hipLaunchKernelGGL((decode_kernel<64, 2, 8, true>), grid, dim3(kDecThreads), 0, stream, a, c->small);
-            } else if (p.head_dim == 128) {
-                hipLaunchKernelGGL((decode_kernel<128, 2, 8, true, kPlanItemsLarge>), grid, dim3(kDecThreads), 0,
-                                   stream, a, c->plan);
-            } else {
-                hipLaunchKernelGGL((decode_kernel<64, 2, 8, true, kPlanItemsLarge>), grid, dim3(kDecThreads), 0,
-                                   stream, a, c->plan);
-            }
-            hipError_t e = hipGetLastError();
-            if (e != hipSuccess || !split) return e;
-            if (p.head_dim == 128)
-                hipLaunchKernelGGL(decode_combine_kernel<128>, cgrid, dim3(kCombThreads), 0, stream, a);
-            else
-                hipLaunchKernelGGL(decode_combine_kernel<64>, cgrid, dim3(kCombThreads), 0, stream, a);
-            return hipGetLastError();
-        }
-    }
-    const int64_t upper = (int64_t)num_sessions * p.num_kv_heads * plan.max_splits;
-    // Persistent grid: one 512-thread workgroup (8 waves, this kernel's
-    // occupancy) on every CU the stream may use.
-    dim3 grid((unsigned)std::min<int64_t>(upper, resident));
-    const NoPlan none{0};
-#define LS_DECODE(DD, PW) \
-    hipLaunchKernelGGL((decode_kernel<DD, 2, PW, false>), grid, dim3(kDecThreads), 0, stream, a, none)
-    const int per_wave = plan.split_tokens / (kDecWaves * kBlock);
-    if (p.head_dim == 128) {
-        if (per_wave == 4) LS_DECODE(128, 4);
-        else LS_DECODE(128, 8);
-    } else {
-        if (per_wave == 4) LS_DECODE(64, 4);
-        else LS_DECODE(64, 8);
-    }
-#undef LS_DECODE
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || plan.max_splits == 1) return e;
-    if (p.head_dim == 128)
-        hipLaunchKernelGGL(decode_combine_kernel<128>, cgrid, dim3(kCombThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL(decode_combine_kernel<64>, cgrid, dim3(kCombThreads), 0, stream, a);
-    return hipGetLastError();
+    return launch_decode_t<true>(p, num_sessions, window_blocks(max_blocks, window, sinks),
+                                 context_lens_host ? walk : nullptr, workspace, workspace_bytes, plan, a, stream);
 }
 
 }  // namespace ls

@@ -101,6 +101,22 @@ struct PrefillArgs {
     float *part_o;                 // [piece][wave][row tile][dim tile][lane][4] unnormalised output
 };
 
+// Sliding window: row j of a turn, at position p = c + j, sees key t when t <= p
+// and either t < sinks or t > p - window.  A query tile walks the blocks that
+// some row of it sees as if they were one shorter context: the
+// ceil(sinks / 16) blocks of the first tokens, then those from key
+// p_first - window + 1 on.  `skip` blocks between the two are left out, so
+// position v of the walk is token v (in the first tokens' blocks) or v + 16 skip.
+// Keys, limits and tiles below are counted on the walk; only table columns are
+// not.  On it a row whose own position is v_p misses keys v in
+// [sinks, v_p - window + 1), the row's hole.
+struct PrefillWindowArgs : PrefillArgs {
+    int32_t window;                // >= 1
+    int32_t sinks;                 // >= 0
+};
+template <bool kWin>
+using PrefillArgsT = typename std::conditional<kWin, PrefillWindowArgs, PrefillArgs>::type;
+
 // Schedule dealt on the host when the caller passes the lengths there: every
 // XCD's (session, KV head) pairs in the order that XCD runs them, with the
 // items (query tiles) of the XCD's entries before each one.
@@ -173,6 +189,17 @@ __device__ __forceinline__ int32_t table_entry(const int32_t *table, int jb, int
     const int jc = max(min(jb, nv - 1), 0);
     const int32_t b = ((const_i32 *)table)[jc];
     // select by mask rather than by branch: the load stays unconditional
+    const int32_t keep = -(int32_t)((unsigned)jb < (unsigned)nv);
+    return b | ~keep;
+}
+
+// The same for block jb of a query tile's walk, of which block `first` is the
+// first one counted and nv are there.
+__device__ __forceinline__ int32_t window_entry(const int32_t *table, int jb, int nv, int first, int sink_blocks,
+                                                int skip, int max_blocks) {
+    typedef const __attribute__((address_space(4))) int32_t const_i32;
+    const int j = first + max(min(jb, nv - 1), 0);
+    const int32_t b = ((const_i32 *)table)[min(j + (j >= sink_blocks ? skip : 0), max_blocks - 1)];
     const int32_t keep = -(int32_t)((unsigned)jb < (unsigned)nv);
     return b | ~keep;
 }
@@ -257,8 +284,9 @@ __device__ __forceinline__ void order_phase() {
 // without that code: the D = 128 loop has no register to spare, and the code
 // cost the 32-turn batch 0.9%.)
 // kSkip: waves skip the key tiles none of their rows sees.
-template <int D, bool kHost, bool kSplit, bool kSkip>
-__global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, PrefillPlanArg<kHost, kSplit> plan) {
+// kWin: rows see a window of keys and the first ones.
+template <int D, bool kHost, bool kSplit, bool kSkip, bool kWin = false>
+__global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin> a, PrefillPlanArg<kHost, kSplit> plan) {
     using C = Geo<D>;
     constexpr int KS = D / 32;           // 32-dim k-steps of QK
     constexpr int NDT = D / 16;          // 16-dim output tiles
@@ -299,7 +327,16 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
             nblk_valid = a.max_blocks;
             if (tid == 0) flag_error(a.err, LS_DEVERR_LENGTH);
         }
-        const int kv_end = c + j_last + 1;                    // keys this tile can see
+        // Blocks that the tile's walk leaves out, and the walk's length.
+        int window = 0, sinks = 0, sink_blocks = 0, skip = 0;
+        if constexpr (kWin) {
+            window = a.window;
+            sinks = a.sinks;
+            sink_blocks = (sinks + kBlock - 1) / kBlock;
+            skip = max(max(c + j0 - window + 1, 0) / kBlock - sink_blocks, 0);
+            nblk_valid = max(nblk_valid - skip, 0);
+        }
+        const int kv_end = c + j_last + 1 - skip * kBlock;    // keys this tile can see
         // This item's key tiles: [tile0, tile0 + ntiles).  Below, keys, blocks
         // and key tiles are counted from tile0.
         int tile0 = 0, ntiles = (kv_end + kKeyTile - 1) / kKeyTile;
@@ -308,10 +345,14 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
             tile0 = key_chunk(all, chunk, chunks);
             ntiles = key_chunk(all, chunk + 1, chunks) - tile0;
         }
-        const int key_base = tile0 * kKeyTile;
+        // (With a window every position below is one of the walk, from tile0 on.)
+        const int key_base = tile0 * kKeyTile + skip * kBlock;
         const int kv_len = c + n - key_base;
         int nb = min(nblk_valid - tile0 * 4, ntiles * 4);     // blocks any row here can see
-        if (kSplit) nb = max(nb, 0);                          // (a part past the end of the table)
+        if (kSplit || kWin) nb = max(nb, 0);                  // (a part past the end of the table)
+        // Keys [hole_lo, hole_hi) are seen by no row of the tile (its first row's hole).
+        const int hole_lo = sinks - tile0 * kKeyTile;
+        const int hole_hi = kWin ? c + j0 - window + 1 - key_base : 0;
 
         if (kSplit && chunks > 1 && ntiles <= 0) {             // a piece without keys
             for (int r = tid; r < kPreRows; r += kPreThreads) a.part_ml[((int64_t)piece * kPreRows + r) * 2] = kNoKey;
@@ -344,11 +385,37 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
             for (int ks = 0; ks < KS; ++ks)
                 qop[rt][ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + ks * 32 + g4 * 8));
         }
+        // With a window no key unit is seen by every row, so the running maximum
+        // starts from the row's score with the key at its own position, which it
+        // always sees.  The row sums then hold a term of 1 (in the part of the keys
+        // with that position), so keys whose probabilities vanish against it do
+        // not count, in whatever part they are.  Lane (c16, g4) loads row c16's
+        // own key as row c16 of a 16-key operand; a position outside the table or
+        // the pool gives zeros.
+        bf16x8 own_key[kWin ? kRT : 1][KS];
+        if constexpr (kWin) {
+    #pragma unroll
+            for (int rt = 0; rt < kRT; ++rt) {
+                const int pos = row_lim[rt] + key_base;
+                const int col = pos >> 4;                      // (kBlock tokens per column)
+                const bool in_table = pos >= 0 && col < a.max_blocks;
+                const int32_t b = a.block_tables[(int64_t)s * a.max_blocks + (in_table ? col : 0)];
+                const bool there = in_table && b >= 0 && b < a.num_blocks;
+                const uint16_t *kt = a.pool + ((int64_t)(there ? b : 0) * 2 * Hkv + g) * (kBlock * D);
+    #pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const u32x4 raw = *reinterpret_cast<const u32x4 *>(kt + ((ks * 4 + g4) * kBlock + (pos & 15)) * 8);
+                    own_key[rt][ks] = __builtin_bit_cast(bf16x8, there ? raw : u32x4{0u, 0u, 0u, 0u});
+                }
+            }
+        }
         // Wait for q here, before the first stage loads are issued, so that no
         // wait for q remains inside the key loop (vmcnt(0), other counters untouched).
         __builtin_amdgcn_s_waitcnt(0x0F70);
         // smallest causal limit among this wave's rows: units past it need masking
         const int wave_lim_min = c + min(j0 + (wave * kWaveRows) / G, n - 1) - key_base;
+        // end of its rows' longest hole
+        const int wave_hole_max = kWin ? c + min(j0 + (wave * kWaveRows + kWaveRows - 1) / G, n - 1) - key_base - window + 1 : 0;
 
         // Key tiles some row of this wave sees: none when its rows are all padding,
         // fewer than the workgroup's where the tile spans many tokens.  Past them
@@ -375,7 +442,11 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
             const int p = q * 64 + lane;
             v_voff[e] = (p % D) * 32 + (p / D) * 16;
         }
-        const int32_t *table = a.block_tables + (int64_t)s * a.max_blocks + (nb > 0 ? tile0 * 4 : 0);
+        const int32_t *table = a.block_tables + (int64_t)s * a.max_blocks + (!kWin && nb > 0 ? tile0 * 4 : 0);
+        auto entry = [&](int jb) {
+            if constexpr (kWin) return window_entry(table, jb, nb, tile0 * 4, sink_blocks, skip, a.max_blocks);
+            else return table_entry(table, jb, nb);
+        };
         const uint32_t slab_elems = (uint32_t)(2 * Hkv * kBlock * D);
         const uint32_t nblocks32 = (uint32_t)min(a.num_blocks, (int64_t)0x7fffffff);
         const uint16_t *kbase = a.pool + (int64_t)g * (kBlock * D);
@@ -388,8 +459,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
     #pragma unroll
             for (int e = 0; e < C::kLoadsK; ++e) load_kb<D>(vbase, slab_elems, nblocks32, b, stage + kb_off[e], v_voff[e]);
         };
-        auto id_k = [&](int t) { return table_entry(table, 4 * t + 2 + blk, nb); };
-        auto id_v = [&](int t) { return table_entry(table, 4 * t + blk, nb); };
+        auto id_k = [&](int t) { return entry(4 * t + 2 + blk); };
+        auto id_v = [&](int t) { return entry(4 * t + blk); };
 
         float nm[kRT], lsum[kRT];             // -m' (running row max * scale * log2 e),
         f32x4 o[kRT][NDT];                    // partial row sums, unnormalised output
@@ -452,7 +523,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
         // keys 8*g4 + 4*sb + i); only units that reach past the smallest causal
         // limit of the wave's rows need it.
         auto mask_unit = [&](f32x4 (&acc)[kRT][2], int key0) {
-            if (key0 + 31 <= wave_lim_min) return;
+            if (key0 + 31 <= wave_lim_min && !(kWin && key0 < wave_hole_max && key0 + 31 >= hole_lo)) return;
     #pragma unroll
             for (int rt = 0; rt < kRT; ++rt) {
                 const int lim = row_lim[rt] - key0 - 8 * g4;
@@ -460,7 +531,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
                 for (int sb = 0; sb < 2; ++sb)
     #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (4 * sb + i > lim) acc[rt][sb][i] = -INFINITY;
+                        if (4 * sb + i > lim || (kWin && 4 * sb + i >= hole_lo - key0 - 8 * g4 && 4 * sb + i <= lim - window))
+                            acc[rt][sb][i] = -INFINITY;
             }
         };
         // Largest of a lane's 8 values of one row tile (NaN-propagating).
@@ -561,18 +633,24 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
         // or blocks never loaded) are zeroed in the staged V tile of key tile j
         // before it is used, so that 0 * NaN cannot reach O.  Only the last key
         // tile can hold such keys; one extra LDS barrier, once per workgroup.
+        // With a window so are those of keys that no row of the tile sees, in the
+        // last block of the first tokens and the first one of the window.
         auto zero_v_tail = [&](uint8_t *lv, int j) {
             constexpr int kChunks = 4 * 2 * D;                    // (block, half, dim) chunks of 8 tokens
             for (int ci = tid; ci < kChunks; ci += kPreThreads) {
                 const int bi = ci / (2 * D), hf = (ci / D) & 1;
                 const int t0 = j * kKeyTile + bi * kBlock + hf * 8;
-                if (t0 + 8 <= kv_len) continue;
+                if (t0 + 8 <= kv_len && !(kWin && t0 < hole_hi && t0 + 8 > hole_lo)) continue;
                 u32x4 *chunk = reinterpret_cast<u32x4 *>(lv + ci * 16);
                 u32x4 x = *chunk;
     #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int t = t0 + 2 * w;
                     x[w] &= t + 1 < kv_len ? 0xFFFFFFFFu : (t < kv_len ? 0x0000FFFFu : 0u);
+                    if constexpr (kWin) {
+                        if (t >= hole_lo && t < hole_hi) x[w] &= 0xFFFF0000u;
+                        if (t + 1 >= hole_lo && t + 1 < hole_hi) x[w] &= 0x0000FFFFu;
+                    }
                 }
                 *chunk = x;
             }
@@ -628,16 +706,29 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
         // its probabilities are 0.
     #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) {
-            nm[rt] = -xmax16_32(lane_max(sa[rt])) * sl2;
-            if (kSplit && row_lim[rt] < 0) nm[rt] = 0.f;
+            if constexpr (kWin) {
+                // Score (A-row 4 g4 + i, row c16) of the own keys: the diagonal.
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    #pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(own_key[rt][ks], qop[rt][ks], acc, 0, 0, 0);
+                float x = -INFINITY;
+    #pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (4 * g4 + i == c16) x = acc[i];
+                nm[rt] = -xmax16_32(x) * sl2;
+            } else {
+                nm[rt] = -xmax16_32(lane_max(sa[rt])) * sl2;
+                if (kSplit && row_lim[rt] < 0) nm[rt] = 0.f;
+            }
         }
         // A row whose scores in the first unit are all -inf has no maximum to
         // start from: -inf - (-inf) is NaN, and a stand-in far below the scores
         // to come would cost them their low bits.  Any part can begin so, not
         // only the context; the row starts from its first unit that holds more,
         // found here with K straight from the pool (rare).  Without one its
-        // probabilities are 0.
-        if constexpr (kSplit) {
+        // probabilities are 0.  (With a window: a row whose own key scores -inf.)
+        if constexpr (kSplit || kWin) {
             auto lost = [&] {
                 bool any = false;
     #pragma unroll
@@ -645,8 +736,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
                 return __any(any);
             };
             if (lost()) {
-                for (int u = 1; u < 2 * wave_tiles && lost(); ++u) {
-                    const int32_t b0 = table_entry(table, 2 * u, nb), b1 = table_entry(table, 2 * u + 1, nb);
+                for (int u = kWin ? 0 : 1; u < 2 * wave_tiles && lost(); ++u) {
+                    const int32_t b0 = entry(2 * u), b1 = entry(2 * u + 1);
                     const uint32_t b = (uint32_t)(c16 >> 3 ? b1 : b0);
                     const bool there = b < nblocks32;
                     const uint16_t *kt = kbase + (uint64_t)(there ? b : 0u) * slab_elems;
@@ -692,7 +783,9 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
             idk = id_k(j + 3);
             idv = id_v(j + 3);
             const bool live = j < wave_tiles;
-            if (j < ntiles && (j + 1) * kKeyTile > kv_len) zero_v_tail(vs, j);
+            if (j < ntiles && ((j + 1) * kKeyTile > kv_len ||
+                               (kWin && j * kKeyTile < hole_hi && (j + 1) * kKeyTile > hole_lo)))
+                zero_v_tail(vs, j);
             load_k(kn, ik);
             load_v(vn, iv);
             if (live) {
@@ -748,7 +841,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
                 const float l = xsum16_32(lsum[rt]);
                 if (g4 == 0) {
                     // (a zero sum: every score of the row here is -inf)
-                    ml[rt * 32] = row_lim[rt] < 0 || l == 0.f ? kNoKey : -nm[rt];
+                    ml[rt * 32] = (!kWin && row_lim[rt] < 0) || l == 0.f ? kNoKey : -nm[rt];
                     ml[rt * 32 + 1] = l;
                 }
     #pragma unroll
@@ -889,7 +982,10 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgs a, Pre
             const int nt = max(a.cu[sp + 1] - a.cu[sp], 0);
             const int items = min((nt + qtok - 1) / qtok, QT);
             sm_items[p] = items;
-            sm_work[p] = (int64_t)items * (2 * (int64_t)max(a.ctx[sp], 0) + nt);
+            if constexpr (kWin)
+                sm_work[p] = (int64_t)items * min((int64_t)max(a.ctx[sp], 0) + nt, (int64_t)a.window + a.sinks + qtok);
+            else
+                sm_work[p] = (int64_t)items * (2 * (int64_t)max(a.ctx[sp], 0) + nt);
         }
         if (tid == 0 && (P & 1)) sm_work[P] = -1;              // pad to 2 (never counts)
         __syncthreads();
@@ -1114,8 +1210,10 @@ SplitChoice choose_split(const PrefillPair *pr, int np, int64_t cus) {   // pr: 
 
 // The pairs of the batch in session order; false when the batch exceeds the
 // plan's capacity (the device deals the schedule then).
-bool collect_pairs(int32_t S, int32_t hkv, int32_t qtok, const int32_t *lens, PrefillHostPlan &plan, PrefillPair *pr,
-                   int &np) {
+// With a window a tile's walk is at most the first tokens' blocks, the window and
+// the tile's tokens long.
+bool collect_pairs(int32_t S, int32_t hkv, int32_t qtok, const int32_t *lens, int32_t window, int32_t sinks,
+                   PrefillHostPlan &plan, PrefillPair *pr, int &np) {
     if (S > kPlanPairs || S * hkv > kPlanPairs) return false;
     np = 0;
     for (int s = 0; s < S; ++s) {
@@ -1124,9 +1222,13 @@ bool collect_pairs(int32_t S, int32_t hkv, int32_t qtok, const int32_t *lens, Pr
         if (items > 0xFFFF) return false;                  // beyond the plan's 16-bit counts
         plan.session_items[s] = (uint16_t)items;
         if (items == 0) continue;
-        const int64_t len = (int64_t)c + n;
+        int64_t len = (int64_t)c + n, twice = 2 * (int64_t)c + n;
+        if (window) {
+            len = std::min<int64_t>(len, (int64_t)window + sinks + qtok + 2 * kBlock - 2);
+            twice = std::min<int64_t>(twice, 2 * len);
+        }
         for (int g = 0; g < hkv; ++g)
-            pr[np++] = PrefillPair{(int64_t)items * (2 * (int64_t)c + n), len, s * hkv + g, items,
+            pr[np++] = PrefillPair{(int64_t)items * twice, len, s * hkv + g, items,
                                    (int32_t)((len + kKeyTile - 1) / kKeyTile)};
     }
     for (int s = S; s < kPlanPairs; ++s) plan.session_items[s] = 0;
@@ -1280,7 +1382,8 @@ bool prefill_split_items(int32_t num_sessions, int32_t num_kv_heads, int32_t gro
     int np = 0;
     int32_t split_tiles = 0;
     int64_t total = 0;
-    if (!collect_pairs(num_sessions, num_kv_heads, kPreRows / group, lens_host, plan, pairs_of, np) || np == 0) return true;
+    if (!collect_pairs(num_sessions, num_kv_heads, kPreRows / group, lens_host, 0, 0, plan, pairs_of, np) || np == 0)
+        return true;
     if (!plan_prefill_split(pairs_of, np, cus, plan, merge, split_tiles, total)) return true;
     if (total > room || split_tiles > merged_room) return false;
     for (int x = 0; x < kXcds; ++x) {
@@ -1304,28 +1407,12 @@ __global__ void clear_counters_kernel(uint32_t *counters) {
     if ((int)threadIdx.x < kPrefillCounters) counters[threadIdx.x] = 0u;
 }
 
-hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads,
-                          const uint16_t *q, const int32_t *cu_new_lens,
-                          const int32_t *reused_lens, const int32_t *lens_host, int32_t total_tokens,
-                          int32_t max_new_len, const int32_t *block_tables, int32_t max_blocks,
-                          float scale, uint16_t *out, void *workspace, size_t workspace_bytes, bool counters_cleared,
-                          unsigned int *err, hipStream_t stream) {
-    if (num_sessions <= 0 || max_new_len <= 0) return hipSuccess;
-    PrefillArgs a;
-    a.pool = p.layer_base(layer);
-    a.num_blocks = p.num_blocks;
-    a.num_kv_heads = p.num_kv_heads;
-    a.group = num_q_heads / p.num_kv_heads;
-    a.num_sessions = num_sessions;
-    a.total = total_tokens;
-    a.q = q;
-    a.out = out;
-    a.cu = cu_new_lens;
-    a.ctx = reused_lens;
-    a.block_tables = block_tables;
-    a.max_blocks = max_blocks;
-    a.scale_log2 = scale * kLog2eP;
-    a.err = err;
+namespace {
+
+template <bool kWin>
+hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32_t *lens_host, int32_t total_tokens,
+                            int32_t max_new_len, int32_t max_blocks, int32_t window, int32_t sinks, void *workspace,
+                            size_t workspace_bytes, bool counters_cleared, PrefillArgsT<kWin> &a, hipStream_t stream) {
     // Waves skip what none of their rows sees where that shortens the longest
     // tiles: the longest turn fits half a query tile, so that no SIMD runs two
     // waves with rows (2 turns of 18-24 tokens over 3854-6172, 4 heads per KV
@@ -1348,7 +1435,7 @@ hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, in
     PrefillSplitPlan plan;
     PrefillPair pairs_of[kPlanPairs];
     int np = 0;
-    if (lens_host && collect_pairs(num_sessions, p.num_kv_heads, qtok, lens_host, plan, pairs_of, np)) {
+    if (lens_host && collect_pairs(num_sessions, p.num_kv_heads, qtok, lens_host, window, sinks, plan, pairs_of, np)) {
         if (np == 0) return hipSuccess;
         // Items are taken through the counters of a workspace; ~10% more
         // workgroups than items let the faster XCDs take over the slower ones'
@@ -1375,14 +1462,15 @@ hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, in
             a.part_o = reinterpret_cast<float *>(parts + (size_t)kPrefillSplitPieces * kPreRows * 2 * sizeof(float));
             const dim3 grid = queue_grid(items), mgrid((unsigned)(split_tiles * (kPreWaves * kRT * p.head_dim / 16 / kMergeWaves)));
             if (p.head_dim == 128)
-                hipLaunchKernelGGL((prefill_kernel<128, true, true, true>), grid, dim3(kPreThreads), 0, stream, a, plan);
+                hipLaunchKernelGGL((prefill_kernel<128, true, true, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, plan);
             else
-                hipLaunchKernelGGL((prefill_kernel<64, true, true, true>), grid, dim3(kPreThreads), 0, stream, a, plan);
+                hipLaunchKernelGGL((prefill_kernel<64, true, true, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, plan);
             if (hipError_t e = hipGetLastError()) return e;
+            const PrefillArgs &m = a;
             if (p.head_dim == 128)
-                hipLaunchKernelGGL(prefill_merge_kernel<128>, mgrid, dim3(kMergeThreads), 0, stream, a, merge);
+                hipLaunchKernelGGL(prefill_merge_kernel<128>, mgrid, dim3(kMergeThreads), 0, stream, m, merge);
             else
-                hipLaunchKernelGGL(prefill_merge_kernel<64>, mgrid, dim3(kMergeThreads), 0, stream, a, merge);
+                hipLaunchKernelGGL(prefill_merge_kernel<64>, mgrid, dim3(kMergeThreads), 0, stream, m, merge);
             return hipGetLastError();
         }
         // (The split planner may have reordered the pairs: back to session order.)
@@ -1397,13 +1485,13 @@ hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, in
         }
         const PrefillHostPlan &whole = plan;
         if (p.head_dim == 128 && skip)
-            hipLaunchKernelGGL((prefill_kernel<128, true, false, true>), grid, dim3(kPreThreads), 0, stream, a, whole);
+            hipLaunchKernelGGL((prefill_kernel<128, true, false, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
         else if (p.head_dim == 128)
-            hipLaunchKernelGGL((prefill_kernel<128, true, false, false>), grid, dim3(kPreThreads), 0, stream, a, whole);
+            hipLaunchKernelGGL((prefill_kernel<128, true, false, false, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
         else if (skip)
-            hipLaunchKernelGGL((prefill_kernel<64, true, false, true>), grid, dim3(kPreThreads), 0, stream, a, whole);
+            hipLaunchKernelGGL((prefill_kernel<64, true, false, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
         else
-            hipLaunchKernelGGL((prefill_kernel<64, true, false, false>), grid, dim3(kPreThreads), 0, stream, a, whole);
+            hipLaunchKernelGGL((prefill_kernel<64, true, false, false, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
         return hipGetLastError();
     }
     // An XCD holds at most ceil(pairs / 8) pairs of at most qtiles items each;
@@ -1415,14 +1503,46 @@ hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, in
     const PrefillNoPlan none{0};
     const dim3 g((unsigned)grid);
     if (p.head_dim == 128 && skip)
-        hipLaunchKernelGGL((prefill_kernel<128, false, false, true>), g, dim3(kPreThreads), 0, stream, a, none);
+        hipLaunchKernelGGL((prefill_kernel<128, false, false, true, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
     else if (p.head_dim == 128)
-        hipLaunchKernelGGL((prefill_kernel<128, false, false, false>), g, dim3(kPreThreads), 0, stream, a, none);
+        hipLaunchKernelGGL((prefill_kernel<128, false, false, false, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
     else if (skip)
-        hipLaunchKernelGGL((prefill_kernel<64, false, false, true>), g, dim3(kPreThreads), 0, stream, a, none);
+        hipLaunchKernelGGL((prefill_kernel<64, false, false, true, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
     else
-        hipLaunchKernelGGL((prefill_kernel<64, false, false, false>), g, dim3(kPreThreads), 0, stream, a, none);
+        hipLaunchKernelGGL((prefill_kernel<64, false, false, false, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
     return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads,
+                          const uint16_t *q, const int32_t *cu_new_lens,
+                          const int32_t *reused_lens, const int32_t *lens_host, int32_t total_tokens,
+                          int32_t max_new_len, const int32_t *block_tables, int32_t max_blocks,
+                          float scale, uint16_t *out, void *workspace, size_t workspace_bytes, bool counters_cleared,
+                          int32_t window, int32_t sinks, unsigned int *err, hipStream_t stream) {
+    if (num_sessions <= 0 || max_new_len <= 0) return hipSuccess;
+    PrefillWindowArgs a;
+    a.pool = p.layer_base(layer);
+    a.num_blocks = p.num_blocks;
+    a.num_kv_heads = p.num_kv_heads;
+    a.group = num_q_heads / p.num_kv_heads;
+    a.num_sessions = num_sessions;
+    a.total = total_tokens;
+    a.q = q;
+    a.out = out;
+    a.cu = cu_new_lens;
+    a.ctx = reused_lens;
+    a.block_tables = block_tables;
+    a.max_blocks = max_blocks;
+    a.scale_log2 = scale * kLog2eP;
+    a.err = err;
+    a.window = window;
+    a.sinks = sinks;
+    return window ? launch_prefill_t<true>(p, num_sessions, lens_host, total_tokens, max_new_len, max_blocks, window, sinks,
+                                           workspace, workspace_bytes, counters_cleared, a, stream)
+                  : launch_prefill_t<false>(p, num_sessions, lens_host, total_tokens, max_new_len, max_blocks, 0, 0,
+                                            workspace, workspace_bytes, counters_cleared, a, stream);
 }
 
 }  // namespace ls

@@ -48,6 +48,15 @@ _lib.paged_attn_decode_static.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _p, 
                                           _p, _p]
 _lib.paged_attn_prefill.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _i32, _i32, _p,
                                     _i32, _f32, _p, _p, _sz, _p]
+_lib.ls_decode_window_workspace_bytes.argtypes = [_p, _i32, _i32, _i32, _i32, _i32]
+_lib.ls_decode_window_workspace_bytes.restype = _sz
+_lib.paged_attn_decode_window.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _p, _i32, _p, _p, _i32, _i32,
+                                          _f32, _p, _p, _sz, _p]
+_lib.paged_attn_prefill_window.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _i32, _i32, _p,
+                                           _i32, _i32, _i32, _f32, _p, _p, _sz, _p]
+_lib.kv_tables_update.argtypes = [_p, _i32, _p, _p, _p, _i32, _p, _i32, _p, _p, _i32, _i32, _i32, _i32,
+                                  _p, _p, _p, _p, _p]
+_lib.kv_append.argtypes = [_p, _i32, _i32, _p, _p, _i64, _i64, _p, _p, _p]
 _f64 = ctypes.c_double
 _lib.kv_blocks_stash.argtypes = [_p, _i32, _p, _p, _p, _sz, _i32, _p, _sz, _f64, _p]
 _lib.kv_blocks_restore.argtypes = [_p, _i32, _p, _p, _p, _sz, _i32, _p, _sz, _f64, _p]
@@ -58,13 +67,14 @@ _lib.ls_last_error.restype = ctypes.c_char_p
 _lib.ls_version.restype = ctypes.c_char_p
 for _f in (_lib.kv_pool_create, _lib.kv_pool_destroy, _lib.paged_attn_decode,
            _lib.paged_attn_decode_static,
-           _lib.paged_attn_prefill, _lib.kv_blocks_stash, _lib.kv_blocks_restore,
+           _lib.paged_attn_prefill, _lib.paged_attn_decode_window, _lib.paged_attn_prefill_window,
+           _lib.kv_tables_update, _lib.kv_append, _lib.kv_blocks_stash, _lib.kv_blocks_restore,
            _lib.kv_blocks_restore_layers,
            _lib.ls_device_errors):
     _f.restype = ctypes.c_int
 
 LS_OK, LS_EINVAL, LS_ENOMEM, LS_EHIP, LS_EUNSUPPORTED = 0, -22, -12, -5, -95
-LS_DEVERR_BLOCK_ID, LS_DEVERR_LENGTH, LS_DEVERR_INTERNAL = 0x1, 0x2, 0x4
+LS_DEVERR_BLOCK_ID, LS_DEVERR_LENGTH, LS_DEVERR_INTERNAL, LS_DEVERR_FREE_LIST = 0x1, 0x2, 0x4, 0x8
 PREFILL_COUNTER_BYTES = 256            # LS_PREFILL_COUNTER_BYTES
 PREFILL_WORKSPACE_BYTES = 68157696     # LS_PREFILL_WORKSPACE_BYTES
 
@@ -281,22 +291,8 @@ def paged_attn_decode_static(pool: KVPool, layer: int, q: torch.Tensor, block_ta
     return out
 
 
-def paged_attn_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: torch.Tensor,
-                       reused_lens: torch.Tensor, max_new_len: int, block_tables: torch.Tensor,
-                       scale: float, out: torch.Tensor, k_new: Optional[torch.Tensor] = None,
-                       v_new: Optional[torch.Tensor] = None, lens_host=None,
-                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """q/out: [T][Hq][D] bf16; cu_new_lens int32 [S+1]; reused_lens int32 [S];
-    k_new/v_new [T][Hkv][D] bf16; lens_host: optional host [S][2] of (n_s, c_s);
-    workspace: optional device tensor of PREFILL_WORKSPACE_BYTES bytes (item
-    counters that let faster XCDs take over the slower ones' last tiles, and room
-    for partial results when few query tiles have their keys split over the GPU;
-    used with lens_host; PREFILL_COUNTER_BYTES are enough for the counters alone)."""
-    if q.dim() != 3:
-        raise ValueError("q must be [T][Hq][D]")
-    total, hq = q.shape[0], q.shape[1]
-    s = reused_lens.shape[0] if reused_lens.dim() == 1 else -1
-    d, hkv = pool.head_dim, pool.num_kv_heads
+def _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new):
+    """Shapes, types and devices of a prefill call's tensors (raises ValueError)."""
     rows, new = (total, hq, d), (total, hkv, d)
     if not (_fits(q, rows, _BF16) and _fits(out, rows, _BF16) and _fits(reused_lens, (s,), _I32)
             and _fits(cu_new_lens, (s + 1,), _I32) and block_tables.dim() == 2
@@ -315,6 +311,25 @@ def paged_attn_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: t
                         (v_new, "v_new")):
             if t is not None:
                 _dev(t, name)
+
+
+def paged_attn_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: torch.Tensor,
+                       reused_lens: torch.Tensor, max_new_len: int, block_tables: torch.Tensor,
+                       scale: float, out: torch.Tensor, k_new: Optional[torch.Tensor] = None,
+                       v_new: Optional[torch.Tensor] = None, lens_host=None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q/out: [T][Hq][D] bf16; cu_new_lens int32 [S+1]; reused_lens int32 [S];
+    k_new/v_new [T][Hkv][D] bf16; lens_host: optional host [S][2] of (n_s, c_s);
+    workspace: optional device tensor of PREFILL_WORKSPACE_BYTES bytes (item
+    counters that let faster XCDs take over the slower ones' last tiles, and room
+    for partial results when few query tiles have their keys split over the GPU;
+    used with lens_host; PREFILL_COUNTER_BYTES are enough for the counters alone)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [T][Hq][D]")
+    total, hq = q.shape[0], q.shape[1]
+    s = reused_lens.shape[0] if reused_lens.dim() == 1 else -1
+    d, hkv = pool.head_dim, pool.num_kv_heads
+    _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new)
     keep, hl = _host_i32(lens_host, "lens_host", 2 * s)
     if workspace is not None:
         _dev(workspace, "workspace")
@@ -326,6 +341,135 @@ def paged_attn_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: t
            "paged_attn_prefill")
     del keep
     return out
+
+
+def decode_window_workspace_bytes(pool: KVPool, num_sessions: int, num_q_heads: int,
+                                  max_blocks_per_session: int, window: int, sinks: int = 0) -> int:
+    return int(_lib.ls_decode_window_workspace_bytes(pool.handle, num_sessions, num_q_heads,
+                                                     max_blocks_per_session, window, sinks))
+
+
+def paged_attn_decode_window(pool: KVPool, layer: int, q: torch.Tensor, block_tables: torch.Tensor,
+                             context_lens: torch.Tensor, window: int, sinks: int, scale: float,
+                             out: torch.Tensor, workspace: torch.Tensor,
+                             k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                             context_lens_host=None, stream=None) -> torch.Tensor:
+    """paged_attn_decode whose query sees the last ``window`` keys (its own position included) and
+    the first ``sinks``; workspace of decode_window_workspace_bytes."""
+    if q.dim() != 3:
+        raise ValueError("q must be [S][Hq][D]")
+    s, hq = q.shape[0], q.shape[1]
+    d, hkv = pool.head_dim, pool.num_kv_heads
+    _decode_args(s, hq, hkv, d, q, out, block_tables, context_lens, k_new, v_new)
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        _dev(workspace, "workspace")
+    keep, hl = _host_i32(context_lens_host, "context_lens_host", s)
+    _check(_lib.paged_attn_decode_window(pool.handle, layer, s, hq, _ptr(q), _ptr(k_new), _ptr(v_new),
+                                         _ptr(block_tables), block_tables.shape[1], _ptr(context_lens), hl,
+                                         window, sinks, float(scale), _ptr(out), _ptr(workspace),
+                                         _nbytes(workspace), _stream(stream)),
+           "paged_attn_decode_window")
+    del keep
+    return out
+
+
+def paged_attn_prefill_window(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: torch.Tensor,
+                              reused_lens: torch.Tensor, max_new_len: int, block_tables: torch.Tensor,
+                              window: int, sinks: int, scale: float, out: torch.Tensor,
+                              k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                              lens_host=None, workspace: Optional[torch.Tensor] = None,
+                              stream=None) -> torch.Tensor:
+    """paged_attn_prefill whose rows see the last ``window`` keys (their own position included) and
+    the first ``sinks``."""
+    if q.dim() != 3:
+        raise ValueError("q must be [T][Hq][D]")
+    total, hq = q.shape[0], q.shape[1]
+    s = reused_lens.shape[0] if reused_lens.dim() == 1 else -1
+    d, hkv = pool.head_dim, pool.num_kv_heads
+    _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new)
+    keep, hl = _host_i32(lens_host, "lens_host", 2 * s)
+    if workspace is not None:
+        _dev(workspace, "workspace")
+    _check(_lib.paged_attn_prefill_window(pool.handle, layer, s, hq, _ptr(q), _ptr(k_new), _ptr(v_new),
+                                          _ptr(cu_new_lens), _ptr(reused_lens), hl, total,
+                                          int(max_new_len), _ptr(block_tables), block_tables.shape[1],
+                                          window, sinks, float(scale), _ptr(out), _ptr(workspace),
+                                          0 if workspace is None else _nbytes(workspace), _stream(stream)),
+           "paged_attn_prefill_window")
+    del keep
+    return out
+
+
+_I64 = (torch.int64,)
+
+
+def _vector(t: torch.Tensor, name: str, n, dtypes):
+    """Check a contiguous device vector of n values (None: any number)."""
+    if not (t.is_cuda and t.dtype in dtypes and t.dim() == 1 and (n is None or t.shape[0] == n) and t.is_contiguous()):
+        _shape(t, name, (n,), dtypes)
+        _dev(t, name)
+
+
+def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tensor, max_new_len: int,
+                     block_tables: torch.Tensor, next_lens: torch.Tensor, cu_new_lens: torch.Tensor,
+                     reused_lens: Optional[torch.Tensor], slot_map: torch.Tensor,
+                     free_ring: Optional[torch.Tensor] = None, free_counts: Optional[torch.Tensor] = None,
+                     next_counts: Optional[torch.Tensor] = None, window: int = 0, sinks: int = 0,
+                     stream=None) -> torch.Tensor:
+    """A step's tables, slots and lengths from seq_lens and new_lens (int32 [S]): writes the new
+    blocks' entries of block_tables int32 [S][maxb], next_lens and reused_lens int32 [S],
+    cu_new_lens int32 [S+1] and slot_map int64 [T] (-1 behind the last token); free_ring int32 [R]
+    with free_counts -> next_counts int64 [2] = (taken, given).  next_lens may be seq_lens,
+    next_counts free_counts."""
+    s = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
+    for t, name, n in ((seq_lens, "seq_lens", s), (new_lens, "new_lens", s), (next_lens, "next_lens", s),
+                       (cu_new_lens, "cu_new_lens", s + 1), (reused_lens, "reused_lens", s),
+                       (free_ring, "free_ring", None)):
+        if t is not None:
+            _vector(t, name, n, _I32)
+    _vector(slot_map, "slot_map", None, _I64)
+    for t, name in ((free_counts, "free_counts"), (next_counts, "next_counts")):
+        if t is not None:
+            _vector(t, name, 2, _I64)
+    if not (block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32)):
+        _shape(block_tables, "block_tables", (s, None), torch.int32)
+        _dev(block_tables, "block_tables")
+    _check(_lib.kv_tables_update(pool.handle, s, _ptr(seq_lens), _ptr(new_lens), _ptr(block_tables),
+                                 block_tables.shape[1], _ptr(free_ring),
+                                 0 if free_ring is None else free_ring.shape[0], _ptr(free_counts),
+                                 _ptr(next_counts), window, sinks, slot_map.shape[0], int(max_new_len),
+                                 _ptr(next_lens), _ptr(cu_new_lens), _ptr(reused_lens), _ptr(slot_map),
+                                 _stream(stream)),
+           "kv_tables_update")
+    return slot_map
+
+
+def _rows(t: torch.Tensor, name: str, shape) -> int:
+    """Check rows [T][Hkv][D] of a device tensor, each row contiguous; elements from row to row."""
+    _shape(t, name, shape, _BF16)
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if shape[0] and (t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2])):
+        raise ValueError("each row of %s must be contiguous" % name)
+    return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+
+
+def kv_append(pool: KVPool, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, slot_map: torch.Tensor,
+              slot_map_host=None, stream=None) -> None:
+    """Write rows k_new, v_new [T][Hkv][D] (bf16; rows may be strided, as views of a fused projection
+    are) into the slots of slot_map int64 [T] (negative: left out)."""
+    shape = (slot_map.shape[0] if slot_map.dim() == 1 else -1, pool.num_kv_heads, pool.head_dim)
+    _vector(slot_map, "slot_map", None, _I64)
+    ks, vs = _rows(k_new, "k_new", shape), _rows(v_new, "v_new", shape)
+    keep = None
+    if slot_map_host is not None:
+        keep = np.ascontiguousarray(np.asarray(slot_map_host).reshape(-1), dtype=np.int64)
+        if keep.size != shape[0]:
+            raise ValueError("slot_map_host must hold %d values (got %d)" % (shape[0], keep.size))
+    _check(_lib.kv_append(pool.handle, layer, shape[0], _ptr(k_new), _ptr(v_new), ks, vs, _ptr(slot_map),
+                          None if keep is None else keep.__array_interface__["data"][0], _stream(stream)),
+           "kv_append")
+    del keep
 
 
 def _host_ids(ids):
