@@ -98,30 +98,130 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(
     }
 }
 
-// Thread = 8 dims of one row of one KV head: a 16-byte chunk of the K tile, and
-// 8 values, 32 bytes apart, of the V tile.
+// Workgroup (kRows consecutive rows, KV head).  Bound by bandwidth (every row is
+// read and written once), or by latency when there are few.  K goes straight
+// from registers to its tile: a wave moves 16 rows x 4 chunks of 16 bytes, so
+// that consecutive slots make 256 contiguous bytes.  V is turned through LDS: a
+// slot's values lie 32 bytes apart in the dim-major tile, and only with the
+// neighbouring slots at hand do they make whole 16-byte stores.  The rows are
+// therefore cut into segments, of consecutive rows in consecutive slots of one
+// block, and a segment belongs to the workgroup that holds its first row, which
+// reads up to 15 rows of the next workgroup's for it (which then skips them):
+// any order of slots is served, runs of a session's tokens by whole 32-byte
+// lines.  Half segments shorter than 8 slots are stored value by value; a read,
+// a merge and a wider write would race with other calls' slots of the block.
+constexpr int kAppendAhead = 15;                  // rows past its own that a workgroup may read
+
+template <int D, int kRows>
 __global__ __launch_bounds__(kAppendThreads) void append_slots_kernel(
-    uint16_t *__restrict__ layer_pool, int64_t num_blocks, int32_t num_kv_heads, int32_t head_dim,
-    const uint16_t *__restrict__ k_new, const uint16_t *__restrict__ v_new, int64_t k_stride, int64_t v_stride,
-    const int64_t *__restrict__ slots, int64_t chunks, unsigned int *err) {
-    const int per_head = head_dim / 8, per_row = num_kv_heads * per_head;
-    for (int64_t c = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x; c < chunks; c += (int64_t)gridDim.x * kAppendThreads) {
-        const int64_t row = c / per_row;
-        const int in_row = (int)(c % per_row), g = in_row / per_head, d8 = in_row % per_head;
-        const int64_t slot = slots[row];
-        if (slot < 0) continue;
-        if (slot >= num_blocks * kBlock) {
-            flag_error(err, LS_DEVERR_BLOCK_ID);
-            continue;
-        }
-        const int t = (int)(slot % kBlock);
-        uint16_t *ktile = layer_pool + ((slot / kBlock) * 2 * num_kv_heads + g) * (kBlock * head_dim);
-        uint16_t *vtile = ktile + (int64_t)num_kv_heads * (kBlock * head_dim);
-        *reinterpret_cast<u32x4 *>(ktile + (d8 * kBlock + t) * 8) =
-            *reinterpret_cast<const u32x4 *>(k_new + row * k_stride + in_row * 8);
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(v_new + row * v_stride + in_row * 8);
+    uint16_t *__restrict__ layer_pool, int64_t num_blocks, int32_t num_kv_heads, const uint16_t *__restrict__ k_new,
+    const uint16_t *__restrict__ v_new, int64_t k_stride, int64_t v_stride, const int64_t *__restrict__ slots,
+    int32_t total, unsigned int *err) {
+    static_assert(kRows + kAppendAhead < kWave && kRows % kBlock == 0, "a lane per row, and the row that ends the last segment");
+    constexpr int kChunks = D / 8;                              // 16-byte chunks of a row
+    constexpr int kPitch = D + 8;                               // (16 bytes of padding: a column's two halves in distinct banks)
+    __shared__ __attribute__((aligned(16))) uint16_t sv[kRows + kAppendAhead][kPitch];
+    __shared__ int64_t sm_slot[kWave];                          // -1: left out
+    __shared__ int64_t sm_tile[kRows];                          // segments: V tile (elements from block 0's),
+    __shared__ uint32_t sm_segment[kRows];                      // first row | first slot << 8 | rows << 16
+    __shared__ int sm_segments, sm_begin, sm_end;               // rows [begin, end) are in segments that start here
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int g = blockIdx.y;
+    const int64_t row0 = (int64_t)blockIdx.x * kRows;
+    const int rows = (int)min((int64_t)kRows + kAppendAhead, total - row0);      // rows there are to look at
+    // K rows, and with few rows, where latency counts, V rows too, are requested
+    // before the slots are known.
+    auto k_row = [&](int c) { return c % kBlock + c / (kBlock * kChunks) * kBlock; };
+    auto k_chunk = [&](int c) { return c / kBlock % kChunks; };
+    constexpr int kLoadsK = (kRows * kChunks + kAppendThreads - 1) / kAppendThreads;
+    constexpr bool kEarly = kRows == kBlock;
+    u32x4 kreg[kLoadsK], vreg[kEarly ? kLoadsK : 1];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vtile[(d8 * 8 + e) * kBlock + t] = (uint16_t)(v[e / 2] >> (16 * (e % 2)));
+    for (int i = 0; i < kLoadsK; ++i) {
+        const int c = tid + i * kAppendThreads, r = min(k_row(c), rows - 1);
+        if (kRows * kChunks % kAppendThreads == 0 || c < kRows * kChunks)
+            kreg[i] = *reinterpret_cast<const u32x4 *>(k_new + (row0 + r) * k_stride + g * D + k_chunk(c) * 8);
+    }
+    if constexpr (kEarly)
+#pragma unroll
+        for (int i = 0; i < kLoadsK; ++i) {
+            const int c = tid + i * kAppendThreads, r = min(c / kChunks, rows - 1);
+            if (kRows * kChunks % kAppendThreads == 0 || c < kRows * kChunks)
+                vreg[i] = *reinterpret_cast<const u32x4 *>(v_new + (row0 + r) * v_stride + g * D + c % kChunks * 8);
+        }
+    if (wave == 0) {
+        const int64_t raw = lane < rows ? slots[row0 + lane] : -1;
+        const bool past = raw >= num_blocks * kBlock;
+        if (past && lane < kRows && g == 0) flag_error(err, LS_DEVERR_BLOCK_ID);
+        const int64_t slot = past ? -1 : raw;
+        int64_t before = __shfl_up(slot, 1);
+        if (lane == 0) before = row0 > 0 ? slots[row0 - 1] : -1;
+        // (a row left out counts as a first row, and is dropped from the list)
+        const bool first = slot < 0 || before < 0 || slot != before + 1 || slot % kBlock == 0;
+        const uint64_t firsts = __ballot(first);
+        const uint64_t mine = __ballot(first && slot >= 0 && lane < kRows);
+        if ((mine >> lane) & 1) {
+            const int k = __popcll(mine & ((1ull << lane) - 1));
+            const uint32_t n = (uint32_t)__builtin_ctzll(firsts >> (lane + 1)) + 1;      // (the lanes past the rows are firsts)
+            sm_segment[k] = (uint32_t)lane | (uint32_t)(slot % kBlock) << 8 | n << 16;
+            sm_tile[k] = ((slot / kBlock) * 2 + 1) * num_kv_heads * (kBlock * D);
+        }
+        sm_slot[lane] = slot;
+        if (lane == 0) {
+            const int last = mine ? 63 - __builtin_clzll(mine) : 0;
+            sm_segments = __popcll(mine);
+            sm_begin = mine ? __builtin_ctzll(mine) : 0;
+            sm_end = mine ? last + 1 + __builtin_ctzll(firsts >> (last + 1)) : 0;
+        }
+    }
+    __syncthreads();
+    const int begin = sm_begin, end = sm_end, segments = sm_segments;
+    const int64_t tile = (int64_t)kBlock * D;
+    uint16_t *const head = layer_pool + g * tile;               // K tile of block 0
+    // ---- V rows to LDS
+    if constexpr (kEarly)
+#pragma unroll
+        for (int i = 0; i < kLoadsK; ++i) {
+            const int c = tid + i * kAppendThreads;
+            if (c < kRows * kChunks) *reinterpret_cast<u32x4 *>(&sv[c / kChunks][c % kChunks * 8]) = vreg[i];
+        }
+    for (int c = tid + (kEarly ? kRows * kChunks : 0); c < (kRows + kAppendAhead) * kChunks; c += kAppendThreads) {
+        const int r = c / kChunks, d8 = c % kChunks;
+        if (r >= begin && r < end)
+            *reinterpret_cast<u32x4 *>(&sv[r][d8 * 8]) =
+                *reinterpret_cast<const u32x4 *>(v_new + (row0 + r) * v_stride + g * D + d8 * 8);
+    }
+    // ---- K
+#pragma unroll
+    for (int i = 0; i < kLoadsK; ++i) {
+        const int c = tid + i * kAppendThreads;
+        if (c >= kRows * kChunks) break;
+        const int64_t slot = sm_slot[k_row(c)];
+        if (slot < 0) continue;
+        uint16_t *ktile = head + (slot / kBlock) * 2 * num_kv_heads * tile;
+        *reinterpret_cast<u32x4 *>(ktile + (k_chunk(c) * kBlock + slot % kBlock) * 8) = kreg[i];
+    }
+    __syncthreads();
+    // ---- V: a thread has one dim of every (kAppendThreads / D)-th segment.
+    const int d = tid % D;
+    for (int k = tid / D; k < segments; k += kAppendThreads / D) {
+        const uint32_t seg = sm_segment[k];
+        uint16_t *dst = head + sm_tile[k] + d * kBlock;
+        const int o = (int)(seg >> 8) & 0xFF, end_slot = o + (int)(seg >> 16);
+        const uint16_t *src = &sv[seg & 0xFF][d] - o * kPitch;  // slot t's value: src[t * kPitch]
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int lo = max(o, half * 8), hi = min(end_slot, half * 8 + 8);
+            if (hi - lo == 8) {
+                u32x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    w[e] = src[(half * 8 + 2 * e) * kPitch] | (uint32_t)src[(half * 8 + 2 * e + 1) * kPitch] << 16;
+                *reinterpret_cast<u32x4 *>(dst + half * 8) = w;
+            } else {
+                for (int t = lo; t < hi; ++t) dst[t] = src[t * kPitch];
+            }
+        }
     }
 }
 
@@ -130,11 +230,21 @@ __global__ __launch_bounds__(kAppendThreads) void append_slots_kernel(
 hipError_t launch_append_slots(const PoolGeom &p, int layer, int32_t total_tokens, const uint16_t *k_new,
                                const uint16_t *v_new, int64_t k_stride, int64_t v_stride, const int64_t *slot_map,
                                unsigned int *err, hipStream_t stream) {
-    const int64_t chunks = (int64_t)total_tokens * p.num_kv_heads * (p.head_dim / 8);
-    const int64_t grid = (chunks + kAppendThreads - 1) / kAppendThreads;
-    hipLaunchKernelGGL(append_slots_kernel, dim3((unsigned)(grid < 65536 ? grid : 65536)), dim3(kAppendThreads), 0, stream,
-                       p.layer_base(layer), p.num_blocks, p.num_kv_heads, p.head_dim, k_new, v_new, k_stride, v_stride,
-                       slot_map, chunks, err);
+    // 48 rows per workgroup where that gives every CU two workgroups, else 16.
+    const int64_t wide = ((int64_t)total_tokens + 47) / 48;
+    const bool many = wide * p.num_kv_heads >= 2 * (p.num_cus > 0 ? p.num_cus : 256);
+    const dim3 grid((unsigned)(many ? wide : ((int64_t)total_tokens + 15) / 16), (unsigned)p.num_kv_heads);
+#define LS_APPEND(DD, ROWS) \
+    hipLaunchKernelGGL((append_slots_kernel<DD, ROWS>), grid, dim3(kAppendThreads), 0, stream, p.layer_base(layer), \
+                       p.num_blocks, p.num_kv_heads, k_new, v_new, k_stride, v_stride, slot_map, total_tokens, err)
+    if (p.head_dim == 128) {
+        if (many) LS_APPEND(128, 48);
+        else LS_APPEND(128, 16);
+    } else {
+        if (many) LS_APPEND(64, 48);
+        else LS_APPEND(64, 16);
+    }
+#undef LS_APPEND
     return hipGetLastError();
 }
 

@@ -458,15 +458,22 @@ def kv_append(pool: KVPool, layer: int, k_new: torch.Tensor, v_new: torch.Tensor
               slot_map_host=None, stream=None) -> None:
     """Write rows k_new, v_new [T][Hkv][D] (bf16; rows may be strided, as views of a fused projection
     are) into the slots of slot_map int64 [T] (negative: left out)."""
-    shape = (slot_map.shape[0] if slot_map.dim() == 1 else -1, pool.num_kv_heads, pool.head_dim)
-    _vector(slot_map, "slot_map", None, _I64)
-    ks, vs = _rows(k_new, "k_new", shape), _rows(v_new, "v_new", shape)
+    h, d = pool.num_kv_heads, pool.head_dim
+    shape = (slot_map.shape[0] if slot_map.dim() == 1 else -1, h, d)
+    kst, vst = k_new.stride(), v_new.stride()
+    if (k_new.shape == shape and v_new.shape == shape and kst[1:] == (d, 1) and vst[1:] == (d, 1) and k_new.is_cuda
+            and v_new.is_cuda and k_new.dtype in _BF16 and v_new.dtype in _BF16 and slot_map.is_cuda
+            and slot_map.dtype in _I64 and slot_map.is_contiguous() and shape[0] > 1):
+        ks, vs = kst[0], vst[0]
+    else:
+        _vector(slot_map, "slot_map", None, _I64)
+        ks, vs = _rows(k_new, "k_new", shape), _rows(v_new, "v_new", shape)
     keep = None
     if slot_map_host is not None:
         keep = np.ascontiguousarray(np.asarray(slot_map_host).reshape(-1), dtype=np.int64)
         if keep.size != shape[0]:
             raise ValueError("slot_map_host must hold %d values (got %d)" % (shape[0], keep.size))
-    _check(_lib.kv_append(pool.handle, layer, shape[0], _ptr(k_new), _ptr(v_new), ks, vs, _ptr(slot_map),
+    _check(_lib.kv_append(pool.handle, layer, shape[0], k_new.data_ptr(), v_new.data_ptr(), ks, vs, slot_map.data_ptr(),
                           None if keep is None else keep.__array_interface__["data"][0], _stream(stream)),
            "kv_append")
     del keep
