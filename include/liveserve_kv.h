@@ -346,7 +346,7 @@ ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num
  *                 attention still reads them: enqueue it before the next
  *                 kv_tables_update on the same ring.  Blocks behind the window of
  *                 seq_lens[s] count as given back before.  0: none are given back
- *   total_new_tokens   host int: slots in slot_map, >= the sum of new_lens
+ *   total_new_tokens   host int below 2^31 - 1: slots in slot_map, >= the sum of new_lens
  *   max_new_len        host int: no new_lens[s] is larger
  *   next_lens     device int32 [num_sessions]: seq_lens[s] + new_lens[s]
  *   cu_new_lens   device int32 [num_sessions + 1]: prefix sums of new_lens
@@ -357,14 +357,14 @@ ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num
  *
  * Inputs and outputs are apart, so a call can be made again with the same
  * result; next_lens may be seq_lens and next_counts free_counts, for a loop that
- * advances itself.  All sessions are served or none: a length out of range, one
+ * advances itself; no other arrays may overlap.  All sessions are served or none: a length out of range, one
  * that does not fit its table, or more rows than total_new_tokens is flagged
  * LS_DEVERR_LENGTH, and too few free blocks or no room in the ring
  * LS_DEVERR_FREE_LIST; then tables, ring and counters stay as they are (next_counts =
  * free_counts, next_lens = seq_lens), cu_new_lens is all 0 and slot_map all -1.  An id
  * outside the pool is copied as it stands and flagged (LS_DEVERR_BLOCK_ID), its
  * tokens' slots are -1.  The pool gives the range of ids; its memory is not touched.
- * Errors: LS_EINVAL (NULL or misaligned pointers, negative sizes, free_ring without
+ * Errors: LS_EINVAL (NULL, misaligned or overlapping arrays, sizes out of range, free_ring without
  * counters or the other way round, a window without free_ring, a window or sinks out
  * of range, more than 2^27 - 1 blocks per session), LS_EHIP.
  */

@@ -584,6 +584,7 @@ ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t
     if (ls_status st = check_pool(pool)) return st;
     if (num_sessions < 0 || total_new_tokens < 0 || max_new_len < 0)
         return fail(LS_EINVAL, "num_sessions, total_new_tokens and max_new_len must be >= 0");
+    if (total_new_tokens == INT32_MAX) return fail(LS_EINVAL, "total_new_tokens must be less than %d", INT32_MAX);
     if (max_blocks_per_session <= 0 || max_blocks_per_session > INT32_MAX / kBlock)
         return fail(LS_EINVAL, "max_blocks_per_session (%d) must be in [1, %d]", max_blocks_per_session, INT32_MAX / kBlock);
     if (!cu_new_lens || (total_new_tokens > 0 && !slot_map))
@@ -598,11 +599,33 @@ ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t
     } else if (ring_size || free_counts || next_counts || window) {
         return fail(LS_EINVAL, "ring_size, counters and a window need a free ring");
     }
-    for (const void *ptr : {(const void *)seq_lens, (const void *)new_lens, (const void *)block_tables, (const void *)free_ring,
-                            (const void *)next_lens, (const void *)cu_new_lens, (const void *)reused_lens})
-        if (!aligned(ptr, 4)) return fail(LS_EINVAL, "int32 arrays must be 4-byte aligned");
-    if (!aligned(slot_map, 8) || !aligned(free_counts, 8) || !aligned(next_counts, 8))
-        return fail(LS_EINVAL, "slot_map and the counters must be 8-byte aligned");
+    // Every array is memory of its own, but for lengths and counters that advance in place.
+    struct Range {
+        const void *at;
+        size_t bytes, align;
+    };
+    const size_t S = (size_t)num_sessions;
+    const Range arrays[] = {{seq_lens, S * 4, 4},
+                            {next_lens, S * 4, 4},
+                            {free_counts, 16, 8},
+                            {next_counts, 16, 8},
+                            {new_lens, S * 4, 4},
+                            {block_tables, S * (size_t)max_blocks_per_session * 4, 4},
+                            {free_ring, (size_t)ring_size * 4, 4},
+                            {cu_new_lens, (S + 1) * 4, 4},
+                            {reused_lens, S * 4, 4},
+                            {slot_map, (size_t)total_new_tokens * 8, 8}};
+    for (const Range &x : arrays) {
+        if (!aligned(x.at, x.align)) return fail(LS_EINVAL, "an array is not aligned to its type");
+        for (const Range &y : arrays) {
+            if (&y <= &x || !x.at || !y.at) continue;
+            const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+            if (a >= b + y.bytes || b >= a + x.bytes) continue;
+            const bool in_place = x.at == y.at && ((&x == &arrays[0] && &y == &arrays[1]) || (&x == &arrays[2] && &y == &arrays[3]));
+            if (!in_place)
+                return fail(LS_EINVAL, "arrays overlap (only next_lens may be seq_lens, and next_counts free_counts)");
+        }
+    }
     if (ls_status st = check_device(pool->geom)) return st;
     unsigned int *err = device_error_word();
     if (!err) return fail(LS_EHIP, "cannot resolve the device error word");

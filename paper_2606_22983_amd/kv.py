@@ -422,6 +422,28 @@ def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tenso
     with free_counts -> next_counts int64 [2] = (taken, given).  next_lens may be seq_lens,
     next_counts free_counts."""
     s = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
+    one, two = (s,), (2,)
+    if not (_fits(seq_lens, one, _I32) and _fits(new_lens, one, _I32) and _fits(next_lens, one, _I32)
+            and _fits(cu_new_lens, (s + 1,), _I32) and (reused_lens is None or _fits(reused_lens, one, _I32))
+            and _fits(slot_map, slot_map.shape[:1], _I64) and _fits(block_tables, (s, block_tables.shape[-1]), _I32)
+            and (free_ring is None or _fits(free_ring, free_ring.shape[:1], _I32))
+            and (free_counts is None or _fits(free_counts, two, _I64))
+            and (next_counts is None or _fits(next_counts, two, _I64))):
+        _tables_args(s, seq_lens, new_lens, block_tables, next_lens, cu_new_lens, reused_lens, slot_map, free_ring,
+                     free_counts, next_counts)
+    _check(_lib.kv_tables_update(pool.handle, s, seq_lens.data_ptr(), new_lens.data_ptr(), block_tables.data_ptr(),
+                                 block_tables.shape[1], _ptr(free_ring),
+                                 0 if free_ring is None else free_ring.shape[0], _ptr(free_counts),
+                                 _ptr(next_counts), window, sinks, slot_map.shape[0], int(max_new_len),
+                                 next_lens.data_ptr(), cu_new_lens.data_ptr(), _ptr(reused_lens), slot_map.data_ptr(),
+                                 _stream(stream)),
+           "kv_tables_update")
+    return slot_map
+
+
+def _tables_args(s, seq_lens, new_lens, block_tables, next_lens, cu_new_lens, reused_lens, slot_map, free_ring,
+                 free_counts, next_counts):
+    """Shapes, types and devices of kv_tables_update's tensors (raises ValueError)."""
     for t, name, n in ((seq_lens, "seq_lens", s), (new_lens, "new_lens", s), (next_lens, "next_lens", s),
                        (cu_new_lens, "cu_new_lens", s + 1), (reused_lens, "reused_lens", s),
                        (free_ring, "free_ring", None)):
@@ -434,14 +456,6 @@ def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tenso
     if not (block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32)):
         _shape(block_tables, "block_tables", (s, None), torch.int32)
         _dev(block_tables, "block_tables")
-    _check(_lib.kv_tables_update(pool.handle, s, _ptr(seq_lens), _ptr(new_lens), _ptr(block_tables),
-                                 block_tables.shape[1], _ptr(free_ring),
-                                 0 if free_ring is None else free_ring.shape[0], _ptr(free_counts),
-                                 _ptr(next_counts), window, sinks, slot_map.shape[0], int(max_new_len),
-                                 _ptr(next_lens), _ptr(cu_new_lens), _ptr(reused_lens), _ptr(slot_map),
-                                 _stream(stream)),
-           "kv_tables_update")
-    return slot_map
 
 
 def _rows(t: torch.Tensor, name: str, shape) -> int:

@@ -74,8 +74,8 @@ def test_prefill_window_rejects(lib, pool, kw, status):  # noqa: F811
 
 
 def tables(lib, pool, **kw):  # noqa: F811
-    a = dict(S=4, lens=F, new=F, bt=F, maxb=8, ring=F, size=100, counts=F, after=F, W=16, sinks=0, total=9, longest=5, next=F, cu=F,
-             reused=None, slots=F)
+    a = dict(S=4, lens=F, new=F + 0x100, bt=F + 0x1000, maxb=8, ring=F + 0x2000, size=100, counts=F + 0x200, after=F + 0x300, W=16,
+             sinks=0, total=9, longest=5, next=F + 0x400, cu=F + 0x500, reused=None, slots=F + 0x3000)
     a.update(kw)
     return lib.kv_tables_update(pool, a["S"], P(a["lens"]), P(a["new"]), P(a["bt"]), a["maxb"], P(a["ring"]), a["size"], P(a["counts"]),
                                 P(a["after"]), a["W"], a["sinks"], a["total"], a["longest"], P(a["next"]), P(a["cu"]), P(a["reused"]),
@@ -87,10 +87,18 @@ def tables(lib, pool, **kw):  # noqa: F811
     dict(next=None), dict(cu=None), dict(slots=None), dict(size=0), dict(size=-3), dict(counts=None), dict(after=None), dict(W=-1),
     dict(W=(1 << 29) + 1), dict(sinks=-1), dict(sinks=(1 << 29) + 1), dict(ring=None), dict(ring=None, size=0, counts=None, after=None),
     dict(ring=None, size=0, counts=None, W=0), dict(lens=F + 2), dict(ring=F + 1), dict(slots=F + 4), dict(counts=F + 4),
-    dict(reused=F + 2),
+    dict(reused=F + 2), dict(total=2**31 - 1), dict(next=F + 4), dict(next=F - 4), dict(after=F + 0x208), dict(reused=F), dict(cu=F + 0x40c),
+    dict(reused=F + 0x400), dict(slots=F + 0x2000 + 396), dict(ring=F + 0x1000), dict(new=F), dict(bt=F + 0x2000 - 124),
 ])
 def test_tables_update_rejects(lib, pool, kw):  # noqa: F811
     assert tables(lib, pool, **kw) == LS_EINVAL
+
+
+def test_tables_update_takes_lengths_and_counters_in_place(lib, pool):  # noqa: F811
+    import torch
+    if not torch.cuda.is_available():                  # past the checks, there is no device to launch on
+        assert tables(lib, pool, next=F, after=F + 0x200) == LS_EHIP
+        assert tables(lib, pool, ring=None, size=0, counts=None, after=None, W=0, reused=F + 0x600) == LS_EHIP
 
 
 def append(lib, pool, **kw):  # noqa: F811
