@@ -310,6 +310,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
     const int S = a.num_sessions;
     const int G = a.group;
     const int qtok = kPreRows / G;       // new tokens per query tile
+    const int lg = __builtin_ctz(G);     // (G is 1, 2, 4 or 8)
     const int QT = a.qtiles;
     const int Hkv = a.num_kv_heads;
 
@@ -318,9 +319,10 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
     // `piece` of the workspace).
     auto run_item = [&](const int s, const int g, const int qt, const int chunk, const int chunks, const int piece) {
         const int n = a.cu[s + 1] - a.cu[s];
+        const int c_early = kWin ? a.ctx[s] : 0;              // (requested with the turn's rows)
         const int j0 = qt * qtok;
         if (j0 >= n || a.cu[s] < 0 || a.cu[s + 1] > a.total) return;   // (lengths outside q: flagged above)
-        const int c = a.ctx[s];
+        const int c = kWin ? c_early : a.ctx[s];
         const int j_last = min(j0 + qtok, n) - 1;
         int nblk_valid = (c + n + kBlock - 1) / kBlock;
         if (nblk_valid > a.max_blocks) {
@@ -373,8 +375,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
     #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) {
             const int r = wave * kWaveRows + rt * 16 + c16;
-            const int jl = j0 + r / G;
-            const int h = r % G;
+            const int jl = j0 + (kWin ? r >> lg : r / G);
+            const int h = kWin ? r & (G - 1) : r % G;
             row_ok[rt] = jl < n;
             const int jc = min(jl, n - 1);
             row_lim[rt] = c + jc - key_base;
@@ -385,33 +387,15 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             for (int ks = 0; ks < KS; ++ks)
                 qop[rt][ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + ks * 32 + g4 * 8));
         }
-        // With a window no key unit is seen by every row, so the running maximum
-        // starts from the row's score with the key at its own position, which it
-        // always sees.  The row sums then hold a term of 1 (in the part of the keys
-        // with that position), so keys whose probabilities vanish against it do
-        // not count, in whatever part they are.  Lane (c16, g4) loads row c16's
-        // own key as row c16 of a 16-key operand; a position outside the table or
-        // the pool gives zeros.
-        bf16x8 own_key[kWin ? kRT : 1][KS];
+        int first_ids = -1;                                   // block `lane` of the walk, from tile0 on
         if constexpr (kWin) {
-    #pragma unroll
-            for (int rt = 0; rt < kRT; ++rt) {
-                const int pos = row_lim[rt] + key_base;
-                const int col = pos >> 4;                      // (kBlock tokens per column)
-                const bool in_table = pos >= 0 && col < a.max_blocks;
-                const int32_t b = a.block_tables[(int64_t)s * a.max_blocks + (in_table ? col : 0)];
-                const bool there = in_table && b >= 0 && b < a.num_blocks;
-                const uint16_t *kt = a.pool + ((int64_t)(there ? b : 0) * 2 * Hkv + g) * (kBlock * D);
-    #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 raw = *reinterpret_cast<const u32x4 *>(kt + ((ks * 4 + g4) * kBlock + (pos & 15)) * 8);
-                    own_key[rt][ks] = __builtin_bit_cast(bf16x8, there ? raw : u32x4{0u, 0u, 0u, 0u});
-                }
-            }
+            const int at = tile0 * 4 + lane;
+            const int32_t id = a.block_tables[(int64_t)s * a.max_blocks + min(at + (at >= sink_blocks ? skip : 0), a.max_blocks - 1)];
+            first_ids = lane < nb ? id : -1;
         }
         // Wait for q here, before the first stage loads are issued, so that no
         // wait for q remains inside the key loop (vmcnt(0), other counters untouched).
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+        if constexpr (!kWin) __builtin_amdgcn_s_waitcnt(0x0F70);
         // smallest causal limit among this wave's rows: units past it need masking
         const int wave_lim_min = c + min(j0 + (wave * kWaveRows) / G, n - 1) - key_base;
         // end of its rows' longest hole
@@ -519,26 +503,70 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
                         acc[rt][sb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[sb][ks], qop[rt][ks], acc[rt][sb], 0, 0, 0);
             }
         };
-        // Causal mask of a unit whose first key is key0 (lane group g4 holds unit
-        // keys 8*g4 + 4*sb + i); only units that reach past the smallest causal
-        // limit of the wave's rows need it.
-        auto mask_unit = [&](f32x4 (&acc)[kRT][2], int key0) {
-            if (key0 + 31 <= wave_lim_min && !(kWin && key0 < wave_hole_max && key0 + 31 >= hole_lo)) return;
-    #pragma unroll
-            for (int rt = 0; rt < kRT; ++rt) {
-                const int lim = row_lim[rt] - key0 - 8 * g4;
-    #pragma unroll
-                for (int sb = 0; sb < 2; ++sb)
-    #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (4 * sb + i > lim || (kWin && 4 * sb + i >= hole_lo - key0 - 8 * g4 && 4 * sb + i <= lim - window))
-                            acc[rt][sb][i] = -INFINITY;
-            }
-        };
         // Largest of a lane's 8 values of one row tile (NaN-propagating).
         auto lane_max = [&](const f32x4 (&acc)[2]) {
             const f32x4 x0 = acc[0], x1 = acc[1];
             return fmax3(fmax3(x0[0], x0[1], x0[2]), fmax3(x0[3], x1[0], x1[1]), fmax3(x1[2], x1[3], x1[3]));
+        };
+        // Causal mask of a unit whose first key is key0 (lane group g4 holds unit
+        // keys 8*g4 + 4*sb + i); only units that reach past the smallest causal
+        // limit of the wave's rows need it.
+        // With a window, units that reach into some row's hole do too.  And no unit
+        // is seen by every row: a row's running maximum starts from the first unit
+        // that holds a finite score of it (a row that is `unset` has none so far:
+        // all its scores, and probabilities, are then -inf and 0 whatever the
+        // maximum is taken for).
+        bool unset[kRT];
+    #pragma unroll
+        for (int rt = 0; rt < kRT; ++rt) unset[rt] = true;
+        bool pending = kWin;                           // some row of the wave is unset
+        auto mask_unit = [&](f32x4 (&acc)[kRT][2], int key0) {
+            if constexpr (kWin) {
+                const bool in_hole = key0 < wave_hole_max && key0 + 31 >= hole_lo;
+                if (key0 + 31 <= wave_lim_min && !in_hole && !pending) return;
+                if (in_hole && key0 < hole_lo) {       // the last of the first tokens
+    #pragma unroll
+                    for (int rt = 0; rt < kRT; ++rt) {
+                        const int lim = row_lim[rt] - key0 - 8 * g4, lo = hole_lo - key0 - 8 * g4;
+    #pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e > lim || (e >= lo && e <= lim - window)) acc[rt][e / 4][e % 4] = -INFINITY;
+                    }
+                } else {                               // 0 <= row_lim - key < window
+                    const unsigned seen = in_hole ? (unsigned)window : 0x80000000u;
+    #pragma unroll
+                    for (int rt = 0; rt < kRT; ++rt) {
+                        const int lim = row_lim[rt] - key0 - 8 * g4;
+    #pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if ((unsigned)(lim - e) >= seen) acc[rt][e / 4][e % 4] = -INFINITY;
+                    }
+                }
+                if (pending) {
+                    bool left = false;
+    #pragma unroll
+                    for (int rt = 0; rt < kRT; ++rt) {
+                        const float most = xmax16_32(lane_max(acc[rt]));
+                        if (unset[rt] && most > -INFINITY) {
+                            nm[rt] = -most * sl2;
+                            unset[rt] = false;
+                        }
+                        left = left || unset[rt];
+                    }
+                    pending = __any(left);
+                }
+            } else {
+                if (key0 + 31 <= wave_lim_min) return;
+    #pragma unroll
+                for (int rt = 0; rt < kRT; ++rt) {
+                    const int lim = row_lim[rt] - key0 - 8 * g4;
+    #pragma unroll
+                    for (int sb = 0; sb < 2; ++sb)
+    #pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (4 * sb + i > lim) acc[rt][sb][i] = -INFINITY;
+                }
+            }
         };
         // Scores -> exp2 arguments S * scale * log2(e) - m' (phase B).
         auto scale_unit = [&](f32x4 (&acc)[kRT][2]) {
@@ -681,21 +709,40 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         float us_e[kRT], us_o[kRT];
     #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) pop_o[rt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-        int32_t idk = id_k(-1), idv = id_v(-1);
-        load_k(k3, idk);                      // stage -1: K unit 0 (its V part is empty)
-        load_v(v3, idv);
-        idk = id_k(0); idv = id_v(0);
-        load_k(k0, idk);
-        load_v(v0, idv);
-        idk = id_k(1); idv = id_v(1);
-        load_k(k1, idk);
-        load_v(v1, idv);
-        idk = id_k(2); idv = id_v(2);
+        int32_t idk, idv;
+        auto zero_v_first = [&] {
+            for (int ci = tid; ci < 2 * C::kBlockBytes / 16; ci += kPreThreads)
+                *reinterpret_cast<u32x4 *>(v3 + 2 * C::kBlockBytes + ci * 16) = u32x4{0u, 0u, 0u, 0u};
+        };
+        if constexpr (kWin) {
+            // The ids of the first stages' blocks, requested with q, a lane each (a
+            // scalar load after the other takes 3.5 us, of the 12 that an item's
+            // start and end take beside its key tiles).
+            auto first_id = [&](int jb) { return jb >= 0 ? __builtin_amdgcn_readlane(first_ids, jb) : -1; };
+            load_k(k3, first_id(blk - 2));
+            zero_v_first();                   // (no load goes there, and the barrier below is enough)
+            load_k(k0, first_id(blk + 2));
+            load_v(v0, first_id(blk));
+            load_k(k1, first_id(blk + 6));
+            load_v(v1, first_id(blk + 4));
+            idk = first_id(blk + 10);
+            idv = first_id(blk + 8);
+        } else {
+            idk = id_k(-1), idv = id_v(-1);
+            load_k(k3, idk);                  // stage -1: K unit 0 (its V part is empty)
+            load_v(v3, idv);
+            idk = id_k(0); idv = id_v(0);
+            load_k(k0, idk);
+            load_v(v0, idv);
+            idk = id_k(1); idv = id_v(1);
+            load_k(k1, idk);
+            load_v(v1, idv);
+            idk = id_k(2); idv = id_v(2);
+        }
         stage_barrier<D>();                   // stages -1 and 0 have landed
         // V of unit -1 (second half of stage -1's V): zeros, so that the first
         // tile's P V of that unit (with P = 0) adds nothing.
-        for (int ci = tid; ci < 2 * C::kBlockBytes / 16; ci += kPreThreads)
-            *reinterpret_cast<u32x4 *>(v3 + 2 * C::kBlockBytes + ci * 16) = u32x4{0u, 0u, 0u, 0u};
+        if constexpr (!kWin) zero_v_first();
         read_k(k3 + C::kUnitBytes);           // unit 0 = second unit of stage -1
         qk_mfma(sa);
         read_k(k0);                           // unit 1
@@ -706,18 +753,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         // its probabilities are 0.
     #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) {
-            if constexpr (kWin) {
-                // Score (A-row 4 g4 + i, row c16) of the own keys: the diagonal.
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(own_key[rt][ks], qop[rt][ks], acc, 0, 0, 0);
-                float x = -INFINITY;
-    #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (4 * g4 + i == c16) x = acc[i];
-                nm[rt] = -xmax16_32(x) * sl2;
-            } else {
+            if constexpr (!kWin) {
                 nm[rt] = -xmax16_32(lane_max(sa[rt])) * sl2;
                 if (kSplit && row_lim[rt] < 0) nm[rt] = 0.f;
             }
@@ -727,8 +763,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         // to come would cost them their low bits.  Any part can begin so, not
         // only the context; the row starts from its first unit that holds more,
         // found here with K straight from the pool (rare).  Without one its
-        // probabilities are 0.  (With a window: a row whose own key scores -inf.)
-        if constexpr (kSplit || kWin) {
+        // probabilities are 0.
+        if constexpr (kSplit && !kWin) {
             auto lost = [&] {
                 bool any = false;
     #pragma unroll
@@ -736,7 +772,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
                 return __any(any);
             };
             if (lost()) {
-                for (int u = kWin ? 0 : 1; u < 2 * wave_tiles && lost(); ++u) {
+                for (int u = 1; u < 2 * wave_tiles && lost(); ++u) {
                     const int32_t b0 = entry(2 * u), b1 = entry(2 * u + 1);
                     const uint32_t b = (uint32_t)(c16 >> 3 ? b1 : b0);
                     const bool there = b < nblocks32;
@@ -770,10 +806,12 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             }
         }
         scale_unit(sa);
-        __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the zeros are written
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        if constexpr (!kWin) {
+            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): the zeros are written
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        }
 
         // The loads are issued on every path, so outstanding loads are counted
         // exactly; only the compute of tiles past the last one is skipped.
@@ -856,10 +894,11 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             const float inv = 1.f / xsum16_32(lsum[rt]);
             if (!row_ok[rt]) continue;
             int64_t at = row_out[rt];
-            if constexpr (kSplit) {                            // derived again: 64 bits less to keep through the loop
+            if constexpr (kSplit || kWin) {                    // derived again: 64 bits less to keep through the loop
                 int r = wave * kWaveRows + rt * 16 + c16;
                 asm volatile("" : "+v"(r));
-                at = (((int64_t)a.cu[s] + j0 + r / G) * hq_total + g * G + r % G) * D;
+                const int jl = kWin ? r >> lg : r / G, h = kWin ? r & (G - 1) : r % G;
+                at = (((int64_t)a.cu[s] + j0 + jl) * hq_total + g * G + h) * D;
             }
             uint16_t *orow = a.out + at;
     #pragma unroll
@@ -1141,6 +1180,11 @@ int32_t key_parts(int32_t tiles, int32_t target) { return (tiles + target - 1) /
 // D = 128, so the costs below, which were chosen by trial, stand for 5 us per
 // item (one turn shows 8) and 10 for the merge (its launch takes 7).
 constexpr int kMinPartTiles = 16;      // key tiles per part: below, an item's start and the merge cost what a part saves
+// With a window the unsplit call is short itself, and shorter parts pay: at 16
+// least tiles the turn of 301 tokens (window 2048) has 3 parts and takes 43.8 us,
+// at 8 41.0, at 6 36.4, at 4 36.7; a turn of 100 (window 1024, 32/4 heads) 44.5,
+// 30.5, 30.4, 28.6; one of 64 (4096, 16/4 heads of 64) 29.8, 24.0, 23.2, 21.6.
+constexpr int kMinPartTilesWindow = 4;
 constexpr int kMaxParts = 32;
 constexpr int kSplitMaxWaves = 6;      // whole waves from which nothing is split
 constexpr int kItemTiles = 3;          // an item's start-up and drain
@@ -1148,7 +1192,7 @@ constexpr int kMergeTiles = 6;         // the merge launch ...
 constexpr int kPiecesPerMergeTile = 32;   // ... and one more per so many pieces (written and read back)
 constexpr double kSplitGain = 0.93;
 
-SplitChoice choose_split(const PrefillPair *pr, int np, int64_t cus) {   // pr: longest tile first
+SplitChoice choose_split(const PrefillPair *pr, int np, int64_t cus, int min_part) {   // pr: longest tile first
     SplitChoice best;
     int64_t items = 0, total = 0;
     for (int i = 0; i < np; ++i) {
@@ -1186,7 +1230,7 @@ SplitChoice choose_split(const PrefillPair *pr, int np, int64_t cus) {   // pr: 
         };
         const int64_t longest = item_tiles(w * cus);
         for (int m = 1; m <= 2; ++m) {
-            int32_t lo = (int32_t)std::max<int64_t>(kMinPartTiles, (longest + kMaxParts - 1) / kMaxParts);
+            int32_t lo = (int32_t)std::max<int64_t>(min_part, (longest + kMaxParts - 1) / kMaxParts);
             int32_t hi = (int32_t)longest - 1;
             int64_t st, si;
             if (lo > hi || pieces_at(hi, st, si) > m * cus) continue;
@@ -1282,10 +1326,10 @@ void plan_prefill_host(PrefillPair *pr, int np, PrefillHostPlan &plan, int32_t &
 // items, left some XCDs with 40 items for 32 CUs: 587 us for four turns
 // instead of 500 unsplit); the parts, longest first, each to the XCD with the
 // least work so far.
-bool plan_prefill_split(PrefillPair *pr, int np, int64_t cus, PrefillSplitPlan &plan, PrefillMergePlan &merge,
-                        int32_t &split_tiles, int64_t &items) {
+bool plan_prefill_split(PrefillPair *pr, int np, int64_t cus, int min_part, PrefillSplitPlan &plan,
+                        PrefillMergePlan &merge, int32_t &split_tiles, int64_t &items) {
     std::stable_sort(pr, pr + np, [](const PrefillPair &x, const PrefillPair &y) { return x.len > y.len; });
-    const SplitChoice split = choose_split(pr, np, cus);
+    const SplitChoice split = choose_split(pr, np, cus, min_part);
     if (!split.target) return false;
     struct Entry {
         int64_t len;
@@ -1384,7 +1428,7 @@ bool prefill_split_items(int32_t num_sessions, int32_t num_kv_heads, int32_t gro
     int64_t total = 0;
     if (!collect_pairs(num_sessions, num_kv_heads, kPreRows / group, lens_host, 0, 0, plan, pairs_of, np) || np == 0)
         return true;
-    if (!plan_prefill_split(pairs_of, np, cus, plan, merge, split_tiles, total)) return true;
+    if (!plan_prefill_split(pairs_of, np, cus, kMinPartTiles, plan, merge, split_tiles, total)) return true;
     if (total > room || split_tiles > merged_room) return false;
     for (int x = 0; x < kXcds; ++x) {
         int e = plan.start[x];
@@ -1444,6 +1488,15 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
             const int64_t per_xcd = (items + kXcds - 1) / kXcds + (items + 10 * kXcds - 1) / (10 * kXcds);
             return dim3((unsigned)(kXcds * per_xcd));
         };
+        // Where every item has a CU of its own the counters even nothing out, and
+        // cost the 1.3 us of an atomic: windowed calls go without them.
+        const int64_t cus = stream_cus(p, stream);
+        auto longest_list = [&] { return *std::max_element(plan.total, plan.total + kXcds); };
+        auto alone = [&] { return (int64_t)longest_list() * kXcds <= cus; };
+        auto index_grid = [&] {
+            a.queue = nullptr;
+            return dim3((unsigned)(kXcds * longest_list()));
+        };
         if (workspace) {
             a.queue = static_cast<uint32_t *>(workspace);
             if (!counters_cleared) {
@@ -1456,11 +1509,13 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
         int32_t split_tiles = 0;
         int64_t items = 0;
         if (workspace && workspace_bytes >= LS_PREFILL_WORKSPACE_BYTES &&
-            plan_prefill_split(pairs_of, np, stream_cus(p, stream), plan, merge, split_tiles, items)) {
+            plan_prefill_split(pairs_of, np, cus, kWin ? kMinPartTilesWindow : kMinPartTiles, plan, merge, split_tiles, items)) {
             uint8_t *parts = static_cast<uint8_t *>(workspace) + LS_PREFILL_COUNTER_BYTES;
             a.part_ml = reinterpret_cast<float *>(parts);
             a.part_o = reinterpret_cast<float *>(parts + (size_t)kPrefillSplitPieces * kPreRows * 2 * sizeof(float));
-            const dim3 grid = queue_grid(items), mgrid((unsigned)(split_tiles * (kPreWaves * kRT * p.head_dim / 16 / kMergeWaves)));
+            dim3 grid = queue_grid(items);
+            if (kWin && alone()) grid = index_grid();
+            const dim3 mgrid((unsigned)(split_tiles * (kPreWaves * kRT * p.head_dim / 16 / kMergeWaves)));
             if (p.head_dim == 128)
                 hipLaunchKernelGGL((prefill_kernel<128, true, true, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, plan);
             else
@@ -1482,6 +1537,7 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
             int64_t total = 0;
             for (int x = 0; x < kXcds; ++x) total += plan.total[x];
             grid = queue_grid(total);
+            if (kWin && alone()) grid = index_grid();
         }
         const PrefillHostPlan &whole = plan;
         if (p.head_dim == 128 && skip)
