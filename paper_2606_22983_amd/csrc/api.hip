@@ -323,7 +323,8 @@ ls_status decode_call(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int
                                                   max_blocks_per_session))
             return st;
     const DecodePlan plan = plan_decode(p, num_sessions, num_q_heads,
-                                        windowed ? window_blocks(max_blocks_per_session, window, sinks) : max_blocks_per_session);
+                                        windowed ? window_blocks(max_blocks_per_session, window, sinks) : max_blocks_per_session,
+                                        windowed);
     if (!plan.supported)
         return fail(LS_EUNSUPPORTED, "batch of %d sessions with %d blocks each exceeds the decode "
                     "limits (2048 sessions, 16384 blocks per session)", num_sessions, max_blocks_per_session);
@@ -549,7 +550,9 @@ ls_status paged_attn_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
 size_t ls_decode_window_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
                                         int32_t max_blocks_per_session, int32_t window, int32_t sinks) {
     if (!pool || max_blocks_per_session <= 0 || check_window(window, sinks, max_blocks_per_session) != LS_OK) return 0;
-    return ls_decode_workspace_bytes(pool, num_sessions, num_q_heads, window_blocks(max_blocks_per_session, window, sinks));
+    if (num_sessions <= 0 || num_q_heads <= 0) return 0;
+    return plan_decode(pool->geom, num_sessions, num_q_heads, window_blocks(max_blocks_per_session, window, sinks), true)
+        .recommended();
 }
 
 ls_status paged_attn_decode_window(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,

@@ -60,6 +60,7 @@ struct SmallDecodePlan {
 struct DecodePlan {
     int split_tokens;               // tokens per split (multiple of 64)
     int max_splits;                 // splits of the longest possible session
+    bool windowed;                  // the sessions' walks (see launch_decode) are planned
     bool supported;                 // false when a session could need too many splits
     size_t ml_bytes;                // fp32 [S][Hkv][max_splits][G][2]
     size_t acc_bytes;               // fp32 [S][Hkv][max_splits][G][D]
@@ -70,9 +71,11 @@ struct DecodePlan {
 // lens_host null: every session may be as long as its table.  cus: CUs of the
 // stream.  bytes: room for counts and partials.
 SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,
-                           int32_t max_blocks, const int32_t *lens_host, int32_t appended, size_t bytes);
+                           int32_t max_blocks, const int32_t *lens_host, int32_t appended, size_t bytes,
+                           bool windowed);
+// windowed: for sessions of which a window is seen (max_blocks_per_session: window_blocks).
 DecodePlan plan_decode(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads,
-                       int32_t max_blocks_per_session);
+                       int32_t max_blocks_per_session, bool windowed = false);
 // The small batch's plan that a call on a stream of `cus` CUs runs with this
 // workspace, or one without split_tokens: the persistent kernel.
 SmallDecodePlan choose_small(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,

@@ -62,7 +62,20 @@ constexpr int kMaxSplits = 256;              // combine kernel's LDS capacity
 constexpr int kMaxBatch = 2048;              // sessions per decode call (LDS prefix sums)
 constexpr int kMaxGroup = 8;                 // query heads per KV head
 constexpr int kMaxDeviceSplit = 2048;       // longest split of the kernel's own schedule (two chunks)
-constexpr int kKeyBins = kMaxDeviceSplit / kBlock + 1;   // short-split block counts 0..128
+// With a window the kernel's own splits hold one more block per wave (5 or 9):
+// windows are mostly powers of two, and a walk of 1024 keys takes 65 blocks at
+// any offset, and one more of first tokens.  In splits of 64 blocks the last two
+// are an item of their own, and sessions are merged by a launch of its own (256
+// sessions of window 1024 at 16/2 heads 66.8 -> 58.2 us, 64 of 4096 at 32/4 88.4
+// -> 86.3, 256 of 2048 at 8/8 heads of 64 183 -> 178).  Host plans keep chunks of
+// 1024, whose leftover of two blocks is a chunk of the same item: nine blocks
+// unrolled are slower there (50.8 -> 54.6 us).
+constexpr int kWindowPerWave = 9, kWindowPerWaveShort = 5;
+constexpr int kWindowChunk = kWindowPerWave * kDecWaves * kBlock;          // 1152
+constexpr int kWindowChunkShort = kWindowPerWaveShort * kDecWaves * kBlock;   // 640
+constexpr int kMaxDeviceSplitWindow = 2 * kWindowChunk;
+template <bool kWin>
+constexpr int kKeyBins = (kWin ? kMaxDeviceSplitWindow : kMaxDeviceSplit) / kBlock + 1;   // short-split block counts 0..128 (144)
 static_assert(kMaxBatch * kMaxSplits <= 0xFFFFF && kMaxBatch < 4096,
               "work-row counts must fit the packed scan (20 + 12 bits)");
 constexpr int kSpinLimit = 1 << 22;          // bound of the merge-slot wait (~0.1 s)
@@ -406,8 +419,8 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
     __shared__ int sm_skip[kWin ? kMaxBatch : 1];   // blocks its walk leaves out
     __shared__ int sm_porder[kMaxBatch];        // sessions of the short-split rows, in row order
     __shared__ int sm_key[kDecThreads];         // block count of a session's short split (-1: none)
-    __shared__ unsigned long long sm_kmask[kKeyBins][kDecThreads / 64];  // sessions per short-split key
-    __shared__ int sm_kabove[kKeyBins + 1];     // sessions with a larger key (suffix counts)
+    __shared__ unsigned long long sm_kmask[kKeyBins<kWin>][kDecThreads / 64];  // sessions per short-split key
+    __shared__ int sm_kabove[kKeyBins<kWin> + 1];     // sessions with a larger key (suffix counts)
     __shared__ uint8_t sm_own[kMaxBatch];       // 1: the session's own new token is attended (fits the table)
     __shared__ unsigned sm_wave_tot[kDecWaves];
     // Per-item merge slots (double-buffered): each wave leaves its (m, l, O) of
@@ -431,7 +444,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
     int full_rows = 0, total_rows = 0;
     if constexpr (!kHost) {
         constexpr int kMaskWords = kDecThreads / 64;
-        for (int i = tid; i < kKeyBins * kMaskWords; i += kDecThreads) sm_kmask[i / kMaskWords][i % kMaskWords] = 0ull;
+        for (int i = tid; i < kKeyBins<kWin> * kMaskWords; i += kDecThreads) sm_kmask[i / kMaskWords][i % kMaskWords] = 0ull;
         // ---- work rows: full splits per session (prefix sum) and short splits.
         // Both counts share one unsigned scan: full rows in bits 0..19 (at most
         // kMaxBatch * kMaxSplits = 2^19 in total), short rows (at most kMaxBatch)
@@ -484,10 +497,10 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         if (S <= kDecThreads && tid < kWave) {
             // Suffix sums over the key bins, one wave: bins 64*c + lane in chunk c.
             int carry = 0;
-            for (int c = (kKeyBins + kWave - 1) / kWave - 1; c >= 0; --c) {
+            for (int c = (kKeyBins<kWin> + kWave - 1) / kWave - 1; c >= 0; --c) {
                 const int bin = c * kWave + tid;
                 int cnt = 0;
-                if (bin < kKeyBins)
+                if (bin < kKeyBins<kWin>)
                     for (int w = 0; w < kDecThreads / 64; ++w) cnt += __popcll(sm_kmask[bin][w]);
                 // inclusive suffix scan of cnt over the lanes (higher lanes first)
                 int x = cnt;
@@ -496,7 +509,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
                     const int y = __shfl_down(x, off);
                     if (tid + off < kWave) x += y;
                 }
-                if (bin < kKeyBins) sm_kabove[bin] = carry + x - cnt;
+                if (bin < kKeyBins<kWin>) sm_kabove[bin] = carry + x - cnt;
                 carry += __shfl(x, 0);
             }
         }
@@ -570,14 +583,22 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
     // unconditional (its index clamped into the table row) and the id is
     // validated only when it is used, so nothing waits for this load until the
     // chunk is processed.
-    auto fetch_ids = [&](int s_, int split_, int c_, int skip_) -> int {
-        const int j = split_ * (T / kBlock) + c_ * (kChunk / kBlock) + lane;
-        return a.block_tables[(int64_t)s_ * a.max_blocks + min(walk_column(a, j, skip_), a.max_blocks - 1)];
+    // (A chunk of more than 64 blocks has the ids past the 64th in a second
+    // register, of the first lanes.)
+    constexpr int kChunkIds = kChunk / kBlock;
+    constexpr bool kWide = kChunkIds > kWave;
+    static_assert(kChunkIds <= kWave + kDecWaves, "the blocks past the 64th are each wave's last");
+    auto fetch_ids = [&](int s_, int split_, int c_, int skip_, int &more) -> int {
+        const int j = split_ * (T / kBlock) + c_ * kChunkIds + lane;
+        const int32_t *row = a.block_tables + (int64_t)s_ * a.max_blocks;
+        if constexpr (kWide) more = row[min(walk_column(a, j + kWave, skip_), a.max_blocks - 1)];
+        return row[min(walk_column(a, j, skip_), a.max_blocks - 1)];
     };
     auto skip_of = [&](int s_) -> int { return kWin ? sm_skip[kWin ? s_ : 0] : 0; };
     // Validated id (or -1) of entry idx of a fetched id register.
-    auto checked_id = [&](int ids, int idx, int nb) -> int {
-        const int b = __builtin_amdgcn_readlane(ids, min(idx, kWave - 1));
+    auto checked_id = [&](int ids, int more, int idx, int nb) -> int {
+        int b = __builtin_amdgcn_readlane(ids, min(idx, kWave - 1));
+        if (kWide && idx >= kWave) b = __builtin_amdgcn_readlane(more, min(idx - kWave, kWave - 1));
         const bool in_split = idx < nb;
         const bool ok = in_split && b >= 0 && b < a.num_blocks;
         if (in_split && !ok && lane == 0) flag_error(a.err, LS_DEVERR_BLOCK_ID);
@@ -612,7 +633,12 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
     // Each wave keeps the fetched block ids of the current and the next chunk in
     // its own LDS slots (double-buffered; read back with readlane), so no value
     // loaded from memory is carried around the loop.
-    __shared__ int sm_ids[kDecWaves][2][kMaxSplitTokens / kBlock];
+    __shared__ int sm_ids[kDecWaves][2][kWide ? kChunkIds : kMaxSplitTokens / kBlock];
+    auto keep_ids = [&](int slot, int ids, int more) {
+        if (lane < kMaxSplitTokens / kBlock) sm_ids[wave][slot][lane] = ids;
+        if constexpr (kWide)
+            if (lane < kChunkIds - kWave) sm_ids[wave][slot][kWave + lane] = more;
+    };
     int k = 0, c = 0;                  // current item (index in this workgroup's list) and chunk
     int s = 0, g = 0, split = 0;
     bool last_planned = false;
@@ -624,7 +650,8 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         if constexpr (kHost && kWin) walk_len(a, s, false, first_skip);
         else first_skip = skip_of(s);
     }
-    int ids_pre = have ? fetch_ids(s, split, 0, first_skip) : -1;
+    int more_pre = -1;
+    const int ids_pre = have ? fetch_ids(s, split, 0, first_skip, more_pre) : -1;
     if (have) load_q(s, g, qop);
     if constexpr (kHost) {
         // The schedule came with the arguments, so only the lengths are needed.
@@ -639,11 +666,11 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         __syncthreads();
     }
     if (have) {
-        if (lane < kMaxSplitTokens / kBlock) sm_ids[wave][0][lane] = ids_pre;
+        keep_ids(0, ids_pre, more_pre);
         const int nb = chunk_blocks(sm_len[s], split, 0);
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) {
-            bb[j] = checked_id(ids_pre, wave + j * kDecWaves, nb);
+            bb[j] = checked_id(ids_pre, more_pre, wave + j * kDecWaves, nb);
             load_block<D>(r[j], a.pool, a.num_kv_heads, g, bb[j], koff, voff);
         }
     }
@@ -659,11 +686,13 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         const int cur_s = s, cur_g = g, cur_split = split, cur_c = c;
         const bool cur_last_planned = last_planned;
         const int cur_ids = lane < kMaxSplitTokens / kBlock ? sm_ids[wave][u & 1][lane] : -1;
+        int cur_more = -1;
+        if constexpr (kWide) cur_more = sm_ids[wave][u & 1][kWave + min(lane, kChunkIds - kWave - 1)];
         const int t_split_end = min(L, cur_split * T + T);
         const int t0 = cur_split * T + cur_c * kChunk;
         const bool last_chunk = t0 + kChunk >= t_split_end;
         // Next chunk: the same item's, or the next item's first; its ids fetched now.
-        int next_ids = -1;
+        int next_ids = -1, next_more = -1;
         if (last_chunk) {
             ++k;
             c = 0;
@@ -671,12 +700,12 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         } else {
             ++c;
         }
-        if (have) next_ids = fetch_ids(s, split, c, skip_of(s));
+        if (have) next_ids = fetch_ids(s, split, c, skip_of(s), next_more);
         const int nsplit = L > 0 ? (L + T - 1) / T : 1;
         const int blk0 = t0 / kBlock;
         const int nblk = chunk_blocks(L, cur_split, cur_c);
         const int my_n = wave < nblk ? (nblk - wave + kDecWaves - 1) / kDecWaves : 0;
-        auto bid = [&](int it) -> int { return checked_id(cur_ids, wave + it * kDecWaves, nblk); };
+        auto bid = [&](int it) -> int { return checked_id(cur_ids, cur_more, wave + it * kDecWaves, nblk); };
 
         // A new item's running max starts at a finite floor: a block whose keys
         // are all masked then leaves (m, l, O) unchanged instead of producing NaN.
@@ -691,15 +720,36 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         // blocks) with forward-only exits, so the compiler sees straight-line
         // code and waits only for the block it is about to use.  A block with a
         // bad id is processed as fully masked.
+        if constexpr (kWide) {
+            // (written out: nine blocks are more than the compiler unrolls)
+            auto step = [&](auto at) __attribute__((always_inline)) -> bool {
+                constexpr int i = decltype(at)::value, j = i % kDepth;
+                if (i >= my_n) return false;
+                const int tb = (blk0 + wave + i * kDecWaves) * kBlock;
+                process_block<D, kWin>(r[j], qop, tb, bb[j] >= 0 ? Lp : 0, a.scale_log2, g4, m, lsum, o, hole_lo, hole_hi);
+                if constexpr (i + kDepth < kMaxPerWave) {
+                    bb[j] = bid(i + kDepth);
+                    load_block<D>(r[j], a.pool, a.num_kv_heads, cur_g, bb[j], koff, voff);
+                }
+                return true;
+            };
+            static_assert(kMaxPerWave == 9 || !kWide, "a step per block");
+            (void)(step(std::integral_constant<int, 0>{}) && step(std::integral_constant<int, 1>{}) &&
+                   step(std::integral_constant<int, 2>{}) && step(std::integral_constant<int, 3>{}) &&
+                   step(std::integral_constant<int, 4>{}) && step(std::integral_constant<int, 5>{}) &&
+                   step(std::integral_constant<int, 6>{}) && step(std::integral_constant<int, 7>{}) &&
+                   step(std::integral_constant<int, 8>{}));
+        } else {
 #pragma unroll
-        for (int i = 0; i < kMaxPerWave; ++i) {
-            if (i >= my_n) break;
-            const int j = i % kDepth;
-            const int tb = (blk0 + wave + i * kDecWaves) * kBlock;
-            process_block<D, kWin>(r[j], qop, tb, bb[j] >= 0 ? Lp : 0, a.scale_log2, g4, m, lsum, o, hole_lo, hole_hi);
-            if (i + kDepth < kMaxPerWave) {
-                bb[j] = bid(i + kDepth);
-                load_block<D>(r[j], a.pool, a.num_kv_heads, cur_g, bb[j], koff, voff);
+            for (int i = 0; i < kMaxPerWave; ++i) {
+                if (i >= my_n) break;
+                const int j = i % kDepth;
+                const int tb = (blk0 + wave + i * kDecWaves) * kBlock;
+                process_block<D, kWin>(r[j], qop, tb, bb[j] >= 0 ? Lp : 0, a.scale_log2, g4, m, lsum, o, hole_lo, hole_hi);
+                if (i + kDepth < kMaxPerWave) {
+                    bb[j] = bid(i + kDepth);
+                    load_block<D>(r[j], a.pool, a.num_kv_heads, cur_g, bb[j], koff, voff);
+                }
             }
         }
         // The step's own token (position Lp): the wave that held its block attends
@@ -710,18 +760,18 @@ __global__ __launch_bounds__(kDecThreads) void decode_kernel(DecodeArgsT<kWin> a
         if (own && cur_split == nsplit - 1 && last_chunk) {
             const int bl = Lp / kBlock - blk0;             // the token's block within the chunk
             if (wave == bl % kDecWaves) {
-                attend_own<D>(a, cur_s, cur_g, Lp, checked_id(cur_ids, bl, nblk), qop, g4, c16, lane, m, lsum, o);
+                attend_own<D>(a, cur_s, cur_g, Lp, checked_id(cur_ids, cur_more, bl, nblk), qop, g4, c16, lane, m, lsum, o);
             }
         }
         // Request the next chunk's first blocks (and a new item's q) before
         // merging this item.
         if (have) {
-            if (lane < kMaxSplitTokens / kBlock) sm_ids[wave][(u + 1) & 1][lane] = next_ids;
+            keep_ids((u + 1) & 1, next_ids, next_more);
             const int nb = chunk_blocks(sm_len[s], split, c);
             if (c == 0) load_q(s, g, qop);
 #pragma unroll
             for (int j = 0; j < kDepth; ++j) {
-                bb[j] = checked_id(next_ids, wave + j * kDecWaves, nb);
+                bb[j] = checked_id(next_ids, next_more, wave + j * kDecWaves, nb);
                 load_block<D>(r[j], a.pool, a.num_kv_heads, g, bb[j], koff, voff);
             }
         }
@@ -893,11 +943,17 @@ constexpr int kSmallRows = 256;
 struct SmallRows {
     uint32_t row[kSmallRows];
 };
-template <bool kHost>
-using SmallRowsArg = typename std::conditional<kHost, SmallRows, NoPlan>::type;
+// With a window also the blocks that each row's walk leaves out, so that the
+// block ids need not wait for the length.
+struct SmallWindowRows : SmallRows {
+    int32_t skip[kSmallRows];
+};
+template <bool kHost, bool kWin>
+using SmallRowsArg =
+    typename std::conditional<!kHost, NoPlan, typename std::conditional<kWin, SmallWindowRows, SmallRows>::type>::type;
 
 template <int D, int kDepth, bool kLoop, bool kHost, bool kWin = false>
-__global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<kWin> a, SmallRowsArg<kHost> rows) {
+__global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<kWin> a, SmallRowsArg<kHost, kWin> rows) {
     __shared__ float sm_m[kDecWaves][kMaxGroup];
     __shared__ float sm_l[kDecWaves][kMaxGroup];
     __shared__ __attribute__((aligned(16))) float sm_o[kDecWaves][kMaxGroup][D];
@@ -946,10 +1002,11 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<k
     }
 
     // Block ids of the split (one per lane), q and the length, all in flight at once.
-    // (With a window the table columns hang on the length.)
-    int skip = 0;
-    if constexpr (kWin) walk_len(a, s, false, skip);
-    const int id_at = min(walk_column(a, split * (T / kBlock) + lane, skip), a.max_blocks - 1);
+    // (With a window the table columns hang on the length, the host's if it gave one.)
+    int skip = 0, skip_used = 0;
+    if constexpr (kWin && kHost) skip_used = rows.skip[row];
+    else if constexpr (kWin) walk_len(a, s, false, skip_used);
+    const int id_at = min(walk_column(a, split * (T / kBlock) + lane, skip_used), a.max_blocks - 1);
     const int ids = a.block_tables[(int64_t)s * a.max_blocks + id_at];
     bf16x8 qop[D / 32];
     {
@@ -963,6 +1020,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<k
     }
     const bool first = split == 0 && g == 0 && tid == 0;
     const int L = walk_len(a, s, first, skip);
+    if (kWin && kHost && skip != skip_used && first) flag_error(a.err, LS_DEVERR_LENGTH);   // not the host's length
     int hole_lo, hole_hi;
     walk_hole(a, L, hole_lo, hole_hi);
     const int own = a.appended && a.lens[s] >= 0 && a.lens[s] + 1 <= a.max_blocks * kBlock;
@@ -1248,9 +1306,18 @@ struct SmallSize {
 };
 constexpr SmallSize kSmallSizes128[] = {{256, 1}, {512, 1}, {256, 2}, {768, 1}, {1024, 1}};
 constexpr SmallSize kSmallSizes64[] = {{512, 3}, {1024, 1}};
+// With a window the sizes go up to the longest walk and no further (a session of
+// 272 keys is two blocks per wave and one more, not 512 keys' four), 384 and 640
+// among them: walks are mostly the window's length, one block or two over a power
+// of two.  100 random batches: 0.968 of the time with the sizes above in the
+// geometric mean, 0.71 to 1.02 but for one (5 sessions of 300-2200 keys in a
+// window of 3600, lengths on the device: 8.0 -> 8.8 us).  Splits of even length,
+// of sessions that take several, were up to 10% slower than whole ones and a rest.
+constexpr SmallSize kWindowSizes128[] = {{256, 1}, {384, 1}, {512, 1}, {640, 1}, {256, 2}, {1024, 1}};
+constexpr SmallSize kWindowSizes64[] = {{512, 3}, {640, 3}, {1024, 1}};
 
 SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,
-                           int32_t max_blocks, const int32_t *lens_host, int32_t appended, size_t bytes) {
+                           int32_t max_blocks, const int32_t *lens_host, int32_t appended, size_t bytes, bool windowed) {
     const SmallDecodePlan none;
     const int64_t hkv = p.num_kv_heads;
     if (p.head_dim != 128 || !lens_host) cus = p.num_cus > 0 ? p.num_cus : 256;
@@ -1268,8 +1335,13 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
     const bool wide = p.head_dim == 128;
     const SmallSize *size = wide ? kSmallSizes128 : kSmallSizes64;
     const SmallSize *end = wide ? std::end(kSmallSizes128) : std::end(kSmallSizes64);
+    if (windowed) {
+        size = wide ? kWindowSizes128 : kWindowSizes64;
+        end = wide ? std::end(kWindowSizes128) : std::end(kWindowSizes64);
+    }
     for (; size != end; ++size) {
-        const int T = size->tokens;
+        int T = size->tokens;
+        if (windowed) T = (int)std::min<int64_t>(T, (longest + kBlock - 1) / kBlock * kBlock);
         if (T < kMaxSplitTokens && (int64_t)T * T < 8 * longest) continue;
         SmallDecodePlan plan;
         if (T >= longest) {
@@ -1287,7 +1359,7 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
             // D = 128, splits from 512 on, one or two query heads per KV head:
             // below 3/5 of the longest (8 of 9 batches 1-9% slower here, one 1%
             // faster; with more query heads nine are 4-26% faster here).
-            if (lens_host && num_sessions * hkv > cus) {
+            if (lens_host && !windowed && num_sessions * hkv > cus) {
                 const int64_t even = longest * num_sessions;
                 if (wide ? T > 256 && G <= 2 && 5 * total < 3 * even
                          : T == kMaxSplitTokens && (num_sessions * hkv > 2 * cus || 4 * total < 3 * even))
@@ -1304,7 +1376,7 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
         // batches that this leaves out 5 are 0-3% faster for it and 12 slower,
         // those with the fewest splits most (4 sessions of 1000-40,000 keys in
         // tables of 64k at 2 heads, D = 64: 21.7 us, 15.1 without).
-        if (!lens_host && T == kMaxSplitTokens) continue;
+        if (!lens_host && !windowed && T == kMaxSplitTokens) continue;
         int64_t rows = 0;                          // of the grid
         double resident;                           // workgroups with keys, expected
         if (lens_host) {
@@ -1314,6 +1386,7 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
         } else {
             rows = num_sessions * ((longest + T - 1) / T);
             resident = (double)(num_sessions * hkv) * (0.5 * (double)longest / T + 0.5) / 1.1;
+            if (windowed) resident = (double)(rows * hkv);        // (walks are mostly as long as they get)
         }
         if (resident > (double)(size->per_cu * cus)) continue;
         plan.split_tokens = T;
@@ -1327,7 +1400,7 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
 }
 
 DecodePlan plan_decode(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads,
-                       int32_t max_blocks_per_session) {
+                       int32_t max_blocks_per_session, bool windowed) {
     DecodePlan plan{};
     const int64_t max_tokens = (int64_t)max_blocks_per_session * kBlock;
     const int64_t work = (int64_t)num_sessions * p.num_kv_heads * max_tokens;
@@ -1343,6 +1416,8 @@ DecodePlan plan_decode(const PoolGeom &p, int32_t num_sessions, int32_t num_q_he
              3 * cus)
         T = kMaxDeviceSplit;
     while (T < kMaxSplitTokens && (max_tokens + T - 1) / T > kMaxSplits) T *= 2;
+    plan.windowed = windowed;
+    if (windowed) T = T == 512 ? kWindowChunkShort : T / kMaxSplitTokens * kWindowChunk;
     plan.split_tokens = T;
     plan.max_splits = (int)((max_tokens + T - 1) / T);
     if (plan.max_splits < 1) plan.max_splits = 1;
@@ -1361,7 +1436,7 @@ DecodePlan plan_decode(const PoolGeom &p, int32_t num_sessions, int32_t num_q_he
         const int64_t shortest = p.head_dim == 128 ? kSmallSizes128[0].tokens : kSmallSizes64[0].tokens;
         const int64_t wgs = std::min(3 * cus, sg * ((max_tokens + shortest - 1) / shortest));
         const size_t most = pad((size_t)wgs * G * (p.head_dim + 2) * sizeof(float)) + 512;
-        const SmallDecodePlan dev = plan_small(p, cus, num_sessions, num_q_heads, max_blocks_per_session, nullptr, 0, SIZE_MAX);
+        const SmallDecodePlan dev = plan_small(p, cus, num_sessions, num_q_heads, max_blocks_per_session, nullptr, 0, SIZE_MAX, windowed);
         plan.small_bytes = std::max(dev.total(), (size_t)sg * kArrivedStride * sizeof(uint64_t) + most);
     }
     return plan;
@@ -1416,7 +1491,7 @@ struct PlanRow {
 };
 
 bool plan_decode_host(int S, int num_kv_heads, const int32_t *lens_host, int appended, int W, int t_min,
-                      int t_dev, bool dev_merges, DecodeHostPlanLarge &plan, int &t_out, bool &any_split) {
+                      int t_dev, bool dev_merges, bool windowed, DecodeHostPlanLarge &plan, int &t_out, bool &any_split) {
     if (W < 1 || W > kPlanMaxWg || S > 4096 || num_kv_heads > 255) return false;
     int64_t max_len = 1;
     for (int s = 0; s < S; ++s) max_len = std::max<int64_t>(max_len, (int64_t)lens_host[s] + appended);
@@ -1538,7 +1613,10 @@ bool plan_decode_host(int S, int num_kv_heads, const int32_t *lens_host, int app
     int best_t = 0;
     int64_t best_est = INT64_MAX;
     for (int T : cands) {
-        T = std::max(T, t_min);
+        // (Unsplit sessions need no room for partial results, which is why a split
+        // is no shorter than the kernel's own.  Plans without a window, whose own
+        // splits are powers of two, keep to it all the same.)
+        if (T != t_whole || !windowed) T = std::max(T, t_min);
         if (T % unit || T > t_whole) continue;
         if (!build(T)) continue;
         const int64_t est = snake() + (T < max_len ? kMergeCostTokens : 0);
@@ -1569,8 +1647,10 @@ struct CachedPlan {
     DecodeHostPlan small;                      // the same plan, when it fits
 };
 
-const CachedPlan *cached_decode_plan(int S, int hkv, const int32_t *lens_host, int appended, int W, int t_min,
-                                    int t_dev, bool dev_merges) {
+const CachedPlan *cached_decode_plan(int S, int hkv, const int32_t *lens_host, int appended, int W, const DecodePlan &dev) {
+    // (the least split of a host plan: the kernel's own, in whole 1024-token chunks)
+    const int t_min = (dev.split_tokens + 1023) / 1024 * 1024, t_dev = dev.split_tokens;
+    const bool dev_merges = dev.max_splits > 1;
     static thread_local CachedPlan cache[4];
     static thread_local int next_victim = 0;
     int64_t tokens = 0;
@@ -1599,7 +1679,7 @@ const CachedPlan *cached_decode_plan(int S, int hkv, const int32_t *lens_host, i
     c.t_dev = t_dev;
     c.dev_merges = dev_merges;
     c.tokens = tokens;
-    c.host = plan_decode_host(S, hkv, lens_host, appended, W, t_min, t_dev, dev_merges, c.plan, c.T, c.split);
+    c.host = plan_decode_host(S, hkv, lens_host, appended, W, t_min, t_dev, dev_merges, dev.windowed, c.plan, c.T, c.split);
     if (c.host) {
         const int items = c.plan.start[W] & ~kPlanCompactBit;
         const int words = (c.plan.start[W] & kPlanCompactBit) ? (items + 1) / 2 : items;
@@ -1632,13 +1712,11 @@ const CachedPlan *cached_decode_plan(int S, int hkv, const int32_t *lens_host, i
 SmallDecodePlan plan_small_call(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,
                                 int32_t max_blocks, const int32_t *lens_host, int32_t appended, size_t bytes,
                                 const DecodePlan &plan) {
-    const SmallDecodePlan sp = plan_small(p, cus, num_sessions, num_q_heads, max_blocks, lens_host, appended, bytes);
+    const SmallDecodePlan sp = plan_small(p, cus, num_sessions, num_q_heads, max_blocks, lens_host, appended, bytes, plan.windowed);
     if (!sp.split_tokens || sp.single || p.head_dim == 128 || !lens_host) return sp;
     const int64_t whole = (int64_t)num_sessions * p.num_kv_heads, split = (int64_t)sp.rows * p.num_kv_heads;
     if (split > (whole <= cus ? cus : 2 * cus)) {
-        const CachedPlan *c = cached_decode_plan(num_sessions, p.num_kv_heads, lens_host, appended, (int)cus,
-                                                 std::max(plan.split_tokens, 1024), plan.split_tokens,
-                                                 plan.max_splits > 1);
+        const CachedPlan *c = cached_decode_plan(num_sessions, p.num_kv_heads, lens_host, appended, (int)cus, plan);
         if (c->host && !c->split) return {};
     }
     return sp;
@@ -1665,8 +1743,7 @@ DecodeSchedule decode_schedule(const PoolGeom &p, int32_t num_sessions, int32_t 
     DecodeSchedule sc{plan.split_tokens, false, plan.max_splits > 1};
     if (context_lens_host) {
         const CachedPlan *c = cached_decode_plan(num_sessions, p.num_kv_heads, context_lens_host, appended,
-                                                 stream_cus(p, stream), std::max(plan.split_tokens, 1024),
-                                                 plan.split_tokens, plan.max_splits > 1);
+                                                 stream_cus(p, stream), plan);
         if (c->host) sc = DecodeSchedule{c->T, true, c->split};
     }
     return sc;
@@ -1681,6 +1758,7 @@ namespace {
 
 template <bool kWin>
 hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk_blocks, const int32_t *walk_lens_host,
+                           const int32_t *walk_skips,
                            void *workspace, size_t workspace_bytes, const DecodePlan &plan, DecodeArgsT<kWin> &a,
                            hipStream_t stream) {
     const int32_t num_q_heads = a.group * p.num_kv_heads;
@@ -1701,11 +1779,28 @@ hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk
         a.part_ml = reinterpret_cast<float *>(ws + sp.count_bytes);
         a.part_acc = reinterpret_cast<float *>(ws + sp.count_bytes + sp.ml_bytes);
         const dim3 grid((unsigned)(sp.rows * p.num_kv_heads));
-        const int per_wave = sp.split_tokens / (kDecWaves * kBlock);
+        const int per_wave = (sp.split_tokens + kDecWaves * kBlock - 1) / (kDecWaves * kBlock);
 #define LS_SMALL(DD, DEPTH, LOOP) \
     hipLaunchKernelGGL((decode_small_kernel<DD, DEPTH, LOOP, decltype(rows)::value, kWin>), grid, dim3(kDecThreads), 0, stream, a, arg)
         auto launch = [&](auto rows, const auto &arg) {
-            if (p.head_dim == 128) {
+            if constexpr (kWin) {
+                // All of a wave's blocks in flight at once, but at D = 128 only where
+                // every workgroup has a CU: from three blocks on, the registers
+                // leave a CU to one workgroup (143 sessions of 544 keys at 4 heads:
+                // 31.6 us, 35.4 with five in flight).
+                if (p.head_dim == 128) {
+                    if (per_wave <= 2) LS_SMALL(128, 2, false);
+                    else if (per_wave > 5 || (int64_t)grid.x > resident) LS_SMALL(128, 2, true);
+                    else if (per_wave <= 3) LS_SMALL(128, 3, false);
+                    else if (per_wave <= 4) LS_SMALL(128, 4, false);
+                    else LS_SMALL(128, 5, false);
+                } else {
+                    if (per_wave <= 2) LS_SMALL(64, 2, false);
+                    else if (per_wave <= 3) LS_SMALL(64, 3, false);
+                    else if (per_wave <= 4) LS_SMALL(64, 4, false);
+                    else LS_SMALL(64, 4, true);
+                }
+            } else if (p.head_dim == 128) {
                 if (per_wave <= 2) LS_SMALL(128, 2, false);
                 else if (per_wave <= 4) LS_SMALL(128, 4, false);
                 else LS_SMALL(128, 2, true);
@@ -1715,12 +1810,15 @@ hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk
             }
         };
         if (walk_lens_host && !sp.single) {
-            SmallRows list;
+            typename std::conditional<kWin, SmallWindowRows, SmallRows>::type list;
             int n = 0;
             for (int32_t s = 0; s < num_sessions; ++s) {
                 const int64_t L = (int64_t)walk_lens_host[s] + a.appended;
                 const int ns = (int)std::max<int64_t>(1, (L + sp.split_tokens - 1) / sp.split_tokens);
-                for (int k = 0; k < ns; ++k) list.row[n++] = (uint32_t)s | ((uint32_t)k << 12) | ((uint32_t)ns << 22);
+                for (int k = 0; k < ns; ++k) {
+                    if constexpr (kWin) list.skip[n] = walk_skips[s];
+                    list.row[n++] = (uint32_t)s | ((uint32_t)k << 12) | ((uint32_t)ns << 22);
+                }
             }
             launch(std::true_type{}, list);
         } else {
@@ -1740,8 +1838,7 @@ hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk
     // Host lengths: the schedule is planned here and passed with the arguments.
     if (walk_lens_host) {
         const CachedPlan *c = cached_decode_plan(num_sessions, p.num_kv_heads, walk_lens_host, a.appended,
-                                                 (int)resident, std::max(plan.split_tokens, 1024),
-                                                 plan.split_tokens, plan.max_splits > 1);
+                                                 (int)resident, plan);
         if (c->host) {
             const bool split = c->split;
             a.split_tokens = c->T;
@@ -1768,13 +1865,14 @@ hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk
     const NoPlan none{0};
 #define LS_DECODE(DD, PW) \
     hipLaunchKernelGGL((decode_kernel<DD, 2, PW, false, kPlanItemsSmall, kWin>), grid, dim3(kDecThreads), 0, stream, a, none)
+    constexpr int kShort = kWin ? kWindowPerWaveShort : 4, kLong = kWin ? kWindowPerWave : 8;
     const int per_wave = plan.split_tokens / (kDecWaves * kBlock);
     if (p.head_dim == 128) {
-        if (per_wave == 4) LS_DECODE(128, 4);
-        else LS_DECODE(128, 8);
+        if (per_wave == kShort) LS_DECODE(128, kShort);
+        else LS_DECODE(128, kLong);
     } else {
-        if (per_wave == 4) LS_DECODE(64, 4);
-        else LS_DECODE(64, 8);
+        if (per_wave == kShort) LS_DECODE(64, kShort);
+        else LS_DECODE(64, kLong);
     }
 #undef LS_DECODE
     hipError_t e = hipGetLastError();
@@ -1809,18 +1907,18 @@ hipError_t launch_decode(const PoolGeom &p, int layer, int32_t num_sessions, int
     a.window = window;
     a.sinks = sinks;
     if (!window)
-        return launch_decode_t<false>(p, num_sessions, max_blocks, context_lens_host, workspace, workspace_bytes, plan,
+        return launch_decode_t<false>(p, num_sessions, max_blocks, context_lens_host, nullptr, workspace, workspace_bytes, plan,
                                       a, stream);
     // The planners see the walks: their lengths (without the appended token, as
     // those of whole sessions) and the most blocks one has.
-    int32_t walk[kMaxBatch];
+    int32_t walk[kMaxBatch], skips[kMaxBatch];
     if (context_lens_host)
         for (int32_t s = 0; s < num_sessions; ++s) {
-            const int32_t L = context_lens_host[s] + a.appended;
-            walk[s] = context_lens_host[s] - window_skip(L, window, sinks) * kBlock;
+            skips[s] = window_skip(context_lens_host[s] + a.appended, window, sinks);
+            walk[s] = context_lens_host[s] - skips[s] * kBlock;
         }
     return launch_decode_t<true>(p, num_sessions, window_blocks(max_blocks, window, sinks),
-                                 context_lens_host ? walk : nullptr, workspace, workspace_bytes, plan, a, stream);
+                                 context_lens_host ? walk : nullptr, skips, workspace, workspace_bytes, plan, a, stream);
 }
 
 }  // namespace ls

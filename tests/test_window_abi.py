@@ -42,7 +42,7 @@ def test_window_bounds_the_workspace_and_the_table(lib, pool):  # noqa: F811
     lib.ls_decode_workspace_bytes.restype = SZ
     wide = f(pool, 64, 32, 100000, 1024, 4)
     assert 0 < wide == f(pool, 64, 32, 67, 1024, 4) == f(pool, 64, 32, 1 << 26, 1024, 4)      # 65 blocks of a window, 1 of sinks ...
-    assert f(pool, 64, 32, 16, 1024, 4) == lib.ls_decode_workspace_bytes(pool, 64, 32, 16)
+    assert f(pool, 64, 32, 16, 1024, 4) < wide
     for bad in ((0, 4), (-1, 0), (16, -1), ((1 << 29) + 1, 0)):
         assert f(pool, 64, 32, 100, *bad) == 0
     assert f(None, 64, 32, 100, 64, 0) == 0 and f(pool, 64, 32, 0, 64, 0) == 0
