@@ -102,14 +102,18 @@ struct PrefillArgs {
 };
 
 // Sliding window: row j of a turn, at position p = c + j, sees key t when t <= p
-// and either t < sinks or t > p - window.  A query tile walks the blocks that
-// some row of it sees as if they were one shorter context: the
-// ceil(sinks / 16) blocks of the first tokens, then those from key
-// p_first - window + 1 on.  `skip` blocks between the two are left out, so
-// position v of the walk is token v (in the first tokens' blocks) or v + 16 skip.
-// Keys, limits and tiles below are counted on the walk; only table columns are
-// not.  On it a row whose own position is v_p misses keys v in
-// [sinks, v_p - window + 1), the row's hole.
+// and either t < sinks or t > p - window.  A query tile walks the keys that its
+// rows see as if they were one shorter context, in two parts:
+//   the first tokens' 32-key units, as many as hold `sinks` keys, of which a row
+//   sees the keys below sinks and at most p;
+//   the window's blocks, from that of key max(p_first - window + 1, sinks) on
+//   (p_first: the tile's first row), of which a row sees keys from sinks and from
+//   p - window + 1 up to p.
+// So a unit needs one range test at most: position v of the walk is token v in
+// the first part and token v + 16 shift_blocks (which may be negative: a block may
+// be in both parts, for different keys) in the second.  Keys, limits and tiles
+// below are counted on the walk; only table columns are not.  A tile all of whose
+// rows are first tokens has no second part.
 struct PrefillWindowArgs : PrefillArgs {
     int32_t window;                // >= 1
     int32_t sinks;                 // >= 0
@@ -193,13 +197,21 @@ __device__ __forceinline__ int32_t table_entry(const int32_t *table, int jb, int
     return b | ~keep;
 }
 
-// The same for block jb of a query tile's walk, of which block `first` is the
-// first one counted and nv are there.
-__device__ __forceinline__ int32_t window_entry(const int32_t *table, int jb, int nv, int first, int sink_blocks,
-                                                int skip, int max_blocks) {
+// A query tile's walk (see PrefillWindowArgs).
+struct Walk {
+    int first_blocks;              // blocks that the first tokens' units span (INT_MAX: there is no second part)
+    int sink_blocks;               // of which so many hold a first token: the last one stands for the others
+    int shift_blocks;              // table column less block number, in the second part
+};
+
+// The same for block jb of a walk, of which block `first` is the first one
+// counted and nv are there.
+__device__ __forceinline__ int walk_column(const Walk &w, int j) {
+    return j < w.first_blocks ? min(j, w.sink_blocks - 1) : j + w.shift_blocks;
+}
+__device__ __forceinline__ int32_t window_entry(const int32_t *table, int jb, int nv, int first, const Walk &w) {
     typedef const __attribute__((address_space(4))) int32_t const_i32;
-    const int j = first + max(min(jb, nv - 1), 0);
-    const int32_t b = ((const_i32 *)table)[min(j + (j >= sink_blocks ? skip : 0), max_blocks - 1)];
+    const int32_t b = ((const_i32 *)table)[walk_column(w, first + max(min(jb, nv - 1), 0))];
     const int32_t keep = -(int32_t)((unsigned)jb < (unsigned)nv);
     return b | ~keep;
 }
@@ -329,16 +341,26 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             nblk_valid = a.max_blocks;
             if (tid == 0) flag_error(a.err, LS_DEVERR_LENGTH);
         }
-        // Blocks that the tile's walk leaves out, and the walk's length.
-        int window = 0, sinks = 0, sink_blocks = 0, skip = 0;
+        // The tile's walk; its first part's keys, and the second part's first that a row sees.
+        int window = 0, sinks = 0, shift = 0, first_keys = 0, seen_from = 0;
+        Walk walk = {0, 0, 0};
         if constexpr (kWin) {
             window = a.window;
             sinks = a.sinks;
-            sink_blocks = (sinks + kBlock - 1) / kBlock;
-            skip = max(max(c + j0 - window + 1, 0) / kBlock - sink_blocks, 0);
-            nblk_valid = max(nblk_valid - skip, 0);
+            walk.sink_blocks = min((sinks + kBlock - 1) / kBlock, nblk_valid);
+            walk.first_blocks = INT32_MAX;
+            first_keys = INT32_MAX;
+            if (c + j_last >= sinks) {
+                walk.first_blocks = (sinks + 31) / 32 * 2;
+                first_keys = walk.first_blocks * kBlock;
+                const int from = max(c + j0 - window + 1, sinks);
+                walk.shift_blocks = from / kBlock - walk.first_blocks;
+                seen_from = first_keys + from % kBlock;
+                nblk_valid = max(nblk_valid - walk.shift_blocks, 0);
+            }
+            shift = walk.shift_blocks * kBlock;
         }
-        const int kv_end = c + j_last + 1 - skip * kBlock;    // keys this tile can see
+        const int kv_end = c + j_last + 1 - shift;            // keys this tile can see
         // This item's key tiles: [tile0, tile0 + ntiles).  Below, keys, blocks
         // and key tiles are counted from tile0.
         int tile0 = 0, ntiles = (kv_end + kKeyTile - 1) / kKeyTile;
@@ -348,13 +370,18 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             ntiles = key_chunk(all, chunk + 1, chunks) - tile0;
         }
         // (With a window every position below is one of the walk, from tile0 on.)
-        const int key_base = tile0 * kKeyTile + skip * kBlock;
+        const int key_base = tile0 * kKeyTile + shift;
         const int kv_len = c + n - key_base;
         int nb = min(nblk_valid - tile0 * 4, ntiles * 4);     // blocks any row here can see
         if (kSplit || kWin) nb = max(nb, 0);                  // (a part past the end of the table)
-        // Keys [hole_lo, hole_hi) are seen by no row of the tile (its first row's hole).
-        const int hole_lo = sinks - tile0 * kKeyTile;
-        const int hole_hi = kWin ? c + j0 - window + 1 - key_base : 0;
+        if (kWin && nb == 0) walk = {INT32_MAX, 1, 0};        // (its table reads stay in column 0)
+        // Keys [dead_lo, dead_hi) are seen by no row of the tile: the end of the
+        // first tokens' last unit, and the keys before the window's first.
+        const int dead_lo = sinks - tile0 * kKeyTile;
+        const int dead_hi = !kWin ? 0 : first_keys == INT32_MAX ? INT32_MAX : seen_from - tile0 * kKeyTile;
+        // The key tiles that hold such keys: dead_count from dead_tile on.
+        const int dead_tile = max(dead_lo, 0) / kKeyTile;
+        const int dead_count = dead_hi > max(dead_lo, 0) ? (dead_hi - 1) / kKeyTile + 1 - dead_tile : 0;
 
         if (kSplit && chunks > 1 && ntiles <= 0) {             // a piece without keys
             for (int r = tid; r < kPreRows; r += kPreThreads) a.part_ml[((int64_t)piece * kPreRows + r) * 2] = kNoKey;
@@ -389,8 +416,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         }
         int first_ids = -1;                                   // block `lane` of the walk, from tile0 on
         if constexpr (kWin) {
-            const int at = tile0 * 4 + lane;
-            const int32_t id = a.block_tables[(int64_t)s * a.max_blocks + min(at + (at >= sink_blocks ? skip : 0), a.max_blocks - 1)];
+            const int32_t id = a.block_tables[(int64_t)s * a.max_blocks + walk_column(walk, tile0 * 4 + min(lane, max(nb - 1, 0)))];
             first_ids = lane < nb ? id : -1;
         }
         // Wait for q here, before the first stage loads are issued, so that no
@@ -398,8 +424,10 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         if constexpr (!kWin) __builtin_amdgcn_s_waitcnt(0x0F70);
         // smallest causal limit among this wave's rows: units past it need masking
         const int wave_lim_min = c + min(j0 + (wave * kWaveRows) / G, n - 1) - key_base;
-        // end of its rows' longest hole
-        const int wave_hole_max = kWin ? c + min(j0 + (wave * kWaveRows + kWaveRows - 1) / G, n - 1) - key_base - window + 1 : 0;
+        // and with a window the units that all its rows see whole: those that start
+        // at one of `wave_whole` keys from wave_from on (all in the window's part)
+        const int wave_from = kWin ? max(c + min(j0 + ((wave * kWaveRows + kWaveRows - 1) >> lg), n - 1) - window + 1, sinks) - key_base : 0;
+        const int wave_whole = max(wave_lim_min - 30 - wave_from, 0);
 
         // Key tiles some row of this wave sees: none when its rows are all padding,
         // fewer than the workgroup's where the tile spans many tokens.  Past them
@@ -428,7 +456,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         }
         const int32_t *table = a.block_tables + (int64_t)s * a.max_blocks + (!kWin && nb > 0 ? tile0 * 4 : 0);
         auto entry = [&](int jb) {
-            if constexpr (kWin) return window_entry(table, jb, nb, tile0 * 4, sink_blocks, skip, a.max_blocks);
+            if constexpr (kWin) return window_entry(table, jb, nb, tile0 * 4, walk);
             else return table_entry(table, jb, nb);
         };
         const uint32_t slab_elems = (uint32_t)(2 * Hkv * kBlock * D);
@@ -511,8 +539,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         // Causal mask of a unit whose first key is key0 (lane group g4 holds unit
         // keys 8*g4 + 4*sb + i); only units that reach past the smallest causal
         // limit of the wave's rows need it.
-        // With a window, units that reach into some row's hole do too.  And no unit
-        // is seen by every row: a row's running maximum starts from the first unit
+        // With a window, units that hold a key some row does not see yet, or any
+        // more, do too.  And no unit is seen by every row: a row's running maximum starts from the first unit
         // that holds a finite score of it (a row that is `unset` has none so far:
         // all its scores, and probabilities, are then -inf and 0 whatever the
         // maximum is taken for).
@@ -522,25 +550,18 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         bool pending = kWin;                           // some row of the wave is unset
         auto mask_unit = [&](f32x4 (&acc)[kRT][2], int key0) {
             if constexpr (kWin) {
-                const bool in_hole = key0 < wave_hole_max && key0 + 31 >= hole_lo;
-                if (key0 + 31 <= wave_lim_min && !in_hole && !pending) return;
-                if (in_hole && key0 < hole_lo) {       // the last of the first tokens
+                if (!pending && (unsigned)(key0 - wave_from) < (unsigned)wave_whole) return;
+                const bool first = key0 + tile0 * kKeyTile < first_keys;
     #pragma unroll
-                    for (int rt = 0; rt < kRT; ++rt) {
-                        const int lim = row_lim[rt] - key0 - 8 * g4, lo = hole_lo - key0 - 8 * g4;
+                for (int rt = 0; rt < kRT; ++rt) {
+                    // Keys of the unit up to lim are seen, `seen` of them.
+                    int lim = row_lim[rt], seen = INT32_MAX;
+                    if (first) lim = min(lim + shift, dead_lo - 1);
+                    else seen = max(min(window, lim + key_base - sinks + 1), 0);
+                    lim -= key0 + 8 * g4;
     #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e > lim || (e >= lo && e <= lim - window)) acc[rt][e / 4][e % 4] = -INFINITY;
-                    }
-                } else {                               // 0 <= row_lim - key < window
-                    const unsigned seen = in_hole ? (unsigned)window : 0x80000000u;
-    #pragma unroll
-                    for (int rt = 0; rt < kRT; ++rt) {
-                        const int lim = row_lim[rt] - key0 - 8 * g4;
-    #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if ((unsigned)(lim - e) >= seen) acc[rt][e / 4][e % 4] = -INFINITY;
-                    }
+                    for (int e = 0; e < 8; ++e)
+                        if ((unsigned)(lim - e) >= (unsigned)seen) acc[rt][e / 4][e % 4] = -INFINITY;
                 }
                 if (pending) {
                     bool left = false;
@@ -668,7 +689,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             for (int ci = tid; ci < kChunks; ci += kPreThreads) {
                 const int bi = ci / (2 * D), hf = (ci / D) & 1;
                 const int t0 = j * kKeyTile + bi * kBlock + hf * 8;
-                if (t0 + 8 <= kv_len && !(kWin && t0 < hole_hi && t0 + 8 > hole_lo)) continue;
+                if (t0 + 8 <= kv_len && !(kWin && t0 < dead_hi && t0 + 8 > dead_lo)) continue;
                 u32x4 *chunk = reinterpret_cast<u32x4 *>(lv + ci * 16);
                 u32x4 x = *chunk;
     #pragma unroll
@@ -676,8 +697,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
                     const int t = t0 + 2 * w;
                     x[w] &= t + 1 < kv_len ? 0xFFFFFFFFu : (t < kv_len ? 0x0000FFFFu : 0u);
                     if constexpr (kWin) {
-                        if (t >= hole_lo && t < hole_hi) x[w] &= 0xFFFF0000u;
-                        if (t + 1 >= hole_lo && t + 1 < hole_hi) x[w] &= 0x0000FFFFu;
+                        if (t >= dead_lo && t < dead_hi) x[w] &= 0xFFFF0000u;
+                        if (t + 1 >= dead_lo && t + 1 < dead_hi) x[w] &= 0x0000FFFFu;
                     }
                 }
                 *chunk = x;
@@ -821,8 +842,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             idk = id_k(j + 3);
             idv = id_v(j + 3);
             const bool live = j < wave_tiles;
-            if (j < ntiles && ((j + 1) * kKeyTile > kv_len ||
-                               (kWin && j * kKeyTile < hole_hi && (j + 1) * kKeyTile > hole_lo)))
+            if (j < ntiles && ((j + 1) * kKeyTile > kv_len || (kWin && (unsigned)(j - dead_tile) < (unsigned)dead_count)))
                 zero_v_tail(vs, j);
             load_k(kn, ik);
             load_v(vn, iv);
@@ -901,6 +921,20 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
                 at = (((int64_t)a.cu[s] + j0 + jl) * hq_total + g * G + h) * D;
             }
             uint16_t *orow = a.out + at;
+            if constexpr (kWin) {
+                // Lanes of neighbouring rows of 16 trade halves of two dim tiles, so
+                // that each stores 16 bytes: an item's 64 KiB took 2.2 us in pieces
+                // of 8.
+    #pragma unroll
+                for (int dt = 0; dt < NDT; dt += 2) {
+                    const auto x = __builtin_amdgcn_permlane16_swap(pack_bf16x2(o[rt][dt][0] * inv, o[rt][dt][1] * inv),
+                                                                    pack_bf16x2(o[rt][dt + 1][0] * inv, o[rt][dt + 1][1] * inv), false, false);
+                    const auto y = __builtin_amdgcn_permlane16_swap(pack_bf16x2(o[rt][dt][2] * inv, o[rt][dt][3] * inv),
+                                                                    pack_bf16x2(o[rt][dt + 1][2] * inv, o[rt][dt + 1][3] * inv), false, false);
+                    *reinterpret_cast<u32x4 *>(orow + (dt + (g4 & 1)) * 16 + (g4 & 2) * 4) = u32x4{x[0], y[0], x[1], y[1]};
+                }
+                continue;
+            }
     #pragma unroll
             for (int dt = 0; dt < NDT; ++dt) {
                 const u32x2 w = u32x2{pack_bf16x2(o[rt][dt][0] * inv, o[rt][dt][1] * inv),
@@ -1268,7 +1302,8 @@ bool collect_pairs(int32_t S, int32_t hkv, int32_t qtok, const int32_t *lens, in
         if (items == 0) continue;
         int64_t len = (int64_t)c + n, twice = 2 * (int64_t)c + n;
         if (window) {
-            len = std::min<int64_t>(len, (int64_t)window + sinks + qtok + 2 * kBlock - 2);
+            const int64_t first = (sinks + 31) / 32 * 32;
+            len = std::min<int64_t>(len + first, (int64_t)window + first + qtok + 2 * kBlock - 2);
             twice = std::min<int64_t>(twice, 2 * len);
         }
         for (int g = 0; g < hkv; ++g)
