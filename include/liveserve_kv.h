@@ -363,7 +363,8 @@ ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num
  * LS_DEVERR_FREE_LIST; then tables, ring and counters stay as they are (next_counts =
  * free_counts, next_lens = seq_lens), cu_new_lens is all 0 and slot_map all -1.  An id
  * outside the pool is copied as it stands and flagged (LS_DEVERR_BLOCK_ID), its
- * tokens' slots are -1.  The pool gives the range of ids; its memory is not touched.
+ * tokens' slots are -1.  A session with new_lens[s] = 0 gets no slot: an appending
+ * decode of this step leaves it out, since its next block may not be its own.  The pool gives the range of ids; its memory is not touched.
  * Errors: LS_EINVAL (NULL, misaligned or overlapping arrays, sizes out of range, free_ring without
  * counters or the other way round, a window without free_ring, a window or sinks out
  * of range, more than 2^27 - 1 blocks per session), LS_EHIP.

@@ -967,7 +967,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             const int nt = a.cu[sp + 1] - a.cu[sp];
             int planned = QT;
             if constexpr (kHost) planned = plan.session_items[sp];
-            if (nt < 0 || nt > planned * qtok || a.ctx[sp] < 0 || a.cu[sp] < 0 || a.cu[sp + 1] > a.total)
+            if (nt < 0 || nt > planned * qtok || a.ctx[sp] < 0 || a.cu[sp] < 0 || a.cu[sp + 1] > a.total ||
+                (kWin && nt > 0 && (int64_t)a.ctx[sp] + nt > (int64_t)a.max_blocks * kBlock))
                 flag_error(a.err, LS_DEVERR_LENGTH);
         }
     int s, g, qt, chunk = 0, chunks = 1, piece = 0;

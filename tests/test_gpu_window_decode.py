@@ -107,6 +107,18 @@ def test_schedules(kv, oracle_lib, s, lo, hi, window, sinks, hq, hkv, d):
     Case(kv, oracle_lib, lens, window, sinks, hq, hkv, d, bool(s % 2), seed=s).check(what="%d sessions W %d" % (s, window))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_as_many_sessions_as_a_call_takes(kv, oracle_lib, d):
+    rng = np.random.default_rng(d)
+    Case(kv, oracle_lib, rng.integers(1, 500, 2048), 90, 3, 4, 1, d, True, seed=d).check(what="2048 sessions")
+
+
+def test_a_table_of_two_million_tokens(kv, oracle_lib):
+    """Positions and table columns far past the blocks that a call may read (16384)."""
+    cols = 1 << 17
+    Case(kv, oracle_lib, [cols * BLOCK - 1, 5, 100000], 700, 20, 8, 2, 128, True, seed=41, extra_cols=0).check(what="long cache")
+
+
 @pytest.mark.parametrize("host", [False, True])
 def test_small_workspace_runs_the_persistent_kernel(kv, oracle_lib, host):
     """The least workspace a call takes leaves the single-launch schedule no room."""

@@ -113,6 +113,22 @@ def test_schedules(kv, oracle_lib, turns, window, sinks, hq, hkv, d):
     c.check(what="%d turns W %d" % (len(turns), window), rows=rows)
 
 
+@pytest.mark.parametrize("sessions,hkv", [(70, 8), (40, 8), (300, 1)])
+def test_many_pairs(kv, oracle_lib, sessions, hkv):
+    """More (session, KV head) pairs than a host plan holds (256), or than the kernel schedules (512)."""
+    rng = np.random.default_rng(sessions)
+    turns = [(int(rng.integers(1, 40)), int(rng.integers(0, 300))) for _ in range(sessions)]
+    c = Case(kv, oracle_lib, turns, 100, 5, 2 * hkv, hkv, 64, True, seed=sessions)
+    c.check(what="%d sessions of %d heads" % (sessions, hkv))
+
+
+def test_a_table_of_two_million_tokens(kv, oracle_lib):
+    cols = 1 << 17
+    c = Case(kv, oracle_lib, [(50, cols * BLOCK - 50), (20, 300)], 300, 4, 8, 2, 64, True, seed=41, extra_cols=0)
+    assert c.tables.shape[1] == cols
+    c.check(what="long cache")
+
+
 @pytest.mark.parametrize("shape", ["rising", "falling", "spike", "sinks", "own"])
 def test_peaky_scores(kv, oracle_lib, shape):
     """Keys far larger than the row's own (whose score the running maximum starts from), or far smaller."""
@@ -234,5 +250,14 @@ def test_bad_lengths_and_ids_are_flagged(kv, oracle_lib):
     c.dctx.copy_(i32_dev([c.tables.shape[1] * BLOCK, 50]))
     c.run("device")
     assert kv.ls_device_errors() & kv.LS_DEVERR_LENGTH
+    c.dctx.copy_(i32_dev([2**31 - 10, 50]))
+    c.run("device")
+    assert kv.ls_device_errors() & kv.LS_DEVERR_LENGTH
     c.dctx.copy_(i32_dev(c.c))
+    keep = c.tables.clone()
+    c.tables[0, 110 // BLOCK] = -2
+    for mode in ("device", "full"):
+        c.run(mode)                                  # an id outside the pool: its keys are absent
+    kv.ls_device_errors()
+    c.tables.copy_(keep)
     c.check(what="afterwards")
