@@ -98,9 +98,12 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(
     }
 }
 
-// Workgroup (kRows consecutive rows, KV head).  Bound by bandwidth (every row is
-// read and written once), or by latency when there are few.  K goes straight
-// from registers to its tile: a wave moves 16 rows x 4 chunks of 16 bytes, so
+// Workgroup (kRows consecutive rows, KV head).  Bound by bandwidth when there are
+// many rows, each read and written once (19817 rows of 4 heads x 128 dims, 162 MB:
+// 28.8 us or 5.64 TB/s while half of it stays cached, 45 us or 3.6 TB/s from HBM;
+// 6.17 is what a plain read and write of as much reaches), by latency when there
+// are few (2.6 us inside a graph for one row, 3.4 for 256 lone slots of 2 heads).  K goes straight
+// from registers to its tile: a wave moves up to 16 rows x 4 chunks of 16 bytes, so
 // that consecutive slots make 256 contiguous bytes.  V is turned through LDS: a
 // slot's values lie 32 bytes apart in the dim-major tile, and only with the
 // neighbouring slots at hand do they make whole 16-byte stores.  The rows are
@@ -117,7 +120,9 @@ __global__ __launch_bounds__(kAppendThreads) void append_slots_kernel(
     uint16_t *__restrict__ layer_pool, int64_t num_blocks, int32_t num_kv_heads, const uint16_t *__restrict__ k_new,
     const uint16_t *__restrict__ v_new, int64_t k_stride, int64_t v_stride, const int64_t *__restrict__ slots,
     int32_t total, unsigned int *err) {
-    static_assert(kRows + kAppendAhead < kWave && kRows % kBlock == 0, "a lane per row, and the row that ends the last segment");
+    static_assert(kRows + kAppendAhead < kWave, "a lane per row, and the row that ends the last segment");
+    constexpr int kRun = kRows < kBlock ? kRows : kBlock;       // rows whose chunks a K store interleaves
+    static_assert(kRows % kRun == 0, "whole runs");
     constexpr int kChunks = D / 8;                              // 16-byte chunks of a row
     constexpr int kPitch = D + 8;                               // (16 bytes of padding: a column's two halves in distinct banks)
     __shared__ __attribute__((aligned(16))) uint16_t sv[kRows + kAppendAhead][kPitch];
@@ -131,10 +136,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_slots_kernel(
     const int rows = (int)min((int64_t)kRows + kAppendAhead, total - row0);      // rows there are to look at
     // K rows, and with few rows, where latency counts, V rows too, are requested
     // before the slots are known.
-    auto k_row = [&](int c) { return c % kBlock + c / (kBlock * kChunks) * kBlock; };
-    auto k_chunk = [&](int c) { return c / kBlock % kChunks; };
+    auto k_row = [&](int c) { return c % kRun + c / (kRun * kChunks) * kRun; };
+    auto k_chunk = [&](int c) { return c / kRun % kChunks; };
     constexpr int kLoadsK = (kRows * kChunks + kAppendThreads - 1) / kAppendThreads;
-    constexpr bool kEarly = kRows == kBlock;
+    constexpr bool kEarly = kRows <= kBlock;
     u32x4 kreg[kLoadsK], vreg[kEarly ? kLoadsK : 1];
 #pragma unroll
     for (int i = 0; i < kLoadsK; ++i) {
@@ -230,19 +235,27 @@ __global__ __launch_bounds__(kAppendThreads) void append_slots_kernel(
 hipError_t launch_append_slots(const PoolGeom &p, int layer, int32_t total_tokens, const uint16_t *k_new,
                                const uint16_t *v_new, int64_t k_stride, int64_t v_stride, const int64_t *slot_map,
                                unsigned int *err, hipStream_t stream) {
-    // 48 rows per workgroup where that gives every CU two workgroups, else 16.
-    const int64_t wide = ((int64_t)total_tokens + 47) / 48;
-    const bool many = wide * p.num_kv_heads >= 2 * (p.num_cus > 0 ? p.num_cus : 256);
-    const dim3 grid((unsigned)(many ? wide : ((int64_t)total_tokens + 15) / 16), (unsigned)p.num_kv_heads);
+    // Rows per workgroup by how many workgroups that leaves each CU (us inside a
+    // graph, 128 dims, 2 KV heads).  Fewer than one of 16 rows: 4, since a slot
+    // without its neighbours costs 128 narrow stores, which then spread over more
+    // CUs (256 lone slots 3.4 against 4.6; runs of 16 slots the same, 2.9).  From 8 of
+    // 48 rows on, 48: less of what the next workgroup's segments need is read twice
+    // (65536 rows 21.2 against 21.9); below, 16 (32768 rows 12.1 either way, 16384 rows 6.5 against 7.8).
+    const int64_t cus = p.num_cus > 0 ? p.num_cus : 256;
+    auto groups = [&](int rows) { return ((int64_t)total_tokens + rows - 1) / rows * p.num_kv_heads; };
+    const int rows = groups(48) >= 8 * cus ? 48 : groups(16) >= cus ? 16 : 4;
+    const dim3 grid((unsigned)(groups(rows) / p.num_kv_heads), (unsigned)p.num_kv_heads);
 #define LS_APPEND(DD, ROWS) \
     hipLaunchKernelGGL((append_slots_kernel<DD, ROWS>), grid, dim3(kAppendThreads), 0, stream, p.layer_base(layer), \
                        p.num_blocks, p.num_kv_heads, k_new, v_new, k_stride, v_stride, slot_map, total_tokens, err)
     if (p.head_dim == 128) {
-        if (many) LS_APPEND(128, 48);
-        else LS_APPEND(128, 16);
+        if (rows == 48) LS_APPEND(128, 48);
+        else if (rows == 16) LS_APPEND(128, 16);
+        else LS_APPEND(128, 4);
     } else {
-        if (many) LS_APPEND(64, 48);
-        else LS_APPEND(64, 16);
+        if (rows == 48) LS_APPEND(64, 48);
+        else if (rows == 16) LS_APPEND(64, 16);
+        else LS_APPEND(64, 4);
     }
 #undef LS_APPEND
     return hipGetLastError();

@@ -267,6 +267,23 @@ def test_append_in_any_order_and_with_rows_left_out(kv, oracle_lib, d):
     append_case(kv, oracle_lib, swapped, 1, d, False, 40)
 
 
+@pytest.mark.parametrize("hkv,d", [(32, 64), (32, 128), (7, 64), (7, 128)])
+@pytest.mark.parametrize("rows", [40, 900, 4000, 15000])
+def test_append_row_counts(kv, oracle_lib, hkv, d, rows):
+    """From few rows, a few per workgroup, to many: runs of turns, lone slots and rows left out, mixed."""
+    if rows * hkv > 130000:
+        rows = 4001
+    rng = np.random.default_rng(rows + hkv)
+    lens, left = [], rows
+    while left > 0:
+        lens.append(min(left, int(rng.choice([1, 2, 15, 16, 17, 40, 200]))))
+        left -= lens[-1]
+    nb = sum((n + 30) // 16 for n in lens)
+    slots = runs(rng, nb, lens)
+    slots[rng.random(rows) < 0.02] = -1
+    append_case(kv, oracle_lib, slots, hkv, d, rows % 2 == 0, nb, host=True)
+
+
 def test_append_large_and_slots_past_the_pool(kv, oracle_lib):
     rng = np.random.default_rng(3)
     append_case(kv, oracle_lib, runs(rng, 900, rng.integers(1, 700, 20)), 4, 128, True, 900)
