@@ -16,7 +16,6 @@ namespace ls {
 
 namespace {
 
-constexpr int kTabRows = 4;             // rows per thread up to which one workgroup does the whole step
 
 struct TablesArgs {
     int64_t num_blocks;
@@ -75,22 +74,23 @@ __device__ __forceinline__ int ring_at(int first, unsigned i, int size) {
 // p: its slot; the table entry of the block it opens (p a multiple of 16); the
 // block that the next position's window leaves behind (dead(p + 1) =
 // dead(p) + 1).  What hangs on the other sessions are three prefix sums (rows,
-// blocks taken, blocks given), which every workgroup makes for itself, kThreads
-// sessions at a time.  A step of a decode batch moves a few KB, so the chain of
-// latencies is what it costs (lengths, scan, ids, stores), and one workgroup
-// without a second pass over the lengths is the shortest; a step of many rows is
-// spread over as many workgroups as it has kThreads rows.
+// blocks taken, blocks given), which every workgroup makes for itself, kPer
+// consecutive sessions a thread.  A step moves a few KB, so the chain of latencies
+// is what it costs (lengths, scan, ids, stores), and one pass over the lengths with
+// a thread for each row is the shortest (256 sessions of one row: 3.6 us inside a
+// graph, of which 2.5 are what any launch takes; 32 turns of 19817 rows in all: 4.4).
 //
 // write_state: lengths, prefix sums and counters are written, by workgroup 0.
 // Where they are the inputs' own memory and there are other workgroups, which
 // still read them, a launch of one workgroup without rows does that afterwards.
-template <int kThreads>
+template <int kThreads, int kPer>
 __global__ __launch_bounds__(kThreads) void tables_kernel(TablesArgs a, int rows_per_wg, int write_state) {
     constexpr int kWaves = kThreads / kWave;
+    constexpr int kChunk = kThreads * kPer;       // sessions at a time
     __shared__ unsigned sm_scan[3][kWaves];
     __shared__ unsigned sm_bad[kWaves];
-    __shared__ int sm_cu[kThreads + 1], sm_len[kThreads];
-    __shared__ unsigned sm_take[kThreads], sm_give[kThreads];
+    __shared__ int sm_cu[kChunk], sm_len[kChunk];
+    __shared__ unsigned sm_take[kChunk], sm_give[kChunk];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int S = a.num_sessions;
     int64_t taken = 0, given = 0;
@@ -98,12 +98,16 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(TablesArgs a, int rows
         taken = a.counts[0];
         given = a.counts[1];
     }
-    // Prefix sums of the chunk of sessions from s0 on: exclusive ones in `before`, totals in `all`.
-    // bad: lengths that cannot be served (of any of the chunk's sessions).
-    auto scan = [&](int s0, SessionStep &t, unsigned (&before)[3], unsigned (&all)[3], bool &bad) {
-        t = SessionStep{0, 0, 0u, 0u};
-        const bool wrong = s0 + tid < S && !session_step(a, s0 + tid, t);
-        const unsigned v[3] = {(unsigned)t.n, t.need, t.gives};
+    // Adds session s's step to v; false as session_step.
+    auto add = [&](int s, SessionStep &t, unsigned (&v)[3]) {
+        const bool ok = session_step(a, s, t);
+        v[0] = add_rows(v[0], (unsigned)t.n);
+        v[1] += t.need;
+        v[2] += t.gives;
+        return ok;
+    };
+    // Prefix sums of the threads' v: exclusive ones in `before`, totals in `all`; whether any thread's is wrong.
+    auto scan = [&](const unsigned (&v)[3], bool wrong, unsigned (&before)[3], unsigned (&all)[3]) {
         unsigned x[3] = {v[0], v[1], v[2]};
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
@@ -115,48 +119,62 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(TablesArgs a, int rows
             }
         }
         const bool any_wrong = __any(wrong);
+        // What the lanes before have: the difference, but for rows that have saturated
+        // (the step is refused then, and no prefix sum used).
+        before[0] = x[0] - v[0];
+        before[1] = x[1] - v[1];
+        before[2] = x[2] - v[2];
         if (lane == kWave - 1) {
 #pragma unroll
             for (int k = 0; k < 3; ++k) sm_scan[k][wave] = x[k];
             sm_bad[wave] = any_wrong;
         }
         __syncthreads();
-        unsigned first[3] = {0u, 0u, 0u}, is_bad = 0u;
+        unsigned is_bad = 0u;
         all[0] = all[1] = all[2] = 0u;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             if (w == wave) {
-                first[0] = all[0];
-                first[1] = all[1];
-                first[2] = all[2];
+                before[0] += all[0];
+                before[1] += all[1];
+                before[2] += all[2];
             }
             all[0] = add_rows(all[0], sm_scan[0][w]);
             all[1] += sm_scan[1][w];
             all[2] += sm_scan[2][w];
             is_bad |= sm_bad[w];
         }
-        bad = is_bad != 0u;
-        before[0] = add_rows(first[0], x[0]) - v[0];
-        before[1] = first[1] + x[1] - v[1];
-        before[2] = first[2] + x[2] - v[2];
+        return is_bad != 0u;
     };
-    SessionStep t;
+    SessionStep t[kPer];
     unsigned before[3], all[3];
-    bool wrong;
-    scan(0, t, before, all, wrong);
+    // The thread's sessions of the chunk from s0 on, and their sums.
+    auto chunk = [&](int s0) {
+        unsigned v[3] = {0u, 0u, 0u};
+        bool wrong = false;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            t[k] = SessionStep{0, 0, 0u, 0u};
+            if (s0 + tid * kPer + k < S && !add(s0 + tid * kPer + k, t[k], v)) wrong = true;
+        }
+        return scan(v, wrong, before, all);
+    };
+    bool wrong = chunk(0);
     // ---- totals: the step is refused as a whole when some length is out of
     // range, or rows, free blocks or the ring's room do not suffice.
     unsigned sum[3] = {all[0], all[1], all[2]};
-    for (int s0 = kThreads; s0 < S; s0 += kThreads) {
-        SessionStep u;
-        unsigned b[3], c[3];
-        bool w;
-        __syncthreads();                             // (the last chunk's sums are read)
-        scan(s0, u, b, c, w);
-        wrong = wrong || w;
-        sum[0] = add_rows(sum[0], c[0]);
-        sum[1] += c[1];
-        sum[2] += c[2];
+    if (S > kChunk) {
+        unsigned v[3] = {0u, 0u, 0u}, b[3], rest[3];
+        bool w = false;
+        for (int s = kChunk + tid; s < S; s += kThreads) {
+            SessionStep u;
+            if (!add(s, u, v)) w = true;
+        }
+        __syncthreads();                             // (the first chunk's sums are read)
+        wrong = scan(v, w, b, rest) || wrong;
+        sum[0] = add_rows(sum[0], rest[0]);
+        sum[1] += rest[1];
+        sum[2] += rest[2];
     }
     unsigned bad = wrong || sum[0] > (unsigned)a.total ? LS_DEVERR_LENGTH : 0u;
     if (a.ring && !bad) {
@@ -165,8 +183,9 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(TablesArgs a, int rows
             bad = LS_DEVERR_FREE_LIST;
     }
     if (bad) sum[0] = sum[1] = sum[2] = 0u;
-    __syncthreads();                                 // every wave has the counters and lengths (outputs may be the same memory)
-    if (write_state && blockIdx.x == 0 && tid == 0) {
+    const bool state = write_state && blockIdx.x == 0;
+    __syncthreads();                                 // every wave has the counters and the chunk's lengths (outputs may be the same memory)
+    if (state && tid == 0) {
         if (bad) flag_error(a.err, bad);
         a.cu[0] = 0;
         if (a.ring) {
@@ -179,26 +198,32 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(TablesArgs a, int rows
     const int first_kept = (a.sinks + kBlock - 1) / kBlock;
     unsigned carry[3] = {0u, 0u, 0u};
     for (int s0 = 0;;) {
-        const int s = s0 + tid;
-        if (bad) t.n = 0;
-        if (write_state && blockIdx.x == 0 && s < S) {
-            if (a.reused) a.reused[s] = t.L;
-            a.next_lens[s] = t.L + t.n;
-            a.cu[s + 1] = bad ? 0 : (int)(carry[0] + before[0]) + t.n;
+        unsigned at[3] = {carry[0] + before[0], carry[1] + before[1], carry[2] + before[2]};
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int e = tid * kPer + k, s = s0 + e;
+            if (bad) t[k].n = 0;
+            if (state && s < S) {
+                if (a.reused) a.reused[s] = t[k].L;
+                a.next_lens[s] = t[k].L + t[k].n;
+                a.cu[s + 1] = bad ? 0 : (int)at[0] + t[k].n;
+            }
+            sm_cu[e] = (int)at[0];
+            sm_len[e] = t[k].L;
+            sm_take[e] = at[1];
+            sm_give[e] = at[2];
+            at[0] += (unsigned)t[k].n;
+            at[1] += t[k].need;
+            at[2] += t[k].gives;
         }
-        sm_cu[tid] = (int)(carry[0] + before[0]);
-        sm_len[tid] = t.L;
-        sm_take[tid] = carry[1] + before[1];
-        sm_give[tid] = carry[2] + before[2];
         const int chunk_rows = (int)(carry[0] + all[0]);               // rows of the sessions up to this chunk's last
-        if (tid == 0) sm_cu[kThreads] = chunk_rows;
         __syncthreads();
         // ---- this workgroup's rows of the chunk's sessions
         if (!bad)
             for (int64_t r = max(row0, (int64_t)carry[0]) + tid; r < min(row1, (int64_t)chunk_rows); r += kThreads) {
                 int e = 0;                           // the row's session: the last one that starts at or before it
 #pragma unroll
-                for (int step = kThreads / 2; step > 0; step >>= 1)
+                for (int step = kChunk / 2; step > 0; step >>= 1)
                     if (sm_cu[e + step] <= r) e += step;
                 const int L = sm_len[e], i = (int)r - sm_cu[e], pos = L + i, b0 = (L + kBlock - 1) / kBlock;
                 int32_t *row = a.tables + (int64_t)(s0 + e) * a.max_blocks;
@@ -225,10 +250,10 @@ __global__ __launch_bounds__(kThreads) void tables_kernel(TablesArgs a, int rows
         carry[0] = add_rows(carry[0], all[0]);
         carry[1] += all[1];
         carry[2] += all[2];
-        s0 += kThreads;
-        if (s0 >= S) break;
+        s0 += kChunk;
+        if (s0 >= S || (!state && carry[0] >= row1)) break;
         __syncthreads();
-        scan(s0, t, before, all, wrong);
+        chunk(s0);
     }
     for (int64_t r = max(row0, (int64_t)sum[0]) + tid; r < row1; r += kThreads) a.slots[r] = -1;
 }
@@ -260,15 +285,32 @@ hipError_t launch_tables(const PoolGeom &p, int32_t num_sessions, const int32_t 
     a.reused = reused_lens;
     a.slots = slot_map;
     a.err = err;
-    const bool small = num_sessions <= 256;
-    const int threads = small ? 256 : 1024;
+    // Threads per workgroup, sessions per thread and workgroups (us inside a graph).
+    // - State apart from the inputs: a thread per row, 256 in a workgroup, for more
+    //   than 256 sessions 4 of them a thread (256 sessions of 4 rows 3.8, against 5.5
+    //   when one workgroup does all rows; 1024 sessions of one row 4.9, against 5.7 in
+    //   one workgroup of 1024 threads with a session each).  Past 1024 sessions 1024
+    //   threads, so that up to 4096 make one pass (4096 sessions 9.8; 14.6 with 256 threads).
+    // - State in place: the two launches that several workgroups take cost 6.9 (256
+    //   sessions), 9.3 (1024) and 16.7 (2048), so one workgroup does the step while
+    //   its rows are few: up to 512 with 256 threads (two rows of 256 sessions: 4.4,
+    //   5.6 with 1024), up to 2048, or 4096 with many sessions, with 1024 (8 rows of
+    //   256 sessions 6.9, 4 rows of 1024 sessions 8.8, a row of 2048 sessions 9.1).
+    const bool same = next_lens == seq_lens || (free_ring && next_counts == free_counts);
+    const bool many = num_sessions > 256, most = num_sessions > 1024;
+    const bool one = same && total_tokens <= (many ? 4096 : 2048);
+    const int threads = most || (one && (many || total_tokens > 512)) ? 1024 : 256;
     auto launch = [&](int64_t grid, int rows, int state) {
-        if (small) hipLaunchKernelGGL(tables_kernel<256>, dim3((unsigned)grid), dim3(256), 0, stream, a, rows, state);
-        else hipLaunchKernelGGL(tables_kernel<1024>, dim3((unsigned)grid), dim3(1024), 0, stream, a, rows, state);
+#define LS_TABLES(THREADS, PER) \
+    hipLaunchKernelGGL((tables_kernel<THREADS, PER>), dim3((unsigned)grid), dim3(THREADS), 0, stream, a, rows, state)
+        if (most) LS_TABLES(1024, 4);
+        else if (threads == 1024) LS_TABLES(1024, 1);
+        else if (many) LS_TABLES(256, 4);
+        else LS_TABLES(256, 1);
+#undef LS_TABLES
         return hipGetLastError();
     };
-    if (total_tokens <= kTabRows * threads) return launch(1, total_tokens, 1);
-    const bool same = next_lens == seq_lens || (free_ring && next_counts == free_counts);
+    if (one || total_tokens <= threads) return launch(1, total_tokens, 1);
     const hipError_t e = launch(((int64_t)total_tokens + threads - 1) / threads, threads, same ? 0 : 1);
     return e != hipSuccess || !same ? e : launch(1, 0, 1);
 }

@@ -119,7 +119,9 @@ def test_steps(kv, oracle_lib, lens, new, window, sinks, ring):
 
 # small and large steps: a decode step, more sessions than a workgroup has threads, turns of many rows
 LARGE = [(256, 1, 1, 0, 5000, 1024), (1500, 1, 1, 0, 300, 64), (3000, 0, 3, 0, 100, 16), (32, 256, 2048, 2000, 9000, 1024), (1, 20000, 20000, 5, 5, 0),
-         (1, 9000, 9000, 0, 0, 256), (200, 1, 90, 0, 700, 128), (2, 1, 5000, 100, 200, 0)]
+         (1, 9000, 9000, 0, 0, 256), (200, 1, 90, 0, 700, 128), (2, 1, 5000, 100, 200, 0),
+         (256, 2, 2, 0, 90, 32), (256, 3, 9, 0, 90, 32), (257, 0, 2, 0, 90, 32), (1024, 1, 1, 0, 90, 32), (1025, 0, 9, 0, 90, 32),
+         (4096, 1, 1, 0, 40, 16), (4097, 0, 1, 0, 40, 16), (9000, 0, 3, 0, 40, 16)]
 
 
 @pytest.mark.parametrize("s,lo,hi,clo,chi,window", LARGE)
