@@ -621,7 +621,7 @@ ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t
     for (const Range &x : arrays) {
         if (!aligned(x.at, x.align)) return fail(LS_EINVAL, "an array is not aligned to its type");
         for (const Range &y : arrays) {
-            if (&y <= &x || !x.at || !y.at) continue;
+            if (&y <= &x || !x.at || !y.at || !x.bytes || !y.bytes) continue;
             const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
             if (a >= b + y.bytes || b >= a + x.bytes) continue;
             const bool in_place = x.at == y.at && ((&x == &arrays[0] && &y == &arrays[1]) || (&x == &arrays[2] && &y == &arrays[3]));

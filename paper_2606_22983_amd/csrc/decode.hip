@@ -119,7 +119,11 @@ struct DecodeArgs {
 // are counted on the walk; only table columns are not.  In it the keys not seen
 // are v in [sinks, L_walk - window): at most 15 in the last block of the first
 // tokens and 15 in the window's first block, or, where the two overlap
-// (skip = 0), any number of keys between them.
+// (skip = 0), any number of keys between them.  Bound by HBM over the walk's blocks
+// when the batch fills the GPU (64 sessions of up to 16384 keys, window 4096, 32/4
+// heads: 69.8 us, 6.2 TB/s; 256 of window 1024 at 16/2 heads: 51.0 us, 5.1 TB/s, the
+// walk's two blocks past the window among the reads), by latency when it is small
+// (one session, window 1024: 7.4 us).
 struct DecodeWindowArgs : DecodeArgs {
     int32_t window;                // >= 1
     int32_t sinks;                 // >= 0

@@ -114,6 +114,11 @@ struct PrefillArgs {
 // be in both parts, for different keys) in the second.  Keys, limits and tiles
 // below are counted on the walk; only table columns are not.  A tile all of whose
 // rows are first tokens has no second part.
+// Bound by the matrix cores and the softmax between their products when walks are
+// long (32 turns, 19817 tokens in all, window 4096, 32/4 heads of 128: 2152 us,
+// 1211 TFLOP/s of what the rows see), by the start and end of an item when they are
+// short (8 first turns of 50-700 tokens, window 256, 8/8 heads of 64: 17 us, beside
+// 7 for their append).
 struct PrefillWindowArgs : PrefillArgs {
     int32_t window;                // >= 1
     int32_t sinks;                 // >= 0
@@ -540,10 +545,10 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         // keys 8*g4 + 4*sb + i); only units that reach past the smallest causal
         // limit of the wave's rows need it.
         // With a window, units that hold a key some row does not see yet, or any
-        // more, do too.  And no unit is seen by every row: a row's running maximum starts from the first unit
-        // that holds a finite score of it (a row that is `unset` has none so far:
-        // all its scores, and probabilities, are then -inf and 0 whatever the
-        // maximum is taken for).
+        // more, do too.  And no unit is seen by every row: a row's running maximum
+        // starts from the first unit that holds a finite score of it (a row that is
+        // `unset` has none so far: all its scores, and probabilities, are then -inf
+        // and 0 whatever the maximum is taken for).
         bool unset[kRT];
     #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) unset[rt] = true;
@@ -736,9 +741,8 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
                 *reinterpret_cast<u32x4 *>(v3 + 2 * C::kBlockBytes + ci * 16) = u32x4{0u, 0u, 0u, 0u};
         };
         if constexpr (kWin) {
-            // The ids of the first stages' blocks, requested with q, a lane each (a
-            // scalar load after the other takes 3.5 us, of the 12 that an item's
-            // start and end take beside its key tiles).
+            // The ids of the first stages' blocks, requested with q, a lane each: one
+            // scalar load after the other takes 3.5 us of an item's start.
             auto first_id = [&](int jb) { return jb >= 0 ? __builtin_amdgcn_readlane(first_ids, jb) : -1; };
             load_k(k3, first_id(blk - 2));
             zero_v_first();                   // (no load goes there, and the barrier below is enough)

@@ -101,6 +101,12 @@ def test_tables_update_takes_lengths_and_counters_in_place(lib, pool):  # noqa: 
         assert tables(lib, pool, ring=None, size=0, counts=None, after=None, W=0, reused=F + 0x600) == LS_EHIP
 
 
+def test_tables_update_of_no_sessions_compares_no_empty_arrays(lib, pool):  # noqa: F811
+    import torch
+    if not torch.cuda.is_available():
+        assert tables(lib, pool, S=0, lens=F + 0x2010, new=F + 0x3008, bt=F + 0x2020, next=F + 0x2010) == LS_EHIP
+
+
 def append(lib, pool, **kw):  # noqa: F811
     a = dict(layer=0, T=4, k=F, v=F, ks=512, vs=512, slots=F, host=None)
     a.update(kw)
