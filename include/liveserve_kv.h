@@ -308,8 +308,9 @@ ls_status paged_attn_decode_window(ls_kv_pool *pool, int32_t layer, int32_t num_
  * of the turn's own tokens) are read.  K and V values of keys that no row of a
  * query tile (256 / (num_q_heads / num_kv_heads) consecutive new tokens) sees do
  * not reach its rows; a NaN or infinite V that one row of a tile sees may make
- * its other rows NaN, as in paged_attn_prefill.  Other arguments, the workspace and errors
- * as paged_attn_prefill; window, sinks and tables as paged_attn_decode_window.
+ * its other rows NaN, as in paged_attn_prefill.  Other arguments, the workspace
+ * and errors as paged_attn_prefill; window, sinks and tables as
+ * paged_attn_decode_window.
  */
 ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
                                     const void *q, const void *k_new, const void *v_new,
@@ -357,17 +358,18 @@ ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num
  *
  * Inputs and outputs are apart, so a call can be made again with the same
  * result; next_lens may be seq_lens and next_counts free_counts, for a loop that
- * advances itself; no other arrays may overlap.  All sessions are served or none: a length out of range, one
- * that does not fit its table, or more rows than total_new_tokens is flagged
- * LS_DEVERR_LENGTH, and too few free blocks or no room in the ring
- * LS_DEVERR_FREE_LIST; then tables, ring and counters stay as they are (next_counts =
- * free_counts, next_lens = seq_lens), cu_new_lens is all 0 and slot_map all -1.  An id
- * outside the pool is copied as it stands and flagged (LS_DEVERR_BLOCK_ID), its
- * tokens' slots are -1.  A session with new_lens[s] = 0 gets no slot: an appending
- * decode of this step leaves it out, since its next block may not be its own.  The pool gives the range of ids; its memory is not touched.
- * Errors: LS_EINVAL (NULL, misaligned or overlapping arrays, sizes out of range, free_ring without
- * counters or the other way round, a window without free_ring, a window or sinks out
- * of range, more than 2^27 - 1 blocks per session), LS_EHIP.
+ * advances itself; no other arrays may overlap.  All sessions are served or none: a
+ * length out of range, one that does not fit its table, or more rows than
+ * total_new_tokens is flagged LS_DEVERR_LENGTH, and too few free blocks or no room in
+ * the ring LS_DEVERR_FREE_LIST; then tables, ring and counters stay as they are
+ * (next_counts = free_counts, next_lens = seq_lens), cu_new_lens is all 0 and slot_map
+ * all -1.  An id outside the pool is copied as it stands and flagged
+ * (LS_DEVERR_BLOCK_ID), its tokens' slots are -1.  A session with new_lens[s] = 0 gets
+ * no slot: an appending decode of this step leaves it out, since its next block may
+ * not be its own.  The pool gives the range of ids; its memory is not touched.
+ * Errors: LS_EINVAL (NULL, misaligned or overlapping arrays, sizes out of range,
+ * free_ring without counters or the other way round, a window without free_ring, a
+ * window or sinks out of range, more than 2^27 - 1 blocks per session), LS_EHIP.
  */
 ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t *seq_lens,
                            const int32_t *new_lens, int32_t *block_tables, int32_t max_blocks_per_session,
