@@ -123,7 +123,7 @@ struct DecodeArgs {
 // when the batch fills the GPU (64 sessions of up to 16384 keys, window 4096, 32/4
 // heads: 69.8 us, 6.2 TB/s; 256 of window 1024 at 16/2 heads: 51.0 us, 5.1 TB/s, the
 // walk's two blocks past the window among the reads), by latency when it is small
-// (one session, window 1024: 7.4 us).
+// (one session, window 1024: 7.2 us).
 struct DecodeWindowArgs : DecodeArgs {
     int32_t window;                // >= 1
     int32_t sinks;                 // >= 0
@@ -1310,15 +1310,77 @@ struct SmallSize {
 };
 constexpr SmallSize kSmallSizes128[] = {{256, 1}, {512, 1}, {256, 2}, {768, 1}, {1024, 1}};
 constexpr SmallSize kSmallSizes64[] = {{512, 3}, {1024, 1}};
-// With a window the sizes go up to the longest walk and no further (a session of
-// 272 keys is two blocks per wave and one more, not 512 keys' four), 384 and 640
-// among them: walks are mostly the window's length, one block or two over a power
-// of two.  100 random batches: 0.968 of the time with the sizes above in the
-// geometric mean, 0.71 to 1.02 but for one (5 sessions of 300-2200 keys in a
-// window of 3600, lengths on the device: 8.0 -> 8.8 us).  Splits of even length,
-// of sessions that take several, were up to 10% slower than whole ones and a rest.
-constexpr SmallSize kWindowSizes128[] = {{256, 1}, {384, 1}, {512, 1}, {640, 1}, {256, 2}, {1024, 1}};
-constexpr SmallSize kWindowSizes64[] = {{512, 3}, {640, 3}, {1024, 1}};
+// With a window: walks are mostly of one length, the window's, so that what a
+// split costs shows.  Up to 448 keys a session is one workgroup (a walk of 276
+// keys, one session, D = 128: 5.7 us, in two splits 7.2; of 404 6.6 and 7.2; of 660
+// 8.0 and 7.0), longer walks take the cheapest split of which every CU has at
+// most one: `us` is its time over that of the shortest, in tenths (a walk of 1316
+// keys in splits of 192 to 640: 7.2 to 10.2 at D = 128, 5.7 to 8.7 at D = 64), to
+// which comes that of reading the partial results, eight splits at once.  270
+// random batches against a list of few sizes, the shortest that fits: 0.987 of the
+// time in the geometric mean, 26 of them 5-22% faster, 5 3-5% slower.
+struct WindowSplit {
+    int tokens, us128, us64;
+};
+constexpr WindowSplit kWindowSplits[] = {{128, 0, 0},   {192, 2, 2},   {256, 4, 4},   {320, 10, 8},  {384, 13, 10}, {448, 18, 13},
+                                         {512, 22, 15}, {576, 30, 24}, {640, 32, 30}, {768, 34, 31}, {896, 45, 32}, {1024, 46, 34}};
+constexpr int kWindowSingle = 448, kWindowMerge128 = 9, kWindowMerge64 = 8;
+// Where none fits, several per CU: at D = 128 only of sessions that take three or
+// more (32 sessions of window 2048 at 4 heads 28.2 us in splits of 576, 32.6 by the
+// persistent kernel; 64 of window 1024, two splits each, 28.6 and 26.7).
+constexpr SmallSize kWindowSizes128[] = {{576, 2}, {768, 2}, {1024, 2}};
+constexpr SmallSize kWindowSizes64[] = {{384, 2}, {448, 2}, {512, 3}, {640, 3}};
+
+// longest: keys of the longest walk.
+static SmallDecodePlan plan_small_window(const PoolGeom &p, int64_t cus, int32_t num_sessions, int G, int64_t longest,
+                                         const int32_t *lens_host, int32_t appended, size_t bytes) {
+    const bool wide = p.head_dim == 128;
+    const int64_t hkv = p.num_kv_heads;
+    auto pad = [](size_t b) { return (b + 255) & ~(size_t)255; };
+    // Splits of T keys; without split_tokens when there are more than per_cu per CU.
+    auto split = [&](int T, int per_cu) {
+        SmallDecodePlan plan;
+        int64_t rows = 0;
+        if (lens_host) {
+            for (int32_t s = 0; s < num_sessions; ++s) rows += std::max<int64_t>(1, ((int64_t)lens_host[s] + appended + T - 1) / T);
+            if (rows > kSmallRows) return plan;
+        } else {
+            rows = num_sessions * ((longest + T - 1) / T);            // (walks are mostly as long as they get)
+        }
+        if (rows * hkv > per_cu * cus) return plan;
+        plan.rows = (int)rows;
+        plan.count_bytes = (size_t)(num_sessions * hkv) * kArrivedStride * sizeof(uint64_t);
+        plan.ml_bytes = pad((size_t)(rows * hkv) * G * 2 * sizeof(float));
+        plan.acc_bytes = pad((size_t)(rows * hkv) * G * p.head_dim * sizeof(float));
+        if (plan.total() <= bytes) plan.split_tokens = T;
+        return plan;
+    };
+    const int64_t whole = (longest + kBlock - 1) / kBlock * kBlock;
+    SmallDecodePlan best;
+    if (whole > kWindowSingle) {
+        int64_t least = INT64_MAX;
+        for (const WindowSplit &c : kWindowSplits) {
+            if (c.tokens >= whole) break;
+            const int64_t merges = (longest + 8 * c.tokens - 1) / (8 * c.tokens);
+            const int64_t cost = wide ? c.us128 + merges * kWindowMerge128 : c.us64 + merges * kWindowMerge64;
+            if (cost >= least) continue;
+            const SmallDecodePlan plan = split(c.tokens, 1);
+            if (!plan.split_tokens) continue;
+            best = plan;
+            least = cost;
+        }
+        const SmallSize *size = wide ? kWindowSizes128 : kWindowSizes64;
+        const SmallSize *end = wide ? std::end(kWindowSizes128) : std::end(kWindowSizes64);
+        for (; size != end && !best.split_tokens; ++size)
+            if (size->tokens < whole && (!wide || longest > 2 * size->tokens)) best = split(size->tokens, size->per_cu);
+    }
+    if (!best.split_tokens && whole <= kMaxSplitTokens) {
+        best.split_tokens = (int)whole;
+        best.rows = num_sessions;
+        best.single = true;
+    }
+    return best;
+}
 
 SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,
                            int32_t max_blocks, const int32_t *lens_host, int32_t appended, size_t bytes, bool windowed) {
@@ -1335,17 +1397,13 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
         }
     }
     const int G = num_q_heads / p.num_kv_heads;
+    if (windowed) return plan_small_window(p, cus, num_sessions, G, longest, lens_host, appended, bytes);
     auto pad = [](size_t b) { return (b + 255) & ~(size_t)255; };
     const bool wide = p.head_dim == 128;
     const SmallSize *size = wide ? kSmallSizes128 : kSmallSizes64;
     const SmallSize *end = wide ? std::end(kSmallSizes128) : std::end(kSmallSizes64);
-    if (windowed) {
-        size = wide ? kWindowSizes128 : kWindowSizes64;
-        end = wide ? std::end(kWindowSizes128) : std::end(kWindowSizes64);
-    }
     for (; size != end; ++size) {
-        int T = size->tokens;
-        if (windowed) T = (int)std::min<int64_t>(T, (longest + kBlock - 1) / kBlock * kBlock);
+        const int T = size->tokens;
         if (T < kMaxSplitTokens && (int64_t)T * T < 8 * longest) continue;
         SmallDecodePlan plan;
         if (T >= longest) {
@@ -1363,7 +1421,7 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
             // D = 128, splits from 512 on, one or two query heads per KV head:
             // below 3/5 of the longest (8 of 9 batches 1-9% slower here, one 1%
             // faster; with more query heads nine are 4-26% faster here).
-            if (lens_host && !windowed && num_sessions * hkv > cus) {
+            if (lens_host && num_sessions * hkv > cus) {
                 const int64_t even = longest * num_sessions;
                 if (wide ? T > 256 && G <= 2 && 5 * total < 3 * even
                          : T == kMaxSplitTokens && (num_sessions * hkv > 2 * cus || 4 * total < 3 * even))
@@ -1380,7 +1438,7 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
         // batches that this leaves out 5 are 0-3% faster for it and 12 slower,
         // those with the fewest splits most (4 sessions of 1000-40,000 keys in
         // tables of 64k at 2 heads, D = 64: 21.7 us, 15.1 without).
-        if (!lens_host && !windowed && T == kMaxSplitTokens) continue;
+        if (!lens_host && T == kMaxSplitTokens) continue;
         int64_t rows = 0;                          // of the grid
         double resident;                           // workgroups with keys, expected
         if (lens_host) {
@@ -1390,7 +1448,6 @@ SmallDecodePlan plan_small(const PoolGeom &p, int64_t cus, int32_t num_sessions,
         } else {
             rows = num_sessions * ((longest + T - 1) / T);
             resident = (double)(num_sessions * hkv) * (0.5 * (double)longest / T + 0.5) / 1.1;
-            if (windowed) resident = (double)(rows * hkv);        // (walks are mostly as long as they get)
         }
         if (resident > (double)(size->per_cu * cus)) continue;
         plan.split_tokens = T;
@@ -1437,7 +1494,7 @@ DecodePlan plan_decode(const PoolGeom &p, int32_t num_sessions, int32_t num_q_he
     // Room for decode_small_kernel: its plan for device lengths, or any for host
     // lengths (at most three workgroups per CU, see plan_small, and one per split).
     if (sg <= 3 * cus) {
-        const int64_t shortest = p.head_dim == 128 ? kSmallSizes128[0].tokens : kSmallSizes64[0].tokens;
+        const int64_t shortest = windowed ? kWindowSplits[0].tokens : p.head_dim == 128 ? kSmallSizes128[0].tokens : kSmallSizes64[0].tokens;
         const int64_t wgs = std::min(3 * cus, sg * ((max_tokens + shortest - 1) / shortest));
         const size_t most = pad((size_t)wgs * G * (p.head_dim + 2) * sizeof(float)) + 512;
         const SmallDecodePlan dev = plan_small(p, cus, num_sessions, num_q_heads, max_blocks_per_session, nullptr, 0, SIZE_MAX, windowed);

@@ -107,6 +107,20 @@ def test_schedules(kv, oracle_lib, s, lo, hi, window, sinks, hq, hkv, d):
     Case(kv, oracle_lib, lens, window, sinks, hq, hkv, d, bool(s % 2), seed=s).check(what="%d sessions W %d" % (s, window))
 
 
+# (sessions, window): walks of one workgroup and of splits of each size, one per CU and several
+SPLITS = [(1, 400), (1, 440), (1, 540), (3, 700), (6, 1300), (2, 2900), (1, 8000), (14, 1000), (20, 1500), (30, 600), (33, 2048),
+          (64, 2000), (60, 900), (90, 430)]
+
+
+@pytest.mark.parametrize("s,window", SPLITS)
+@pytest.mark.parametrize("hq,hkv,d", [(8, 4, 128), (4, 4, 64), (2, 2, 128), (8, 2, 64)])
+def test_split_sizes(kv, oracle_lib, s, window, hq, hkv, d):
+    rng = np.random.default_rng(s * window)
+    lens = rng.integers(window // 2, 2 * window, s)
+    lens[0] = 2 * window + 7
+    Case(kv, oracle_lib, lens, window, 4, hq, hkv, d, bool(window % 3), seed=s).check(what="%d sessions W %d" % (s, window))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_as_many_sessions_as_a_call_takes(kv, oracle_lib, d):
     rng = np.random.default_rng(d)
