@@ -1011,7 +1011,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<k
     if constexpr (kWin && kHost) skip_used = rows.skip[row];
     else if constexpr (kWin) walk_len(a, s, false, skip_used);
     const int id_at = min(walk_column(a, split * (T / kBlock) + lane, skip_used), a.max_blocks - 1);
-    const int ids = a.block_tables[(int64_t)s * a.max_blocks + id_at];
+    int ids = a.block_tables[(int64_t)s * a.max_blocks + id_at];
     bf16x8 qop[D / 32];
     {
         const uint16_t *qrow = a.q + ((int64_t)s * Hkv * G + g * G + (c16 < G ? c16 : 0)) * D;
@@ -1024,7 +1024,12 @@ __global__ __launch_bounds__(kDecThreads) void decode_small_kernel(DecodeArgsT<k
     }
     const bool first = split == 0 && g == 0 && tid == 0;
     const int L = walk_len(a, s, first, skip);
-    if (kWin && kHost && skip != skip_used && first) flag_error(a.err, LS_DEVERR_LENGTH);   // not the host's length
+    // (Not the host's length: the columns of the device's, or a row would be read
+    // from, and the step's own written to, blocks that are not its own.)
+    if constexpr (kWin && kHost)
+        if (skip != skip_used)
+            ids = a.block_tables[(int64_t)s * a.max_blocks +
+                                 min(walk_column(a, split * (T / kBlock) + lane, skip), a.max_blocks - 1)];
     int hole_lo, hole_hi;
     walk_hole(a, L, hole_lo, hole_hi);
     const int own = a.appended && a.lens[s] >= 0 && a.lens[s] + 1 <= a.max_blocks * kBlock;
