@@ -376,7 +376,9 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         }
         // (With a window every position below is one of the walk, from tile0 on.)
         const int key_base = tile0 * kKeyTile + shift;
-        const int kv_len = c + n - key_base;
+        // Keys from here on have their V zeroed: the end of the turn, with a window
+        // the end of what the tile's rows see.
+        const int kv_len = (kWin ? c + j_last + 1 : c + n) - key_base;
         int nb = min(nblk_valid - tile0 * 4, ntiles * 4);     // blocks any row here can see
         if (kSplit || kWin) nb = max(nb, 0);                  // (a part past the end of the table)
         if (kWin && nb == 0) walk = {INT32_MAX, 1, 0};        // (its table reads stay in column 0)
@@ -687,8 +689,9 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         // or blocks never loaded) are zeroed in the staged V tile of key tile j
         // before it is used, so that 0 * NaN cannot reach O.  Only the last key
         // tile can hold such keys; one extra LDS barrier, once per workgroup.
-        // With a window so are those of keys that no row of the tile sees, in the
-        // last block of the first tokens and the first one of the window.
+        // With a window so are those of all keys that no row of the tile sees: the
+        // turn's later tokens, and what the last block of the first tokens and the
+        // first one of the window hold besides.
         auto zero_v_tail = [&](uint8_t *lv, int j) {
             constexpr int kChunks = 4 * 2 * D;                    // (block, half, dim) chunks of 8 tokens
             for (int ci = tid; ci < kChunks; ci += kPreThreads) {
