@@ -227,7 +227,9 @@ ls_status paged_attn_decode_static(ls_kv_pool *pool, int32_t layer, int32_t num_
  *                  A turn longer than max_new_len (device lengths only) is flagged
  *                  (LS_DEVERR_LENGTH) and its rows past max_new_len are not written.
  *   block_tables   device int32 [num_sessions][max_blocks_per_session], covering
- *                  c_s + n_s tokens
+ *                  c_s + n_s tokens.  An id outside the pool is flagged
+ *                  (LS_DEVERR_BLOCK_ID) where the call appends to it; attention reads
+ *                  such a block's keys and values as zeros and does not flag it
  *   out            device bf16 [total_new_tokens][num_q_heads][head_dim]
  *   workspace      optional device memory (16-byte aligned) of workspace_bytes >=
  *                  LS_PREFILL_COUNTER_BYTES, or NULL (LS_ENOMEM if too small,
@@ -265,7 +267,10 @@ ls_status paged_attn_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
  * `sinks` ones, and blocks behind the window can be used again.  All entry
  * points of this section refuse (LS_EINVAL) a call made while another device
  * than the pool's is current, q, out, k_new, v_new or a workspace that is not
- * 16-byte aligned, and index arrays that are not aligned to their type.
+ * 16-byte aligned, and index arrays that are not aligned to their type.  The two
+ * attention calls leave out the keys of a block whose id, among the table entries
+ * that they read, is outside the pool, and flag it (LS_DEVERR_BLOCK_ID); a row
+ * left without a key has no defined output.
  * ---------------------------------------------------------------------- */
 
 /* Largest window and most first tokens. */

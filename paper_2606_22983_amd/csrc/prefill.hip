@@ -322,6 +322,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
     __shared__ int sm_order[kMaxPairs];
     __shared__ float sm_rank_work[kMaxPairs];
     __shared__ int sm_grab[2];
+    __shared__ int sm_absent[kWin ? kPreWaves : 1];   // some block of the item's walk is not in the pool
 
     const int tid = threadIdx.x;
     const int S = a.num_sessions;
@@ -421,10 +422,12 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             for (int ks = 0; ks < KS; ++ks)
                 qop[rt][ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(qrow + ks * 32 + g4 * 8));
         }
-        int first_ids = -1;                                   // block `lane` of the walk, from tile0 on
+        int first_ids = -1, own_id = 0;                       // blocks `lane` and 64 + `tid` of the walk, from tile0 on
         if constexpr (kWin) {
-            const int32_t id = a.block_tables[(int64_t)s * a.max_blocks + walk_column(walk, tile0 * 4 + min(lane, max(nb - 1, 0)))];
+            const int32_t *row = a.block_tables + (int64_t)s * a.max_blocks;
+            const int32_t id = row[walk_column(walk, tile0 * 4 + min(lane, max(nb - 1, 0)))];
             first_ids = lane < nb ? id : -1;
+            if (nb > kWave) own_id = row[walk_column(walk, tile0 * 4 + min(kWave + tid, nb - 1))];
         }
         // Wait for q here, before the first stage loads are issued, so that no
         // wait for q remains inside the key loop (vmcnt(0), other counters untouched).
@@ -432,9 +435,11 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         // smallest causal limit among this wave's rows: units past it need masking
         const int wave_lim_min = c + min(j0 + (wave * kWaveRows) / G, n - 1) - key_base;
         // and with a window the units that all its rows see whole: those that start
-        // at one of `wave_whole` keys from wave_from on (all in the window's part)
-        const int wave_from = kWin ? max(c + min(j0 + ((wave * kWaveRows + kWaveRows - 1) >> lg), n - 1) - window + 1, sinks) - key_base : 0;
-        const int wave_whole = max(wave_lim_min - 30 - wave_from, 0);
+        // at one of `wave_whole` keys from wave_from on (all in the window's part);
+        // wave_from kAbsent: blocks of the walk are not in the pool
+        constexpr int kAbsent = INT32_MIN;
+        int wave_from = kWin ? max(c + min(j0 + ((wave * kWaveRows + kWaveRows - 1) >> lg), n - 1) - window + 1, sinks) - key_base : 0;
+        int wave_whole = max(wave_lim_min - 30 - wave_from, 0);
 
         // Key tiles some row of this wave sees: none when its rows are all padding,
         // fewer than the workgroup's where the tile spans many tokens.  Past them
@@ -558,6 +563,15 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         auto mask_unit = [&](f32x4 (&acc)[kRT][2], int key0) {
             if constexpr (kWin) {
                 if (!pending && (unsigned)(key0 - wave_from) < (unsigned)wave_whole) return;
+                if (__builtin_expect(wave_from == kAbsent, 0)) {
+                    // (lane group g4 holds keys of the unit's block g4 / 2)
+                    const uint32_t b0 = (uint32_t)entry(key0 / kBlock), b1 = (uint32_t)entry(key0 / kBlock + 1);
+                    if ((g4 >> 1 ? b1 : b0) >= nblocks32)
+    #pragma unroll
+                        for (int rt = 0; rt < kRT; ++rt)
+    #pragma unroll
+                            for (int e = 0; e < 8; ++e) acc[rt][e / 4][e % 4] = -INFINITY;
+                }
                 const bool first = key0 + tile0 * kKeyTile < first_keys;
     #pragma unroll
                 for (int rt = 0; rt < kRT; ++rt) {
@@ -739,6 +753,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
     #pragma unroll
         for (int rt = 0; rt < kRT; ++rt) pop_o[rt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
         int32_t idk, idv;
+        bool some_absent = false;
         auto zero_v_first = [&] {
             for (int ci = tid; ci < 2 * C::kBlockBytes / 16; ci += kPreThreads)
                 *reinterpret_cast<u32x4 *>(v3 + 2 * C::kBlockBytes + ci * 16) = u32x4{0u, 0u, 0u, 0u};
@@ -755,6 +770,17 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
             load_v(v1, first_id(blk + 4));
             idk = first_id(blk + 10);
             idv = first_id(blk + 8);
+            // Ids outside the pool are flagged, and their keys masked (mask_unit).  Every
+            // wave has the first 64; the others are a thread's each.
+            bool absent = lane < nb && (uint32_t)first_ids >= nblocks32;
+            if (__builtin_expect(nb > kWave, 0)) {
+                absent = absent || (uint32_t)own_id >= nblocks32;
+                for (int b = kWave + kPreThreads + tid; b < nb; b += kPreThreads)
+                    absent = absent || (uint32_t)window_entry(table, b, nb, tile0 * 4, walk) >= nblocks32;
+            }
+            some_absent = __any(absent);
+            if (__builtin_expect(some_absent, 0) && absent) flag_error(a.err, LS_DEVERR_BLOCK_ID);
+            if (nb > kWave && lane == 0) sm_absent[wave] = some_absent;
         } else {
             idk = id_k(-1), idv = id_v(-1);
             load_k(k3, idk);                  // stage -1: K unit 0 (its V part is empty)
@@ -774,6 +800,13 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         read_k(k3 + C::kUnitBytes);           // unit 0 = second unit of stage -1
         qk_mfma(sa);
         read_k(k0);                           // unit 1
+        if constexpr (kWin) {
+            if (nb > kWave) some_absent = __any(sm_absent[lane % kPreWaves]);
+            if (__builtin_expect(some_absent, 0)) {           // no unit is seen whole
+                wave_from = kAbsent;
+                wave_whole = 0;
+            }
+        }
         mask_unit(sa, 0);
         // The first unit's row maxima start the running maxima.  Every row sees
         // key 0; in a later part of the keys, a row that does not see the first
