@@ -1554,6 +1554,22 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
     a.part_o = nullptr;
     const int qtok = kPreRows / a.group;
     a.qtiles = (max_new_len + qtok - 1) / qtok;
+    // An unsplit call's kernel.
+    auto launch = [&](auto host, const dim3 &grid, const auto &arg) {
+        constexpr bool kHost = decltype(host)::value;
+        if (skip) {
+            if (p.head_dim == 128)
+                hipLaunchKernelGGL((prefill_kernel<128, kHost, false, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, arg);
+            else
+                hipLaunchKernelGGL((prefill_kernel<64, kHost, false, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, arg);
+        } else if constexpr (!kWin) {
+            if (p.head_dim == 128)
+                hipLaunchKernelGGL((prefill_kernel<128, kHost, false, false>), grid, dim3(kPreThreads), 0, stream, a, arg);
+            else
+                hipLaunchKernelGGL((prefill_kernel<64, kHost, false, false>), grid, dim3(kPreThreads), 0, stream, a, arg);
+        }
+        return hipGetLastError();
+    };
     PrefillSplitPlan plan;
     PrefillPair pairs_of[kPlanPairs];
     int np = 0;
@@ -1567,7 +1583,8 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
             return dim3((unsigned)(kXcds * per_xcd));
         };
         // Where every item has a CU of its own the counters even nothing out, and
-        // cost the 1.3 us of an atomic: windowed calls go without them.
+        // cost the 1.3 us of an atomic and, in a call that appends nothing, the launch
+        // that clears them: windowed calls go without.
         const int64_t cus = stream_cus(p, stream);
         auto longest_list = [&] { return *std::max_element(plan.total, plan.total + kXcds); };
         auto alone = [&] { return (int64_t)longest_list() * kXcds <= cus; };
@@ -1575,13 +1592,12 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
             a.queue = nullptr;
             return dim3((unsigned)(kXcds * longest_list()));
         };
-        if (workspace) {
-            a.queue = static_cast<uint32_t *>(workspace);
-            if (!counters_cleared) {
-                hipLaunchKernelGGL(clear_counters_kernel, dim3(1), dim3(kWave), 0, stream, a.queue);
-                if (hipError_t e = hipGetLastError()) return e;
-            }
-        }
+        if (workspace) a.queue = static_cast<uint32_t *>(workspace);
+        auto clear_counters = [&] {
+            if (!a.queue || counters_cleared) return hipSuccess;
+            hipLaunchKernelGGL(clear_counters_kernel, dim3(1), dim3(kWave), 0, stream, a.queue);
+            return hipGetLastError();
+        };
         // Splitting needs the counters (items of many lengths) and room for the pieces.
         PrefillMergePlan merge;
         int32_t split_tiles = 0;
@@ -1593,6 +1609,7 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
             a.part_o = reinterpret_cast<float *>(parts + (size_t)kPrefillSplitPieces * kPreRows * 2 * sizeof(float));
             dim3 grid = queue_grid(items);
             if (kWin && alone()) grid = index_grid();
+            if (hipError_t e = clear_counters()) return e;
             const dim3 mgrid((unsigned)(split_tiles * (kPreWaves * kRT * p.head_dim / 16 / kMergeWaves)));
             if (p.head_dim == 128)
                 hipLaunchKernelGGL((prefill_kernel<128, true, true, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, plan);
@@ -1617,16 +1634,9 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
             grid = queue_grid(total);
             if (kWin && alone()) grid = index_grid();
         }
+        if (hipError_t e = clear_counters()) return e;
         const PrefillHostPlan &whole = plan;
-        if (p.head_dim == 128 && skip)
-            hipLaunchKernelGGL((prefill_kernel<128, true, false, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
-        else if (p.head_dim == 128)
-            hipLaunchKernelGGL((prefill_kernel<128, true, false, kWin, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
-        else if (skip)
-            hipLaunchKernelGGL((prefill_kernel<64, true, false, true, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
-        else
-            hipLaunchKernelGGL((prefill_kernel<64, true, false, kWin, kWin>), grid, dim3(kPreThreads), 0, stream, a, whole);
-        return hipGetLastError();
+        return launch(std::true_type{}, grid, whole);
     }
     // An XCD holds at most ceil(pairs / 8) pairs of at most qtiles items each;
     // workgroups past an XCD's item count exit at once.
@@ -1634,17 +1644,7 @@ hipError_t launch_prefill_t(const PoolGeom &p, int32_t num_sessions, const int32
     const int64_t grid = (pairs + kXcds - 1) / kXcds * kXcds * a.qtiles;
     if (grid > 0x7FFFFFFFLL) return hipErrorInvalidConfiguration;
     a.resident = grid <= stream_cus(p, stream) ? 1 : 0;
-    const PrefillNoPlan none{0};
-    const dim3 g((unsigned)grid);
-    if (p.head_dim == 128 && skip)
-        hipLaunchKernelGGL((prefill_kernel<128, false, false, true, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
-    else if (p.head_dim == 128)
-        hipLaunchKernelGGL((prefill_kernel<128, false, false, kWin, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
-    else if (skip)
-        hipLaunchKernelGGL((prefill_kernel<64, false, false, true, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
-    else
-        hipLaunchKernelGGL((prefill_kernel<64, false, false, kWin, kWin>), g, dim3(kPreThreads), 0, stream, a, none);
-    return hipGetLastError();
+    return launch(std::false_type{}, dim3((unsigned)grid), PrefillNoPlan{0});
 }
 
 }  // namespace
