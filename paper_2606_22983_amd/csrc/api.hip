@@ -725,6 +725,26 @@ int32_t ls_internal_small_decode(const ls_kv_pool *pool, int32_t num_sessions, i
         .split_tokens;
 }
 
+// The same of a windowed decode.
+int32_t ls_internal_small_decode_window(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                        int32_t max_blocks_per_session, int32_t window, int32_t sinks,
+                                        const int32_t *context_lens_host, int32_t appended, const void *workspace,
+                                        size_t workspace_bytes, hipStream_t stream) {
+    if (!pool || num_sessions <= 0 || max_blocks_per_session <= 0 || check_heads(pool->geom, num_q_heads) != LS_OK ||
+        check_window(window, sinks, max_blocks_per_session) != LS_OK)
+        return -1;
+    const PoolGeom &p = pool->geom;
+    const DecodePlan plan = plan_decode(p, num_sessions, num_q_heads,
+                                        window_blocks(max_blocks_per_session, window, sinks), true);
+    if (!plan.supported ||
+        (context_lens_host &&
+         check_decode_lens_host(num_sessions, context_lens_host, appended, max_blocks_per_session) != LS_OK))
+        return -1;
+    return choose_small_window(p, stream_cus(p, stream), num_sessions, num_q_heads, max_blocks_per_session, window, sinks,
+                               context_lens_host, appended, workspace, workspace_bytes, plan)
+        .split_tokens;
+}
+
 // Items of a prefill's split plan (0: nothing is split), written to items as
 // PrefillPlanItem; its merged tiles to merged.  -1: more than room.
 int32_t ls_internal_split_prefill(int32_t num_sessions, int32_t num_kv_heads, int32_t group, const int32_t *lens_host,

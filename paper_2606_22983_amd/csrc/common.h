@@ -82,6 +82,12 @@ SmallDecodePlan choose_small(const PoolGeom &p, int64_t cus, int32_t num_session
                              int32_t max_blocks, const int32_t *lens_host, int32_t appended, const void *workspace,
                              size_t workspace_bytes, const DecodePlan &plan);
 
+// For the tests: the same of a windowed call, whose plan is for window_blocks.
+SmallDecodePlan choose_small_window(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,
+                                    int32_t max_blocks, int32_t window, int32_t sinks, const int32_t *lens_host,
+                                    int32_t appended, const void *workspace, size_t workspace_bytes,
+                                    const DecodePlan &plan);
+
 // An item of a prefill call that splits keys, where its plan puts it: the
 // slot-th of an XCD's list, over part `chunk` of `chunks` of query tile `tile`
 // of (session, KV head) `pair`; its result goes to `piece` (chunks > 1).

@@ -1945,7 +1945,27 @@ hipError_t launch_decode_t(const PoolGeom &p, int32_t num_sessions, int32_t walk
     return e != hipSuccess || plan.max_splits == 1 ? e : combine();
 }
 
+// The planners see a windowed batch's walks: their lengths (without the appended
+// token, as those of whole sessions) and the most blocks one has.
+void host_walks(int32_t num_sessions, const int32_t *lens_host, int32_t appended, int32_t window, int32_t sinks,
+                int32_t *walk, int32_t *skips) {
+    for (int32_t s = 0; s < num_sessions; ++s) {
+        skips[s] = window_skip(lens_host[s] + appended, window, sinks);
+        walk[s] = lens_host[s] - skips[s] * kBlock;
+    }
+}
+
 }  // namespace
+
+SmallDecodePlan choose_small_window(const PoolGeom &p, int64_t cus, int32_t num_sessions, int32_t num_q_heads,
+                                    int32_t max_blocks, int32_t window, int32_t sinks, const int32_t *lens_host,
+                                    int32_t appended, const void *workspace, size_t workspace_bytes,
+                                    const DecodePlan &plan) {
+    int32_t walk[kMaxBatch], skips[kMaxBatch];
+    if (lens_host) host_walks(num_sessions, lens_host, appended, window, sinks, walk, skips);
+    return choose_small(p, cus, num_sessions, num_q_heads, window_blocks(max_blocks, window, sinks),
+                        lens_host ? walk : nullptr, appended, workspace, workspace_bytes, plan);
+}
 
 hipError_t launch_decode(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads,
                          const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
@@ -1975,14 +1995,8 @@ hipError_t launch_decode(const PoolGeom &p, int layer, int32_t num_sessions, int
     if (!window)
         return launch_decode_t<false>(p, num_sessions, max_blocks, context_lens_host, nullptr, workspace, workspace_bytes, plan,
                                       a, stream);
-    // The planners see the walks: their lengths (without the appended token, as
-    // those of whole sessions) and the most blocks one has.
     int32_t walk[kMaxBatch], skips[kMaxBatch];
-    if (context_lens_host)
-        for (int32_t s = 0; s < num_sessions; ++s) {
-            skips[s] = window_skip(context_lens_host[s] + a.appended, window, sinks);
-            walk[s] = context_lens_host[s] - skips[s] * kBlock;
-        }
+    if (context_lens_host) host_walks(num_sessions, context_lens_host, a.appended, window, sinks, walk, skips);
     return launch_decode_t<true>(p, num_sessions, window_blocks(max_blocks, window, sinks),
                                  context_lens_host ? walk : nullptr, skips, workspace, workspace_bytes, plan, a, stream);
 }
