@@ -425,8 +425,9 @@ def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tenso
     one, two = (s,), (2,)
     if not (_fits(seq_lens, one, _I32) and _fits(new_lens, one, _I32) and _fits(next_lens, one, _I32)
             and _fits(cu_new_lens, (s + 1,), _I32) and (reused_lens is None or _fits(reused_lens, one, _I32))
-            and _fits(slot_map, slot_map.shape[:1], _I64) and _fits(block_tables, (s, block_tables.shape[-1]), _I32)
-            and (free_ring is None or _fits(free_ring, free_ring.shape[:1], _I32))
+            and _fits(slot_map, (slot_map.numel(),), _I64) and block_tables.dim() == 2
+            and _fits(block_tables, (s, block_tables.shape[1]), _I32)
+            and (free_ring is None or _fits(free_ring, (free_ring.numel(),), _I32))
             and (free_counts is None or _fits(free_counts, two, _I64))
             and (next_counts is None or _fits(next_counts, two, _I64))):
         _tables_args(s, seq_lens, new_lens, block_tables, next_lens, cu_new_lens, reused_lens, slot_map, free_ring,
