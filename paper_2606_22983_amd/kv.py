@@ -105,11 +105,13 @@ def _shape(t: torch.Tensor, name: str, shape, dtype=None):
     return t
 
 
-def _dev(t: torch.Tensor, name: str, dtype=None):
+def _dev(t: torch.Tensor, name: str, dtype=None, dev=None):
     if dtype is not None and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
         raise ValueError("%s must have dtype %s (got %s)" % (name, dtype, t.dtype))
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
+    if dev is not None and t.get_device() != dev:
+        raise ValueError("%s must be on the pool's device (%d, got %d)" % (name, dev, t.get_device()))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return t
@@ -138,10 +140,11 @@ _BF16 = (torch.bfloat16, torch.int16)
 _I32 = (torch.int32,)
 
 
-def _fits(t: torch.Tensor, shape, dtypes) -> bool:
+def _fits(t: torch.Tensor, shape, dtypes, dev=None) -> bool:
     """Whether t passes _shape and _dev, in one test.  A small batch's decode takes 7 us of GPU
     time, and a call's checks, one by one, took more than that (15 us a call on the host)."""
-    return t.shape == shape and t.dtype in dtypes and t.is_cuda and t.is_contiguous()
+    return (t.shape == shape and t.dtype in dtypes and (t.is_cuda if dev is None else t.get_device() == dev)
+            and t.is_contiguous())
 
 
 def version() -> str:
@@ -158,6 +161,7 @@ class KVPool:
     def __init__(self, handle, kv, num_layers, num_blocks, num_kv_heads, head_dim, block_size):
         self.handle = handle
         self.kv = kv
+        self.device = None if kv is None else kv.get_device()
         self.num_layers = num_layers
         self.num_blocks = num_blocks
         self.num_kv_heads = num_kv_heads
@@ -216,12 +220,12 @@ def _host_i32(a, name: str, n: int):
     return arr, arr.__array_interface__["data"][0]
 
 
-def _decode_args(s, hq, hkv, d, q, out, block_tables, context_lens, k_new, v_new):
+def _decode_args(s, hq, hkv, d, q, out, block_tables, context_lens, k_new, v_new, dev=None):
     """Shapes, types and devices of a decode call's tensors (raises ValueError)."""
     rows, new = (s, hq, d), (s, hkv, d)
-    if (_fits(q, rows, _BF16) and _fits(out, rows, _BF16) and _fits(context_lens, (s,), _I32)
-            and block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32)
-            and (k_new is None or _fits(k_new, new, _BF16)) and (v_new is None or _fits(v_new, new, _BF16))):
+    if (_fits(q, rows, _BF16, dev) and _fits(out, rows, _BF16, dev) and _fits(context_lens, (s,), _I32, dev)
+            and block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32, dev)
+            and (k_new is None or _fits(k_new, new, _BF16, dev)) and (v_new is None or _fits(v_new, new, _BF16, dev))):
         return
     _shape(q, "q", rows, _BF16)
     _shape(out, "out", rows, _BF16)
@@ -233,7 +237,7 @@ def _decode_args(s, hq, hkv, d, q, out, block_tables, context_lens, k_new, v_new
     for t, name in ((q, "q"), (out, "out"), (block_tables, "block_tables"), (context_lens, "context_lens"),
                     (k_new, "k_new"), (v_new, "v_new")):
         if t is not None:
-            _dev(t, name)
+            _dev(t, name, dev=dev)
 
 
 def paged_attn_decode(pool: KVPool, layer: int, q: torch.Tensor, block_tables: torch.Tensor,
@@ -291,13 +295,13 @@ def paged_attn_decode_static(pool: KVPool, layer: int, q: torch.Tensor, block_ta
     return out
 
 
-def _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new):
+def _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new, dev=None):
     """Shapes, types and devices of a prefill call's tensors (raises ValueError)."""
     rows, new = (total, hq, d), (total, hkv, d)
-    if not (_fits(q, rows, _BF16) and _fits(out, rows, _BF16) and _fits(reused_lens, (s,), _I32)
-            and _fits(cu_new_lens, (s + 1,), _I32) and block_tables.dim() == 2
-            and _fits(block_tables, (s, block_tables.shape[1]), _I32)
-            and (k_new is None or _fits(k_new, new, _BF16)) and (v_new is None or _fits(v_new, new, _BF16))):
+    if not (_fits(q, rows, _BF16, dev) and _fits(out, rows, _BF16, dev) and _fits(reused_lens, (s,), _I32, dev)
+            and _fits(cu_new_lens, (s + 1,), _I32, dev) and block_tables.dim() == 2
+            and _fits(block_tables, (s, block_tables.shape[1]), _I32, dev)
+            and (k_new is None or _fits(k_new, new, _BF16, dev)) and (v_new is None or _fits(v_new, new, _BF16, dev))):
         _shape(q, "q", (total, hq, d), _BF16)
         _shape(out, "out", (total, hq, d), _BF16)
         _shape(reused_lens, "reused_lens", (None,), torch.int32)
@@ -310,7 +314,7 @@ def _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_
                         (reused_lens, "reused_lens"), (block_tables, "block_tables"), (k_new, "k_new"),
                         (v_new, "v_new")):
             if t is not None:
-                _dev(t, name)
+                _dev(t, name, dev=dev)
 
 
 def paged_attn_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: torch.Tensor,
@@ -360,9 +364,9 @@ def paged_attn_decode_window(pool: KVPool, layer: int, q: torch.Tensor, block_ta
         raise ValueError("q must be [S][Hq][D]")
     s, hq = q.shape[0], q.shape[1]
     d, hkv = pool.head_dim, pool.num_kv_heads
-    _decode_args(s, hq, hkv, d, q, out, block_tables, context_lens, k_new, v_new)
-    if not (workspace.is_cuda and workspace.is_contiguous()):
-        _dev(workspace, "workspace")
+    _decode_args(s, hq, hkv, d, q, out, block_tables, context_lens, k_new, v_new, pool.device)
+    if not (workspace.get_device() == pool.device and workspace.is_contiguous()):
+        _dev(workspace, "workspace", dev=pool.device)
     keep, hl = _host_i32(context_lens_host, "context_lens_host", s)
     _check(_lib.paged_attn_decode_window(pool.handle, layer, s, hq, _ptr(q), _ptr(k_new), _ptr(v_new),
                                          _ptr(block_tables), block_tables.shape[1], _ptr(context_lens), hl,
@@ -386,10 +390,10 @@ def paged_attn_prefill_window(pool: KVPool, layer: int, q: torch.Tensor, cu_new_
     total, hq = q.shape[0], q.shape[1]
     s = reused_lens.shape[0] if reused_lens.dim() == 1 else -1
     d, hkv = pool.head_dim, pool.num_kv_heads
-    _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new)
+    _prefill_args(total, s, hq, hkv, d, q, out, cu_new_lens, reused_lens, block_tables, k_new, v_new, pool.device)
     keep, hl = _host_i32(lens_host, "lens_host", 2 * s)
     if workspace is not None:
-        _dev(workspace, "workspace")
+        _dev(workspace, "workspace", dev=pool.device)
     _check(_lib.paged_attn_prefill_window(pool.handle, layer, s, hq, _ptr(q), _ptr(k_new), _ptr(v_new),
                                           _ptr(cu_new_lens), _ptr(reused_lens), hl, total,
                                           int(max_new_len), _ptr(block_tables), block_tables.shape[1],
@@ -403,11 +407,11 @@ def paged_attn_prefill_window(pool: KVPool, layer: int, q: torch.Tensor, cu_new_
 _I64 = (torch.int64,)
 
 
-def _vector(t: torch.Tensor, name: str, n, dtypes):
-    """Check a contiguous device vector of n values (None: any number)."""
-    if not (t.is_cuda and t.dtype in dtypes and t.dim() == 1 and (n is None or t.shape[0] == n) and t.is_contiguous()):
+def _vector(t: torch.Tensor, name: str, n, dtypes, dev=None):
+    """Check a contiguous vector of n values (None: any number) on the device dev (None: any GPU)."""
+    if not (t.dim() == 1 and _fits(t, (t.shape[0] if n is None else n,), dtypes, dev)):
         _shape(t, name, (n,), dtypes)
-        _dev(t, name)
+        _dev(t, name, dev=dev)
 
 
 def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tensor, max_new_len: int,
@@ -422,16 +426,16 @@ def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tenso
     with free_counts -> next_counts int64 [2] = (taken, given).  next_lens may be seq_lens,
     next_counts free_counts."""
     s = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
-    one, two = (s,), (2,)
-    if not (_fits(seq_lens, one, _I32) and _fits(new_lens, one, _I32) and _fits(next_lens, one, _I32)
-            and _fits(cu_new_lens, (s + 1,), _I32) and (reused_lens is None or _fits(reused_lens, one, _I32))
-            and _fits(slot_map, (slot_map.numel(),), _I64) and block_tables.dim() == 2
-            and _fits(block_tables, (s, block_tables.shape[1]), _I32)
-            and (free_ring is None or _fits(free_ring, (free_ring.numel(),), _I32))
-            and (free_counts is None or _fits(free_counts, two, _I64))
-            and (next_counts is None or _fits(next_counts, two, _I64))):
+    one, two, dev = (s,), (2,), pool.device
+    if not (_fits(seq_lens, one, _I32, dev) and _fits(new_lens, one, _I32, dev) and _fits(next_lens, one, _I32, dev)
+            and _fits(cu_new_lens, (s + 1,), _I32, dev) and (reused_lens is None or _fits(reused_lens, one, _I32, dev))
+            and _fits(slot_map, (slot_map.numel(),), _I64, dev) and block_tables.dim() == 2
+            and _fits(block_tables, (s, block_tables.shape[1]), _I32, dev)
+            and (free_ring is None or _fits(free_ring, (free_ring.numel(),), _I32, dev))
+            and (free_counts is None or _fits(free_counts, two, _I64, dev))
+            and (next_counts is None or _fits(next_counts, two, _I64, dev))):
         _tables_args(s, seq_lens, new_lens, block_tables, next_lens, cu_new_lens, reused_lens, slot_map, free_ring,
-                     free_counts, next_counts)
+                     free_counts, next_counts, dev)
     _check(_lib.kv_tables_update(pool.handle, s, seq_lens.data_ptr(), new_lens.data_ptr(), block_tables.data_ptr(),
                                  block_tables.shape[1], _ptr(free_ring),
                                  0 if free_ring is None else free_ring.shape[0], _ptr(free_counts),
@@ -443,27 +447,29 @@ def kv_tables_update(pool: KVPool, seq_lens: torch.Tensor, new_lens: torch.Tenso
 
 
 def _tables_args(s, seq_lens, new_lens, block_tables, next_lens, cu_new_lens, reused_lens, slot_map, free_ring,
-                 free_counts, next_counts):
+                 free_counts, next_counts, dev):
     """Shapes, types and devices of kv_tables_update's tensors (raises ValueError)."""
     for t, name, n in ((seq_lens, "seq_lens", s), (new_lens, "new_lens", s), (next_lens, "next_lens", s),
                        (cu_new_lens, "cu_new_lens", s + 1), (reused_lens, "reused_lens", s),
                        (free_ring, "free_ring", None)):
         if t is not None:
-            _vector(t, name, n, _I32)
-    _vector(slot_map, "slot_map", None, _I64)
+            _vector(t, name, n, _I32, dev)
+    _vector(slot_map, "slot_map", None, _I64, dev)
     for t, name in ((free_counts, "free_counts"), (next_counts, "next_counts")):
         if t is not None:
-            _vector(t, name, 2, _I64)
-    if not (block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32)):
+            _vector(t, name, 2, _I64, dev)
+    if not (block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32, dev)):
         _shape(block_tables, "block_tables", (s, None), torch.int32)
-        _dev(block_tables, "block_tables")
+        _dev(block_tables, "block_tables", dev=dev)
 
 
-def _rows(t: torch.Tensor, name: str, shape) -> int:
+def _rows(t: torch.Tensor, name: str, shape, dev=None) -> int:
     """Check rows [T][Hkv][D] of a device tensor, each row contiguous; elements from row to row."""
     _shape(t, name, shape, _BF16)
     if not t.is_cuda:
         raise ValueError("%s must be a device tensor" % name)
+    if dev is not None and t.get_device() != dev:
+        raise ValueError("%s must be on the pool's device (%d, got %d)" % (name, dev, t.get_device()))
     if shape[0] and (t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2])):
         raise ValueError("each row of %s must be contiguous" % name)
     return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
@@ -473,16 +479,16 @@ def kv_append(pool: KVPool, layer: int, k_new: torch.Tensor, v_new: torch.Tensor
               slot_map_host=None, stream=None) -> None:
     """Write rows k_new, v_new [T][Hkv][D] (bf16; rows may be strided, as views of a fused projection
     are) into the slots of slot_map int64 [T] (negative: left out)."""
-    h, d = pool.num_kv_heads, pool.head_dim
+    h, d, dev = pool.num_kv_heads, pool.head_dim, pool.device
     shape = (slot_map.shape[0] if slot_map.dim() == 1 else -1, h, d)
     kst, vst = k_new.stride(), v_new.stride()
-    if (k_new.shape == shape and v_new.shape == shape and kst[1:] == (d, 1) and vst[1:] == (d, 1) and k_new.is_cuda
-            and v_new.is_cuda and k_new.dtype in _BF16 and v_new.dtype in _BF16 and slot_map.is_cuda
-            and slot_map.dtype in _I64 and slot_map.is_contiguous() and shape[0] > 1):
+    if (k_new.shape == shape and v_new.shape == shape and kst[1:] == (d, 1) and vst[1:] == (d, 1)
+            and k_new.get_device() == v_new.get_device() == slot_map.get_device() == dev
+            and k_new.dtype in _BF16 and v_new.dtype in _BF16 and slot_map.dtype in _I64 and slot_map.is_contiguous() and shape[0] > 1):
         ks, vs = kst[0], vst[0]
     else:
-        _vector(slot_map, "slot_map", None, _I64)
-        ks, vs = _rows(k_new, "k_new", shape), _rows(v_new, "v_new", shape)
+        _vector(slot_map, "slot_map", None, _I64, dev)
+        ks, vs = _rows(k_new, "k_new", shape, dev), _rows(v_new, "v_new", shape, dev)
     keep = None
     if slot_map_host is not None:
         keep = np.ascontiguousarray(np.asarray(slot_map_host).reshape(-1), dtype=np.int64)

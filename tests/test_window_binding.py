@@ -116,3 +116,11 @@ def test_tensors_on_the_host(kv, pool):
         for name, t in tensors.items():
             with pytest.raises(ValueError):
                 call(**dict(tensors, **{name: Tensor(*t.shape, dtype=t.dtype, device=-1)}))
+
+
+def test_tensors_on_another_gpu(kv, pool):
+    """Their memory is not the pool's device's: a kernel that reads it faults."""
+    for call, tensors in calls(kv, pool):
+        for name, t in tensors.items():
+            with pytest.raises(ValueError, match="pool's device"):
+                call(**dict(tensors, **{name: Tensor(*t.shape, dtype=t.dtype, device=1)}))
