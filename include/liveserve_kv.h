@@ -369,9 +369,27 @@ ls_status paged_attn_prefill_window(ls_kv_pool *pool, int32_t layer, int32_t num
  * the ring LS_DEVERR_FREE_LIST; then tables, ring and counters stay as they are
  * (next_counts = free_counts, next_lens = seq_lens), cu_new_lens is all 0 and slot_map
  * all -1.  An id outside the pool is copied as it stands and flagged
- * (LS_DEVERR_BLOCK_ID), its tokens' slots are -1.  A session with new_lens[s] = 0 gets
- * no slot: an appending decode of this step leaves it out, since its next block may
- * not be its own.  The pool gives the range of ids; its memory is not touched.
+ * (LS_DEVERR_BLOCK_ID), its tokens' slots are -1.  The pool gives the range of ids; its
+ * memory is not touched.
+ *
+ * Sessions without a new token (new_lens[s] = 0), and all sessions of a refused step, get
+ * no slot, and the block of their next position may belong to another session by now.  A
+ * decode with k_new and v_new does not know that: it writes every session's row at
+ * context_lens[s].  A step in which sessions may idle, or that may be refused, therefore
+ * appends by kv_append and attends without k_new and v_new.  Either its rows are those of
+ * the sessions that have any, back to back as cu_new_lens says, and
+ * paged_attn_prefill_window (max_new_len 1) attends over reused_lens; or they are one per
+ * session, kv_append takes slot_map[cu_new_lens[s]] for those with a new token and -1 for
+ * the others, and paged_attn_decode_window attends over next_lens (rows of sessions without
+ * a new token then mean nothing).
+ *
+ * A block that is in two sessions' tables would be given back twice: with a window, tables
+ * share none.  Nothing gives back the blocks of a session that ends.  Those it holds at
+ * length L are the columns below ceil(sinks / 16) and those from ceil(sinks / 16) +
+ * max(0, floor((L - window + 1) / 16) - ceil(sinks / 16)) to ceil(L / 16) - 1 (without a
+ * window, all below ceil(L / 16)); between two steps of the ring, in stream order, the caller
+ * writes their ids to entries given, given + 1, .. of it and adds their number to `given`.
+ *
  * Errors: LS_EINVAL (NULL, misaligned or overlapping arrays, sizes out of range,
  * free_ring without counters or the other way round, a window without free_ring, a
  * window or sinks out of range, more than 2^27 - 1 blocks per session), LS_EHIP.
