@@ -21,7 +21,11 @@
 //   O^T[16 dims   x 16 heads] += V^T[16 x 16 tokens] . P^T     (16x16x16 bf16)
 // The MFMA accumulator layout of S^T (lane: head = lane%16, tokens 4*(lane/16)+i)
 // is exactly the B-operand layout PV needs, so the probabilities never leave
-// registers.  K tiles are chunk-major ([D/8][16 tokens][8 dims]) and V tiles
+// registers.  They are rounded to bf16 for that product (the running sum adds the
+// fp32 ones up), since more bits would take a second product with the remainder
+// per block: a probability is then off by 2^-8 of itself at most, and an output's
+// RMS error against 64 bits is 2.0-2.1e-3 of it, of which 1.6e-3 is the rounding
+// of the bf16 output.  K tiles are chunk-major ([D/8][16 tokens][8 dims]) and V tiles
 // dim-major in the pool, so both operands load straight from HBM into their
 // MFMA lanes: each K load instruction reads 1 KiB contiguous (lane l: bytes
 // 16l .. 16l+15 of the k-step's chunks), each V load 512 contiguous bytes;
@@ -118,8 +122,8 @@ struct DecodeArgs {
 // v (v < 16 ceil(sinks / 16)) or v + 16 skip.  Below, lengths, splits and blocks
 // are counted on the walk; only table columns are not.  In it the keys not seen
 // are v in [sinks, L_walk - window): at most 15 in the last block of the first
-// tokens and 15 in the window's first block, or, where the two overlap
-// (skip = 0), any number of keys between them.  Bound by HBM over the walk's blocks
+// tokens and 15 in the window's first block (no block of a walk lies between the
+// two, also where skip = 0).  Bound by HBM over the walk's blocks
 // when the batch fills the GPU (64 sessions of up to 16384 keys, window 4096, 32/4
 // heads: 69.8 us, 6.2 TB/s; 256 of window 1024 at 16/2 heads: 51.0 us, 5.1 TB/s, the
 // walk's two blocks past the window among the reads), by latency when it is small

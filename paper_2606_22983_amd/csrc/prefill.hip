@@ -19,7 +19,12 @@
 // of PV, and they are 8 consecutive tokens of one block, i.e. one 16-byte
 // chunk of the block's dim-major V tile.  So P stays in registers (rounded to
 // bf16; the row sums add up the same rounded values) and every MFMA operand is
-// one 16-byte LDS read.  Scores are exact fp32 sums of bf16 products; the
+// one 16-byte LDS read.  The rounding is chosen for the matrix instruction: P of
+// more bits would be two bf16 parts and a second product, half as many matrix
+// instructions again in a kernel that they bound.  A probability is off by 2^-8 of
+// itself at most, the same in O and in the row sum, and an output's RMS error
+// against 64 bits is 2.0-2.3e-3 of it, of which 1.6e-3 is the rounding of the bf16
+// output.  Scores are exact fp32 sums of bf16 products; the
 // softmax scale is applied in fp32 (folding it into q before the MFMA would
 // round q * scale to bf16, an error that grows with the score magnitude).
 // Softmax statistics stay in fp32.  A row's running max m' is set from its
@@ -115,10 +120,15 @@ struct PrefillArgs {
 // below are counted on the walk; only table columns are not.  A tile all of whose
 // rows are first tokens has no second part.
 // Bound by the matrix cores and the softmax between their products when walks are
-// long (32 turns, 19817 tokens in all, window 4096, 32/4 heads of 128: 2152 us,
-// 1211 TFLOP/s of what the rows see), by the start and end of an item when they are
-// short (8 first turns of 50-700 tokens, window 256, 8/8 heads of 64: 17 us, beside
-// 7 for their append).
+// long (32 turns, 19817 tokens in all, window 4096, 32/4 heads of 128: 2185-2245 us,
+// 1161-1193 TFLOP/s of what the rows see), by the start and end of an item when they
+// are short (8 first turns of 50-700 tokens, window 256, 8/8 heads of 64: 18 us,
+// beside 7 for their append).
+//
+// Table entries that name no block (tables hold stale ids by design): an item looks
+// over the ids of its walk while its first stages load, flags those outside the pool
+// and has its waves mask their keys, by taking no unit for one that all rows see.
+// That, and V zeroed behind the tile's last key, cost 1.2% over 27 random calls.
 struct PrefillWindowArgs : PrefillArgs {
     int32_t window;                // >= 1
     int32_t sinks;                 // >= 0
