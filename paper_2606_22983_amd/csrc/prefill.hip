@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kPreThreads) void prefill_kernel(PrefillArgsT<kWin>
         bool pending = kWin;                           // some row of the wave is unset
         auto mask_unit = [&](f32x4 (&acc)[kRT][2], int key0) {
             if constexpr (kWin) {
-                if (!pending && (unsigned)(key0 - wave_from) < (unsigned)wave_whole) return;
+                if (!pending && (unsigned)key0 - (unsigned)wave_from < (unsigned)wave_whole) return;
                 if (__builtin_expect(wave_from == kAbsent, 0)) {
                     // (lane group g4 holds keys of the unit's block g4 / 2)
                     const uint32_t b0 = (uint32_t)entry(key0 / kBlock), b1 = (uint32_t)entry(key0 / kBlock + 1);
