@@ -76,8 +76,9 @@ typedef enum {
                                        decode context, a context past its block table, a
                                        turn longer than max_new_len); see each call */
 #define LS_DEVERR_INTERNAL 0x4u     /* an internal bounded wait expired (a library bug) */
-#define LS_DEVERR_FREE_LIST 0x8u    /* kv_tables_update: too few free blocks, no room to give
-                                       blocks back, or counters that cannot be */
+#define LS_DEVERR_FREE_LIST 0x8u    /* kv_tables_update, kv_evict: too few free blocks, no room to
+                                       give blocks back, or counters that cannot be */
+#define LS_DEVERR_GROUP    0x10u    /* prefix groups that cannot be; see paged_attn_decode_shared */
 
 typedef struct ls_kv_pool ls_kv_pool;
 
@@ -422,6 +423,173 @@ ls_status kv_tables_update(ls_kv_pool *pool, int32_t num_sessions, const int32_t
 ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const void *k_new, const void *v_new,
                     int64_t k_stride, int64_t v_stride, const int64_t *slot_map, const int64_t *slot_map_host,
                     hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Sessions that share a prefix, and caches bounded by what attention uses.
+ * Sessions of one service begin with the same instructions, whose blocks their
+ * tables can have in common (block-level allocation, §5.1); and a history that
+ * grows without end (§2.1, §5) can be cut to the tokens that later ones attend to.
+ * All entry points of this section refuse (LS_EINVAL) a call made while another
+ * device than the pool's is current, q, out, weights or a workspace that is not
+ * 16-byte aligned, and index arrays that are not aligned to their type.  They
+ * neither append nor allocate: a step's rows are in the pool before (kv_append,
+ * or a prefill's k_new and v_new).
+ * ---------------------------------------------------------------------- */
+
+/*
+ * paged_attn_decode_shared — paged_attn_decode for a batch in which groups of
+ * sessions have the first blocks of their tables in common: the group's shared keys
+ * are read, and attended to by all of its query rows, once for the group.
+ *
+ *   num_groups, num_members   host ints: groups, and their members in all (0 and 0,
+ *                  with the three arrays NULL: no session shares)
+ *   group_starts   device int32 [num_groups + 1]: prefix sums of the groups' sizes, from
+ *                  0 to num_members
+ *   group_members  device int32 [num_members]: sessions, each at most once; a session in
+ *                  no group is computed on its own
+ *   prefix_blocks  device int32 [num_groups]: P, 0 .. max_blocks_per_session.  The first P
+ *                  blocks of the members' tables hold the same keys; the table row of the
+ *                  group's longest member is the one that is read.  A member may be
+ *                  shorter than the prefix: it attends to its context_lens[s] keys
+ *   context_lens   device int32 [num_sessions]: keys in the pool, the step's own included.
+ *                  0: the session sits the step out, its output row is zeros.  A negative
+ *                  length counts as 0 and one past the table as the table's; both are
+ *                  flagged (LS_DEVERR_LENGTH)
+ *   workspace      device, >= ls_decode_shared_workspace_bytes(...) bytes; no
+ *                  initialisation is needed, concurrent calls need their own
+ *
+ * Groups that cannot be (starts that do not rise from 0 to num_members, a member
+ * outside the batch or twice, a prefix outside the table) are flagged
+ * (LS_DEVERR_GROUP), and every session is computed on its own, over its own table.
+ * Ids outside the pool are flagged (LS_DEVERR_BLOCK_ID) and their keys left out.
+ * V of slots behind the longest member's keys does not reach the output; a NaN or
+ * infinite V that one row of a group sees may make the group's other rows NaN.
+ * Results depend on the lengths and on the stream's CUs, by the order of fp32 sums,
+ * and not on how often the call is made.  Other arguments as paged_attn_decode.
+ *
+ * Supported: num_q_heads / num_kv_heads in {1, 2, 4, 8}; at most 2048 sessions, 2048
+ * groups and 16384 blocks per session (LS_EUNSUPPORTED).  Other errors: LS_EINVAL (also
+ * more members than sessions, more groups than members), LS_ENOMEM, LS_EHIP.
+ */
+size_t ls_decode_shared_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                        int32_t num_groups, int32_t num_members);
+ls_status paged_attn_decode_shared(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                   const void *q, const int32_t *block_tables, int32_t max_blocks_per_session,
+                                   const int32_t *context_lens, int32_t num_groups, const int32_t *group_starts,
+                                   int32_t num_members, const int32_t *group_members, const int32_t *prefix_blocks,
+                                   float scale, void *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Accumulated attention weights.  Beside the pool the caller keeps two arrays of
+ * its shape, with an entry per layer, block, KV head and slot:
+ *
+ *   weights     device fp32  [num_layers][num_blocks][num_kv_heads][16]
+ *   positions   device int32 [num_layers][num_blocks][num_kv_heads][16]
+ *
+ * An entry belongs to the token in that slot: its weight is the sum of the
+ * probabilities that queries have given it, over the steps and over the query heads of
+ * its KV head; its position is the token's place in the conversation, which stays when
+ * an eviction moves the token to another slot.  Entries of slots without a token mean
+ * nothing and need no initialisation.
+ *
+ *   reused_lens      device int32 [num_sessions]: tokens in the cache before the step
+ *                    (kv_tables_update's).  Keys t >= reused_lens[s] are new: their weight is
+ *                    set to this call's sum and their position to first_positions[s] + t -
+ *                    reused_lens[s]; older keys' weights are added to
+ *   first_positions  device int32 [num_sessions] or NULL: the position of the session's first
+ *                    new token (NULL: its place in the cache, reused_lens[s])
+ *   first_lens       device int32 [num_sessions] or NULL: keys t < first_lens[s] are never
+ *                    evicted, and no entry of theirs is read or written.  Blocks that are in
+ *                    several sessions' tables lie below it (or below a group's prefix)
+ *
+ * paged_attn_decode_weights — paged_attn_decode_shared that also adds the weights up.
+ * Keys of a group's shared prefix get none.  reused_lens NULL (and first_positions and
+ * positions NULL): no key is new.  Every query counts, so a session without a new token
+ * sits out with a length of 0.  The workspace (ls_decode_weights_workspace_bytes, which
+ * holds the scores of every block of the pool) is 16-byte aligned.  Other arguments,
+ * limits and errors as paged_attn_decode_shared.
+ */
+size_t ls_decode_weights_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                         int32_t num_groups, int32_t num_members);
+ls_status paged_attn_decode_weights(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                    const void *q, const int32_t *block_tables, int32_t max_blocks_per_session,
+                                    const int32_t *context_lens, const int32_t *reused_lens,
+                                    const int32_t *first_positions, const int32_t *first_lens, int32_t num_groups,
+                                    const int32_t *group_starts, int32_t num_members, const int32_t *group_members,
+                                    const int32_t *prefix_blocks, float scale, void *out, float *weights,
+                                    int32_t *positions, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * kv_weights_prefill — the weights of a turn: adds up what the last `rows` new tokens of
+ * each session's turn (all of a shorter turn) give to the session's keys, causally: new
+ * token j sees keys 0 .. reused_lens[s] + j.  The turn's K are in the pool already
+ * (after paged_attn_prefill with k_new, or kv_append); V is not read and no output
+ * row computed.  A turn without new tokens leaves its session's entries as they are.
+ *
+ *   q              device bf16 [total_new_tokens][num_q_heads][head_dim], as the prefill's
+ *   cu_new_lens    device int32 [num_sessions + 1], total_new_tokens, max_new_len: as
+ *                  paged_attn_prefill.  A turn that is negative, longer than max_new_len, past
+ *                  total_new_tokens or past its table is flagged (LS_DEVERR_LENGTH) and left
+ *                  out
+ *   rows           >= 1
+ *   workspace      device, >= ls_weights_prefill_workspace_bytes(...) bytes, 16-byte
+ *                  aligned; its size depends on max_new_len, rows and
+ *                  max_blocks_per_session
+ *
+ * Ids outside the pool are flagged (LS_DEVERR_BLOCK_ID) and their keys left out.
+ * Supported: num_q_heads / num_kv_heads in {1, 2, 4, 8}, at most 2048 sessions and 16384
+ * blocks per session (LS_EUNSUPPORTED).  Other errors: LS_EINVAL, LS_ENOMEM, LS_EHIP.
+ */
+size_t ls_weights_prefill_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                          int32_t total_new_tokens, int32_t max_new_len, int32_t rows,
+                                          int32_t max_blocks_per_session);
+ls_status kv_weights_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads, const void *q,
+                             const int32_t *cu_new_lens, const int32_t *reused_lens, int32_t total_new_tokens,
+                             int32_t max_new_len, const int32_t *block_tables, int32_t max_blocks_per_session,
+                             int32_t rows, const int32_t *first_positions, const int32_t *first_lens, float scale,
+                             float *weights, int32_t *positions, void *workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/*
+ * kv_evict — cut the sessions that have more than `limit` tokens to `budget`.  Of a
+ * session with L = seq_lens[s] > limit tokens, every layer of [layer_begin, layer_begin +
+ * layer_count) and every KV head keeps m = min(L, max(budget, first_lens[s] + recent)),
+ * each its own: the first first_lens[s] slots; the tokens at positions >=
+ * next_positions[s] - recent; then those of the largest weight, of equal ones (a NaN
+ * ranks below every number) those in lower slots.  The tokens that stay at slots >= m
+ * move to the slots below m that were freed, the i-th of these to the i-th of those,
+ * with K, V, weight and position; all other slots stay as they are.  Attention does
+ * not depend on the order of its keys.
+ *
+ *   seq_lens       device int32 [num_sessions]: tokens in the cache
+ *   next_positions device int32 [num_sessions]: the position of the next token to come
+ *   budget, limit, recent   1 <= budget <= limit, 0 <= recent <= budget
+ *   weights_next, positions_next   where the entries of slots below next_lens[s] go (of all
+ *                  sessions).  Both apart from weights and positions, so that a call can
+ *                  be made again with the same result, or both the same as these
+ *   next_lens      device int32 [num_sessions], apart from seq_lens: m, or L if not more than
+ *                  limit
+ *   free_ring, ring_size, free_counts, next_counts   as kv_tables_update: the blocks from
+ *                  ceil(m / 16) to ceil(L / 16) - 1 go back to the ring, in session order.
+ *                  Their table entries stay; calls of other layers for the same lengths are
+ *                  made without a ring.  NULL, 0, NULL, NULL: none go back
+ *
+ * Called for all layers at once, after the step's attention and before the next
+ * kv_tables_update, which then takes next_lens.  All sessions are served or none: a
+ * length outside its table is flagged LS_DEVERR_LENGTH, no room in the ring or
+ * counters that cannot be LS_DEVERR_FREE_LIST; then next_lens = seq_lens, next_counts =
+ * free_counts and nothing moves.  Tokens of a block whose id is outside the pool rank
+ * lowest and are not moved (LS_DEVERR_BLOCK_ID).  Apart from shared blocks below
+ * first_lens, no block is in two sessions' tables.  Errors: LS_EINVAL (also arrays that
+ * overlap and are not said to be the same), LS_EUNSUPPORTED (more than 65535 layers, KV
+ * heads), LS_EHIP.
+ */
+ls_status kv_evict(ls_kv_pool *pool, int32_t layer_begin, int32_t layer_count, int32_t num_sessions,
+                   const int32_t *seq_lens, const int32_t *block_tables, int32_t max_blocks_per_session, int32_t budget,
+                   int32_t limit, int32_t recent, const int32_t *first_lens, const int32_t *next_positions,
+                   const float *weights, const int32_t *positions, float *weights_next, int32_t *positions_next,
+                   int32_t *next_lens, int32_t *free_ring, int32_t ring_size, const int64_t *free_counts,
+                   int64_t *next_counts, hipStream_t stream);
 
 /*
  * Arguments shared by the three block-copy calls below.

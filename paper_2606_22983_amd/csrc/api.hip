@@ -403,6 +403,72 @@ ls_status prefill_call(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, in
     return e == hipSuccess ? LS_OK : hip_fail(e, "prefill launch");
 }
 
+// Checks that the decodes with shared prefixes or weights and the weights of a turn have in common.
+ls_status check_cache_call(const PoolGeom &p, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                           int32_t max_blocks, float scale) {
+    if (layer < 0 || layer >= p.num_layers)
+        return fail(LS_EINVAL, "layer %d outside [0, %d)", layer, p.num_layers);
+    if (num_sessions < 0) return fail(LS_EINVAL, "num_sessions must be >= 0");
+    if (ls_status st = check_heads(p, num_q_heads)) return st;
+    if (max_blocks <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
+    if (!(scale > 0.f)) return fail(LS_EINVAL, "scale must be a positive number");
+    if (num_sessions > kMaxCacheSessions || max_blocks > kMaxCacheBlocks || p.num_kv_heads > 65535)
+        return fail(LS_EUNSUPPORTED, "%d sessions with %d blocks each exceed the limits (%d sessions, %d blocks per session)",
+                    num_sessions, max_blocks, kMaxCacheSessions, kMaxCacheBlocks);
+    return LS_OK;
+}
+
+ls_status check_groups(int32_t num_sessions, int32_t num_groups, int32_t num_members, const int32_t *starts,
+                       const int32_t *members, const int32_t *prefix) {
+    if (num_groups < 0 || num_members < 0 || num_groups > num_members || num_members > num_sessions)
+        return fail(LS_EINVAL, "%d groups of %d members in all, of %d sessions", num_groups, num_members, num_sessions);
+    if (num_groups ? !starts || !members || !prefix : num_members || starts || members || prefix)
+        return fail(LS_EINVAL, "group_starts, group_members and prefix_blocks come with groups, and groups with them");
+    if (!aligned(starts, 4) || !aligned(members, 4) || !aligned(prefix, 4))
+        return fail(LS_EINVAL, "group_starts, group_members and prefix_blocks must be 4-byte aligned");
+    return LS_OK;
+}
+
+// paged_attn_decode_shared, or with weighted paged_attn_decode_weights.
+ls_status shared_call(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads, const SharedCall &c,
+                      bool weighted, size_t workspace_bytes, hipStream_t stream) {
+    if (ls_status st = check_pool(pool)) return st;
+    const PoolGeom &p = pool->geom;
+    if (ls_status st = check_cache_call(p, layer, num_sessions, num_q_heads, c.max_blocks, c.scale)) return st;
+    if (ls_status st = check_groups(num_sessions, c.num_groups, c.num_members, c.group_starts, c.group_members, c.prefix_blocks))
+        return st;
+    if (num_sessions == 0) return LS_OK;
+    if (!c.q || !c.block_tables || !c.context_lens || !c.out || !c.workspace)
+        return fail(LS_EINVAL, "q, block_tables, context_lens, out and workspace must not be NULL");
+    if (weighted) {
+        if (!c.weights) return fail(LS_EINVAL, "weights must not be NULL");
+        if (c.reused_lens ? !c.positions : c.positions || c.first_positions)
+            return fail(LS_EINVAL, "positions come with reused_lens, and first_positions with both");
+    }
+    if (!aligned(c.q, 16) || !aligned(c.out, 16) || !aligned(c.weights, 16) || !aligned(c.positions, 16) || !aligned(c.workspace, 16))
+        return fail(LS_EINVAL, "q, out, weights, positions and workspace must be 16-byte aligned");
+    if (!aligned(c.block_tables, 4) || !aligned(c.context_lens, 4) || !aligned(c.reused_lens, 4) ||
+        !aligned(c.first_positions, 4) || !aligned(c.first_lens, 4))
+        return fail(LS_EINVAL, "tables, lengths and positions must be 4-byte aligned");
+    const SharedPlan plan = plan_shared(p, num_sessions, num_q_heads, c.num_groups, c.num_members, weighted);
+    if (workspace_bytes < plan.total)
+        return fail(LS_ENOMEM, "workspace_bytes (%zu) < required (%zu)", workspace_bytes, plan.total);
+    if (ls_status st = check_device(p)) return st;
+    unsigned int *err = device_error_word();
+    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
+    hipError_t e = launch_shared(p, layer, num_sessions, num_q_heads, c, plan, err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "decode launch");
+}
+
+size_t shared_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads, int32_t num_groups,
+                    int32_t num_members, bool weighted) {
+    if (!pool || num_sessions <= 0 || num_sessions > kMaxCacheSessions || num_q_heads <= 0 ||
+        num_q_heads % pool->geom.num_kv_heads || !supported_group(num_q_heads / pool->geom.num_kv_heads) ||
+        num_groups < 0 || num_groups > num_members || num_members > num_sessions || (!num_groups && num_members))
+        return 0;
+    return plan_shared(pool->geom, num_sessions, num_q_heads, num_groups, num_members, weighted).total;
+}
+
 }  // namespace
 
 // Message for ls_last_error() from code outside this file (the KV manager).
@@ -663,6 +729,205 @@ ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const
     hipError_t e = launch_append_slots(p, layer, total_tokens, static_cast<const uint16_t *>(k_new),
                                        static_cast<const uint16_t *>(v_new), k_stride, v_stride, slot_map, err, stream);
     return e == hipSuccess ? LS_OK : hip_fail(e, "append launch");
+}
+
+size_t ls_decode_shared_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                        int32_t num_groups, int32_t num_members) {
+    return shared_bytes(pool, num_sessions, num_q_heads, num_groups, num_members, false);
+}
+
+ls_status paged_attn_decode_shared(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                   const void *q, const int32_t *block_tables, int32_t max_blocks_per_session,
+                                   const int32_t *context_lens, int32_t num_groups, const int32_t *group_starts,
+                                   int32_t num_members, const int32_t *group_members, const int32_t *prefix_blocks,
+                                   float scale, void *out, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    SharedCall c = {};
+    c.q = static_cast<const uint16_t *>(q);
+    c.block_tables = block_tables;
+    c.max_blocks = max_blocks_per_session;
+    c.context_lens = context_lens;
+    c.num_groups = num_groups;
+    c.num_members = num_members;
+    c.group_starts = group_starts;
+    c.group_members = group_members;
+    c.prefix_blocks = prefix_blocks;
+    c.scale = scale;
+    c.out = static_cast<uint16_t *>(out);
+    c.workspace = workspace;
+    return shared_call(pool, layer, num_sessions, num_q_heads, c, false, workspace_bytes, stream);
+}
+
+size_t ls_decode_weights_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                         int32_t num_groups, int32_t num_members) {
+    return shared_bytes(pool, num_sessions, num_q_heads, num_groups, num_members, true);
+}
+
+ls_status paged_attn_decode_weights(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads,
+                                    const void *q, const int32_t *block_tables, int32_t max_blocks_per_session,
+                                    const int32_t *context_lens, const int32_t *reused_lens,
+                                    const int32_t *first_positions, const int32_t *first_lens, int32_t num_groups,
+                                    const int32_t *group_starts, int32_t num_members, const int32_t *group_members,
+                                    const int32_t *prefix_blocks, float scale, void *out, float *weights,
+                                    int32_t *positions, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    SharedCall c = {};
+    c.q = static_cast<const uint16_t *>(q);
+    c.block_tables = block_tables;
+    c.max_blocks = max_blocks_per_session;
+    c.context_lens = context_lens;
+    c.num_groups = num_groups;
+    c.num_members = num_members;
+    c.group_starts = group_starts;
+    c.group_members = group_members;
+    c.prefix_blocks = prefix_blocks;
+    c.scale = scale;
+    c.out = static_cast<uint16_t *>(out);
+    c.weights = weights;
+    c.positions = positions;
+    c.reused_lens = reused_lens;
+    c.first_positions = first_positions;
+    c.first_lens = first_lens;
+    c.workspace = workspace;
+    return shared_call(pool, layer, num_sessions, num_q_heads, c, true, workspace_bytes, stream);
+}
+
+size_t ls_weights_prefill_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
+                                          int32_t total_new_tokens, int32_t max_new_len, int32_t rows,
+                                          int32_t max_blocks_per_session) {
+    if (!pool || num_sessions <= 0 || num_sessions > kMaxCacheSessions || num_q_heads <= 0 ||
+        num_q_heads % pool->geom.num_kv_heads || !supported_group(num_q_heads / pool->geom.num_kv_heads) ||
+        max_new_len <= 0 || max_new_len > total_new_tokens || rows <= 0 || max_blocks_per_session <= 0 ||
+        max_blocks_per_session > kMaxCacheBlocks)
+        return 0;
+    return plan_observe(pool->geom, num_sessions, num_q_heads, max_new_len, rows, max_blocks_per_session).total;
+}
+
+ls_status kv_weights_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int32_t num_q_heads, const void *q,
+                             const int32_t *cu_new_lens, const int32_t *reused_lens, int32_t total_new_tokens,
+                             int32_t max_new_len, const int32_t *block_tables, int32_t max_blocks_per_session,
+                             int32_t rows, const int32_t *first_positions, const int32_t *first_lens, float scale,
+                             float *weights, int32_t *positions, void *workspace, size_t workspace_bytes,
+                             hipStream_t stream) {
+    if (ls_status st = check_pool(pool)) return st;
+    const PoolGeom &p = pool->geom;
+    if (ls_status st = check_cache_call(p, layer, num_sessions, num_q_heads, max_blocks_per_session, scale)) return st;
+    if (total_new_tokens < 0 || max_new_len < 0) return fail(LS_EINVAL, "total_new_tokens and max_new_len must be >= 0");
+    if (rows < 1) return fail(LS_EINVAL, "rows (%d) must be >= 1", rows);
+    if (max_new_len > total_new_tokens)
+        return fail(LS_EINVAL, "max_new_len (%d) exceeds total_new_tokens (%d)", max_new_len, total_new_tokens);
+    if (num_sessions == 0 || total_new_tokens == 0 || max_new_len == 0) return LS_OK;
+    if (!q || !cu_new_lens || !reused_lens || !block_tables || !weights || !positions || !workspace)
+        return fail(LS_EINVAL, "q, cu_new_lens, reused_lens, block_tables, weights, positions and workspace must not be NULL");
+    if (!aligned(q, 16) || !aligned(weights, 16) || !aligned(positions, 16) || !aligned(workspace, 16))
+        return fail(LS_EINVAL, "q, weights, positions and workspace must be 16-byte aligned");
+    if (!aligned(cu_new_lens, 4) || !aligned(reused_lens, 4) || !aligned(block_tables, 4) || !aligned(first_positions, 4) ||
+        !aligned(first_lens, 4))
+        return fail(LS_EINVAL, "tables, lengths and positions must be 4-byte aligned");
+    const ObservePlan plan = plan_observe(p, num_sessions, num_q_heads, max_new_len, rows, max_blocks_per_session);
+    if (workspace_bytes < plan.total)
+        return fail(LS_ENOMEM, "workspace_bytes (%zu) < required (%zu)", workspace_bytes, plan.total);
+    if (ls_status st = check_device(p)) return st;
+    unsigned int *err = device_error_word();
+    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
+    ObserveCall c = {};
+    c.q = static_cast<const uint16_t *>(q);
+    c.cu_new_lens = cu_new_lens;
+    c.reused_lens = reused_lens;
+    c.total_new_tokens = total_new_tokens;
+    c.max_new_len = max_new_len;
+    c.block_tables = block_tables;
+    c.max_blocks = max_blocks_per_session;
+    c.rows = rows;
+    c.scale = scale;
+    c.weights = weights;
+    c.positions = positions;
+    c.first_positions = first_positions;
+    c.first_lens = first_lens;
+    c.workspace = workspace;
+    hipError_t e = launch_observe(p, layer, num_sessions, num_q_heads, c, plan, err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "weights launch");
+}
+
+ls_status kv_evict(ls_kv_pool *pool, int32_t layer_begin, int32_t layer_count, int32_t num_sessions,
+                   const int32_t *seq_lens, const int32_t *block_tables, int32_t max_blocks_per_session, int32_t budget,
+                   int32_t limit, int32_t recent, const int32_t *first_lens, const int32_t *next_positions,
+                   const float *weights, const int32_t *positions, float *weights_next, int32_t *positions_next,
+                   int32_t *next_lens, int32_t *free_ring, int32_t ring_size, const int64_t *free_counts,
+                   int64_t *next_counts, hipStream_t stream) {
+    if (ls_status st = check_pool(pool)) return st;
+    const PoolGeom &p = pool->geom;
+    if (layer_begin < 0 || layer_count < 1 || layer_begin > p.num_layers - layer_count)
+        return fail(LS_EINVAL, "layer range [%d, %d + %d) outside [0, %d)", layer_begin, layer_begin, layer_count, p.num_layers);
+    if (num_sessions < 0) return fail(LS_EINVAL, "num_sessions must be >= 0");
+    if (max_blocks_per_session <= 0 || max_blocks_per_session > INT32_MAX / kBlock)
+        return fail(LS_EINVAL, "max_blocks_per_session (%d) must be in [1, %d]", max_blocks_per_session, INT32_MAX / kBlock);
+    if (budget < 1 || limit < budget || recent < 0 || recent > budget)
+        return fail(LS_EINVAL, "budget (%d) must be in [1, limit (%d)] and recent (%d) in [0, budget]", budget, limit, recent);
+    if (free_ring ? ring_size < 1 || !free_counts || !next_counts : ring_size || free_counts || next_counts)
+        return fail(LS_EINVAL, "a free ring comes with its size (%d) and counters, and these with a ring", ring_size);
+    if (num_sessions > 0 && (!seq_lens || !block_tables || !next_positions || !weights || !positions || !weights_next ||
+                             !positions_next || !next_lens))
+        return fail(LS_EINVAL, "seq_lens, block_tables, next_positions, weights, positions, weights_next, positions_next and "
+                    "next_lens must not be NULL");
+    if ((weights_next == weights) != (positions_next == positions))
+        return fail(LS_EINVAL, "weights_next and positions_next are both the arrays before, or both apart");
+    if (layer_count > 65535 || p.num_kv_heads > 65535)
+        return fail(LS_EUNSUPPORTED, "at most 65535 layers a call and 65535 KV heads");
+    // Arrays that are written are memory of their own, but for those that advance in place.
+    struct Range {
+        const void *at;
+        size_t bytes, align;
+    };
+    const size_t S = (size_t)num_sessions, entries = (size_t)p.num_layers * (size_t)p.num_blocks * (size_t)p.num_kv_heads * kBlock * 4;
+    const Range arrays[] = {{weights, entries, 16},
+                            {weights_next, entries, 16},
+                            {positions, entries, 16},
+                            {positions_next, entries, 16},
+                            {free_counts, 16, 8},
+                            {next_counts, 16, 8},
+                            {next_lens, S * 4, 4},
+                            {free_ring, (size_t)ring_size * 4, 4},
+                            {seq_lens, S * 4, 4},
+                            {block_tables, S * (size_t)max_blocks_per_session * 4, 4},
+                            {first_lens, S * 4, 4},
+                            {next_positions, S * 4, 4}};
+    constexpr int kPaired = 6, kWritten = 8;       // the first six are pairs; those behind kWritten are only read
+    for (int i = 0; i < (int)(sizeof arrays / sizeof *arrays); ++i) {
+        const Range &x = arrays[i];
+        if (!aligned(x.at, x.align)) return fail(LS_EINVAL, "an array is not aligned (weights and positions to 16 bytes)");
+        for (int j = 0; j < i && j < kWritten; ++j) {
+            const Range &y = arrays[j];
+            if (!x.at || !y.at || !x.bytes || !y.bytes) continue;
+            const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+            if (a >= b + y.bytes || b >= a + x.bytes) continue;
+            if (!(x.at == y.at && i < kPaired && i % 2 == 1 && j == i - 1))
+                return fail(LS_EINVAL, "arrays overlap (only weights_next, positions_next and next_counts may be the arrays "
+                            "before)");
+        }
+    }
+    if (ls_status st = check_device(p)) return st;
+    unsigned int *err = device_error_word();
+    if (!err) return fail(LS_EHIP, "cannot resolve the device error word");
+    EvictCall c = {};
+    c.num_sessions = num_sessions;
+    c.seq_lens = seq_lens;
+    c.block_tables = block_tables;
+    c.max_blocks = max_blocks_per_session;
+    c.budget = budget;
+    c.limit = limit;
+    c.recent = recent;
+    c.first_lens = first_lens;
+    c.next_positions = next_positions;
+    c.weights = weights;
+    c.positions = positions;
+    c.weights_next = weights_next;
+    c.positions_next = positions_next;
+    c.next_lens = next_lens;
+    c.free_ring = free_ring;
+    c.ring_size = ring_size;
+    c.free_counts = free_counts;
+    c.next_counts = next_counts;
+    hipError_t e = launch_evict(p, layer_begin, layer_count, c, err, stream);
+    return e == hipSuccess ? LS_OK : hip_fail(e, "eviction launch");
 }
 
 ls_status kv_blocks_stash(ls_kv_pool *pool, int32_t n, const int32_t *block_ids,

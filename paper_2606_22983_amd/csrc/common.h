@@ -176,6 +176,84 @@ hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, in
                           float scale, uint16_t *out, void *workspace, size_t workspace_bytes, bool counters_cleared,
                           int32_t window, int32_t sinks, unsigned int *err, hipStream_t stream);
 
+// Most sessions and blocks per session of the decodes with shared prefixes or
+// weights and of a turn's weights.
+constexpr int32_t kMaxCacheSessions = 2048, kMaxCacheBlocks = 16384;
+
+// Decode with shared prefixes, and with accumulated weights (weights not null).
+struct SharedCall {
+    const uint16_t *q;
+    const int32_t *block_tables;
+    int32_t max_blocks;
+    const int32_t *context_lens;
+    int32_t num_groups, num_members;
+    const int32_t *group_starts, *group_members, *prefix_blocks;
+    float scale;
+    uint16_t *out;
+    float *weights;                // all layers, as positions
+    int32_t *positions;
+    const int32_t *reused_lens, *first_positions, *first_lens;
+    void *workspace;
+};
+// Its workspace: offsets of the schedule, the parts' states and the scores.
+struct SharedPlan {
+    size_t tile_slots, own_slots;
+    size_t at[7];
+    size_t total;
+};
+SharedPlan plan_shared(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads, int32_t num_groups,
+                       int32_t num_members, bool weights);
+hipError_t launch_shared(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads, const SharedCall &c,
+                         const SharedPlan &plan, unsigned int *err, hipStream_t stream);
+
+// Accumulated weights of a turn's last rows.
+struct ObserveCall {
+    const uint16_t *q;
+    const int32_t *cu_new_lens, *reused_lens;
+    int32_t total_new_tokens, max_new_len;
+    const int32_t *block_tables;
+    int32_t max_blocks;
+    int32_t rows;
+    float scale;
+    float *weights;                // all layers, as positions
+    int32_t *positions;
+    const int32_t *first_positions, *first_lens;
+    void *workspace;
+};
+struct ObservePlan {
+    int32_t whole_rows;            // rows of a KV head, at most
+    int32_t row_cap;               // of one round
+    int32_t blocks;                // per wave
+    int32_t chunks;                // of a table
+    size_t lse_at;
+    size_t total;
+};
+ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads, int32_t max_new_len, int32_t rows,
+                         int32_t max_blocks);
+hipError_t launch_observe(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads, const ObserveCall &c,
+                          const ObservePlan &plan, unsigned int *err, hipStream_t stream);
+
+// Eviction by accumulated weight (free_ring null: no block is given back).
+struct EvictCall {
+    int32_t num_sessions;
+    const int32_t *seq_lens;
+    const int32_t *block_tables;
+    int32_t max_blocks;
+    int32_t budget, limit, recent;
+    const int32_t *first_lens, *next_positions;
+    const float *weights;          // all layers, as the other three
+    const int32_t *positions;
+    float *weights_next;
+    int32_t *positions_next;
+    int32_t *next_lens;
+    int32_t *free_ring;
+    int32_t ring_size;
+    const int64_t *free_counts;
+    int64_t *next_counts;
+};
+hipError_t launch_evict(const PoolGeom &p, int32_t layer_begin, int32_t layer_count, const EvictCall &c, unsigned int *err,
+                        hipStream_t stream);
+
 // ---------------------------------------------------------------------------
 // Device helpers
 // ---------------------------------------------------------------------------

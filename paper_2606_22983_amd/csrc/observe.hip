@@ -1,0 +1,326 @@
+// Accumulated attention weights of a turn: what the last rows of the turn's queries
+// attend to (next-turn prefill over reused context, §5, §3), summed per key and KV
+// head, so that an eviction can tell the keys that later tokens will use.
+//
+// With rows i at positions p_i of the observed queries of one KV head (tokens times
+// query heads) and scores x_it = scale q_i.k_t for t <= p_i,
+//   w_t += sum_i e^(x_it - m_i) / l_i,   m_i = max_t x_it,   l_i = sum_t e^(x_it - m_i).
+// l is known only after all keys, so the scores are computed twice, from K alone (V is
+// not read), in three launches:
+//   rows    (m, l) of each row over each chunk of keys
+//   lse     their sum over the chunks, as log2(l) + m
+//   keys    e^(x - lse) summed over the rows, added to the weights
+// A wave keeps the K tiles of its blocks in registers, as the A operand of
+// S^T[16 tokens x 16 rows] = K . Q^T, and walks over the rows 16 at a time, so K is
+// read once a launch however many rows there are, and the rows (a few hundred KB)
+// come from L2.  A lane's scores belong to one row (lane % 16): sums over keys end
+// with two lane exchanges, sums over rows stay in the lane until the last row.
+// Bound by the matrix and exponential units when rows are many, by K when few.
+#include <algorithm>
+
+#include "common.h"
+
+namespace ls {
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kObThreads = 256;
+constexpr int kObWaves = kObThreads / kWave;
+constexpr int kObRows = 1024;                // rows of a KV head at a time (LDS); more take another round
+constexpr float kNoMax = -1.0e30f;
+constexpr int kRawBuffer = 0x00020000;
+
+struct ObserveArgs {
+    const uint16_t *pool;          // layer base
+    int64_t num_blocks;
+    int32_t num_kv_heads, group;
+    const uint16_t *q;             // [T][Hq][D]
+    const int32_t *cu;             // [S + 1]
+    const int32_t *reused;         // [S]
+    int32_t num_sessions, total, max_new;
+    const int32_t *tables;         // [S][max_blocks]
+    int32_t max_blocks;
+    int32_t rows;                  // observed tokens of a turn
+    float scale_log2;
+    int32_t row0;                  // first row of the round
+    int32_t row_cap;               // rows of the round, at most
+    int32_t chunks;                // chunks of a table, at most
+    float2 *part;                  // [S][Hkv][chunks][row_cap] (m, l)
+    float *lse;                    // [S][Hkv][row_cap]
+    float *weights;                // layer base, [num_blocks][Hkv][16]
+    int32_t *positions;
+    const int32_t *begin;          // [S] or null
+    const int32_t *first;          // [S] or null
+    unsigned int *err;
+};
+
+// A session's turn.
+struct Turn {
+    int q0;                        // row of q of its first token
+    int n, c;                      // new tokens, tokens before (0 and 0: not a turn that can be)
+    int j0;                        // first observed token
+    int rows;                      // rows of the round (tokens x group)
+};
+
+__device__ __forceinline__ Turn turn_of(const ObserveArgs &a, int s, bool may_flag) {
+    Turn t;
+    t.q0 = a.cu[s];
+    t.n = a.cu[s + 1] - t.q0;
+    t.c = a.reused[s];
+    if (t.q0 < 0 || t.n < 0 || t.n > a.max_new || t.n > a.total - t.q0 || t.c < 0 || (int64_t)t.c + t.n > (int64_t)a.max_blocks * kBlock) {
+        if (may_flag) flag_error(a.err, LS_DEVERR_LENGTH);
+        t.q0 = t.n = t.c = 0;
+    }
+    t.j0 = max(t.n - a.rows, 0);
+    t.rows = min(max((t.n - t.j0) * a.group - a.row0, 0), a.row_cap);
+    return t;
+}
+
+__device__ __forceinline__ float max_xor_16_32(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_xor_16_32(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// One chunk of kObWaves * KB blocks of a (session, KV head); wave w has blocks
+// w KB .. w KB + KB - 1 of it.  kKeys false: the rows' launch, true: the keys'.
+template <int D, int KB, bool kKeys>
+__global__ __launch_bounds__(kObThreads) void observe_kernel(ObserveArgs a) {
+    __shared__ float2 sm[kKeys ? 1 : kObWaves][kKeys ? 1 : kObRows];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c16 = lane % 16, g4 = lane / 16;
+    const int chunk = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+    const int H = a.num_kv_heads, G = a.group;
+    const Turn t = turn_of(a, s, kKeys && chunk == 0 && h == 0 && a.row0 == 0);
+    const int keys = t.c + t.n, col0 = (chunk * kObWaves + wave) * KB;
+    if (t.n == 0 || (a.row0 && !t.rows) || chunk * kObWaves * KB * kBlock >= keys) return;
+    // ---- the wave's K tiles
+    bf16x8 k[KB][D / 32];
+    int id[KB];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        int x = -1;
+        if ((col0 + b) * kBlock < keys) {
+            x = a.tables[(int64_t)s * a.max_blocks + col0 + b];
+            if (x < 0 || x >= a.num_blocks) {
+                if (kKeys && lane == 0) flag_error(a.err, LS_DEVERR_BLOCK_ID);
+                x = -1;
+            }
+        }
+        id[b] = __builtin_amdgcn_readfirstlane(x);
+        const uint16_t *kt = a.pool + ((int64_t)max(id[b], 0) * 2 * H + h) * (kBlock * D);
+        const __amdgpu_buffer_rsrc_t rk =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(kt), 0, id[b] < 0 ? 0 : kBlock * D * 2, kRawBuffer);
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks)
+            k[b][ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16, ks * 4 * kBlock * 16, 0));
+    }
+    bool absent = false;
+#pragma unroll
+    for (int b = 0; b < KB; ++b) absent = absent || id[b] < 0;
+    const int wkey0 = col0 * kBlock;               // the wave's first key
+    const int64_t pair = (int64_t)s * H + h;
+    const int p0 = t.c + t.j0;                     // position of the first observed token
+    // Rows before this one see none of the chunk's keys.
+    const int unseen = max(chunk * kObWaves * KB * kBlock - p0, 0) * G - a.row0;
+    const int tile0 = max(unseen, 0) / 16;
+    float sum[kKeys ? KB : 1][4] = {};
+    const uint16_t *qbase = a.q + ((int64_t)(t.q0 + t.j0) * H + h) * G * D;
+    auto load_q = [&](bf16x8 (&dst)[D / 32], int tile) {
+        const int row = tile * 16 + c16;
+        u32x4 x = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) {
+            if (row < t.rows) {
+                const int at = a.row0 + row;
+                x = *reinterpret_cast<const u32x4 *>(qbase + ((int64_t)(at / G) * H * G + at % G) * D + ks * 32 + g4 * 8);
+            }
+            dst[ks] = __builtin_bit_cast(bf16x8, x);
+        }
+    };
+    const int tiles = (t.rows + 15) / 16;
+    bf16x8 q[2][D / 32];
+    if (tile0 < tiles) load_q(q[0], tile0);
+    auto work = [&](const bf16x8 (&qt)[D / 32], int tile) {
+        const int row = tile * 16 + c16, pos = p0 + (a.row0 + row) / G;
+        const int first_pos = p0 + (a.row0 + tile * 16) / G;
+        // Some row of the tile does not see every key of the wave.
+        const bool partial = first_pos < wkey0 + KB * kBlock - 1 || absent;
+        float x[KB][4];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], qt[ks], acc, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[b][e] = acc[e] * a.scale_log2;
+                if (partial && (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0)) x[b][e] = -INFINITY;
+            }
+        }
+        if constexpr (kKeys) {
+            const float lse = row < t.rows ? a.lse[pair * a.row_cap + row] : INFINITY;
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[b][e] - lse);
+        } else {
+            float m = kNoMax, l = 0.f;
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, x[b][e]);
+            m = max_xor_16_32(m);
+#pragma unroll
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(x[b][e] - m);
+            l = sum_xor_16_32(l);
+            if (g4 == 0) sm[wave][row] = make_float2(m, l);
+        }
+    };
+    for (int tile = tile0; tile < tiles; tile += 2) {
+        if (tile + 1 < tiles) load_q(q[1], tile + 1);
+        work(q[0], tile);
+        if (tile + 1 >= tiles) break;
+        if (tile + 2 < tiles) load_q(q[0], tile + 2);
+        work(q[1], tile + 1);
+    }
+    if constexpr (!kKeys) {
+        __syncthreads();
+        for (int row = tid; row < t.rows; row += kObThreads) {
+            float m = kNoMax, l = 0.f;
+            if (row >= tile0 * 16) {
+#pragma unroll
+                for (int w = 0; w < kObWaves; ++w) m = fmaxf(m, sm[w][row].x);
+#pragma unroll
+                for (int w = 0; w < kObWaves; ++w) l += __builtin_amdgcn_exp2f(sm[w][row].x - m) * sm[w][row].y;
+            }
+            a.part[(pair * a.chunks + chunk) * a.row_cap + row] = make_float2(m, l);
+        }
+    } else {
+        // ---- sums over the 16 rows' lanes; lane 16 g4 + b has the wave's block b
+        const int first = a.first ? a.first[s] : 0, begin = a.begin ? a.begin[s] : t.c;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int off = 1; off < 16; off <<= 1) sum[b][e] += __shfl_xor(sum[b][e], off);
+            if (c16 == b && id[b] >= 0) {
+                const int64_t at = ((int64_t)id[b] * H + h) * kBlock + 4 * g4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = wkey0 + b * kBlock + 4 * g4 + e;
+                    if (key < first || key >= keys) continue;
+                    const bool fresh = key >= t.c && a.row0 == 0;
+                    a.weights[at + e] = fresh ? sum[b][e] : a.weights[at + e] + sum[b][e];
+                    if (fresh) a.positions[at + e] = begin + (key - t.c);
+                }
+            }
+        }
+    }
+}
+
+// log2 of each row's whole sum.
+__global__ __launch_bounds__(kObThreads) void observe_lse_kernel(ObserveArgs a, int chunk_tokens) {
+    const int h = blockIdx.y, s = blockIdx.z, row = blockIdx.x * kObThreads + threadIdx.x;
+    const Turn t = turn_of(a, s, false);
+    if (row >= t.rows) return;
+    const int64_t pair = (int64_t)s * a.num_kv_heads + h;
+    const int pos = t.c + t.j0 + (a.row0 + row) / a.group, chunks = pos / chunk_tokens + 1;
+    const float2 *p = a.part + pair * a.chunks * a.row_cap + row;
+    float m = kNoMax, l = 0.f;
+    for (int k = 0; k < chunks; ++k) m = fmaxf(m, p[(int64_t)k * a.row_cap].x);
+    for (int k = 0; k < chunks; ++k) {
+        const float2 v = p[(int64_t)k * a.row_cap];
+        l += __builtin_amdgcn_exp2f(v.x - m) * v.y;
+    }
+    // (a row without a key, all of its blocks absent: no weight)
+    a.lse[pair * a.row_cap + row] = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : INFINITY;
+}
+
+template <int D, int KB>
+hipError_t launch_observe_t(ObserveArgs a, int32_t whole_rows, hipStream_t stream) {
+    constexpr int kChunkTokens = kObWaves * KB * kBlock;
+    const dim3 grid((unsigned)a.chunks, (unsigned)a.num_kv_heads, (unsigned)a.num_sessions);
+    for (a.row0 = 0; a.row0 < whole_rows; a.row0 += a.row_cap) {
+        hipLaunchKernelGGL((observe_kernel<D, KB, false>), grid, dim3(kObThreads), 0, stream, a);
+        if (hipError_t e = hipGetLastError()) return e;
+        hipLaunchKernelGGL(observe_lse_kernel, dim3((unsigned)((a.row_cap + kObThreads - 1) / kObThreads), grid.y, grid.z),
+                           dim3(kObThreads), 0, stream, a, kChunkTokens);
+        if (hipError_t e = hipGetLastError()) return e;
+        hipLaunchKernelGGL((observe_kernel<D, KB, true>), grid, dim3(kObThreads), 0, stream, a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+
+constexpr size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads, int32_t max_new_len, int32_t rows,
+                         int32_t max_blocks) {
+    const int64_t G = num_q_heads / p.num_kv_heads, pairs = (int64_t)num_sessions * p.num_kv_heads;
+    const int64_t cus = p.num_cus > 0 ? p.num_cus : 256;
+    ObservePlan o;
+    o.whole_rows = (int32_t)(std::min<int64_t>(rows, max_new_len) * G);
+    o.row_cap = std::min(o.whole_rows, kObRows);
+    // Blocks per wave: as many as leave every CU two workgroups.
+    o.blocks = 8;
+    while (o.blocks > 1 && pairs * ((max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks)) < 2 * cus) o.blocks /= 2;
+    o.chunks = (max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks);
+    o.lse_at = align256((size_t)pairs * (size_t)o.chunks * (size_t)o.row_cap * sizeof(float2));
+    o.total = o.lse_at + align256((size_t)pairs * (size_t)o.row_cap * sizeof(float));
+    return o;
+}
+
+hipError_t launch_observe(const PoolGeom &p, int layer, int32_t num_sessions, int32_t num_q_heads, const ObserveCall &c,
+                          const ObservePlan &plan, unsigned int *err, hipStream_t stream) {
+    uint8_t *ws = static_cast<uint8_t *>(c.workspace);
+    const int64_t entries = (int64_t)layer * p.num_blocks * p.num_kv_heads * kBlock;
+    ObserveArgs a = {};
+    a.pool = p.layer_base(layer);
+    a.num_blocks = p.num_blocks;
+    a.num_kv_heads = p.num_kv_heads;
+    a.group = num_q_heads / p.num_kv_heads;
+    a.q = c.q;
+    a.cu = c.cu_new_lens;
+    a.reused = c.reused_lens;
+    a.num_sessions = num_sessions;
+    a.total = c.total_new_tokens;
+    a.max_new = c.max_new_len;
+    a.tables = c.block_tables;
+    a.max_blocks = c.max_blocks;
+    a.rows = c.rows;
+    a.scale_log2 = c.scale * 1.4426950408889634f;
+    a.row_cap = plan.row_cap;
+    a.chunks = plan.chunks;
+    a.part = reinterpret_cast<float2 *>(ws);
+    a.lse = reinterpret_cast<float *>(ws + plan.lse_at);
+    a.weights = c.weights + entries;
+    a.positions = c.positions + entries;
+    a.begin = c.first_positions;
+    a.first = c.first_lens;
+    a.err = err;
+#define LS_OBSERVE(D) \
+    (plan.blocks == 8   ? launch_observe_t<D, 8>(a, plan.whole_rows, stream) \
+     : plan.blocks == 4 ? launch_observe_t<D, 4>(a, plan.whole_rows, stream) \
+     : plan.blocks == 2 ? launch_observe_t<D, 2>(a, plan.whole_rows, stream) \
+                        : launch_observe_t<D, 1>(a, plan.whole_rows, stream))
+    return p.head_dim == 128 ? LS_OBSERVE(128) : LS_OBSERVE(64);
+#undef LS_OBSERVE
+}
+
+}  // namespace ls

@@ -57,6 +57,20 @@ _lib.paged_attn_prefill_window.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _p,
 _lib.kv_tables_update.argtypes = [_p, _i32, _p, _p, _p, _i32, _p, _i32, _p, _p, _i32, _i32, _i32, _i32,
                                   _p, _p, _p, _p, _p]
 _lib.kv_append.argtypes = [_p, _i32, _i32, _p, _p, _i64, _i64, _p, _p, _p]
+_lib.ls_decode_shared_workspace_bytes.argtypes = [_p, _i32, _i32, _i32, _i32]
+_lib.ls_decode_weights_workspace_bytes.argtypes = [_p, _i32, _i32, _i32, _i32]
+_lib.ls_weights_prefill_workspace_bytes.argtypes = [_p, _i32, _i32, _i32, _i32, _i32, _i32]
+for _f in (_lib.ls_decode_shared_workspace_bytes, _lib.ls_decode_weights_workspace_bytes,
+           _lib.ls_weights_prefill_workspace_bytes):
+    _f.restype = _sz
+_lib.paged_attn_decode_shared.argtypes = [_p, _i32, _i32, _i32, _p, _p, _i32, _p, _i32, _p, _i32, _p, _p, _f32, _p,
+                                          _p, _sz, _p]
+_lib.paged_attn_decode_weights.argtypes = [_p, _i32, _i32, _i32, _p, _p, _i32, _p, _p, _p, _p, _i32, _p, _i32, _p, _p,
+                                           _f32, _p, _p, _p, _p, _sz, _p]
+_lib.kv_weights_prefill.argtypes = [_p, _i32, _i32, _i32, _p, _p, _p, _i32, _i32, _p, _i32, _i32, _p, _p, _f32, _p, _p,
+                                    _p, _sz, _p]
+_lib.kv_evict.argtypes = [_p, _i32, _i32, _i32, _p, _p, _i32, _i32, _i32, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _i32,
+                          _p, _p, _p]
 _f64 = ctypes.c_double
 _lib.kv_blocks_stash.argtypes = [_p, _i32, _p, _p, _p, _sz, _i32, _p, _sz, _f64, _p]
 _lib.kv_blocks_restore.argtypes = [_p, _i32, _p, _p, _p, _sz, _i32, _p, _sz, _f64, _p]
@@ -68,13 +82,15 @@ _lib.ls_version.restype = ctypes.c_char_p
 for _f in (_lib.kv_pool_create, _lib.kv_pool_destroy, _lib.paged_attn_decode,
            _lib.paged_attn_decode_static,
            _lib.paged_attn_prefill, _lib.paged_attn_decode_window, _lib.paged_attn_prefill_window,
-           _lib.kv_tables_update, _lib.kv_append, _lib.kv_blocks_stash, _lib.kv_blocks_restore,
+           _lib.kv_tables_update, _lib.kv_append, _lib.paged_attn_decode_shared,
+           _lib.paged_attn_decode_weights, _lib.kv_weights_prefill, _lib.kv_evict, _lib.kv_blocks_stash, _lib.kv_blocks_restore,
            _lib.kv_blocks_restore_layers,
            _lib.ls_device_errors):
     _f.restype = ctypes.c_int
 
 LS_OK, LS_EINVAL, LS_ENOMEM, LS_EHIP, LS_EUNSUPPORTED = 0, -22, -12, -5, -95
 LS_DEVERR_BLOCK_ID, LS_DEVERR_LENGTH, LS_DEVERR_INTERNAL, LS_DEVERR_FREE_LIST = 0x1, 0x2, 0x4, 0x8
+LS_DEVERR_GROUP = 0x10
 PREFILL_COUNTER_BYTES = 256            # LS_PREFILL_COUNTER_BYTES
 PREFILL_WORKSPACE_BYTES = 68157696     # LS_PREFILL_WORKSPACE_BYTES
 
@@ -138,6 +154,7 @@ def _stream(stream):
 
 _BF16 = (torch.bfloat16, torch.int16)
 _I32 = (torch.int32,)
+_F32 = (torch.float32,)
 
 
 def _fits(t: torch.Tensor, shape, dtypes, dev=None) -> bool:
@@ -498,6 +515,172 @@ def kv_append(pool: KVPool, layer: int, k_new: torch.Tensor, v_new: torch.Tensor
                           None if keep is None else keep.__array_interface__["data"][0], _stream(stream)),
            "kv_append")
     del keep
+
+
+def decode_shared_workspace_bytes(pool: KVPool, num_sessions: int, num_q_heads: int, num_groups: int,
+                                  num_members: int) -> int:
+    return int(_lib.ls_decode_shared_workspace_bytes(pool.handle, num_sessions, num_q_heads, num_groups, num_members))
+
+
+def _group_args(group_starts, group_members, prefix_blocks, dev):
+    """(groups, members) of the three arrays of prefix groups, or of none (raises ValueError)."""
+    if group_starts is None and group_members is None and prefix_blocks is None:
+        return 0, 0
+    if group_starts is None or group_members is None or prefix_blocks is None:
+        raise ValueError("group_starts, group_members and prefix_blocks must all be given, or none")
+    n = prefix_blocks.shape[0] if prefix_blocks.dim() == 1 else -1
+    _vector(prefix_blocks, "prefix_blocks", n, _I32, dev)
+    _vector(group_starts, "group_starts", n + 1, _I32, dev)
+    _vector(group_members, "group_members", None, _I32, dev)
+    return n, group_members.shape[0]
+
+
+def _workspace(t: torch.Tensor, dev):
+    if not (t.get_device() == dev and t.is_contiguous()):
+        _dev(t, "workspace", dev=dev)
+
+
+def _entry_args(pool: KVPool, weights, positions, names=("weights", "positions")):
+    """weights fp32 and positions int32 [layers][blocks][Hkv][16] (raises ValueError)."""
+    shape, dev = (pool.num_layers, pool.num_blocks, pool.num_kv_heads, pool.block_size), pool.device
+    for t, name, dtypes in ((weights, names[0], _F32), (positions, names[1], _I32)):
+        if t is not None and not _fits(t, shape, dtypes, dev):
+            _shape(t, name, shape, dtypes)
+            _dev(t, name, dev=dev)
+
+
+def paged_attn_decode_shared(pool: KVPool, layer: int, q: torch.Tensor, block_tables: torch.Tensor,
+                             context_lens: torch.Tensor, group_starts: Optional[torch.Tensor],
+                             group_members: Optional[torch.Tensor], prefix_blocks: Optional[torch.Tensor],
+                             scale: float, out: torch.Tensor, workspace: torch.Tensor, stream=None) -> torch.Tensor:
+    """paged_attn_decode in which the sessions group_members[group_starts[g]:group_starts[g + 1]] (int32)
+    have the first prefix_blocks[g] blocks of their tables in common, read once for the group;
+    workspace of decode_shared_workspace_bytes.  A length of 0 gives a row of zeros."""
+    if q.dim() != 3:
+        raise ValueError("q must be [S][Hq][D]")
+    s, hq = q.shape[0], q.shape[1]
+    _decode_args(s, hq, pool.num_kv_heads, pool.head_dim, q, out, block_tables, context_lens, None, None, pool.device)
+    groups, members = _group_args(group_starts, group_members, prefix_blocks, pool.device)
+    _workspace(workspace, pool.device)
+    _check(_lib.paged_attn_decode_shared(pool.handle, layer, s, hq, q.data_ptr(), block_tables.data_ptr(),
+                                         block_tables.shape[1], context_lens.data_ptr(), groups, _ptr(group_starts),
+                                         members, _ptr(group_members), _ptr(prefix_blocks), float(scale),
+                                         out.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream(stream)),
+           "paged_attn_decode_shared")
+    return out
+
+
+def decode_weights_workspace_bytes(pool: KVPool, num_sessions: int, num_q_heads: int, num_groups: int = 0,
+                                   num_members: int = 0) -> int:
+    return int(_lib.ls_decode_weights_workspace_bytes(pool.handle, num_sessions, num_q_heads, num_groups, num_members))
+
+
+def paged_attn_decode_weights(pool: KVPool, layer: int, q: torch.Tensor, block_tables: torch.Tensor,
+                              context_lens: torch.Tensor, scale: float, out: torch.Tensor, weights: torch.Tensor,
+                              positions: Optional[torch.Tensor], workspace: torch.Tensor,
+                              reused_lens: Optional[torch.Tensor] = None,
+                              first_positions: Optional[torch.Tensor] = None,
+                              first_lens: Optional[torch.Tensor] = None,
+                              group_starts: Optional[torch.Tensor] = None,
+                              group_members: Optional[torch.Tensor] = None,
+                              prefix_blocks: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """paged_attn_decode_shared that also adds each key's probability, summed over the query heads of its
+    KV head, to weights fp32 [layers][blocks][Hkv][16]; of keys t >= reused_lens[s] the weight is set,
+    and positions (int32, the same shape) to first_positions[s] + t - reused_lens[s].  Keys below
+    first_lens[s] get no weight.  workspace of decode_weights_workspace_bytes."""
+    if q.dim() != 3:
+        raise ValueError("q must be [S][Hq][D]")
+    s, hq = q.shape[0], q.shape[1]
+    _decode_args(s, hq, pool.num_kv_heads, pool.head_dim, q, out, block_tables, context_lens, None, None, pool.device)
+    _entry_args(pool, weights, positions)
+    for t, name in ((reused_lens, "reused_lens"), (first_positions, "first_positions"), (first_lens, "first_lens")):
+        if t is not None:
+            _vector(t, name, s, _I32, pool.device)
+    groups, members = _group_args(group_starts, group_members, prefix_blocks, pool.device)
+    _workspace(workspace, pool.device)
+    _check(_lib.paged_attn_decode_weights(pool.handle, layer, s, hq, q.data_ptr(), block_tables.data_ptr(),
+                                          block_tables.shape[1], context_lens.data_ptr(), _ptr(reused_lens),
+                                          _ptr(first_positions), _ptr(first_lens), groups, _ptr(group_starts), members,
+                                          _ptr(group_members), _ptr(prefix_blocks), float(scale), out.data_ptr(),
+                                          weights.data_ptr(), _ptr(positions), workspace.data_ptr(),
+                                          _nbytes(workspace), _stream(stream)),
+           "paged_attn_decode_weights")
+    return out
+
+
+def weights_prefill_workspace_bytes(pool: KVPool, num_sessions: int, num_q_heads: int, total_new_tokens: int,
+                                    max_new_len: int, rows: int, max_blocks_per_session: int) -> int:
+    return int(_lib.ls_weights_prefill_workspace_bytes(pool.handle, num_sessions, num_q_heads, total_new_tokens,
+                                                       max_new_len, rows, max_blocks_per_session))
+
+
+def kv_weights_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: torch.Tensor,
+                       reused_lens: torch.Tensor, max_new_len: int, block_tables: torch.Tensor, rows: int,
+                       scale: float, weights: torch.Tensor, positions: torch.Tensor, workspace: torch.Tensor,
+                       first_positions: Optional[torch.Tensor] = None, first_lens: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """Adds what the last `rows` tokens of each turn (q [T][Hq][D], K already in the pool) give to the
+    session's keys to weights, as paged_attn_decode_weights; workspace of weights_prefill_workspace_bytes."""
+    if q.dim() != 3:
+        raise ValueError("q must be [T][Hq][D]")
+    total, hq, dev = q.shape[0], q.shape[1], pool.device
+    s = reused_lens.shape[0] if reused_lens.dim() == 1 else -1
+    if not _fits(q, (total, hq, pool.head_dim), _BF16, dev):
+        _shape(q, "q", (total, hq, pool.head_dim), _BF16)
+        _dev(q, "q", dev=dev)
+    for t, name, n in ((reused_lens, "reused_lens", s), (cu_new_lens, "cu_new_lens", s + 1),
+                       (first_positions, "first_positions", s), (first_lens, "first_lens", s)):
+        if t is not None:
+            _vector(t, name, n, _I32, dev)
+    if not (block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32, dev)):
+        _shape(block_tables, "block_tables", (s, None), torch.int32)
+        _dev(block_tables, "block_tables", dev=dev)
+    _entry_args(pool, weights, positions)
+    _workspace(workspace, dev)
+    _check(_lib.kv_weights_prefill(pool.handle, layer, s, hq, q.data_ptr(), cu_new_lens.data_ptr(),
+                                   reused_lens.data_ptr(), total, int(max_new_len), block_tables.data_ptr(),
+                                   block_tables.shape[1], rows, _ptr(first_positions), _ptr(first_lens), float(scale),
+                                   weights.data_ptr(), positions.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
+                                   _stream(stream)),
+           "kv_weights_prefill")
+    return weights
+
+
+def kv_evict(pool: KVPool, seq_lens: torch.Tensor, block_tables: torch.Tensor, budget: int, limit: int, recent: int,
+             next_positions: torch.Tensor, weights: torch.Tensor, positions: torch.Tensor, next_lens: torch.Tensor,
+             weights_next: Optional[torch.Tensor] = None, positions_next: Optional[torch.Tensor] = None,
+             first_lens: Optional[torch.Tensor] = None, layer_begin: int = 0, layer_count: Optional[int] = None,
+             free_ring: Optional[torch.Tensor] = None, free_counts: Optional[torch.Tensor] = None,
+             next_counts: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Cuts sessions of more than `limit` tokens to `budget` in every layer (default: all) and KV head: the
+    first first_lens[s] slots, positions >= next_positions[s] - recent, then the largest weights stay.
+    Writes next_lens int32 [S]; weights_next and positions_next (None: in place) get the entries; free_ring
+    int32 [R] with free_counts -> next_counts int64 [2] takes the blocks back."""
+    s = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
+    dev = pool.device
+    for t, name, n in ((seq_lens, "seq_lens", s), (next_positions, "next_positions", s), (next_lens, "next_lens", s),
+                       (first_lens, "first_lens", s), (free_ring, "free_ring", None)):
+        if t is not None:
+            _vector(t, name, n, _I32, dev)
+    for t, name in ((free_counts, "free_counts"), (next_counts, "next_counts")):
+        if t is not None:
+            _vector(t, name, 2, _I64, dev)
+    if not (block_tables.dim() == 2 and _fits(block_tables, (s, block_tables.shape[1]), _I32, dev)):
+        _shape(block_tables, "block_tables", (s, None), torch.int32)
+        _dev(block_tables, "block_tables", dev=dev)
+    weights_next = weights if weights_next is None else weights_next
+    positions_next = positions if positions_next is None else positions_next
+    _entry_args(pool, weights, positions)
+    _entry_args(pool, weights_next, positions_next, ("weights_next", "positions_next"))
+    if layer_count is None:
+        layer_count = pool.num_layers - layer_begin
+    _check(_lib.kv_evict(pool.handle, layer_begin, layer_count, s, seq_lens.data_ptr(), block_tables.data_ptr(),
+                         block_tables.shape[1], budget, limit, recent, _ptr(first_lens), next_positions.data_ptr(),
+                         weights.data_ptr(), positions.data_ptr(), weights_next.data_ptr(), positions_next.data_ptr(),
+                         next_lens.data_ptr(), _ptr(free_ring), 0 if free_ring is None else free_ring.shape[0],
+                         _ptr(free_counts), _ptr(next_counts), _stream(stream)),
+           "kv_evict")
+    return next_lens
 
 
 def _host_ids(ids):
