@@ -581,8 +581,8 @@ ls_status kv_weights_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
  * free_counts and nothing moves.  Tokens of a block whose id is outside the pool rank
  * lowest and are not moved (LS_DEVERR_BLOCK_ID).  Apart from shared blocks below
  * first_lens, no block is in two sessions' tables.  Errors: LS_EINVAL (also arrays that
- * overlap and are not said to be the same), LS_EUNSUPPORTED (more than 65535 layers, KV
- * heads), LS_EHIP.
+ * overlap and are not said to be the same), LS_EUNSUPPORTED (more than 16384 blocks per
+ * session, 2^20 sessions, 65535 layers or KV heads), LS_EHIP.
  */
 ls_status kv_evict(ls_kv_pool *pool, int32_t layer_begin, int32_t layer_count, int32_t num_sessions,
                    const int32_t *seq_lens, const int32_t *block_tables, int32_t max_blocks_per_session, int32_t budget,

@@ -858,8 +858,7 @@ ls_status kv_evict(ls_kv_pool *pool, int32_t layer_begin, int32_t layer_count, i
     if (layer_begin < 0 || layer_count < 1 || layer_begin > p.num_layers - layer_count)
         return fail(LS_EINVAL, "layer range [%d, %d + %d) outside [0, %d)", layer_begin, layer_begin, layer_count, p.num_layers);
     if (num_sessions < 0) return fail(LS_EINVAL, "num_sessions must be >= 0");
-    if (max_blocks_per_session <= 0 || max_blocks_per_session > INT32_MAX / kBlock)
-        return fail(LS_EINVAL, "max_blocks_per_session (%d) must be in [1, %d]", max_blocks_per_session, INT32_MAX / kBlock);
+    if (max_blocks_per_session <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
     if (budget < 1 || limit < budget || recent < 0 || recent > budget)
         return fail(LS_EINVAL, "budget (%d) must be in [1, limit (%d)] and recent (%d) in [0, budget]", budget, limit, recent);
     if (free_ring ? ring_size < 1 || !free_counts || !next_counts : ring_size || free_counts || next_counts)
@@ -870,8 +869,9 @@ ls_status kv_evict(ls_kv_pool *pool, int32_t layer_begin, int32_t layer_count, i
                     "next_lens must not be NULL");
     if ((weights_next == weights) != (positions_next == positions))
         return fail(LS_EINVAL, "weights_next and positions_next are both the arrays before, or both apart");
-    if (layer_count > 65535 || p.num_kv_heads > 65535)
-        return fail(LS_EUNSUPPORTED, "at most 65535 layers a call and 65535 KV heads");
+    if (layer_count > 65535 || p.num_kv_heads > 65535 || max_blocks_per_session > kMaxCacheBlocks || num_sessions > kMaxEvictSessions)
+        return fail(LS_EUNSUPPORTED, "at most 65535 layers a call and 65535 KV heads, %d sessions and %d blocks per session",
+                    kMaxEvictSessions, kMaxCacheBlocks);
     // Arrays that are written are memory of their own, but for those that advance in place.
     struct Range {
         const void *at;

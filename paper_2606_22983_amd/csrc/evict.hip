@@ -15,14 +15,18 @@ namespace ls {
 
 namespace {
 
-constexpr int kEvThreads = 256;
-constexpr int kEvWaves = kEvThreads / kWave;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kEvMoves = 2048;               // moves at a time (LDS)
-// Tokens whose ranking keys are kept in LDS (a longer session's are computed again for
-// each pass): caches around a budget of 2048, and long prompts.
-constexpr int kEvKeysShort = 2304, kEvKeysLong = 16384;
-constexpr int kBins = 256;                   // of a ranking key's 8 bits
+// Slots whose ranking keys are kept in LDS (a longer session's are computed again for
+// each pass): caches around a budget of a few thousand tokens, and long prompts.
+constexpr int kEvKeysShort = 4096, kEvKeysLong = 16384;
+constexpr int kBins = 2048;                  // of a ranking key's 11 bits
+static_assert(kMaxCacheBlocks * kBlock <= kEvKeysLong * 32, "a bit for each slot where the keys would be");
 constexpr int kPlanThreads = 1024;
+constexpr int kEvSlices = 8;
 
 struct EvictArgs {
     uint16_t *pool;                // layer base of the first layer
@@ -60,6 +64,8 @@ __device__ __forceinline__ int keeps(const EvictArgs &a, int s, int L) {
 // sessions are served or none.
 __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
     __shared__ unsigned sm_wave[kPlanThreads / kWave];
+    __shared__ unsigned sm_at[kPlanThreads];
+    __shared__ int sm_col[kPlanThreads];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, S = a.num_sessions;
     const int64_t cap = (int64_t)a.max_blocks * kBlock;
     int64_t taken = 0, given = 0;
@@ -114,9 +120,9 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
     for (int s0 = 0; s0 < S; s0 += kPlanThreads) {
         const int s = s0 + tid;
         unsigned n = 0u;
-        int L = 0, m = 0;
+        int m = 0;
         if (s < S) {
-            L = m = a.lens[s];
+            const int L = m = a.lens[s];
             if (!bad) {
                 m = keeps(a, s, L);
                 n = a.ring ? (unsigned)(blocks_of(L) - blocks_of(m)) : 0u;
@@ -124,13 +130,21 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
             a.next_lens[s] = m;
         }
         unsigned all;
-        unsigned at = carry + scan(n, all);
-        for (unsigned i = 0; i < n; ++i, ++at) {
-            const int id = a.tables[(int64_t)s * a.max_blocks + blocks_of(m) + i];
+        sm_at[tid] = scan(n, all);
+        sm_col[tid] = blocks_of(m);
+        __syncthreads();
+        // thread = block that goes back: the last session whose blocks begin at or before it
+        for (unsigned i = tid; i < all; i += kPlanThreads) {
+            int e = 0;
+#pragma unroll
+            for (int step = kPlanThreads / 2; step > 0; step >>= 1)
+                if (sm_at[e + step] <= i) e += step;
+            const int id = a.tables[(int64_t)(s0 + e) * a.max_blocks + sm_col[e] + (i - sm_at[e])];
             if (id < 0 || id >= a.num_blocks) flag_error(a.err, LS_DEVERR_BLOCK_ID);
-            a.ring[(given + at) % a.ring_size] = id;
+            a.ring[(given + carry + i) % a.ring_size] = id;
         }
         carry += all;
+        __syncthreads();
     }
 }
 
@@ -141,16 +155,33 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One (session, KV head, layer) per workgroup.
-template <int D, int kKeys>
-__global__ __launch_bounds__(kEvThreads) void evict_kernel(EvictArgs a) {
-    __shared__ uint32_t sm_key[kKeys];
-    __shared__ uint32_t sm_bin[kBins];
-    __shared__ unsigned sm_wave[2][kEvWaves];
+// Weights and positions of four consecutive slots.
+struct Quad {
+    f32x4 w;
+    i32x4 p;
+};
+
+// One (session, KV head, layer) per workgroup, or one of `slices` that all rank the
+// tokens and share the moves (entries apart: none of them writes what another reads).
+//
+// Ranking keys are words in the order of the weights.  The evict-th smallest is found
+// from its digits of 11, 11 and 10 bits by counting; keys below it go, and of those
+// equal to it the ones in the highest slots.  Then waves go over their contiguous
+// shares of the slots, 256 at a time (a lane has four consecutive ones, 16 bytes of
+// an entry array), and number the holes below m and the tokens that stay behind it.
+template <int D, int kThreads, int kKeys>
+__global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
+    constexpr int kWaves = kThreads / kWave;
+    constexpr int kStep = 4 * kWave;               // slots of a wave's step
+    __shared__ __attribute__((aligned(16))) uint32_t sm_key[kKeys];
+    __shared__ __attribute__((aligned(16))) uint32_t sm_bin[kBins];
+    __shared__ uint64_t sm_flags[kKeys / 64];
+    __shared__ unsigned sm_wave[2][kWaves];
     __shared__ int sm_from[kEvMoves], sm_to[kEvMoves];
     __shared__ uint32_t sm_digit, sm_rest;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int s = blockIdx.x, h = blockIdx.y, la = blockIdx.z, H = a.num_kv_heads;
+    const int slice = blockIdx.x / a.num_sessions, s = blockIdx.x % a.num_sessions, h = blockIdx.y, la = blockIdx.z;
+    const int H = a.num_kv_heads, slices = gridDim.x / a.num_sessions;
     const int32_t *table = a.tables + (int64_t)s * a.max_blocks;
     const int64_t entries = (int64_t)la * a.num_blocks * H * kBlock;
     const float *weights = a.weights + entries;
@@ -160,48 +191,79 @@ __global__ __launch_bounds__(kEvThreads) void evict_kernel(EvictArgs a) {
     const bool apart = a.weights_next != a.weights;
     const int L = (int)min((int64_t)max(a.lens[s], 0), (int64_t)a.max_blocks * kBlock);
     const int m = min(max(a.next_lens[s], 0), L);
-    // Entry of a slot, or -1: its block is not in the pool.
-    auto entry = [&](int t) -> int64_t {
-        const int id = table[t / kBlock];
-        return id < 0 || id >= a.num_blocks ? -1 : ((int64_t)id * H + h) * kBlock + t % kBlock;
-    };
     const bool cut = m < L;
-    if (apart)
-        for (int t = tid; t < m; t += kEvThreads) {
-            const int64_t e = entry(t);
+    if (!cut && (!apart || slice)) return;
+    // First entry of a block, or -1: it is not in the pool.
+    auto block_entry = [&](int col) -> int64_t {
+        const int id = table[col];
+        return id < 0 || id >= a.num_blocks ? -1 : ((int64_t)id * H + h) * kBlock;
+    };
+    auto load = [&](int64_t e) { return Quad{*reinterpret_cast<const f32x4 *>(weights + e), *reinterpret_cast<const i32x4 *>(positions + e)}; };
+    if (!cut) {
+        for (int t = tid * 4; t < L; t += kThreads * 4) {
+            const int64_t e = block_entry(t / kBlock);
             if (e < 0) continue;
-            weights_next[e] = weights[e];
-            positions_next[e] = positions[e];
+            const Quad x = load(e + t % kBlock);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t + i < L) {
+                    weights_next[e + t % kBlock + i] = x.w[i];
+                    positions_next[e + t % kBlock + i] = x.p[i];
+                }
         }
-    if (!cut) return;
+        return;
+    }
     const int first = a.first ? min(max(a.first[s], 0), m) : 0;
     const int64_t late = (int64_t)a.next_pos[s] - a.recent;
-    const int evict = L - m;                       // of the slots [first, L)
-    auto key_at = [&](int t) -> uint32_t {
-        const int64_t e = entry(t);
-        if (e < 0) return 0u;
-        return positions[e] >= late ? 0xFFFFFFFFu : rank_key(weights[e]);
+    // Keys of slots t .. t + 3: the largest for first and latest tokens, 0 for absent ones.
+    auto keys_of = [&](int t, bool &missing) -> u32x4 {
+        const int64_t e = block_entry(t / kBlock);
+        u32x4 k = {0u, 0u, 0u, 0u};
+        if (e < 0) missing = true;
+        else {
+            const Quad x = load(e + t % kBlock);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = x.p[i] >= late ? 0xFFFFFFFFu : rank_key(x.w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t + i < first) k[i] = 0xFFFFFFFFu;
+        return k;
     };
     const bool cached = L <= kKeys;
     bool missing = false;
-    if (cached)
-        for (int t = first + tid; t < L; t += kEvThreads) sm_key[t] = key_at(t);
-    for (int t = tid * kBlock; t < L; t += kEvThreads * kBlock) missing = missing || entry(t) < 0;
-    if (missing && la == 0 && h == 0) flag_error(a.err, LS_DEVERR_BLOCK_ID);
-    __syncthreads();
-    auto key = [&](int t) -> uint32_t { return cached ? sm_key[t] : key_at(t); };
-    // ---- the evict-th smallest key, eight bits at a time
-    uint32_t prefix = 0u, rest = (uint32_t)evict;  // of the keys that begin with prefix, the rest-th smallest
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        sm_bin[tid] = 0u;
+    if (cached) {
+#pragma unroll 4
+        for (int t = tid * 4; t < L; t += kThreads * 4) *reinterpret_cast<u32x4 *>(&sm_key[t]) = keys_of(t, missing);
+    } else {
+        for (int t = tid * kBlock; t < L; t += kThreads * kBlock) missing = missing || block_entry(t / kBlock) < 0;
+    }
+    if (missing && la == 0 && h == 0 && slice == 0) flag_error(a.err, LS_DEVERR_BLOCK_ID);
+    auto keys = [&](int t) -> u32x4 {
+        bool unused;
+        return cached ? *reinterpret_cast<const u32x4 *>(&sm_key[t]) : keys_of(t, unused);
+    };
+    // ---- the evict-th smallest key (a table's slots behind L are no tokens)
+    uint32_t prefix = 0u, rest = (uint32_t)(L - m);    // of the keys that begin with prefix, the rest-th smallest
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass < 2 ? 11 : 10;
+        for (int i = tid; i < kBins; i += kThreads) sm_bin[i] = 0u;
         __syncthreads();
-        for (int t = first + tid; t < L; t += kEvThreads) {
-            const uint32_t k = key(t);
-            if (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&sm_bin[(k >> shift) & 255u], 1u);
+        for (int t = tid * 4; t < L; t += kThreads * 4) {
+            const u32x4 k = keys(t);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t + i < L && (pass == 0 || k[i] >> (shift + bits) == prefix >> (shift + bits)))
+                    atomicAdd(&sm_bin[(k[i] >> shift) & ((1u << bits) - 1u)], 1u);
         }
         __syncthreads();
-        // thread = bin: keys in the bins up to and with its own
-        unsigned x = sm_bin[tid];
+        // A thread has kBins / kThreads bins: the one in which the count passes `rest`.
+        constexpr int kPer = kBins / kThreads;
+        unsigned own[kPer], x = 0u;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x += own[i] = sm_bin[tid * kPer + i];
+        const unsigned mine = x;
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
             const unsigned y = __shfl_up(x, off);
@@ -209,86 +271,154 @@ __global__ __launch_bounds__(kEvThreads) void evict_kernel(EvictArgs a) {
         }
         if (lane == kWave - 1) sm_wave[0][wave] = x;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) x += sm_wave[0][w];
-        const unsigned before = x - sm_bin[tid];
-        if (before < rest && rest <= x) {
-            sm_digit = (uint32_t)tid;
-            sm_rest = rest - before;
+        unsigned before = x - mine;
+        for (int w = 0; w < wave; ++w) before += sm_wave[0][w];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (before < rest && rest <= before + own[i]) {
+                sm_digit = (uint32_t)(tid * kPer + i);
+                sm_rest = rest - before;
+            }
+            before += own[i];
         }
         __syncthreads();
         prefix |= sm_digit << shift;
         rest = sm_rest;
     }
-    // Keys below `prefix` go, and of those equal to it the `rest` in the highest slots.
-    const int per = (L - first + kEvThreads - 1) / kEvThreads;
-    const int t0 = min(first + tid * per, L), t1 = min(t0 + per, L);
-    auto scan = [&](unsigned v, int which, unsigned &total) {
-        unsigned x = v;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const unsigned y = __shfl_up(x, off);
-            if (lane >= off) x += y;
-        }
-        if (lane == kWave - 1) sm_wave[which][wave] = x;
+    // ---- numbers of ties, holes and moving tokens
+    const int steps = (L + kStep - 1) / kStep, per = (steps + kWaves - 1) / kWaves;
+    const int t_begin = min(wave * per, steps) * kStep, t_end = min((wave + 1) * per, steps) * kStep;
+    const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;           // lanes before this one
+    // Sums of a wave's value over the waves before, and over all.
+    auto wave_sums = [&](unsigned v, int which, unsigned &all) {
+        if (lane == 0) sm_wave[which][wave] = v;
         __syncthreads();
         unsigned before = 0u;
-        total = 0u;
-        for (int w = 0; w < kEvWaves; ++w) {
-            if (w == wave) before = total;
-            total += sm_wave[which][w];
+        all = 0u;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w == wave) before = all;
+            all += sm_wave[which][w];
         }
-        return before + x - v;
+        return before;
     };
     unsigned ties = 0u, all_ties;
-    for (int t = t0; t < t1; ++t) ties += key(t) == prefix;
-    const unsigned ties_before = scan(ties, 0, all_ties);
-    const unsigned ties_stay = all_ties - rest;
-    auto stays = [&](uint32_t k, unsigned &seen) {  // in the order of the slots
-        const bool tie = k == prefix, yes = k > prefix || (tie && seen < ties_stay);
-        seen += tie;
-        return yes;
+    for (int t0 = t_begin; t0 < t_end; t0 += kStep) {
+        const int t = t0 + lane * 4;
+        const u32x4 k = t < L ? keys(t) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ties += __popcll(__ballot(t + i < L && k[i] == prefix));
+    }
+    const unsigned ties_before = wave_sums(ties, 1, all_ties), ties_stay = all_ties - rest;
+    // Which of the lane's four tokens stay; seen: ties before the step, and after it.
+    auto stays = [&](int t, const u32x4 &k, unsigned &seen, bool (&yes)[4]) {
+        unsigned mine = seen;                       // ties before the lane's first slot
+        uint64_t tie[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            tie[i] = __ballot(t + i < L && k[i] == prefix);
+            mine += __popcll(tie[i] & below);
+            seen += __popcll(tie[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            yes[i] = t + i < L && (k[i] > prefix || (k[i] == prefix && mine < ties_stay));
+            mine += (tie[i] >> lane) & 1u;
+        }
     };
-    // Of the thread's slots those below m, and those behind it.
-    const int h1 = max(min(t1, m), t0), u0 = min(max(t0, m), t1);
+    // A bit for each slot whose token stays: four words a step, bit = lane.  Without keys in
+    // LDS they take the keys' place; moves in place change what keys are computed from.
+    uint64_t *flags = cached ? sm_flags : reinterpret_cast<uint64_t *>(sm_key);
     unsigned seen = ties_before, holes = 0u, movers = 0u, all_holes, all_movers;
-    for (int t = t0; t < h1; ++t) holes += !stays(key(t), seen);
-    const unsigned mover_seen0 = seen;
-    for (int t = u0; t < t1; ++t) movers += stays(key(t), seen);
+    for (int t0 = t_begin; t0 < t_end; t0 += kStep) {
+        const int t = t0 + lane * 4;
+        bool yes[4];
+        const u32x4 k = t < L ? keys(t) : u32x4{0u, 0u, 0u, 0u};
+        stays(t, k, seen, yes);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            holes += __popcll(__ballot(t + i < m && !yes[i]));
+            movers += __popcll(__ballot(t + i >= m && yes[i]));
+            const uint64_t f = __ballot(yes[i]);
+            if (lane == 0) flags[t0 / 64 + i] = f;
+        }
+    }
     __syncthreads();
-    unsigned i = scan(holes, 0, all_holes), j = scan(movers, 1, all_movers);
-    // ---- the moves.  A batch writes weights in place, which keys that are not in LDS are
-    // computed from: a thread goes on behind its last hole, in slots not yet written.
+    unsigned hole0 = wave_sums(holes, 0, all_holes), mover0 = wave_sums(movers, 1, all_movers);
+    // (all_holes = all_movers, since m tokens stay)
+    if (apart && slice == 0)
+        for (int t = tid * 4; t < m; t += kThreads * 4) {
+            const int64_t e = block_entry(t / kBlock);
+            if (e < 0) continue;
+            const Quad x = load(e + t % kBlock);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t + i < m && (flags[t / kStep * 4 + i] >> (t % kStep / 4)) & 1u) {
+                    weights_next[e + t % kBlock + i] = x.w[i];
+                    positions_next[e + t % kBlock + i] = x.p[i];
+                }
+        }
+    // ---- the moves, a batch at a time
+    const unsigned share = (all_movers + slices - 1) / slices, last = min((slice + 1) * share, all_movers);
     constexpr int kLanes = D / 8;                  // of a move: 16 bytes of K and 8 dims of V each
-    unsigned hole_seen = ties_before, mover_seen = mover_seen0;
-    int th = t0, tu = u0;
-    for (unsigned base = 0u; base < all_movers; base += kEvMoves) {
+    for (unsigned base = slice * share; base < last; base += kEvMoves) {
+        const unsigned n = min(last - base, (unsigned)kEvMoves);
+        __syncthreads();                           // the batch before has been read
+        unsigned hole = hole0, mover = mover0;
+        for (int t0 = t_begin; t0 < t_end; t0 += kStep) {
+            const int t = t0 + lane * 4;
+            uint64_t f[4], go[4], come[4];
+            unsigned i_hole = hole, i_mover = mover;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f[i] = flags[t0 / 64 + i];
+                const bool yes = (f[i] >> lane) & 1u;
+                come[i] = __ballot(t + i < m && !yes);
+                go[i] = __ballot(t + i >= m && yes);
+                i_hole += __popcll(come[i] & below);
+                i_mover += __popcll(go[i] & below);
+                hole += __popcll(come[i]);
+                mover += __popcll(go[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if ((come[i] >> lane) & 1u) {
+                    if (i_hole - base < n) sm_to[i_hole - base] = t + i;
+                    ++i_hole;
+                }
+                if ((go[i] >> lane) & 1u) {
+                    if (i_mover - base < n) sm_from[i_mover - base] = t + i;
+                    ++i_mover;
+                }
+            }
+        }
         __syncthreads();
-        for (const unsigned end = base + kEvMoves; th < h1 && i < end; ++th)
-            if (!stays(key(th), hole_seen)) sm_to[i++ - base] = th;
-        for (const unsigned end = base + kEvMoves; tu < t1 && j < end; ++tu)
-            if (stays(key(tu), mover_seen)) sm_from[j++ - base] = tu;
-        __syncthreads();
-        const int n = (int)min(all_movers - base, (unsigned)kEvMoves);
-        for (int x = tid / kLanes; x < n; x += kEvThreads / kLanes) {
-            const int64_t from = entry(sm_from[x]), to = entry(sm_to[x]);
-            if (from < 0 || to < 0) continue;
-            const int c = tid % kLanes;
-            // entry = (block Hkv + h) 16 + slot; a block has 2 Hkv tiles
-            const int64_t fb = from / kBlock / H, tb = to / kBlock / H;
-            const int fo = (int)(from % kBlock), to_o = (int)(to % kBlock);
-            uint16_t *slab = a.pool + (int64_t)la * a.num_blocks * 2 * H * (kBlock * D);
-            const uint16_t *fk = slab + (fb * 2 * H + h) * (int64_t)(kBlock * D), *fv = fk + (int64_t)H * (kBlock * D);
-            uint16_t *tk = slab + (tb * 2 * H + h) * (int64_t)(kBlock * D), *tv = tk + (int64_t)H * (kBlock * D);
-            const uint4 kv = *reinterpret_cast<const uint4 *>(fk + (c * kBlock + fo) * 8);
+        const int c = tid % kLanes;
+        uint16_t *slab = a.pool + (int64_t)la * a.num_blocks * 2 * H * (kBlock * D);
+#pragma unroll 2
+        for (unsigned x = tid / kLanes; x < n; x += kThreads / kLanes) {
+            const int from = sm_from[x], to = sm_to[x], fo = from % kBlock, too = to % kBlock;
+            const int fb = table[from / kBlock], tb = table[to / kBlock];
+            if (fb < 0 || fb >= a.num_blocks || tb < 0 || tb >= a.num_blocks) continue;
+            const uint16_t *fk = slab + ((int64_t)fb * 2 * H + h) * (kBlock * D), *fv = fk + (int64_t)H * (kBlock * D);
+            uint16_t *tk = slab + ((int64_t)tb * 2 * H + h) * (kBlock * D), *tv = tk + (int64_t)H * (kBlock * D);
+            const u32x4 kv = *reinterpret_cast<const u32x4 *>(fk + (c * kBlock + fo) * 8);
             uint16_t v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = fv[(c * 8 + e) * kBlock + fo];
-            *reinterpret_cast<uint4 *>(tk + (c * kBlock + to_o) * 8) = kv;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) tv[(c * 8 + e) * kBlock + to_o] = v[e];
+            const int64_t ef = ((int64_t)fb * H + h) * kBlock + fo, et = ((int64_t)tb * H + h) * kBlock + too;
+            float w = 0.f;
+            int p = 0;
             if (c == 0) {
-                weights_next[to] = weights[from];
-                positions_next[to] = positions[from];
+                w = weights[ef];
+                p = positions[ef];
+            }
+            *reinterpret_cast<u32x4 *>(tk + (c * kBlock + too) * 8) = kv;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tv[(c * 8 + e) * kBlock + too] = v[e];
+            if (c == 0) {
+                weights_next[et] = w;
+                positions_next[et] = p;
             }
         }
     }
@@ -325,15 +455,19 @@ hipError_t launch_evict(const PoolGeom &p, int32_t layer_begin, int32_t layer_co
     hipLaunchKernelGGL(evict_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (!c.num_sessions) return hipSuccess;
-    const dim3 grid((unsigned)c.num_sessions, (unsigned)p.num_kv_heads, (unsigned)layer_count);
+    // With entries apart, and workgroups for a part of the CUs only, several share a (session, KV head,
+    // layer)'s moves.
+    const int64_t whole = (int64_t)c.num_sessions * p.num_kv_heads * layer_count, cus = stream_cus(p, stream);
+    const int slices = c.weights_next != c.weights ? (int)std::max<int64_t>(1, std::min<int64_t>(kEvSlices, 2 * cus / whole)) : 1;
+    const dim3 grid((unsigned)(c.num_sessions * slices), (unsigned)p.num_kv_heads, (unsigned)layer_count);
     const bool narrow = (int64_t)c.max_blocks * kBlock <= kEvKeysShort;
-#define LS_EVICT(D, KEYS) hipLaunchKernelGGL((evict_kernel<D, KEYS>), grid, dim3(kEvThreads), 0, stream, a)
+#define LS_EVICT(D, THREADS, KEYS) hipLaunchKernelGGL((evict_kernel<D, THREADS, KEYS>), grid, dim3(THREADS), 0, stream, a)
     if (p.head_dim == 128) {
-        if (narrow) LS_EVICT(128, kEvKeysShort);
-        else LS_EVICT(128, kEvKeysLong);
+        if (narrow) LS_EVICT(128, 512, kEvKeysShort);
+        else LS_EVICT(128, 1024, kEvKeysLong);
     } else {
-        if (narrow) LS_EVICT(64, kEvKeysShort);
-        else LS_EVICT(64, kEvKeysLong);
+        if (narrow) LS_EVICT(64, 512, kEvKeysShort);
+        else LS_EVICT(64, 1024, kEvKeysLong);
     }
 #undef LS_EVICT
     return hipGetLastError();

@@ -124,7 +124,7 @@ def evict(lib, pool, **kw):  # noqa: F811
 
 
 @pytest.mark.parametrize("kw", [
-    dict(lb=-1), dict(lb=1), dict(lc=0), dict(lc=3), dict(lb=2, lc=1), dict(S=-1), dict(maxb=0), dict(maxb=1 << 27), dict(budget=0),
+    dict(lb=-1), dict(lb=1), dict(lc=0), dict(lc=3), dict(lb=2, lc=1), dict(S=-1), dict(maxb=0), dict(maxb=-7), dict(budget=0),
     dict(limit=49), dict(recent=-1), dict(recent=51), dict(lens=None), dict(bt=None), dict(nextp=None), dict(w=None), dict(pos=None),
     dict(wn=None), dict(pn=None), dict(nextl=None), dict(ring=None), dict(size=0), dict(counts=None), dict(after=None),
     dict(ring=None, size=0), dict(wn=W0), dict(pn=P0), dict(w=W0 + 4), dict(pn=P1 + 8), dict(lens=F + 2), dict(counts=F + 0x404),
@@ -134,6 +134,11 @@ def evict(lib, pool, **kw):  # noqa: F811
 ])
 def test_evict_rejects(lib, pool, kw):  # noqa: F811
     assert evict(lib, pool, **kw) == LS_EINVAL
+
+
+def test_evict_limits(lib, pool):  # noqa: F811
+    assert evict(lib, pool, maxb=16385, bt=F + 0x10000000) == LS_EUNSUPPORTED
+    assert evict(lib, pool, S=(1 << 20) + 1) == LS_EUNSUPPORTED
 
 
 def test_evict_takes_arrays_in_place_and_no_ring(lib, pool):  # noqa: F811
