@@ -19,11 +19,11 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kEvMoves = 2048;               // moves at a time (LDS)
 // Slots whose ranking keys are kept in LDS (a longer session's are computed again for
 // each pass): caches around a budget of a few thousand tokens, and long prompts.
-constexpr int kEvKeysShort = 4096, kEvKeysLong = 16384;
+constexpr int kEvKeysShort = 2560, kEvKeysLong = 16384;
 constexpr int kBins = 2048;                  // of a ranking key's 11 bits
+constexpr int kEvMoves = kBins / 2;          // moves at a time (their slots, where the bins were)
 static_assert(kMaxCacheBlocks * kBlock <= kEvKeysLong * 32, "a bit for each slot where the keys would be");
 constexpr int kPlanThreads = 1024;
 constexpr int kEvSlices = 8;
@@ -177,7 +177,6 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t sm_bin[kBins];
     __shared__ uint64_t sm_flags[kKeys / 64];
     __shared__ unsigned sm_wave[2][kWaves];
-    __shared__ int sm_from[kEvMoves], sm_to[kEvMoves];
     __shared__ uint32_t sm_digit, sm_rest;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int slice = blockIdx.x / a.num_sessions, s = blockIdx.x % a.num_sessions, h = blockIdx.y, la = blockIdx.z;
@@ -359,8 +358,11 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
                 }
         }
     // ---- the moves, a batch at a time
+    int *sm_from = reinterpret_cast<int *>(sm_bin), *sm_to = sm_from + kEvMoves;
     const unsigned share = (all_movers + slices - 1) / slices, last = min((slice + 1) * share, all_movers);
-    constexpr int kLanes = D / 8;                  // of a move: 16 bytes of K and 8 dims of V each
+    // A move takes D / 8 lanes: 16 bytes of K each, and 8 dims of V that are D / 8 apart, so that
+    // neighbours' 2-byte elements, 32 bytes apart, fall into the same lines.
+    constexpr int kLanes = D / 8;
     for (unsigned base = slice * share; base < last; base += kEvMoves) {
         const unsigned n = min(last - base, (unsigned)kEvMoves);
         __syncthreads();                           // the batch before has been read
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
             const u32x4 kv = *reinterpret_cast<const u32x4 *>(fk + (c * kBlock + fo) * 8);
             uint16_t v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fv[(c * 8 + e) * kBlock + fo];
+            for (int e = 0; e < 8; ++e) v[e] = fv[(e * kLanes + c) * kBlock + fo];
             const int64_t ef = ((int64_t)fb * H + h) * kBlock + fo, et = ((int64_t)tb * H + h) * kBlock + too;
             float w = 0.f;
             int p = 0;
@@ -415,7 +417,7 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
             }
             *reinterpret_cast<u32x4 *>(tk + (c * kBlock + too) * 8) = kv;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) tv[(c * 8 + e) * kBlock + too] = v[e];
+            for (int e = 0; e < 8; ++e) tv[(e * kLanes + c) * kBlock + too] = v[e];
             if (c == 0) {
                 weights_next[et] = w;
                 positions_next[et] = p;
@@ -463,10 +465,10 @@ hipError_t launch_evict(const PoolGeom &p, int32_t layer_begin, int32_t layer_co
     const bool narrow = (int64_t)c.max_blocks * kBlock <= kEvKeysShort;
 #define LS_EVICT(D, THREADS, KEYS) hipLaunchKernelGGL((evict_kernel<D, THREADS, KEYS>), grid, dim3(THREADS), 0, stream, a)
     if (p.head_dim == 128) {
-        if (narrow) LS_EVICT(128, 512, kEvKeysShort);
+        if (narrow) LS_EVICT(128, 256, kEvKeysShort);
         else LS_EVICT(128, 1024, kEvKeysLong);
     } else {
-        if (narrow) LS_EVICT(64, 512, kEvKeysShort);
+        if (narrow) LS_EVICT(64, 256, kEvKeysShort);
         else LS_EVICT(64, 1024, kEvKeysLong);
     }
 #undef LS_EVICT

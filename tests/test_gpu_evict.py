@@ -142,7 +142,7 @@ def test_only_the_latest_are_left(kv):
     check(kv, c, 40, 40, 10, "all recent", next_pos=[-2**31 + 3, 5], w=w, pos=pos)      # (more than there is room: lower slots)
 
 
-@pytest.mark.parametrize("n,budget", [(2304, 2000), (2305, 1000), (9000, 700), (16384, 16000), (20000, 5000), (20000, 19990)])
+@pytest.mark.parametrize("n,budget", [(2304, 2000), (2561, 1000), (4100, 2100), (9000, 700), (16384, 16000), (20000, 5000), (20000, 19990)])
 def test_long_sessions(kv, n, budget):
     """Keys in LDS, and sessions longer than it holds; more moves than one batch takes."""
     check(kv, Cache(np.random.default_rng(8), [n, 17], 1, 64), budget, budget, budget // 3, "%d tokens to %d" % (n, budget))
