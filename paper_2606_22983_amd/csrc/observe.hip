@@ -17,6 +17,7 @@
 // with two lane exchanges, sums over rows stay in the lane until the last row.
 // Bound by the matrix and exponential units when rows are many, by K when few.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 
@@ -96,28 +97,32 @@ __device__ __forceinline__ float sum_xor_16_32(float x) {
 // One chunk of kObWaves * KB blocks of a (session, KV head); wave w has blocks
 // w KB .. w KB + KB - 1 of it.  kKeys false: the rows' launch, true: the keys'.
 template <int D, int KB, bool kKeys>
-__global__ __launch_bounds__(kObThreads) void observe_kernel(ObserveArgs a) {
+__global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
     __shared__ float2 sm[kKeys ? 1 : kObWaves][kKeys ? 1 : kObRows];
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c16 = lane % 16, g4 = lane / 16;
-    const int chunk = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
     const int H = a.num_kv_heads, G = a.group;
+    // (A session's chunks are spread over the XCDs: rows are few, and lengths differ.)
+    const uint32_t item = blockIdx.x;
+    const int chunk = item % a.chunks, h = item / a.chunks % H, s = item / a.chunks / H;
     const Turn t = turn_of(a, s, kKeys && chunk == 0 && h == 0 && a.row0 == 0);
     const int keys = t.c + t.n, col0 = (chunk * kObWaves + wave) * KB;
     if (t.n == 0 || (a.row0 && !t.rows) || chunk * kObWaves * KB * kBlock >= keys) return;
-    // ---- the wave's K tiles
+    // ---- the wave's K tiles (ids: lane b has block b's; -1: no key or not in the pool)
     bf16x8 k[KB][D / 32];
+    int ids = -1;
+    if (lane < KB && (col0 + lane) * kBlock < keys) {
+        ids = a.tables[(int64_t)s * a.max_blocks + col0 + lane];
+        if (ids < 0 || ids >= a.num_blocks) {
+            if (kKeys) flag_error(a.err, LS_DEVERR_BLOCK_ID);
+            ids = -1;
+        }
+    }
     int id[KB];
+    bool absent = false;
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-        int x = -1;
-        if ((col0 + b) * kBlock < keys) {
-            x = a.tables[(int64_t)s * a.max_blocks + col0 + b];
-            if (x < 0 || x >= a.num_blocks) {
-                if (kKeys && lane == 0) flag_error(a.err, LS_DEVERR_BLOCK_ID);
-                x = -1;
-            }
-        }
-        id[b] = __builtin_amdgcn_readfirstlane(x);
+        id[b] = __builtin_amdgcn_readlane(ids, b);
+        absent = absent || id[b] < 0;
         const uint16_t *kt = a.pool + ((int64_t)max(id[b], 0) * 2 * H + h) * (kBlock * D);
         const __amdgpu_buffer_rsrc_t rk =
             __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(kt), 0, id[b] < 0 ? 0 : kBlock * D * 2, kRawBuffer);
@@ -125,9 +130,6 @@ __global__ __launch_bounds__(kObThreads) void observe_kernel(ObserveArgs a) {
         for (int ks = 0; ks < D / 32; ++ks)
             k[b][ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16, ks * 4 * kBlock * 16, 0));
     }
-    bool absent = false;
-#pragma unroll
-    for (int b = 0; b < KB; ++b) absent = absent || id[b] < 0;
     const int wkey0 = col0 * kBlock;               // the wave's first key
     const int64_t pair = (int64_t)s * H + h;
     const int p0 = t.c + t.j0;                     // position of the first observed token
@@ -135,59 +137,64 @@ __global__ __launch_bounds__(kObThreads) void observe_kernel(ObserveArgs a) {
     const int unseen = max(chunk * kObWaves * KB * kBlock - p0, 0) * G - a.row0;
     const int tile0 = max(unseen, 0) / 16;
     float sum[kKeys ? KB : 1][4] = {};
-    const uint16_t *qbase = a.q + ((int64_t)(t.q0 + t.j0) * H + h) * G * D;
-    auto load_q = [&](bf16x8 (&dst)[D / 32], int tile) {
-        const int row = tile * 16 + c16;
-        u32x4 x = {0u, 0u, 0u, 0u};
+    const int gs = __builtin_ctz(G);               // (G is 1, 2, 4 or 8)
+    const uint16_t *qbase = a.q + ((int64_t)(t.q0 + t.j0) * H + h) * G * D + g4 * 8;
+    struct RowTile {
+        bf16x8 q[D / 32];
+        float lse;
+    };
+    // Lanes of no row read the last one: a load under a condition waits for the one before it.
+    auto load_q = [&](RowTile &dst, int tile) {
+        const int row = min(tile * 16 + c16, t.rows - 1), at = a.row0 + row;
+        const uint16_t *src = qbase + (int64_t)(at >> gs) * (H * G * D) + (at & (G - 1)) * D;
+        if constexpr (kKeys) dst.lse = a.lse[pair * a.row_cap + row];
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) {
-            if (row < t.rows) {
-                const int at = a.row0 + row;
-                x = *reinterpret_cast<const u32x4 *>(qbase + ((int64_t)(at / G) * H * G + at % G) * D + ks * 32 + g4 * 8);
-            }
-            dst[ks] = __builtin_bit_cast(bf16x8, x);
-        }
+        for (int ks = 0; ks < D / 32; ++ks) dst.q[ks] = *reinterpret_cast<const bf16x8 *>(src + ks * 32);
     };
     const int tiles = (t.rows + 15) / 16;
-    bf16x8 q[2][D / 32];
+    RowTile q[2];
     if (tile0 < tiles) load_q(q[0], tile0);
-    auto work = [&](const bf16x8 (&qt)[D / 32], int tile) {
-        const int row = tile * 16 + c16, pos = p0 + (a.row0 + row) / G;
-        const int first_pos = p0 + (a.row0 + tile * 16) / G;
-        // Some row of the tile does not see every key of the wave.
-        const bool partial = first_pos < wkey0 + KB * kBlock - 1 || absent;
+    // partial: some row of the tile does not see every key of the wave.  (A branch around
+    // code of its own: as selects in the common code the masks cost as much as the sums.)
+    auto tile_of = [&](const RowTile &qt, int tile, auto partial) {
+        const int row = tile * 16 + c16, pos = p0 + ((a.row0 + row) >> gs);
+        const float lse = kKeys && row < t.rows ? qt.lse : INFINITY;     // (no row: no weight)
         float x[KB][4];
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], qt[ks], acc, 0, 0, 0);
+            for (int ks = 0; ks < D / 32; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], qt.q[ks], acc, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[b][e] = acc[e] * a.scale_log2;
-                if (partial && (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0)) x[b][e] = -INFINITY;
+                x[b][e] = acc[e];
+                if constexpr (decltype(partial)::value)
+                    if (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0) x[b][e] = -INFINITY;
+            }
+            if constexpr (kKeys) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[b][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -lse));
             }
         }
-        if constexpr (kKeys) {
-            const float lse = row < t.rows ? a.lse[pair * a.row_cap + row] : INFINITY;
-#pragma unroll
-            for (int b = 0; b < KB; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum[b][e] += __builtin_amdgcn_exp2f(x[b][e] - lse);
-        } else {
+        if constexpr (!kKeys) {
             float m = kNoMax, l = 0.f;
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m = fmaxf(m, x[b][e]);
-            m = max_xor_16_32(m);
+            // (the scale is positive: the largest product has the largest score)
+            m = fmaxf(max_xor_16_32(m) * a.scale_log2, kNoMax);
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(x[b][e] - m);
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -m));
             l = sum_xor_16_32(l);
             if (g4 == 0) sm[wave][row] = make_float2(m, l);
         }
+    };
+    auto work = [&](const RowTile &qt, int tile) {
+        if (p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent) tile_of(qt, tile, std::true_type());
+        else tile_of(qt, tile, std::false_type());
     };
     for (int tile = tile0; tile < tiles; tile += 2) {
         if (tile + 1 < tiles) load_q(q[1], tile + 1);
@@ -253,11 +260,11 @@ __global__ __launch_bounds__(kObThreads) void observe_lse_kernel(ObserveArgs a, 
 template <int D, int KB>
 hipError_t launch_observe_t(ObserveArgs a, int32_t whole_rows, hipStream_t stream) {
     constexpr int kChunkTokens = kObWaves * KB * kBlock;
-    const dim3 grid((unsigned)a.chunks, (unsigned)a.num_kv_heads, (unsigned)a.num_sessions);
+    const dim3 grid((unsigned)(a.chunks * a.num_kv_heads * a.num_sessions));
     for (a.row0 = 0; a.row0 < whole_rows; a.row0 += a.row_cap) {
         hipLaunchKernelGGL((observe_kernel<D, KB, false>), grid, dim3(kObThreads), 0, stream, a);
         if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL(observe_lse_kernel, dim3((unsigned)((a.row_cap + kObThreads - 1) / kObThreads), grid.y, grid.z),
+        hipLaunchKernelGGL(observe_lse_kernel, dim3((unsigned)((a.row_cap + kObThreads - 1) / kObThreads), (unsigned)a.num_kv_heads, (unsigned)a.num_sessions),
                            dim3(kObThreads), 0, stream, a, kChunkTokens);
         if (hipError_t e = hipGetLastError()) return e;
         hipLaunchKernelGGL((observe_kernel<D, KB, true>), grid, dim3(kObThreads), 0, stream, a);

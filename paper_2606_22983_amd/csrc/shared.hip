@@ -223,8 +223,8 @@ struct ShPart {
 };
 
 // The states of R tiles of 16 rows over the wave's pairs of a part.  row_len: keys
-// that the lane's row of each tile sees (0: no row).  all_seen: every row sees every
-// key below `uncut` (a multiple of 16).
+// that the lane's row of each tile sees, shortest: that all rows see; rows: scores of
+// the tile's first ones are kept.
 template <int D, int R, bool kScores, int kPolicy>
 __device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, const uint16_t *const (&qrow)[R],
                                      const int (&row_len)[R], int shortest, int rows, float (&m)[R], float (&lsum)[R],
@@ -234,11 +234,7 @@ __device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, co
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) {
-            u32x4 x = {0u, 0u, 0u, 0u};
-            if (qrow[r]) x = *reinterpret_cast<const u32x4 *>(qrow[r] + ks * 32 + g4 * 8);
-            qop[r][ks] = __builtin_bit_cast(bf16x8, x);
-        }
+        for (int ks = 0; ks < D / 32; ++ks) qop[r][ks] = *reinterpret_cast<const bf16x8 *>(qrow[r] + ks * 32 + g4 * 8);
         m[r] = kNoMax;
         lsum[r] = 0.f;
 #pragma unroll
@@ -421,6 +417,7 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
     const int tid = threadIdx.x, lane = tid % kWave, c16 = lane % 16;
     const int S = a.num_sessions, G = a.group, H = a.num_kv_heads;
     const bool first_wg = blockIdx.x == 0;
+    const int gs = __builtin_ctz(G);           // (G is 1, 2, 4 or 8)
     // ---- the schedule, made by every workgroup for itself
     int ng = a.num_groups;
     bool bad = false;
@@ -580,16 +577,12 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
                         int row_len[R], shortest = INT32_MAX;
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
-                            const int row = r * 16 + c16;
-                            qrow[r] = nullptr;
-                            row_len[r] = 0;
-                            if (row < n) {
-                                const int rank = (t * kTileRows + row) / G, head = (t * kTileRows + row) % G;
-                                const int s = a.members[sm.start[g] + rank];
-                                qrow[r] = a.q + ((int64_t)s * H * G + h * G + head) * D;
-                                row_len[r] = sm.len[s];
-                                shortest = min(shortest, row_len[r]);
-                            }
+                            // (lanes of no row take the last one: a load under a condition waits for the one before)
+                            const int row = t * kTileRows + min(r * 16 + c16, n - 1);
+                            const int s = a.members[sm.start[g] + (row >> gs)];
+                            qrow[r] = a.q + ((int64_t)s * H * G + h * G + (row & (G - 1))) * D;
+                            row_len[r] = sm.len[s];
+                            shortest = min(shortest, row_len[r]);
                         }
 #pragma unroll
                         for (int off = 1; off < 16; off <<= 1) shortest = min(shortest, __shfl_xor(shortest, off));
@@ -635,8 +628,8 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
                 const int64_t row0 = (int64_t)s * H * G + h * G;
                 const ShSink sink = {!whole || kWeights ? a.own_ml + slot * G * 2 : nullptr, whole ? nullptr : a.own_acc + slot * G * D,
                                      a.out + row0 * D, G};
-                const uint16_t *qrow[1] = {c16 < G ? a.q + (row0 + c16) * D : nullptr};
-                const int row_len[1] = {c16 < G ? L : 0};
+                const uint16_t *qrow[1] = {a.q + (row0 + min(c16, G - 1)) * D};
+                const int row_len[1] = {L};
                 float m[1], lsum[1];
                 f32x4 o[1][D / 16];
                 walk<D, 1, kWeights, kStream>(a, part, qrow, row_len, L, G, m, lsum, o);
