@@ -247,11 +247,20 @@ __global__ __launch_bounds__(kObThreads) void observe_lse_kernel(ObserveArgs a, 
     const int64_t pair = (int64_t)s * a.num_kv_heads + h;
     const int pos = t.c + t.j0 + (a.row0 + row) / a.group, chunks = pos / chunk_tokens + 1;
     const float2 *p = a.part + pair * a.chunks * a.row_cap + row;
+    // (eight chunks at a time, so that their loads are in flight together)
     float m = kNoMax, l = 0.f;
-    for (int k = 0; k < chunks; ++k) m = fmaxf(m, p[(int64_t)k * a.row_cap].x);
-    for (int k = 0; k < chunks; ++k) {
-        const float2 v = p[(int64_t)k * a.row_cap];
-        l += __builtin_amdgcn_exp2f(v.x - m) * v.y;
+    for (int k0 = 0; k0 < chunks; k0 += 8) {
+        float2 v[8];
+        float now = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)min(k0 + i, chunks - 1) * a.row_cap];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) now = fmaxf(now, v[i].x);
+        l *= __builtin_amdgcn_exp2f(m - now);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k0 + i < chunks) l += __builtin_amdgcn_exp2f(v[i].x - now) * v[i].y;
+        m = now;
     }
     // (a row without a key, all of its blocks absent: no weight)
     a.lse[pair * a.row_cap + row] = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : INFINITY;
