@@ -412,9 +412,9 @@ ls_status check_cache_call(const PoolGeom &p, int32_t layer, int32_t num_session
     if (ls_status st = check_heads(p, num_q_heads)) return st;
     if (max_blocks <= 0) return fail(LS_EINVAL, "max_blocks_per_session must be > 0");
     if (!(scale > 0.f)) return fail(LS_EINVAL, "scale must be a positive number");
-    if (num_sessions > kMaxCacheSessions || max_blocks > kMaxCacheBlocks || p.num_kv_heads > 65535)
-        return fail(LS_EUNSUPPORTED, "%d sessions with %d blocks each exceed the limits (%d sessions, %d blocks per session)",
-                    num_sessions, max_blocks, kMaxCacheSessions, kMaxCacheBlocks);
+    if (num_sessions > kMaxCacheSessions || max_blocks > kMaxCacheBlocks || p.num_kv_heads > 4096)
+        return fail(LS_EUNSUPPORTED, "%d sessions with %d blocks each and %d KV heads exceed the limits (%d sessions, %d blocks per "
+                    "session, 4096 KV heads)", num_sessions, max_blocks, p.num_kv_heads, kMaxCacheSessions, kMaxCacheBlocks);
     return LS_OK;
 }
 

@@ -31,7 +31,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kObThreads = 256;
 constexpr int kObWaves = kObThreads / kWave;
-constexpr int kObRows = 1024;                // rows of a KV head at a time (LDS); more take another round
+constexpr int kObRows = 1024;                // rows of a KV head at a time (the workspace); more take another round
 constexpr float kNoMax = -1.0e30f;
 constexpr int kRawBuffer = 0x00020000;
 
@@ -94,11 +94,31 @@ __device__ __forceinline__ float sum_xor_16_32(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+typedef __attribute__((address_space(3))) void lds_void;
+
+// Four tiles of 16 rows, one loaded by each wave: a tile's k-step is a kilobyte, in the
+// order of the lanes that take it as the B operand.
+template <int D>
+struct RowStage {
+    __attribute__((aligned(1024))) uint8_t q[kObWaves][D / 32][1024];
+};
+struct LseStage {
+    float lse[kObWaves][kWave];                    // lane: its row's
+};
+
 // One chunk of kObWaves * KB blocks of a (session, KV head); wave w has blocks
 // w KB .. w KB + KB - 1 of it.  kKeys false: the rows' launch, true: the keys'.
+//
+// The rows come through LDS, four tiles a stage, loaded two stages ahead (each wave
+// reading its rows from L2 one tile ahead took 2.4 times as long: a tile takes some
+// 700 cycles, a load up to 4000 when all CUs read).  One barrier a stage: it publishes the next
+// stage and frees the one before, and the loads two stages ahead stay in flight.
 template <int D, int KB, bool kKeys>
 __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
-    __shared__ float2 sm[kKeys ? 1 : kObWaves][kKeys ? 1 : kObRows];
+    // (arrays of their own: reads of one stage do not wait for the loads of another)
+    __shared__ RowStage<D> sq0, sq1, sq2;
+    __shared__ LseStage sl0, sl1, sl2;
+    __shared__ float2 sm[2][kObWaves][kObWaves * 16];      // (m, l) of a stage's rows, by wave
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c16 = lane % 16, g4 = lane / 16;
     const int H = a.num_kv_heads, G = a.group;
     // (A session's chunks are spread over the XCDs: rows are few, and lengths differ.)
@@ -107,6 +127,12 @@ __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
     const Turn t = turn_of(a, s, kKeys && chunk == 0 && h == 0 && a.row0 == 0);
     const int keys = t.c + t.n, col0 = (chunk * kObWaves + wave) * KB;
     if (t.n == 0 || (a.row0 && !t.rows) || chunk * kObWaves * KB * kBlock >= keys) return;
+    const int64_t pair = (int64_t)s * H + h;
+    const int p0 = t.c + t.j0;                     // position of the first observed token
+    const int gs = __builtin_ctz(G);               // (G is 1, 2, 4 or 8)
+    // Rows before this one see none of the chunk's keys.
+    const int unseen = max(chunk * kObWaves * KB * kBlock - p0, 0) * G - a.row0;
+    const int tile0 = max(unseen, 0) / 16, tiles = (t.rows + 15) / 16;
     // ---- the wave's K tiles (ids: lane b has block b's; -1: no key or not in the pool)
     bf16x8 k[KB][D / 32];
     int ids = -1;
@@ -131,40 +157,43 @@ __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
             k[b][ks] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rk, lane * 16, ks * 4 * kBlock * 16, 0));
     }
     const int wkey0 = col0 * kBlock;               // the wave's first key
-    const int64_t pair = (int64_t)s * H + h;
-    const int p0 = t.c + t.j0;                     // position of the first observed token
-    // Rows before this one see none of the chunk's keys.
-    const int unseen = max(chunk * kObWaves * KB * kBlock - p0, 0) * G - a.row0;
-    const int tile0 = max(unseen, 0) / 16;
     float sum[kKeys ? KB : 1][4] = {};
-    const int gs = __builtin_ctz(G);               // (G is 1, 2, 4 or 8)
-    const uint16_t *qbase = a.q + ((int64_t)(t.q0 + t.j0) * H + h) * G * D + g4 * 8;
-    struct RowTile {
-        bf16x8 q[D / 32];
-        float lse;
-    };
-    // Lanes of no row read the last one: a load under a condition waits for the one before it.
-    auto load_q = [&](RowTile &dst, int tile) {
-        const int row = min(tile * 16 + c16, t.rows - 1), at = a.row0 + row;
-        const uint16_t *src = qbase + (int64_t)(at >> gs) * (H * G * D) + (at & (G - 1)) * D;
-        if constexpr (kKeys) dst.lse = a.lse[pair * a.row_cap + row];
+    // ---- the rows.  (The round's first row is a token's first: row0 is a multiple of 1024.)
+    const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t *>(a.q + ((int64_t)(t.q0 + t.j0 + (a.row0 >> gs)) * H + h) * G * D), 0, INT32_MAX, kRawBuffer);
+    const __amdgpu_buffer_rsrc_t rl =
+        __builtin_amdgcn_make_buffer_rsrc(a.lse + pair * a.row_cap, 0, kKeys ? INT32_MAX : 0, kRawBuffer);
+    // Lanes of no row, and stages behind the last, read the last row.
+    auto load_stage = [&](RowStage<D> &sq, LseStage &sl, int tile_first) {
+        const int row = min((tile_first + wave) * 16 + c16, t.rows - 1);
+        const int off = ((row >> gs) * (H * G) + (row & (G - 1))) * (D * 2) + g4 * 16;
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) dst.q[ks] = *reinterpret_cast<const bf16x8 *>(src + ks * 32);
+        for (int ks = 0; ks < D / 32; ++ks)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void *)sq.q[wave][ks], 16, off + ks * 64, 0, 0, 0);
+        if constexpr (kKeys) __builtin_amdgcn_raw_ptr_buffer_load_lds(rl, (lds_void *)sl.lse[wave], 4, row * 4, 0, 0, 0);
     };
-    const int tiles = (t.rows + 15) / 16;
-    RowTile q[2];
-    if (tile0 < tiles) load_q(q[0], tile0);
+    auto stage_barrier = [&]() {
+        // vmcnt: all but the last stage's loads have landed; lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt(0x0070 | (D / 32 + (kKeys ? 1 : 0)));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
     // partial: some row of the tile does not see every key of the wave.  (A branch around
     // code of its own: as selects in the common code the masks cost as much as the sums.)
-    auto tile_of = [&](const RowTile &qt, int tile, auto partial) {
+    auto tile_of = [&](const RowStage<D> &sq, const LseStage &sl, int i, int tile, float2 *res, auto partial) {
         const int row = tile * 16 + c16, pos = p0 + ((a.row0 + row) >> gs);
-        const float lse = kKeys && row < t.rows ? qt.lse : INFINITY;     // (no row: no weight)
+        float lse = 0.f;
+        if constexpr (kKeys) lse = row < t.rows ? sl.lse[i][lane] : INFINITY;     // (no row: no weight)
+        bf16x8 q[D / 32];
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(&sq.q[i][ks][lane * 16]);
         float x[KB][4];
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], qt.q[ks], acc, 0, 0, 0);
+            for (int ks = 0; ks < D / 32; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], q[ks], acc, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 x[b][e] = acc[e];
@@ -189,33 +218,52 @@ __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -m));
             l = sum_xor_16_32(l);
-            if (g4 == 0) sm[wave][row] = make_float2(m, l);
+            if (g4 == 0) res[i * 16 + c16] = make_float2(m, l);
         }
     };
-    auto work = [&](const RowTile &qt, int tile) {
-        if (p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent) tile_of(qt, tile, std::true_type());
-        else tile_of(qt, tile, std::false_type());
-    };
-    for (int tile = tile0; tile < tiles; tile += 2) {
-        if (tile + 1 < tiles) load_q(q[1], tile + 1);
-        work(q[0], tile);
-        if (tile + 1 >= tiles) break;
-        if (tile + 2 < tiles) load_q(q[0], tile + 2);
-        work(q[1], tile + 1);
-    }
-    if constexpr (!kKeys) {
-        __syncthreads();
-        for (int row = tid; row < t.rows; row += kObThreads) {
+    float2 *part = a.part + (pair * a.chunks + chunk) * a.row_cap;
+    if constexpr (!kKeys)
+        for (int row = tid; row < min(tile0 * 16, t.rows); row += kObThreads) part[row] = make_float2(kNoMax, 0.f);
+    auto stage = [&](int st, RowStage<D> &sq, LseStage &sl, RowStage<D> &ahead_q, LseStage &ahead_l) {
+        const int tile_first = tile0 + st * kObWaves;
+        load_stage(ahead_q, ahead_l, tile_first + 2 * kObWaves);
+        const int n = min(tiles - tile_first, kObWaves);
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const int tile = tile_first + i;
+            if (p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent)
+                tile_of(sq, sl, i, tile, sm[st & 1][wave], std::true_type());
+            else
+                tile_of(sq, sl, i, tile, sm[st & 1][wave], std::false_type());
+        }
+        stage_barrier();
+        // The rows of the stage over the waves' keys, by one wave; the stage after the next writes there again.
+        if (!kKeys && wave == st % kObWaves && tile_first * 16 + lane < t.rows) {
             float m = kNoMax, l = 0.f;
-            if (row >= tile0 * 16) {
 #pragma unroll
-                for (int w = 0; w < kObWaves; ++w) m = fmaxf(m, sm[w][row].x);
+            for (int w = 0; w < kObWaves; ++w) m = fmaxf(m, sm[st & 1][w][lane].x);
 #pragma unroll
-                for (int w = 0; w < kObWaves; ++w) l += __builtin_amdgcn_exp2f(sm[w][row].x - m) * sm[w][row].y;
-            }
-            a.part[(pair * a.chunks + chunk) * a.row_cap + row] = make_float2(m, l);
+            for (int w = 0; w < kObWaves; ++w) l += __builtin_amdgcn_exp2f(sm[st & 1][w][lane].x - m) * sm[st & 1][w][lane].y;
+            part[tile_first * 16 + lane] = make_float2(m, l);
         }
-    } else {
+    };
+    const int stages = (tiles - tile0 + kObWaves - 1) / kObWaves;
+    if (stages > 0) {
+        load_stage(sq0, sl0, tile0);
+        load_stage(sq1, sl1, tile0 + kObWaves);
+        stage_barrier();
+        for (int st = 0;;) {
+            stage(st, sq0, sl0, sq2, sl2);
+            if (++st >= stages) break;
+            stage(st, sq1, sl1, sq0, sl0);
+            if (++st >= stages) break;
+            stage(st, sq2, sl2, sq1, sl1);
+            if (++st >= stages) break;
+        }
+        // (no wave's memory ends while loads into it are in flight)
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+    }
+    if constexpr (kKeys) {
         // ---- sums over the 16 rows' lanes; lane 16 g4 + b has the wave's block b
         const int first = a.first ? a.first[s] : 0, begin = a.begin ? a.begin[s] : t.c;
 #pragma unroll
@@ -226,12 +274,13 @@ __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
                 for (int off = 1; off < 16; off <<= 1) sum[b][e] += __shfl_xor(sum[b][e], off);
             if (c16 == b && id[b] >= 0) {
                 const int64_t at = ((int64_t)id[b] * H + h) * kBlock + 4 * g4;
+                const f32x4 was = *reinterpret_cast<const f32x4 *>(a.weights + at);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int key = wkey0 + b * kBlock + 4 * g4 + e;
                     if (key < first || key >= keys) continue;
                     const bool fresh = key >= t.c && a.row0 == 0;
-                    a.weights[at + e] = fresh ? sum[b][e] : a.weights[at + e] + sum[b][e];
+                    a.weights[at + e] = fresh ? sum[b][e] : was[e] + sum[b][e];
                     if (fresh) a.positions[at + e] = begin + (key - t.c);
                 }
             }
