@@ -109,16 +109,16 @@ struct LseStage {
 // One chunk of kObWaves * KB blocks of a (session, KV head); wave w has blocks
 // w KB .. w KB + KB - 1 of it.  kKeys false: the rows' launch, true: the keys'.
 //
-// The rows come through LDS, four tiles a stage, loaded two stages ahead (each wave
-// reading its rows from L2 one tile ahead took 2.4 times as long: a tile takes some
-// 700 cycles, a load up to 4000 when all CUs read).  One barrier a stage: it publishes the next
-// stage and frees the one before, and the loads two stages ahead stay in flight.
+// The rows come through LDS, four tiles a stage, loaded a stage ahead (each wave
+// reading its rows from L2 one tile ahead took longer: a tile takes some 400 cycles, a
+// load up to 4000 when all CUs read).  One barrier a stage publishes the next one and
+// frees the one before.
 template <int D, int KB, bool kKeys>
-__global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
+__global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     // (arrays of their own: reads of one stage do not wait for the loads of another)
-    __shared__ RowStage<D> sq0, sq1, sq2;
-    __shared__ LseStage sl0, sl1, sl2;
-    __shared__ float2 sm[2][kObWaves][kObWaves * 16];      // (m, l) of a stage's rows, by wave
+    __shared__ RowStage<D> sq0, sq1;
+    __shared__ LseStage sl0, sl1;
+    __shared__ float2 sm[3][kObWaves][kObWaves * 16];      // (m, l) of a stage's rows, by wave
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c16 = lane % 16, g4 = lane / 16;
     const int H = a.num_kv_heads, G = a.group;
     // (A session's chunks are spread over the XCDs: rows are few, and lengths differ.)
@@ -173,39 +173,48 @@ __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
         if constexpr (kKeys) __builtin_amdgcn_raw_ptr_buffer_load_lds(rl, (lds_void *)sl.lse[wave], 4, row * 4, 0, 0, 0);
     };
     auto stage_barrier = [&]() {
-        // vmcnt: all but the last stage's loads have landed; lgkmcnt(0)
-        __builtin_amdgcn_s_waitcnt(0x0070 | (D / 32 + (kKeys ? 1 : 0)));
+        __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // partial: some row of the tile does not see every key of the wave.  (A branch around
-    // code of its own: as selects in the common code the masks cost as much as the sums.)
-    auto tile_of = [&](const RowStage<D> &sq, const LseStage &sl, int i, int tile, float2 *res, auto partial) {
-        const int row = tile * 16 + c16, pos = p0 + ((a.row0 + row) >> gs);
-        float lse = 0.f;
-        if constexpr (kKeys) lse = row < t.rows ? sl.lse[i][lane] : INFINITY;     // (no row: no weight)
+    // ---- products of a tile, and what is made of them (by the rows' launch one tile later, in the
+    // same code: the matrix unit has the next tile's while the vector unit has this one's)
+    f32x4 acc[2][KB];
+    float lse[2] = {0.f, 0.f};
+    auto products = [&](const RowStage<D> &sq, const LseStage &sl, int i, f32x4 (&to)[KB], float &row_lse) {
+        if constexpr (kKeys) row_lse = sl.lse[i][lane];
         bf16x8 q[D / 32];
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(&sq.q[i][ks][lane * 16]);
+#pragma unroll
+        for (int b = 0; b < KB; ++b) to[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+            for (int b = 0; b < KB; ++b) to[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], q[ks], to[b], 0, 0, 0);
+    };
+    // Some row of the tile does not see every key of the wave.  (A branch around code of its
+    // own: as selects in the common code the masks cost as much as the sums.)
+    auto is_partial = [&](int tile) { return p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent; };
+    auto consume = [&](const f32x4 (&of)[KB], float row_lse, int tile, auto partial) {
+        const int row = tile * 16 + c16, pos = p0 + ((a.row0 + row) >> gs);
         float x[KB][4];
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b][ks], q[ks], acc, 0, 0, 0);
+        for (int b = 0; b < KB; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[b][e] = acc[e];
+                x[b][e] = of[b][e];
                 if constexpr (decltype(partial)::value)
                     if (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0) x[b][e] = -INFINITY;
             }
-            if constexpr (kKeys) {
+        if constexpr (kKeys) {
+            if (row >= t.rows) row_lse = INFINITY;             // (no row: no weight)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[b][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -lse));
-            }
-        }
-        if constexpr (!kKeys) {
+            for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[b][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -row_lse));
+        } else {
             float m = kNoMax, l = 0.f;
 #pragma unroll
             for (int b = 0; b < KB; ++b)
@@ -218,50 +227,66 @@ __global__ __launch_bounds__(kObThreads, 2) void observe_kernel(ObserveArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -m));
             l = sum_xor_16_32(l);
-            if (g4 == 0) res[i * 16 + c16] = make_float2(m, l);
+            const int n = tile - tile0;
+            if (g4 == 0) sm[n / kObWaves % 3][wave][n % kObWaves * 16 + c16] = make_float2(m, l);
         }
     };
     float2 *part = a.part + (pair * a.chunks + chunk) * a.row_cap;
     if constexpr (!kKeys)
         for (int row = tid; row < min(tile0 * 16, t.rows); row += kObThreads) part[row] = make_float2(kNoMax, 0.f);
+    const int count = tiles - tile0, stages = (count + kObWaves - 1) / kObWaves;
+    // The rows of a finished stage over the waves' keys, by one wave.
+    auto store_rows = [&](int st) {
+        const int row = (tile0 + st * kObWaves) * 16 + lane;
+        if (kKeys || wave != st % kObWaves || row >= t.rows) return;
+        float m = kNoMax, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kObWaves; ++w) m = fmaxf(m, sm[st % 3][w][lane].x);
+#pragma unroll
+        for (int w = 0; w < kObWaves; ++w) l += __builtin_amdgcn_exp2f(sm[st % 3][w][lane].x - m) * sm[st % 3][w][lane].y;
+        part[row] = make_float2(m, l);
+    };
     auto stage = [&](int st, RowStage<D> &sq, LseStage &sl, RowStage<D> &ahead_q, LseStage &ahead_l) {
-        const int tile_first = tile0 + st * kObWaves;
-        load_stage(ahead_q, ahead_l, tile_first + 2 * kObWaves);
-        const int n = min(tiles - tile_first, kObWaves);
-#pragma unroll 1
-        for (int i = 0; i < n; ++i) {
-            const int tile = tile_first + i;
-            if (p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent)
-                tile_of(sq, sl, i, tile, sm[st & 1][wave], std::true_type());
-            else
-                tile_of(sq, sl, i, tile, sm[st & 1][wave], std::false_type());
+        load_stage(ahead_q, ahead_l, tile0 + (st + 1) * kObWaves);
+        if (st >= 2) store_rows(st - 2);           // (its last tile was finished in stage st - 1)
+#pragma unroll
+        for (int i = 0; i < kObWaves; ++i) {
+            const int n = st * kObWaves + i;
+            if (n >= count) break;
+            if constexpr (kKeys) {
+                // (at once: the sums take the registers that a tile's products would wait in, and a
+                // third wave per SIMD gives as much: 152 us for the next-turn batch, 174 one later)
+                products(sq, sl, i, acc[0], lse[0]);
+                if (is_partial(tile0 + n)) consume(acc[0], lse[0], tile0 + n, std::true_type());
+                else consume(acc[0], lse[0], tile0 + n, std::false_type());
+            } else if (n == 0) {
+                products(sq, sl, i, acc[i & 1], lse[i & 1]);
+            } else if (is_partial(tile0 + n - 1)) {
+                products(sq, sl, i, acc[i & 1], lse[i & 1]);
+                consume(acc[(i + 1) & 1], lse[(i + 1) & 1], tile0 + n - 1, std::true_type());
+            } else {
+                products(sq, sl, i, acc[i & 1], lse[i & 1]);
+                consume(acc[(i + 1) & 1], lse[(i + 1) & 1], tile0 + n - 1, std::false_type());
+            }
         }
         stage_barrier();
-        // The rows of the stage over the waves' keys, by one wave; the stage after the next writes there again.
-        if (!kKeys && wave == st % kObWaves && tile_first * 16 + lane < t.rows) {
-            float m = kNoMax, l = 0.f;
-#pragma unroll
-            for (int w = 0; w < kObWaves; ++w) m = fmaxf(m, sm[st & 1][w][lane].x);
-#pragma unroll
-            for (int w = 0; w < kObWaves; ++w) l += __builtin_amdgcn_exp2f(sm[st & 1][w][lane].x - m) * sm[st & 1][w][lane].y;
-            part[tile_first * 16 + lane] = make_float2(m, l);
-        }
     };
-    const int stages = (tiles - tile0 + kObWaves - 1) / kObWaves;
-    if (stages > 0) {
+    if (count > 0) {
         load_stage(sq0, sl0, tile0);
-        load_stage(sq1, sl1, tile0 + kObWaves);
         stage_barrier();
         for (int st = 0;;) {
-            stage(st, sq0, sl0, sq2, sl2);
+            stage(st, sq0, sl0, sq1, sl1);
             if (++st >= stages) break;
             stage(st, sq1, sl1, sq0, sl0);
             if (++st >= stages) break;
-            stage(st, sq2, sl2, sq1, sl1);
-            if (++st >= stages) break;
         }
-        // (no wave's memory ends while loads into it are in flight)
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+        if constexpr (!kKeys) {
+            if (count & 1) consume(acc[0], lse[0], tiles - 1, std::true_type());
+            else consume(acc[1], lse[1], tiles - 1, std::true_type());
+            __syncthreads();
+            if (stages >= 2) store_rows(stages - 2);
+            store_rows(stages - 1);
+        }
     }
     if constexpr (kKeys) {
         // ---- sums over the 16 rows' lanes; lane 16 g4 + b has the wave's block b
@@ -343,7 +368,7 @@ ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_
     o.whole_rows = (int32_t)(std::min<int64_t>(rows, max_new_len) * G);
     o.row_cap = std::min(o.whole_rows, kObRows);
     // Blocks per wave: as many as leave every CU two workgroups.
-    o.blocks = 8;
+    o.blocks = 4;
     while (o.blocks > 1 && pairs * ((max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks)) < 2 * cus) o.blocks /= 2;
     o.chunks = (max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks);
     o.lse_at = align256((size_t)pairs * (size_t)o.chunks * (size_t)o.row_cap * sizeof(float2));
@@ -380,8 +405,7 @@ hipError_t launch_observe(const PoolGeom &p, int layer, int32_t num_sessions, in
     a.first = c.first_lens;
     a.err = err;
 #define LS_OBSERVE(D) \
-    (plan.blocks == 8   ? launch_observe_t<D, 8>(a, plan.whole_rows, stream) \
-     : plan.blocks == 4 ? launch_observe_t<D, 4>(a, plan.whole_rows, stream) \
+    (plan.blocks == 4   ? launch_observe_t<D, 4>(a, plan.whole_rows, stream) \
      : plan.blocks == 2 ? launch_observe_t<D, 2>(a, plan.whole_rows, stream) \
                         : launch_observe_t<D, 1>(a, plan.whole_rows, stream))
     return p.head_dim == 128 ? LS_OBSERVE(128) : LS_OBSERVE(64);
