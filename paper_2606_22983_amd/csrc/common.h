@@ -198,8 +198,8 @@ struct SharedCall {
 };
 // Its workspace: offsets of the schedule, the parts' states and the scores.
 struct SharedPlan {
-    size_t tile_slots, own_slots;
-    size_t at[7];
+    size_t tiles;                  // prefix segments, at most
+    size_t at[8];
     size_t total;
 };
 SharedPlan plan_shared(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads, int32_t num_groups,

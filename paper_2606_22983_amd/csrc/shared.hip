@@ -10,14 +10,16 @@
 // against K and V tiles that are read once per 64 rows, and each session's own
 // keys are walked for it alone.
 //
-// Work: segments = (group, KV head, tile of 64 rows) over the group's blocks, then
-// (session, KV head) over its own blocks.  A block of a segment costs some units
-// (kCost*, from measurement); one workgroup per CU takes an equal contiguous share
-// of all units, so it works on a few parts of segments.  Its four waves take a
-// part's pairs of blocks in turn, each with a state of its own, and merge through
-// LDS.  A segment that one workgroup has whole, without a shared prefix, is written
-// out at once; other parts leave their state in the workspace, at slot (segment +
-// workgroup), which no other part has, and a second kernel adds them up per row.
+// Work: segments = (group, KV head, tile of up to 128 rows) over the group's blocks,
+// then (session, KV head) over its own blocks.  A block of a segment costs some units
+// (kCost*, from measurement).  Workgroups of four waves, two per CU, take equal contiguous
+// shares of all units, so each works on a few parts of segments.  A part with up to 16
+// rows (own keys, small groups): the waves take its pairs of blocks in turn, straight
+// into registers, each with a state of its own, and merge through LDS.  With more rows:
+// the pairs go through LDS, three at a time in flight, and every wave takes them all, for
+// 16 or 32 rows of its own.  A segment that one workgroup has whole, without a shared
+// prefix, is written out at once; other parts leave their state in the workspace, at slot
+// (segment + workgroup), which no other part has, and a second kernel adds them up.
 //
 // Accumulated weights: the probability of a key is known only once its row's sum
 // is, so the first kernel leaves the scores of the own keys (fp32, 4 bytes a head
@@ -29,7 +31,7 @@
 // layout (lane: row lane % 16, tokens 4 (lane / 16) + i) of a pair of blocks is
 // the B operand of O^T[16 dims x 16 rows] += V^T . P^T (16x16x32 over the pair's 32
 // tokens, in the order that the lanes hold them).  Probabilities are rounded to
-// bf16 there, by 2^-9 of themselves at most half a step, while sums, maxima and
+// bf16 there, by half a step (2^-8 of themselves) at most, while sums, maxima and
 // accumulated weights take the fp32 ones.
 #include <algorithm>
 #include <type_traits>
@@ -44,15 +46,20 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kShThreads = 256;
 constexpr int kShWaves = kShThreads / kWave;
-constexpr int kShBatch = 2048;               // sessions (LDS)
-constexpr int kTileRows = 64;                // rows of a prefix segment
-constexpr int kRank = 11;                    // bits of a member's rank (kShBatch of them)
-// Units of a block: own keys (bound by HBM), a prefix tile of 16, 32 or 64 rows.
+constexpr int kShPerCu = 2;                  // workgroups
+// Sessions, members and groups that a kernel's LDS has room for: with the few, two
+// workgroups fit a CU.
+constexpr int kShFew = 512, kShMost = 2048;
+constexpr int kTileRows = 128;               // rows of a prefix segment: two tiles of 16 per wave
+constexpr int kRank = 11;                    // bits of a member's rank (kShMost of them)
+static_assert(kShMost == 1 << kRank && kShMost == kMaxCacheSessions, "ranks fit");
+// Units of a block: own keys (bound by HBM), a prefix tile of up to 16 rows, and a larger one.
 constexpr int kCostOwn = 4;
-constexpr int kCostTile1 = 2, kCostTile2 = 3, kCostTile4 = 4;
+constexpr int kCostFew = 4, kCostTile = 4;
 constexpr int kLeastUnits = kShWaves * 2 * kCostOwn;     // a pair of blocks for each wave
 constexpr float kNoMax = -1.0e30f;           // running maximum of no key
 // The running maximum moves only when a score passes it by this much (log2), so that
@@ -61,25 +68,16 @@ constexpr float kMaxSlack = 8.0f;
 constexpr int kRawBuffer = 0x00020000;       // raw buffer, 32-bit data format
 constexpr int kStream = 2;                   // non-temporal: own keys are read once
 
-// How a session's parts are found by the second kernel.
+// What the second kernel knows of a session.
 struct ShRecord {
-    int64_t own_pos;               // first unit of (s, KV head 0); a KV head further: own_blocks * kCostOwn
-    int64_t tile_pos;              // first unit of its prefix tile at KV head 0
-    int64_t tile_stride;           // units per KV head of its group
     int32_t own_blocks;            // 0: no own key
     int32_t prefix_blocks;         // 0: no prefix
     int32_t tile_seg;              // prefix segment at KV head 0
     int32_t tile_seg_stride;       // prefix segments per KV head of its group
     int32_t tile_row;              // its first row in the tile
-    int32_t tile_cost;             // units of a block of the tile
     int32_t keys;                  // L
-    int32_t unused;
-};
-struct ShHeader {
-    int64_t share;                 // units per workgroup
-    int64_t own_base;              // first unit of the own segments
-    int64_t own_units;             // own blocks of all sessions, per KV head
-    int64_t unused;
+    uint32_t own_before;           // own blocks of the sessions before
+    uint32_t own_all;              // of all sessions
 };
 
 struct SharedArgs {
@@ -97,10 +95,11 @@ struct SharedArgs {
     const int32_t *members;        // [num_members]
     const int32_t *prefix;         // [num_groups] blocks
     float scale_log2;
-    ShHeader *header;
     ShRecord *records;             // [S]
-    float *tile_ml;                // [tile slots][64][2]
-    float *tile_acc;               // [tile slots][64][D]
+    int32_t *tile_first, *tile_last;     // [prefix segments] workgroups of a segment's first and last part
+    int32_t *own_first, *own_last;       // [S][Hkv]
+    float *tile_ml;                // [tile slots][128][2]
+    float *tile_acc;               // [tile slots][128][D]
     float *own_ml;                 // [own slots][G][2]
     float *own_acc;                // [own slots][G][D]
     // Accumulated weights
@@ -113,13 +112,15 @@ struct SharedArgs {
     unsigned int *err;
 };
 
-__device__ __forceinline__ int tile_cost(int rows) {
-    return rows <= 16 ? kCostTile1 : rows <= 32 ? kCostTile2 : kCostTile4;
-}
+__device__ __forceinline__ int tile_cost(int rows) { return rows <= 16 ? kCostFew : kCostTile; }
 // Units per block of all tiles of a group of `rows` rows.
 __device__ __forceinline__ int group_cost(int rows) {
     const int rest = rows % kTileRows;
-    return rows / kTileRows * kCostTile4 + (rest ? tile_cost(rest) : 0);
+    return rows / kTileRows * kCostTile + (rest ? tile_cost(rest) : 0);
+}
+// Keys of session s, clipped to its table.
+__device__ __forceinline__ int keys_of(const SharedArgs &a, int s) {
+    return max(min(a.lens[s], a.max_blocks * kBlock), 0);
 }
 
 __device__ __forceinline__ float max_xor_16_32(float x) {
@@ -142,18 +143,20 @@ struct PairRegs {
     u32x2 v[2][D / 16];            // V^T[dim 16 dt + lane % 16][tokens 4 (lane / 16) .. + 3]
 };
 
-// (id < 0: a descriptor of no bytes, nothing is fetched and zeros arrive)
+// K tile of a block and KV head (id < 0: a descriptor of no bytes, nothing is fetched).
+template <int D>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t *pool, int num_kv_heads, int g, int id, bool v) {
+    const uint16_t *t = pool + ((int64_t)(id < 0 ? 0 : id) * 2 * num_kv_heads + g + (v ? num_kv_heads : 0)) * (kBlock * D);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(t), 0, id < 0 ? 0 : kBlock * D * 2, kRawBuffer);
+}
+
 template <int D, int kPolicy>
 __device__ __forceinline__ void load_pair(PairRegs<D> &r, const uint16_t *pool, int num_kv_heads, int g,
                                           const int (&id)[2], int koff, int voff) {
-    constexpr int kTile = kBlock * D;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        const uint16_t *kt = pool + ((int64_t)(id[b] < 0 ? 0 : id[b]) * 2 * num_kv_heads + g) * kTile;
-        const uint16_t *vt = kt + (int64_t)num_kv_heads * kTile;
-        const int bytes = id[b] < 0 ? 0 : kTile * 2;
-        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(kt), 0, bytes, kRawBuffer);
-        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(vt), 0, bytes, kRawBuffer);
+        const __amdgpu_buffer_rsrc_t rk = tile_rsrc<D>(pool, num_kv_heads, g, id[b], false);
+        const __amdgpu_buffer_rsrc_t rv = tile_rsrc<D>(pool, num_kv_heads, g, id[b], true);
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks)
             r.k[b][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff, ks * 4 * kBlock * 16, kPolicy);
@@ -163,22 +166,25 @@ __device__ __forceinline__ void load_pair(PairRegs<D> &r, const uint16_t *pool, 
     }
 }
 
+// A pair of blocks in LDS, as in the pool; and where waves merge, two a buffer, and the
+// schedule is made.
 template <int D>
-struct ShLds {
-    // The schedule
-    uint32_t cum[kShBatch + 1];    // own blocks of the sessions before
-    int32_t len[kShBatch];
-    int32_t owner[kShBatch];       // its place among the members, or -1
-    uint16_t gid[kShBatch];
-    int32_t start[kShBatch + 1];
-    int32_t prefix[kShBatch];      // blocks of the group
-    uint32_t lead[kShBatch];       // longest member: length, then lowest rank
-    uint32_t gunits[kShBatch + 1]; // units per KV head of the groups before
-    uint32_t gsegs[kShBatch + 1];  // tiles per KV head of the groups before
+struct PairLds {
+    __attribute__((aligned(1024))) uint8_t tile[4][kBlock * D * 2];     // K, K, V, V
+};
+
+template <int kMost>
+struct ShPlan {
+    uint32_t cum[kMost + 1];       // own blocks of the sessions before
+    uint16_t pb[kMost];            // blocks that the session shares
+    uint16_t gid[kMost];
+    uint16_t start[kMost + 1];     // of the group's members
+    uint16_t prefix[kMost];        // blocks of the group
+    uint32_t lead[kMost];          // its longest member: length, then lowest rank
+    uint32_t units[kMost + 1];     // units per KV head of the groups before
+    uint16_t segs[kMost + 1];      // tiles per KV head of the groups before
     unsigned scan[2][kShWaves];
-    // The merge of a part's waves
-    float m[kShWaves][kTileRows], l[kShWaves][kTileRows];
-    __attribute__((aligned(16))) f32x4 o[kShWaves][2][D / 16][kWave];
+    float m[kShWaves][16], l[kShWaves][16];       // the merge of a part's waves
 };
 
 // Exclusive prefix sums of two values per thread, and their totals.
@@ -219,123 +225,133 @@ struct ShPart {
     const int32_t *table;          // its table row
     int head;                      // KV head
     int j0, j1;
+    int shortest;                  // every row sees the keys before
     int longest;                   // no row sees a key from here on
 };
 
-// The states of R tiles of 16 rows over the wave's pairs of a part.  row_len: keys
-// that the lane's row of each tile sees, shortest: that all rows see; rows: scores of
-// the tile's first ones are kept.
-template <int D, int R, bool kScores, int kPolicy>
-__device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, const uint16_t *const (&qrow)[R],
-                                     const int (&row_len)[R], int shortest, int rows, float (&m)[R], float (&lsum)[R],
-                                     f32x4 (&o)[R][D / 16]) {
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
-    bf16x8 qop[R][D / 32];
+// State of a tile of 16 rows: row lane % 16, dims 16 dt + 4 (lane / 16) + i.
+template <int D>
+struct RowState {
+    float m, l;
+    f32x4 o[D / 16];
+    __device__ __forceinline__ void clear() {
+        m = kNoMax;
+        l = 0.f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) qop[r][ks] = *reinterpret_cast<const bf16x8 *>(qrow[r] + ks * 32 + g4 * 8);
-        m[r] = kNoMax;
-        lsum[r] = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int dt = 0; dt < D / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int blocks = part.j1 - part.j0, pairs = (blocks + 1) / 2;
+    // Scores x (log2) of a pair's keys: their probabilities as the operand of the second product.
+    __device__ __forceinline__ bf16x8 take(const float (&x)[2][4]) {
+        const float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
+                                fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+        if (__any(top > m + kMaxSlack)) {
+            const float now = fmaxf(m, max_xor_16_32(top));
+            const float alpha = __builtin_amdgcn_exp2f(m - now);
+            l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) o[dt] *= alpha;
+            m = now;
+        }
+        float p[2][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[b][e] = __builtin_amdgcn_exp2f(x[b][e] - m);
+        l += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
+        const u32x4 pb = {pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]),
+                          pack_bf16x2(p[1][2], p[1][3])};
+        return __builtin_bit_cast(bf16x8, pb);
+    }
+};
+
+// Scores of a pair's products, masked where kPartial.
+template <bool kPartial>
+__device__ __forceinline__ void scores_of(const f32x4 (&s)[2], float scale_log2, int tok0, int row_len, const int (&id)[2],
+                                          float (&x)[2][4]) {
+    const int g4 = threadIdx.x % kWave / 16;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[b][e] = s[b][e] * scale_log2;
+            if constexpr (kPartial)
+                if (tok0 + b * kBlock + 4 * g4 + e >= row_len || id[b] < 0) x[b][e] = -INFINITY;
+        }
+}
+// V of a pair's block b: zeros for tokens from `longest` on, and for an absent block.
+// Slots that no row sees may hold anything (NaN included).
+__device__ __forceinline__ u32x2 seen_v(u32x2 v, int tok0, int b, int longest, int id) {
+    const int valid = id < 0 ? 0 : longest - tok0 - b * kBlock - 4 * (int)(threadIdx.x % kWave / 16);
+    const uint32_t lo = valid >= 2 ? 0xFFFFFFFFu : valid == 1 ? 0x0000FFFFu : 0u;
+    const uint32_t hi = valid >= 4 ? 0xFFFFFFFFu : valid == 3 ? 0x0000FFFFu : 0u;
+    return u32x2{v.x & lo, v.y & hi};
+}
+
+// The id of a part's block, or -1 (none, or not in the pool).
+__device__ __forceinline__ int part_id(const SharedArgs &a, const ShPart &part, int j) {
+    if (j >= part.j1) return -1;
+    const int id = part.table[j];
+    if (id >= 0 && id < a.num_blocks) return id;
+    flag_error(a.err, LS_DEVERR_BLOCK_ID);
+    return -1;
+}
+
+// Up to 16 rows: the wave's pairs of the part.  qrow, row_len: of the lane's row.
+template <int D, bool kScores, int kPolicy>
+__device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, const uint16_t *qrow, int row_len,
+                                     RowState<D> &st) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
+    bf16x8 qop[D / 32];
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) qop[ks] = *reinterpret_cast<const bf16x8 *>(qrow + ks * 32 + g4 * 8);
+    st.clear();
+    const int pairs = (part.j1 - part.j0 + 1) / 2;
     const int mine = pairs > wave ? (pairs - wave + kShWaves - 1) / kShWaves : 0;     // pairs of this wave
     const int koff = lane * 16, voff = c16 * kBlock * 2 + g4 * 8;
-    // Ids of the wave's next 32 pairs: lane 2 i + b holds block b of pair i.
-    int ids = -1;
-    auto fetch_ids = [&](int i0) {
-        const int j = part.j0 + 2 * (wave + kShWaves * (i0 + lane / 2)) + lane % 2;
-        int id = -1;
-        if (j < part.j1) {
-            id = part.table[j];
-            if (id < 0 || id >= a.num_blocks) {
-                flag_error(a.err, LS_DEVERR_BLOCK_ID);
-                id = -1;
-            }
-        }
-        ids = id;
-    };
-    auto pair_ids = [&](int i, int (&id)[2]) {
-        id[0] = __builtin_amdgcn_readlane(ids, (2 * i) % kWave);
-        id[1] = __builtin_amdgcn_readlane(ids, (2 * i + 1) % kWave);
-    };
+    int ids = -1;                              // of the wave's next 32 pairs: lane 2 i + b holds block b of pair i
     PairRegs<D> regs[2];
     int id[2][2] = {{-1, -1}, {-1, -1}};
     auto fetch = [&](PairRegs<D> &r, int (&which)[2], int i) {
         if (i >= mine) return;
-        if (i % (kWave / 2) == 0) fetch_ids(i);
-        pair_ids(i, which);
+        if (i % (kWave / 2) == 0) ids = part_id(a, part, part.j0 + 2 * (wave + kShWaves * (i + lane / 2)) + lane % 2);
+        which[0] = __builtin_amdgcn_readlane(ids, (2 * i) % kWave);
+        which[1] = __builtin_amdgcn_readlane(ids, (2 * i + 1) % kWave);
         load_pair<D, kPolicy>(r, a.pool, a.num_kv_heads, part.head, which, koff, voff);
     };
-    auto work = [&](PairRegs<D> &t, const int (&which)[2], int i) {
-        const int tok0 = (part.j0 + 2 * (wave + kShWaves * i)) * kBlock;
-        // A pair some of whose keys some row does not see.
-        const bool partial = tok0 + 2 * kBlock > shortest || which[0] < 0 || which[1] < 0;
-        if (partial) {
-            // Slots that no row sees may hold anything (NaN included): zero their V.
+    auto work_as = [&](PairRegs<D> &t, const int (&which)[2], int tok0, auto partial) {
+        constexpr bool kPartial = decltype(partial)::value;
+        f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int valid = part.longest - tok0 - b * kBlock - 4 * g4;
-                const uint32_t lo = valid >= 2 ? 0xFFFFFFFFu : valid == 1 ? 0x0000FFFFu : 0u;
-                const uint32_t hi = valid >= 4 ? 0xFFFFFFFFu : valid == 3 ? 0x0000FFFFu : 0u;
+        for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) {
-                    t.v[b][dt].x &= lo;
-                    t.v[b][dt].y &= hi;
-                }
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
+            for (int b = 0; b < 2; ++b)
+                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[b][ks]), qop[ks], s[b], 0, 0, 0);
+        float x[2][4];
+        scores_of<kPartial>(s, a.scale_log2, tok0, row_len, which, x);
+        if constexpr (kScores) {
+            if (c16 < a.group)
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
-                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[b][ks]), qop[r][ks], s[b], 0, 0, 0);
-            float x[2][4];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[b][e] = s[b][e] * a.scale_log2;
-                    if (partial && (tok0 + b * kBlock + 4 * g4 + e >= row_len[r] || which[b] < 0)) x[b][e] = -INFINITY;
-                }
-            if constexpr (kScores) {
-                if (c16 < rows)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        if (which[b] >= 0)
-                            *reinterpret_cast<f32x4 *>(a.scores + (((int64_t)which[b] * a.num_kv_heads + part.head) * a.group + c16) * kBlock + 4 * g4) =
-                                f32x4{x[b][0], x[b][1], x[b][2], x[b][3]};
-            }
-            const float top = fmaxf(fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])),
-                                    fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-            if (__any(top > m[r] + kMaxSlack)) {
-                const float now = fmaxf(m[r], max_xor_16_32(top));
-                const float alpha = __builtin_amdgcn_exp2f(m[r] - now);
-                lsum[r] *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < D / 16; ++dt) o[r][dt] *= alpha;
-                m[r] = now;
-            }
-            float p[2][4];
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) p[b][e] = __builtin_amdgcn_exp2f(x[b][e] - m[r]);
-            lsum[r] += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
-            const u32x4 pb = {pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]),
-                              pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])};
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) {
-                const u32x4 va = {t.v[0][dt].x, t.v[0][dt].y, t.v[1][dt].x, t.v[1][dt].y};
-                o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb),
-                                                                   o[r][dt], 0, 0, 0);
-            }
+                    if (!kPartial || which[b] >= 0)
+                        *reinterpret_cast<f32x4 *>(a.scores + (((int64_t)which[b] * a.num_kv_heads + part.head) * a.group + c16) * kBlock + 4 * g4) =
+                            f32x4{x[b][0], x[b][1], x[b][2], x[b][3]};
         }
+        const bf16x8 p = st.take(x);
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            u32x2 v[2] = {t.v[0][dt], t.v[1][dt]};
+            if constexpr (kPartial)
+                for (int b = 0; b < 2; ++b) v[b] = seen_v(v[b], tok0, b, part.longest, which[b]);
+            const u32x4 va = {v[0].x, v[0].y, v[1].x, v[1].y};
+            st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), p, st.o[dt], 0, 0, 0);
+        }
+    };
+    // (A branch around code of its own: as selects in the common code the masks cost as much
+    // as the rest.)
+    auto work = [&](PairRegs<D> &t, const int (&which)[2], int i) {
+        const int tok0 = (part.j0 + 2 * (wave + kShWaves * i)) * kBlock;
+        if (tok0 + 2 * kBlock > part.shortest || which[0] < 0 || which[1] < 0) work_as(t, which, tok0, std::true_type());
+        else work_as(t, which, tok0, std::false_type());
     };
     fetch(regs[0], id[0], 0);
     for (int i = 0; i < mine; i += 2) {
@@ -345,8 +361,7 @@ __device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, co
         fetch(regs[0], id[0], i + 2);
         work(regs[1], id[1], i + 1);
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r) lsum[r] = sum_xor_16_32(lsum[r]);
+    st.l = sum_xor_16_32(st.l);
 }
 
 // Where a part's state goes.
@@ -357,63 +372,158 @@ struct ShSink {
     int rows;
 };
 
-// Adds the waves' states up and writes them.
-template <int D, int R>
-__device__ __forceinline__ void merge(ShLds<D> &sm, const float (&m)[R], const float (&lsum)[R],
-                                      const f32x4 (&o)[R][D / 16], const ShSink &sink) {
+// Adds the waves' states of 16 rows up and writes them.
+template <int D, int kMost>
+__device__ __forceinline__ void merge(ShPlan<kMost> &sm, PairLds<D> &b0, PairLds<D> &b1, const RowState<D> &st, const ShSink &sink) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
-    constexpr int kHalf = R < 2 ? R : 2;       // tiles at a time
-    if (g4 == 0)
+    // [wave % 2][D / 16][64] of 16 bytes, waves 0 and 1 in b0
+    auto slot = [&](int w, int dt) {
+        return reinterpret_cast<f32x4 *>(w < 2 ? b0.tile[0] : b1.tile[0]) + (w % 2 * (D / 16) + dt) * kWave + lane;
+    };
+    static_assert(sizeof(PairLds<D>) == 2 * (D / 16) * kWave * sizeof(f32x4), "two waves a buffer");
+    if (g4 == 0) {
+        sm.m[wave][c16] = st.m;
+        sm.l[wave][c16] = st.l;
+    }
+    if (c16 < sink.rows)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            sm.m[wave][r * 16 + c16] = m[r];
-            sm.l[wave][r * 16 + c16] = lsum[r];
+        for (int dt = 0; dt < D / 16; ++dt) *slot(wave, dt) = st.o[dt];
+    __syncthreads();
+    if (c16 < sink.rows) {
+        float top = kNoMax, e[kShWaves], l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kShWaves; ++w) top = fmaxf(top, sm.m[w][c16]);
+#pragma unroll
+        for (int w = 0; w < kShWaves; ++w) {
+            e[w] = __builtin_amdgcn_exp2f(sm.m[w][c16] - top);
+            l += e[w] * sm.l[w][c16];
         }
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
-    for (int r0 = 0; r0 < R; r0 += kHalf) {
-        if (r0) __syncthreads();               // the half before has been read
+        for (int k = 0; k < D / 16 / kShWaves; ++k) {
+            const int dt = wave + k * kShWaves, at = c16 * D + dt * 16 + 4 * g4;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < kHalf; ++r)
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) sm.o[wave][r][dt][lane] = o[r0 + r][dt];
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kHalf; ++r) {
-            const int row = (r0 + r) * 16 + c16;
-            float top = kNoMax, e[kShWaves], l = 0.f;
-#pragma unroll
-            for (int w = 0; w < kShWaves; ++w) top = fmaxf(top, sm.m[w][row]);
-#pragma unroll
-            for (int w = 0; w < kShWaves; ++w) {
-                e[w] = __builtin_amdgcn_exp2f(sm.m[w][row] - top);
-                l += e[w] * sm.l[w][row];
-            }
-            const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-#pragma unroll
-            for (int k = 0; k < D / 16 / kShWaves; ++k) {
-                const int dt = wave + k * kShWaves;
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int w = 0; w < kShWaves; ++w) x += sm.o[w][r][dt][lane] * e[w];
-                if (row < sink.rows) {
-                    const int at = row * D + dt * 16 + 4 * g4;
-                    if (sink.acc) *reinterpret_cast<f32x4 *>(sink.acc + at) = x;
-                    else *reinterpret_cast<uint2 *>(sink.out + at) =
-                        make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
-                }
-            }
-            if (sink.ml && wave == 0 && g4 == 0 && row < sink.rows) {
-                sink.ml[2 * row] = top;
-                sink.ml[2 * row + 1] = l;
-            }
+            for (int w = 0; w < kShWaves; ++w) x += *slot(w, dt) * e[w];
+            if (sink.acc) *reinterpret_cast<f32x4 *>(sink.acc + at) = x;
+            else *reinterpret_cast<uint2 *>(sink.out + at) =
+                make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+        }
+        if (sink.ml && wave == 0 && g4 == 0) {
+            sink.ml[2 * c16] = top;
+            sink.ml[2 * c16 + 1] = l;
         }
     }
-    __syncthreads();                           // the next part writes sm again
+    __syncthreads();                           // the next part writes there again
 }
 
-template <int D, bool kWeights>
-__global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
-    __shared__ ShLds<D> sm;
+// More rows: tiles `wave` and `wave` + 4 of 16 of them are this wave's (count of them),
+// and every pair of the part goes through LDS.
+template <int D>
+__device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &part, PairLds<D> &b0, PairLds<D> &b1, PairLds<D> &b2,
+                                          const uint16_t *const (&qrow)[2], const int (&row_len)[2], int count, float *ml, float *acc,
+                                          int rows) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
+    constexpr int kLoads = kBlock * D * 2 / 1024;        // of a tile, a kilobyte each
+    bf16x8 qop[2][D / 32];
+    RowState<D> st[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) qop[r][ks] = *reinterpret_cast<const bf16x8 *>(qrow[r] + ks * 32 + g4 * 8);
+        st[r].clear();
+    }
+    const int pairs = (part.j1 - part.j0 + 1) / 2;
+    int ids_load = -1, ids_work = -1;          // of 64 blocks, for the pair being loaded and the one at work
+    // Tile `wave` of pair i: K, K, V, V.  (Behind the last pair nothing is fetched; the loads count all the same.)
+    auto load = [&](PairLds<D> &to, int i) {
+        if (i % (kWave / 2) == 0) ids_load = part_id(a, part, part.j0 + 2 * i + lane);
+        const int id = i < pairs ? __builtin_amdgcn_readlane(ids_load, (2 * i + wave % 2) % kWave) : -1;
+        const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, id, wave >= 2);
+#pragma unroll
+        for (int kb = 0; kb < kLoads; ++kb)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(to.tile[wave] + kb * 1024), 16, lane * 16, kb * 1024, 0, 0);
+    };
+    auto barrier = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0070 | kLoads);     // vmcnt: all but the last pair's; lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto work_as = [&](PairLds<D> &t, const int (&which)[2], int tok0, auto partial) {
+        constexpr bool kPartial = decltype(partial)::value;
+        f32x4 s[2][2] = {};
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) {
+                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(t.tile[b] + ks * 1024 + lane * 16);
+#pragma unroll
+                for (int r = 0; r < 2; ++r) s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[r][ks], s[r][b], 0, 0, 0);
+            }
+        bf16x8 p[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float x[2][4];
+            scores_of<kPartial>(s[r], a.scale_log2, tok0, row_len[r], which, x);
+            p[r] = st[r].take(x);
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            u32x2 v[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                v[b] = *reinterpret_cast<const u32x2 *>(t.tile[2 + b] + (dt * 16 + c16) * kBlock * 2 + g4 * 8);
+                if constexpr (kPartial) v[b] = seen_v(v[b], tok0, b, part.longest, which[b]);
+            }
+            const u32x4 va = {v[0].x, v[0].y, v[1].x, v[1].y};
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                st[r].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), p[r], st[r].o[dt], 0, 0, 0);
+        }
+    };
+    auto stage = [&](int i, PairLds<D> &t, PairLds<D> &ahead) {
+        load(ahead, i + 2);
+        if (count) {
+            if (i % (kWave / 2) == 0) ids_work = part_id(a, part, part.j0 + 2 * i + lane);
+            const int which[2] = {__builtin_amdgcn_readlane(ids_work, (2 * i) % kWave), __builtin_amdgcn_readlane(ids_work, (2 * i + 1) % kWave)};
+            const int tok0 = (part.j0 + 2 * i) * kBlock;
+            if (tok0 + 2 * kBlock > part.shortest || which[0] < 0 || which[1] < 0) work_as(t, which, tok0, std::true_type());
+            else work_as(t, which, tok0, std::false_type());
+        }
+        barrier();
+    };
+    load(b0, 0);
+    load(b1, 1);
+    barrier();
+    for (int i = 0;;) {
+        stage(i, b0, b2);
+        if (++i >= pairs) break;
+        stage(i, b1, b0);
+        if (++i >= pairs) break;
+        stage(i, b2, b1);
+        if (++i >= pairs) break;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): no load lands in what the next part writes
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = (wave + r * kShWaves) * 16 + c16;
+        const float l = sum_xor_16_32(st[r].l);
+        if (row < rows) {
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4 *>(acc + (int64_t)row * D + dt * 16 + 4 * g4) = st[r].o[dt];
+            if (g4 == 0) *reinterpret_cast<float2 *>(ml + 2 * row) = make_float2(st[r].m, l);
+        }
+    }
+    __syncthreads();
+}
+
+template <int D, int kMost, bool kWeights>
+__global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs a) {
+    __shared__ ShPlan<kMost> sm;
+    __shared__ PairLds<D> b0, b1, b2;
+    int32_t *const owner = reinterpret_cast<int32_t *>(b0.tile[0]);       // a session's place among the members, or -1
+    static_assert(kShMost * 4 <= sizeof(PairLds<D>), "owners fit a buffer");
     const int tid = threadIdx.x, lane = tid % kWave, c16 = lane % 16;
     const int S = a.num_sessions, G = a.group, H = a.num_kv_heads;
     const bool first_wg = blockIdx.x == 0;
@@ -425,16 +535,15 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
         const int x = a.starts[g], y = a.starts[g + 1], pb = a.prefix[g];
         bad = bad || x < 0 || y < x || y > a.num_members || pb < 0 || pb > a.max_blocks || (g == 0 && x != 0) ||
               (g == ng - 1 && y != a.num_members);
-        sm.start[g] = x;
-        sm.start[g + 1] = y;                   // (the same value from two threads)
-        sm.prefix[g] = pb;
+        sm.start[g] = (uint16_t)x;
+        sm.start[g + 1] = (uint16_t)y;         // (the same value from two threads)
+        sm.prefix[g] = (uint16_t)pb;
         sm.lead[g] = 0u;
     }
     for (int s = tid; s < S; s += kShThreads) {
-        sm.owner[s] = -1;
-        const int raw = a.lens[s], cap = a.max_blocks * kBlock;
-        if (first_wg && (raw < 0 || raw > cap)) flag_error(a.err, LS_DEVERR_LENGTH);
-        sm.len[s] = max(min(raw, cap), 0);
+        owner[s] = -1;
+        const int raw = a.lens[s];
+        if (first_wg && (raw < 0 || raw > a.max_blocks * kBlock)) flag_error(a.err, LS_DEVERR_LENGTH);
     }
     bad = __syncthreads_or(bad);
     if (ng && !bad) {
@@ -445,15 +554,16 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
                 wrong = true;
                 continue;
             }
-            int lo = 0, hi = ng;                // the last group that starts at or before i and has it
+            const int len = keys_of(a, s);
+            int lo = 0, hi = ng;               // the last group that starts at or before i
             while (hi - lo > 1) {
                 const int mid = (lo + hi) / 2;
                 if (sm.start[mid] <= i) lo = mid;
                 else hi = mid;
             }
-            if (atomicExch(&sm.owner[s], i) != -1) wrong = true;
+            if (atomicExch(&owner[s], i) != -1) wrong = true;
             sm.gid[s] = (uint16_t)lo;
-            atomicMax(&sm.lead[lo], (uint32_t)sm.len[s] << kRank | (uint32_t)(kShBatch - 1 - (i - sm.start[lo])));
+            atomicMax(&sm.lead[lo], (uint32_t)len << kRank | (uint32_t)(kShMost - 1 - (i - sm.start[lo])));
         }
         bad = __syncthreads_or(wrong);
     }
@@ -462,76 +572,71 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
         if (first_wg && tid == 0) flag_error(a.err, LS_DEVERR_GROUP);
         ng = 0;
         __syncthreads();
-        for (int s = tid; s < S; s += kShThreads) sm.owner[s] = -1;
-        __syncthreads();
+        for (int s = tid; s < S; s += kShThreads) owner[s] = -1;
     }
     {
         const int per = (ng + kShThreads - 1) / kShThreads;
         unsigned v[2] = {0, 0}, all[2];
         for (int g = tid * per; g < min(ng, (tid + 1) * per); ++g) {
             const int rows = (sm.start[g + 1] - sm.start[g]) * G, longest = (int)(sm.lead[g] >> kRank);
-            const int pb = min(sm.prefix[g], (longest + kBlock - 1) / kBlock);
-            sm.prefix[g] = pb;
-            sm.gunits[g] = (unsigned)(group_cost(rows) * pb);
-            sm.gsegs[g] = (unsigned)((rows + kTileRows - 1) / kTileRows);
-            v[0] += sm.gunits[g];
-            v[1] += sm.gsegs[g];
+            const int pb = min((int)sm.prefix[g], (longest + kBlock - 1) / kBlock);
+            sm.prefix[g] = (uint16_t)pb;
+            v[0] += (unsigned)(group_cost(rows) * pb);
+            v[1] += (unsigned)((rows + kTileRows - 1) / kTileRows);
         }
-        scan2(v, all, sm.scan);
+        if (ng) scan2(v, all, sm.scan);
+        else all[0] = all[1] = 0u;
         for (int g = tid * per; g < min(ng, (tid + 1) * per); ++g) {
-            const unsigned u = sm.gunits[g], t = sm.gsegs[g];
-            sm.gunits[g] = v[0];
-            sm.gsegs[g] = v[1];
-            v[0] += u;
-            v[1] += t;
+            const int rows = (sm.start[g + 1] - sm.start[g]) * G;
+            sm.units[g] = v[0];
+            sm.segs[g] = (uint16_t)v[1];
+            v[0] += (unsigned)(group_cost(rows) * sm.prefix[g]);
+            v[1] += (unsigned)((rows + kTileRows - 1) / kTileRows);
         }
         if (tid == 0) {
-            sm.gunits[ng] = all[0];
-            sm.gsegs[ng] = all[1];
+            sm.units[ng] = all[0];
+            sm.segs[ng] = (uint16_t)all[1];
         }
     }
     __syncthreads();
     {
         const int per = (S + kShThreads - 1) / kShThreads;
         unsigned v[2] = {0, 0}, all[2];
-        auto own = [&](int s) {
-            const int pb = sm.owner[s] >= 0 ? sm.prefix[sm.gid[s]] : 0;
-            return max((sm.len[s] + kBlock - 1) / kBlock - pb, 0);
-        };
-        for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) v[0] += (unsigned)own(s);
+        auto own = [&](int s, int pb) { return (unsigned)max((keys_of(a, s) + kBlock - 1) / kBlock - pb, 0); };
+        for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) {
+            sm.pb[s] = owner[s] >= 0 ? sm.prefix[sm.gid[s]] : (uint16_t)0;
+            v[0] += own(s, sm.pb[s]);
+        }
         scan2(v, all, sm.scan);
         for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) {
             sm.cum[s] = v[0];
-            v[0] += (unsigned)own(s);
+            v[0] += own(s, sm.pb[s]);
         }
         if (tid == 0) sm.cum[S] = all[0];
     }
     __syncthreads();
-    const int64_t own_base = (int64_t)H * sm.gunits[ng];
-    const int64_t units = own_base + (int64_t)H * sm.cum[S] * kCostOwn;
-    int64_t share = (units + gridDim.x - 1) / gridDim.x;
-    if (share < kLeastUnits) share = kLeastUnits;
     if (first_wg) {
-        if (tid == 0) *a.header = ShHeader{share, own_base, (int64_t)sm.cum[S], 0};
         for (int s = tid; s < S; s += kShThreads) {
             ShRecord r = {};
             r.own_blocks = (int)(sm.cum[s + 1] - sm.cum[s]);
-            r.own_pos = own_base + (int64_t)H * sm.cum[s] * kCostOwn;
-            r.keys = sm.len[s];
-            if (sm.owner[s] >= 0) {
-                const int g = sm.gid[s], rows = (sm.start[g + 1] - sm.start[g]) * G, row = (sm.owner[s] - sm.start[g]) * G;
-                const int tile = row / kTileRows;
+            r.own_before = sm.cum[s];
+            r.own_all = sm.cum[S];
+            r.keys = keys_of(a, s);
+            if (owner[s] >= 0) {
+                const int g = sm.gid[s], row = (owner[s] - sm.start[g]) * G;
                 r.prefix_blocks = sm.prefix[g];
-                r.tile_pos = (int64_t)H * sm.gunits[g] + (int64_t)tile * kCostTile4 * sm.prefix[g];
-                r.tile_stride = sm.gunits[g + 1] - sm.gunits[g];
-                r.tile_seg = (int)(H * sm.gsegs[g]) + tile;
-                r.tile_seg_stride = (int)(sm.gsegs[g + 1] - sm.gsegs[g]);
+                r.tile_seg = H * sm.segs[g] + row / kTileRows;
+                r.tile_seg_stride = sm.segs[g + 1] - sm.segs[g];
                 r.tile_row = row % kTileRows;
-                r.tile_cost = tile_cost(min(kTileRows, rows - tile * kTileRows));
             }
             a.records[s] = r;
         }
     }
+    __syncthreads();                           // the buffer of the owners is used again
+    const int64_t own_base = (int64_t)H * sm.units[ng];
+    const int64_t units = own_base + (int64_t)H * sm.cum[S] * kCostOwn;
+    int64_t share = (units + gridDim.x - 1) / gridDim.x;
+    if (share < kLeastUnits) share = kLeastUnits;
     // Consecutive shares on one XCD: the tiles of a group and KV head read the same K and V.
     const int W = gridDim.x;
     const int w = W % 8 == 0 ? (int)(blockIdx.x % 8) * (W / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
@@ -547,54 +652,65 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
         int g = 0, hi = ng;
         while (hi - g > 1) {
             const int mid = (g + hi) / 2;
-            if ((int64_t)H * sm.gunits[mid] <= at) g = mid;
+            if ((int64_t)H * sm.units[mid] <= at) g = mid;
             else hi = mid;
         }
-        for (; g < ng && (int64_t)H * sm.gunits[g] < min(u1, own_base); ++g) {
-            const int64_t stride = sm.gunits[g + 1] - sm.gunits[g];
+        for (; g < ng && (int64_t)H * sm.units[g] < min(u1, own_base); ++g) {
+            const int64_t stride = sm.units[g + 1] - sm.units[g];
             if (!stride) continue;
-            const int pb = sm.prefix[g], rows = (sm.start[g + 1] - sm.start[g]) * G, tiles = (rows + kTileRows - 1) / kTileRows;
-            const int64_t gpos = (int64_t)H * sm.gunits[g];
-            const int lead = kShBatch - 1 - (int)(sm.lead[g] & (kShBatch - 1));
-            const int lead_s = a.members[sm.start[g] + lead];
+            const int pb = sm.prefix[g], first = sm.start[g], rows = (sm.start[g + 1] - first) * G;
+            const int tiles = (rows + kTileRows - 1) / kTileRows;
+            const int64_t gpos = (int64_t)H * sm.units[g];
+            const int lead_s = a.members[first + kShMost - 1 - (int)(sm.lead[g] & (kShMost - 1))];
             for (int h = at > gpos ? (int)((at - gpos) / stride) : 0; h < H && gpos + h * stride < u1; ++h) {
                 const int64_t hpos = gpos + h * stride;
-                for (int t = at > hpos ? (int)((at - hpos) / ((int64_t)pb * kCostTile4)) : 0; t < tiles; ++t) {
-                    const int64_t pos = hpos + (int64_t)t * pb * kCostTile4;
+                for (int t = at > hpos ? (int)((at - hpos) / ((int64_t)pb * kCostTile)) : 0; t < tiles; ++t) {
+                    const int64_t pos = hpos + (int64_t)t * pb * kCostTile;
                     if (pos >= u1) break;
-                    const int n = min(kTileRows, rows - t * kTileRows), cost = tile_cost(n);
+                    const int n = min(kTileRows, rows - t * kTileRows);
                     ShPart part;
-                    range(pos, pb, cost, part.j0, part.j1);
+                    range(pos, pb, tile_cost(n), part.j0, part.j1);
                     if (part.j0 >= part.j1) continue;
                     part.table = a.tables + (int64_t)lead_s * a.max_blocks;
                     part.head = h;
                     part.longest = (int)(sm.lead[g] >> kRank);
-                    const int64_t slot = (int64_t)H * sm.gsegs[g] + (int64_t)h * tiles + t + w;
-                    const ShSink sink = {a.tile_ml + slot * kTileRows * 2, a.tile_acc + slot * kTileRows * D, nullptr, n};
-                    auto run = [&](auto tag) {
-                        constexpr int R = decltype(tag)::value;
-                        const uint16_t *qrow[R];
-                        int row_len[R], shortest = INT32_MAX;
-#pragma unroll
-                        for (int r = 0; r < R; ++r) {
-                            // (lanes of no row take the last one: a load under a condition waits for the one before)
-                            const int row = t * kTileRows + min(r * 16 + c16, n - 1);
-                            const int s = a.members[sm.start[g] + (row >> gs)];
-                            qrow[r] = a.q + ((int64_t)s * H * G + h * G + (row & (G - 1))) * D;
-                            row_len[r] = sm.len[s];
-                            shortest = min(shortest, row_len[r]);
-                        }
-#pragma unroll
-                        for (int off = 1; off < 16; off <<= 1) shortest = min(shortest, __shfl_xor(shortest, off));
-                        shortest = __builtin_amdgcn_readfirstlane(shortest);
-                        float m[R], lsum[R];
-                        f32x4 o[R][D / 16];
-                        walk<D, R, false, 0>(a, part, qrow, row_len, shortest, n, m, lsum, o);
-                        merge<D, R>(sm, m, lsum, o, sink);
+                    const int seg = H * sm.segs[g] + h * tiles + t;
+                    const int64_t slot = (int64_t)seg + w;
+                    float *ml = a.tile_ml + slot * kTileRows * 2, *acc = a.tile_acc + slot * kTileRows * D;
+                    if (tid == 0) {
+                        if (part.j0 == 0) a.tile_first[seg] = w;
+                        if (part.j1 == pb) a.tile_last[seg] = w;
+                    }
+                    // (lanes of no row take the last one: a load under a condition waits for the one before)
+                    auto row_of = [&](int row, const uint16_t *&qrow, int &len) {
+                        const int x = t * kTileRows + min(row, n - 1), s = a.members[first + (x >> gs)];
+                        qrow = a.q + ((int64_t)s * H * G + h * G + (x & (G - 1))) * D;
+                        len = keys_of(a, s);
                     };
-                    if (n <= 16) run(std::integral_constant<int, 1>{});
-                    else if (n <= 32) run(std::integral_constant<int, 2>{});
-                    else run(std::integral_constant<int, 4>{});
+                    if (n <= 16) {
+                        const uint16_t *qrow;
+                        int len;
+                        row_of(c16, qrow, len);
+                        part.shortest = len;
+#pragma unroll
+                        for (int off = 1; off < 16; off <<= 1) part.shortest = min(part.shortest, __shfl_xor(part.shortest, off));
+                        part.shortest = __builtin_amdgcn_readfirstlane(part.shortest);
+                        RowState<D> st;
+                        walk<D, false, 0>(a, part, qrow, len, st);
+                        merge<D>(sm, b0, b1, st, ShSink{ml, acc, nullptr, n});
+                    } else {
+                        const int wave = tid / kWave;
+                        const uint16_t *qrow[2];
+                        int len[2];
+                        row_of(wave * 16 + c16, qrow[0], len[0]);
+                        row_of((wave + kShWaves) * 16 + c16, qrow[1], len[1]);
+                        part.shortest = min(len[0], len[1]);
+#pragma unroll
+                        for (int off = 1; off < 16; off <<= 1) part.shortest = min(part.shortest, __shfl_xor(part.shortest, off));
+                        part.shortest = __builtin_amdgcn_readfirstlane(part.shortest);
+                        const int count = (wave * 16 < n) + ((wave + kShWaves) * 16 < n);
+                        tile_walk<D>(a, part, b0, b1, b2, qrow, len, count, ml, acc, n);
+                    }
                 }
             }
         }
@@ -614,7 +730,7 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
             if (spos >= u1) break;
             const int nb = (int)(sm.cum[s + 1] - sm.cum[s]);
             if (!nb) continue;
-            const int pb = sm.owner[s] >= 0 ? sm.prefix[sm.gid[s]] : 0, L = sm.len[s];
+            const int pb = sm.pb[s], L = keys_of(a, s);
             const int64_t stride = (int64_t)nb * kCostOwn;
             for (int h = at > spos ? (int)((at - spos) / stride) : 0; h < H; ++h) {
                 const int64_t pos = spos + h * stride;
@@ -622,66 +738,43 @@ __global__ __launch_bounds__(kShThreads) void shared_kernel(SharedArgs a) {
                 int j0, j1;
                 range(pos, nb, kCostOwn, j0, j1);
                 if (j0 >= j1) continue;
-                ShPart part = {a.tables + (int64_t)s * a.max_blocks, h, pb + j0, pb + j1, L};
+                const ShPart part = {a.tables + (int64_t)s * a.max_blocks, h, pb + j0, pb + j1, L, L};
                 const bool whole = !pb && j0 == 0 && j1 == nb;
-                const int64_t slot = (int64_t)s * H + h + w;
-                const int64_t row0 = (int64_t)s * H * G + h * G;
+                const int seg = s * H + h;
+                const int64_t slot = (int64_t)seg + w, row0 = (int64_t)seg * G;
+                if (tid == 0) {
+                    if (j0 == 0) a.own_first[seg] = w;
+                    if (j1 == nb) a.own_last[seg] = w;
+                }
                 const ShSink sink = {!whole || kWeights ? a.own_ml + slot * G * 2 : nullptr, whole ? nullptr : a.own_acc + slot * G * D,
                                      a.out + row0 * D, G};
-                const uint16_t *qrow[1] = {a.q + (row0 + min(c16, G - 1)) * D};
-                const int row_len[1] = {L};
-                float m[1], lsum[1];
-                f32x4 o[1][D / 16];
-                walk<D, 1, kWeights, kStream>(a, part, qrow, row_len, L, G, m, lsum, o);
-                merge<D, 1>(sm, m, lsum, o, sink);
+                RowState<D> st;
+                walk<D, kWeights, kStream>(a, part, a.q + (row0 + min(c16, G - 1)) * D, L, st);
+                merge<D>(sm, b0, b1, st, sink);
             }
         }
     }
 }
 
-// Calls f(slot, part workgroup) for every part of a segment's blocks.
-template <typename F>
-__device__ __forceinline__ void each_part(int64_t share, int64_t pos, int blocks, int cost, int64_t seg, F f) {
-    const int64_t end = pos + (int64_t)blocks * cost;
-    for (int64_t w = pos / share; w * share < end; ++w) {
-        const int64_t lo = w * share - pos, hi = lo + share;
-        const int64_t j0 = lo > 0 ? (lo + cost - 1) / cost : 0, j1 = hi >= (int64_t)blocks * cost ? blocks : (hi + cost - 1) / cost;
-        if (j0 < j1) f(seg + w);
+// The parts of a row: those of its prefix tile, then its own.
+struct RowParts {
+    int prefix, own;               // how many
+    int64_t prefix_row, own_row;   // rows of the first ones in tile_ml, own_ml
+};
+__device__ __forceinline__ RowParts parts_of(const SharedArgs &a, const ShRecord &r, int s, int h, int head) {
+    RowParts p = {0, 0, 0, 0};
+    const int seg = s * a.num_kv_heads + h, tile = r.tile_seg + h * r.tile_seg_stride;
+    if (r.prefix_blocks) {
+        const int w = a.tile_first[tile];
+        p.prefix = a.tile_last[tile] - w + 1;
+        p.prefix_row = ((int64_t)tile + w) * kTileRows + r.tile_row + head;
     }
-}
-
-// Row state of (session, query head): top is the largest maximum, sum the whole sum.
-template <typename F>
-__device__ __forceinline__ void row_state(const SharedArgs &a, const ShRecord &r, int64_t share, int s, int h, int head,
-                                          float &top, float &sum, F f) {
-    // f(ml, acc row index or such) is called for every part in a fixed order, twice.
-    top = kNoMax;
-    sum = 0.f;
-    const int H = a.num_kv_heads, G = a.group;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-        auto visit = [&](const float *ml, int64_t acc_row, bool tile) {
-            if (pass == 0) {
-                top = fmaxf(top, ml[0]);
-            } else {
-                const float e = __builtin_amdgcn_exp2f(ml[0] - top);
-                sum += e * ml[1];
-                f(e, acc_row, tile);
-            }
-        };
-        if (r.prefix_blocks)
-            each_part(share, r.tile_pos + h * r.tile_stride, r.prefix_blocks, r.tile_cost,
-                      (int64_t)r.tile_seg + (int64_t)h * r.tile_seg_stride, [&](int64_t slot) {
-                          const int64_t row = slot * kTileRows + r.tile_row + head;
-                          visit(a.tile_ml + row * 2, row, true);
-                      });
-        if (r.own_blocks)
-            each_part(share, r.own_pos + (int64_t)h * r.own_blocks * kCostOwn, r.own_blocks, kCostOwn, (int64_t)s * H + h,
-                      [&](int64_t slot) {
-                          const int64_t row = slot * G + head;
-                          visit(a.own_ml + row * 2, row, false);
-                      });
+    if (r.own_blocks) {
+        const int w = a.own_first[seg];
+        p.own = a.own_last[seg] - w + 1;
+        p.own_row = ((int64_t)seg + w) * a.group + head;
     }
+    return p;
 }
 
 // Workgroups below `combine` add up rows of the output, D / 4 threads a row; the
@@ -689,36 +782,59 @@ __device__ __forceinline__ void row_state(const SharedArgs &a, const ShRecord &r
 // weights, four threads a (block, KV head).
 template <int D, bool kWeights>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, int combine) {
-    __shared__ uint32_t sm_cum[kWeights ? kShBatch + 1 : 1];
+    __shared__ uint32_t sm_cum[kWeights ? kShMost + 1 : 1];
     __shared__ float sm_top[8], sm_inv[8];
     const int tid = threadIdx.x, H = a.num_kv_heads, G = a.group, S = a.num_sessions;
-    const ShHeader head = *a.header;
     if ((int)blockIdx.x < combine) {
-        constexpr int kLanes = D / 4;
+        constexpr int kLanes = D / 4, kAhead = 8;
         const int64_t row = (int64_t)blockIdx.x * (kShThreads / kLanes) + tid / kLanes;
         if (row >= (int64_t)S * H * G) return;
         const int s = (int)(row / (H * G)), h = (int)(row % (H * G)) / G, e4 = tid % kLanes * 4;
         const ShRecord r = a.records[s];
-        if (r.own_blocks && !r.prefix_blocks) {
-            // written already, if the workgroup that has its first block has the last one too
-            const int64_t pos = r.own_pos + (int64_t)h * r.own_blocks * kCostOwn;
-            if ((pos / head.share + 1) * head.share - pos > (int64_t)(r.own_blocks - 1) * kCostOwn) return;
-        }
-        float top, sum;
+        const RowParts n = parts_of(a, r, s, h, (int)(row % G));
+        if (n.own == 1 && !n.prefix) return;               // written already
+        // kAhead parts at a time, so that their loads are in flight together
+        float top = kNoMax, sum = 0.f;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        row_state(a, r, head.share, s, h, (int)(row % G), top, sum, [&](float e, int64_t at, bool tile) {
-            x += *reinterpret_cast<const f32x4 *>((tile ? a.tile_acc : a.own_acc) + at * D + e4) * e;
-        });
+        const int parts = n.prefix + n.own;
+        for (int i0 = 0; i0 < parts; i0 += kAhead) {
+            float2 ml[kAhead];
+            f32x4 o[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int i = min(i0 + k, parts - 1);
+                const bool tile = i < n.prefix;
+                const int64_t at = tile ? n.prefix_row + (int64_t)i * kTileRows : n.own_row + (int64_t)(i - n.prefix) * G;
+                ml[k] = reinterpret_cast<const float2 *>(tile ? a.tile_ml : a.own_ml)[at];
+                o[k] = *reinterpret_cast<const f32x4 *>((tile ? a.tile_acc : a.own_acc) + at * D + e4);
+            }
+            float now = top;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) now = fmaxf(now, ml[k].x);
+            const float old = __builtin_amdgcn_exp2f(top - now);
+            sum *= old;
+            x *= old;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const float e = i0 + k < parts ? __builtin_amdgcn_exp2f(ml[k].x - now) : 0.f;
+                if (i0 + k < parts) {
+                    sum += e * ml[k].y;
+                    x += o[k] * e;
+                }
+            }
+            top = now;
+        }
         const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
         *reinterpret_cast<uint2 *>(a.out + row * D + e4) =
             make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
         return;
     }
     if constexpr (kWeights) {
-        for (int s = tid; s < S; s += kShThreads) sm_cum[s] = (uint32_t)((a.records[s].own_pos - head.own_base) / kCostOwn / H);
-        if (tid == 0) sm_cum[S] = (uint32_t)head.own_units;
+        for (int s = tid; s < S; s += kShThreads) sm_cum[s] = a.records[s].own_before;
+        const uint32_t own_all = a.records[0].own_all;
+        if (tid == 0) sm_cum[S] = own_all;
         __syncthreads();
-        const int64_t all = head.own_units * H, n = gridDim.x - combine, w = blockIdx.x - combine;
+        const int64_t all = (int64_t)own_all * H, n = gridDim.x - combine, w = blockIdx.x - combine;
         int64_t per = (all + n - 1) / n;
         per = max(per, (int64_t)(kShThreads / 4));
         const int64_t b0 = w * per, b1 = min(b0 + per, all);
@@ -740,11 +856,29 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
                 const int64_t pos = spos + (int64_t)h * r.own_blocks;
                 if (pos >= b1) break;
                 __syncthreads();                                     // the segment before is done with sm_top
-                if (tid < G) {
-                    float top, sum;
-                    row_state(a, r, head.share, s, h, tid, top, sum, [](float, int64_t, bool) {});
-                    sm_top[tid] = top;
-                    sm_inv[tid] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                if (tid < kWave) {
+                    // lane = (part, query head), eight parts at a time
+                    const int head = tid % 8, lane_part = tid / 8;
+                    const RowParts p = parts_of(a, r, s, h, min(head, G - 1));
+                    float top = kNoMax, sum = 0.f;
+                    for (int i = lane_part; i < p.prefix + p.own; i += kWave / 8) {
+                        const bool tile = i < p.prefix;
+                        const int64_t at = tile ? p.prefix_row + (int64_t)i * kTileRows : p.own_row + (int64_t)(i - p.prefix) * G;
+                        const float2 ml = reinterpret_cast<const float2 *>(tile ? a.tile_ml : a.own_ml)[at];
+                        const float now = fmaxf(top, ml.x);
+                        sum = sum * __builtin_amdgcn_exp2f(top - now) + ml.y * __builtin_amdgcn_exp2f(ml.x - now);
+                        top = now;
+                    }
+#pragma unroll
+                    for (int off = 8; off < kWave; off <<= 1) {
+                        const float t2 = __shfl_xor(top, off), s2 = __shfl_xor(sum, off), now = fmaxf(top, t2);
+                        sum = sum * __builtin_amdgcn_exp2f(top - now) + s2 * __builtin_amdgcn_exp2f(t2 - now);
+                        top = now;
+                    }
+                    if (tid < G) {
+                        sm_top[tid] = top;
+                        sm_inv[tid] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+                    }
                 }
                 __syncthreads();
                 const int j0 = (int)max(b0 - pos, (int64_t)0), j1 = (int)min(b1 - pos, (int64_t)r.own_blocks);
@@ -753,14 +887,18 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
                     const int id = a.tables[(int64_t)s * a.max_blocks + col];
                     if (id < 0 || id >= a.num_blocks || t0 >= r.keys || t0 + 4 <= first) continue;
                     const float *x = a.scores + ((int64_t)id * H + h) * G * kBlock + tid % 4 * 4;
-                    f32x4 p = {0.f, 0.f, 0.f, 0.f};
-                    for (int k = 0; k < G; ++k) {
-                        const f32x4 y = *reinterpret_cast<const f32x4 *>(x + k * kBlock);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) p[e] += __builtin_amdgcn_exp2f(y[e] - sm_top[k]) * sm_inv[k];
-                    }
                     const int64_t at = ((int64_t)id * H + h) * kBlock + tid % 4 * 4;
                     const f32x4 was = *reinterpret_cast<const f32x4 *>(a.weights + at);
+                    f32x4 p = {0.f, 0.f, 0.f, 0.f};
+                    f32x4 y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = *reinterpret_cast<const f32x4 *>(x + min(k, G - 1) * kBlock);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < G) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) p[e] += __builtin_amdgcn_exp2f(y[k][e] - sm_top[k]) * sm_inv[k];
+                        }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int t = t0 + e;
@@ -778,15 +916,21 @@ template <int D>
 hipError_t launch_shared_t(const SharedArgs &a, int grid, hipStream_t stream) {
     const int64_t rows = (int64_t)a.num_sessions * a.num_kv_heads * a.group;
     const int combine = (int)((rows + kShThreads / (D / 4) - 1) / (kShThreads / (D / 4)));
+    const bool few = a.num_sessions <= kShFew;               // (members and groups are no more)
+#define LS_SHARED(MOST, W) hipLaunchKernelGGL((shared_kernel<D, MOST, W>), dim3(grid), dim3(kShThreads), 0, stream, a)
     if (a.weights) {
-        hipLaunchKernelGGL((shared_kernel<D, true>), dim3(grid), dim3(kShThreads), 0, stream, a);
-        if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL((shared_merge_kernel<D, true>), dim3(combine + 4 * grid), dim3(kShThreads), 0, stream, a, combine);
+        if (few) LS_SHARED(kShFew, true);
+        else LS_SHARED(kShMost, true);
     } else {
-        hipLaunchKernelGGL((shared_kernel<D, false>), dim3(grid), dim3(kShThreads), 0, stream, a);
-        if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL((shared_merge_kernel<D, false>), dim3(combine), dim3(kShThreads), 0, stream, a, combine);
+        if (few) LS_SHARED(kShFew, false);
+        else LS_SHARED(kShMost, false);
     }
+#undef LS_SHARED
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.weights)
+        hipLaunchKernelGGL((shared_merge_kernel<D, true>), dim3(combine + 2 * grid), dim3(kShThreads), 0, stream, a, combine);
+    else
+        hipLaunchKernelGGL((shared_merge_kernel<D, false>), dim3(combine), dim3(kShThreads), 0, stream, a, combine);
     return hipGetLastError();
 }
 
@@ -796,19 +940,26 @@ constexpr size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 SharedPlan plan_shared(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads, int32_t num_groups,
                        int32_t num_members, bool weights) {
-    const int64_t H = p.num_kv_heads, G = num_q_heads / p.num_kv_heads, W = p.num_cus > 0 ? p.num_cus : 256;
+    const int64_t H = p.num_kv_heads, G = num_q_heads / p.num_kv_heads, W = kShPerCu * (p.num_cus > 0 ? p.num_cus : 256);
     SharedPlan s;
     // (a slot per segment and one per workgroup; a group has a tile that is not full)
-    s.tile_slots = num_groups ? (size_t)(H * ((int64_t)num_members * G / kTileRows + num_groups) + W) : 0;
-    s.own_slots = (size_t)(num_sessions * H + W);
-    s.at[0] = 0;
-    s.at[1] = s.at[0] + align256(sizeof(ShHeader));
-    s.at[2] = s.at[1] + align256((size_t)num_sessions * sizeof(ShRecord));
-    s.at[3] = s.at[2] + align256(s.tile_slots * kTileRows * 2 * sizeof(float));
-    s.at[4] = s.at[3] + align256(s.tile_slots * kTileRows * (size_t)p.head_dim * sizeof(float));
-    s.at[5] = s.at[4] + align256(s.own_slots * (size_t)G * 2 * sizeof(float));
-    s.at[6] = s.at[5] + align256(s.own_slots * (size_t)G * (size_t)p.head_dim * sizeof(float));
-    s.total = s.at[6] + (weights ? (size_t)p.num_blocks * (size_t)num_q_heads * kBlock * sizeof(float) : 0);
+    const size_t tiles = num_groups ? (size_t)(H * ((int64_t)num_members * G / kTileRows + num_groups)) : 0;
+    const size_t tile_slots = num_groups ? tiles + (size_t)W : 0, own_slots = (size_t)(num_sessions * H + W);
+    const size_t sizes[] = {(size_t)num_sessions * sizeof(ShRecord),
+                            tiles * 2 * sizeof(int32_t),
+                            (size_t)(num_sessions * H) * 2 * sizeof(int32_t),
+                            tile_slots * kTileRows * 2 * sizeof(float),
+                            tile_slots * kTileRows * (size_t)p.head_dim * sizeof(float),
+                            own_slots * (size_t)G * 2 * sizeof(float),
+                            own_slots * (size_t)G * (size_t)p.head_dim * sizeof(float),
+                            weights ? (size_t)p.num_blocks * (size_t)num_q_heads * kBlock * sizeof(float) : 0};
+    static_assert(sizeof sizes / sizeof *sizes == sizeof s.at / sizeof *s.at, "an offset each");
+    s.tiles = tiles;
+    s.total = 0;
+    for (size_t i = 0; i < sizeof sizes / sizeof *sizes; ++i) {
+        s.at[i] = s.total;
+        s.total += align256(sizes[i]);
+    }
     return s;
 }
 
@@ -832,13 +983,16 @@ hipError_t launch_shared(const PoolGeom &p, int layer, int32_t num_sessions, int
     a.members = c.group_members;
     a.prefix = c.prefix_blocks;
     a.scale_log2 = c.scale * 1.4426950408889634f;
-    a.header = reinterpret_cast<ShHeader *>(ws + plan.at[0]);
-    a.records = reinterpret_cast<ShRecord *>(ws + plan.at[1]);
-    a.tile_ml = reinterpret_cast<float *>(ws + plan.at[2]);
-    a.tile_acc = reinterpret_cast<float *>(ws + plan.at[3]);
-    a.own_ml = reinterpret_cast<float *>(ws + plan.at[4]);
-    a.own_acc = reinterpret_cast<float *>(ws + plan.at[5]);
-    a.scores = reinterpret_cast<float *>(ws + plan.at[6]);
+    a.records = reinterpret_cast<ShRecord *>(ws + plan.at[0]);
+    a.tile_first = reinterpret_cast<int32_t *>(ws + plan.at[1]);
+    a.tile_last = a.tile_first + plan.tiles;
+    a.own_first = reinterpret_cast<int32_t *>(ws + plan.at[2]);
+    a.own_last = a.own_first + (int64_t)num_sessions * p.num_kv_heads;
+    a.tile_ml = reinterpret_cast<float *>(ws + plan.at[3]);
+    a.tile_acc = reinterpret_cast<float *>(ws + plan.at[4]);
+    a.own_ml = reinterpret_cast<float *>(ws + plan.at[5]);
+    a.own_acc = reinterpret_cast<float *>(ws + plan.at[6]);
+    a.scores = reinterpret_cast<float *>(ws + plan.at[7]);
     const int64_t entries = (int64_t)layer * p.num_blocks * p.num_kv_heads * kBlock;
     a.weights = c.weights ? c.weights + entries : nullptr;
     a.positions = c.positions ? c.positions + entries : nullptr;
@@ -847,7 +1001,7 @@ hipError_t launch_shared(const PoolGeom &p, int layer, int32_t num_sessions, int
     a.first = c.first_lens;
     a.err = err;
     const int cus = stream_cus(p, stream), most = p.num_cus > 0 ? p.num_cus : 256;
-    const int grid = std::min(cus, most);
+    const int grid = kShPerCu * std::min(cus, most);
     return p.head_dim == 128 ? launch_shared_t<128>(a, grid, stream) : launch_shared_t<64>(a, grid, stream);
 }
 
