@@ -311,8 +311,9 @@ __device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, co
     int ids = -1;                              // of the wave's next 32 pairs: lane 2 i + b holds block b of pair i
     PairRegs<D> regs[2];
     int id[2][2] = {{-1, -1}, {-1, -1}};
+    // (Behind the last pair nothing is fetched, but by as many loads: under a condition of its
+    // own, a pair's loads would be waited for together with those of the pair after it.)
     auto fetch = [&](PairRegs<D> &r, int (&which)[2], int i) {
-        if (i >= mine) return;
         if (i % (kWave / 2) == 0) ids = part_id(a, part, part.j0 + 2 * (wave + kShWaves * (i + lane / 2)) + lane % 2);
         which[0] = __builtin_amdgcn_readlane(ids, (2 * i) % kWave);
         which[1] = __builtin_amdgcn_readlane(ids, (2 * i + 1) % kWave);
