@@ -173,6 +173,7 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
         if constexpr (kKeys) __builtin_amdgcn_raw_ptr_buffer_load_lds(rl, (lds_void *)sl.lse[wave], 4, row * 4, 0, 0, 0);
     };
     auto stage_barrier = [&]() {
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0070);        // vmcnt(0) lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();

@@ -12,12 +12,15 @@
 //
 // Work: segments = (group, KV head, tile of up to 128 rows) over the group's blocks,
 // then (session, KV head) over its own blocks.  A block of a segment costs some units
-// (kCost*, from measurement).  Workgroups of four waves, two per CU, take equal contiguous
-// shares of all units, so each works on a few parts of segments.  A part with up to 16
+// (kCost*).  Workgroups of four waves, two per CU, take equal contiguous shares of the
+// prefix's units and of the own blocks (one of a CU's two begins with the one, the other
+// with the other), so each works on a few parts of segments.  A part with up to 16
 // rows (own keys, small groups): the waves take its pairs of blocks in turn, straight
 // into registers, each with a state of its own, and merge through LDS.  With more rows:
-// the pairs go through LDS, three at a time in flight, and every wave takes them all, for
-// 16 or 32 rows of its own.  A segment that one workgroup has whole, without a shared
+// the pairs go through LDS, and every wave takes them all, for 16 or 32 rows of its own.
+// A workgroup goes through most of the code once or twice a launch, and fetching
+// instructions for the first time took as long as the work: loops are not unrolled, and
+// masked and whole pairs share their code.  A segment that one workgroup has whole, without a shared
 // prefix, is written out at once; other parts leave their state in the workspace, at slot
 // (segment + workgroup), which no other part has, and a second kernel adds them up.
 //
@@ -57,10 +60,11 @@ constexpr int kShFew = 512, kShMost = 2048;
 constexpr int kTileRows = 128;               // rows of a prefix segment: two tiles of 16 per wave
 constexpr int kRank = 11;                    // bits of a member's rank (kShMost of them)
 static_assert(kShMost == 1 << kRank && kShMost == kMaxCacheSessions, "ranks fit");
-// Units of a block: own keys (bound by HBM), a prefix tile of up to 16 rows, and a larger one.
-constexpr int kCostOwn = 4;
-constexpr int kCostFew = 4, kCostTile = 4;
-constexpr int kLeastUnits = kShWaves * 2 * kCostOwn;     // a pair of blocks for each wave
+// Units of a prefix block: of a tile of up to 16 rows, whose pairs the waves share, and of a
+// larger one.
+constexpr int kCostFew = 1, kCostTile = 3;
+// The least share: of prefix units, and of own blocks (a pair for each wave).
+constexpr int kLeastUnits = 4 * kCostTile, kLeastOwn = 2 * kShWaves;
 constexpr float kNoMax = -1.0e30f;           // running maximum of no key
 // The running maximum moves only when a score passes it by this much (log2), so that
 // probabilities reach 2^8 and most pairs of blocks need no rescaling.
@@ -136,13 +140,6 @@ __device__ __forceinline__ float sum_xor_16_32(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Two blocks of K and V in registers.
-template <int D>
-struct PairRegs {
-    u32x4 k[2][D / 32];            // K[token lane % 16][8 dims of k-step]
-    u32x2 v[2][D / 16];            // V^T[dim 16 dt + lane % 16][tokens 4 (lane / 16) .. + 3]
-};
-
 // K tile of a block and KV head (id < 0: a descriptor of no bytes, nothing is fetched).
 template <int D>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t *pool, int num_kv_heads, int g, int id, bool v) {
@@ -150,24 +147,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t *pool
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(t), 0, id < 0 ? 0 : kBlock * D * 2, kRawBuffer);
 }
 
-template <int D, int kPolicy>
-__device__ __forceinline__ void load_pair(PairRegs<D> &r, const uint16_t *pool, int num_kv_heads, int g,
-                                          const int (&id)[2], int koff, int voff) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const __amdgpu_buffer_rsrc_t rk = tile_rsrc<D>(pool, num_kv_heads, g, id[b], false);
-        const __amdgpu_buffer_rsrc_t rv = tile_rsrc<D>(pool, num_kv_heads, g, id[b], true);
-#pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks)
-            r.k[b][ks] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff, ks * 4 * kBlock * 16, kPolicy);
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt)
-            r.v[b][dt] = __builtin_amdgcn_raw_buffer_load_b64(rv, voff, dt * 16 * kBlock * 2, kPolicy);
-    }
-}
-
-// A pair of blocks in LDS, as in the pool; and where waves merge, two a buffer, and the
-// schedule is made.
+// A pair of blocks in LDS, as in the pool; in two of them waves merge, and the schedule is made.
 template <int D>
 struct PairLds {
     __attribute__((aligned(1024))) uint8_t tile[4][kBlock * D * 2];     // K, K, V, V
@@ -225,7 +205,6 @@ struct ShPart {
     const int32_t *table;          // its table row
     int head;                      // KV head
     int j0, j1;
-    int shortest;                  // every row sees the keys before
     int longest;                   // no row sees a key from here on
 };
 
@@ -264,27 +243,21 @@ struct RowState {
     }
 };
 
-// Scores of a pair's products, masked where kPartial.
-template <bool kPartial>
-__device__ __forceinline__ void scores_of(const f32x4 (&s)[2], float scale_log2, int tok0, int row_len, const int (&id)[2],
-                                          float (&x)[2][4]) {
-    const int g4 = threadIdx.x % kWave / 16;
+// Scores of a pair's products.  The row sees keys before row_len; absent: a bit per block
+// that is not in the pool.
+__device__ __forceinline__ void scores_of(const f32x4 (&s)[2], float scale_log2, int tok0, int row_len, int absent, float (&x)[2][4]) {
+    const int left = row_len - tok0 - 4 * (int)(threadIdx.x % kWave / 16);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2; ++b) {
+        const int seen = absent >> b & 1 ? 0 : left - b * kBlock;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[b][e] = s[b][e] * scale_log2;
-            if constexpr (kPartial)
-                if (tok0 + b * kBlock + 4 * g4 + e >= row_len || id[b] < 0) x[b][e] = -INFINITY;
-        }
+        for (int e = 0; e < 4; ++e) x[b][e] = e < seen ? s[b][e] * scale_log2 : -INFINITY;
+    }
 }
-// V of a pair's block b: zeros for tokens from `longest` on, and for an absent block.
-// Slots that no row sees may hold anything (NaN included).
-__device__ __forceinline__ u32x2 seen_v(u32x2 v, int tok0, int b, int longest, int id) {
-    const int valid = id < 0 ? 0 : longest - tok0 - b * kBlock - 4 * (int)(threadIdx.x % kWave / 16);
-    const uint32_t lo = valid >= 2 ? 0xFFFFFFFFu : valid == 1 ? 0x0000FFFFu : 0u;
-    const uint32_t hi = valid >= 4 ? 0xFFFFFFFFu : valid == 3 ? 0x0000FFFFu : 0u;
-    return u32x2{v.x & lo, v.y & hi};
+// Eight tokens of V from token t on, or four: zeros from `longest` on.  Slots that no row
+// sees may hold anything (NaN included).
+__device__ __forceinline__ uint32_t seen_v(uint32_t two, int t, int longest) {
+    return t + 1 < longest ? two : t < longest ? two & 0x0000FFFFu : 0u;
 }
 
 // The id of a part's block, or -1 (none, or not in the pool).
@@ -296,71 +269,87 @@ __device__ __forceinline__ int part_id(const SharedArgs &a, const ShPart &part, 
     return -1;
 }
 
-// Up to 16 rows: the wave's pairs of the part.  qrow, row_len: of the lane's row.
+// Up to 16 rows: the wave's pairs of the part.  qrow, row_len: of the lane's row.  K of the
+// next pair is requested when the first product has taken this one's, V when the second has.
 template <int D, bool kScores, int kPolicy>
 __device__ __forceinline__ void walk(const SharedArgs &a, const ShPart &part, const uint16_t *qrow, int row_len,
                                      RowState<D> &st) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
-    bf16x8 qop[D / 32];
-#pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) qop[ks] = *reinterpret_cast<const bf16x8 *>(qrow + ks * 32 + g4 * 8);
-    st.clear();
     const int pairs = (part.j1 - part.j0 + 1) / 2;
     const int mine = pairs > wave ? (pairs - wave + kShWaves - 1) / kShWaves : 0;     // pairs of this wave
     const int koff = lane * 16, voff = c16 * kBlock * 2 + g4 * 8;
     int ids = -1;                              // of the wave's next 32 pairs: lane 2 i + b holds block b of pair i
-    PairRegs<D> regs[2];
-    int id[2][2] = {{-1, -1}, {-1, -1}};
-    // (Behind the last pair nothing is fetched, but by as many loads: under a condition of its
-    // own, a pair's loads would be waited for together with those of the pair after it.)
-    auto fetch = [&](PairRegs<D> &r, int (&which)[2], int i) {
-        if (i % (kWave / 2) == 0) ids = part_id(a, part, part.j0 + 2 * (wave + kShWaves * (i + lane / 2)) + lane % 2);
-        which[0] = __builtin_amdgcn_readlane(ids, (2 * i) % kWave);
-        which[1] = __builtin_amdgcn_readlane(ids, (2 * i + 1) % kWave);
-        load_pair<D, kPolicy>(r, a.pool, a.num_kv_heads, part.head, which, koff, voff);
+    auto fetch_ids = [&](int i) {
+        ids = part_id(a, part, part.j0 + 2 * (wave + kShWaves * (i + lane / 2)) + lane % 2);
+        // (waited for here, so that the loop's other loads need not be)
+        __builtin_amdgcn_s_waitcnt(0x0F70);
     };
-    auto work_as = [&](PairRegs<D> &t, const int (&which)[2], int tok0, auto partial) {
-        constexpr bool kPartial = decltype(partial)::value;
+    bf16x8 qop[D / 32];
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) qop[ks] = *reinterpret_cast<const bf16x8 *>(qrow + ks * 32 + g4 * 8);
+    fetch_ids(0);
+    st.clear();
+    u32x4 k[2][D / 32];                        // K[token lane % 16][8 dims of k-step]
+    u32x2 v[2][D / 16];                        // V^T[dim 16 dt + lane % 16][tokens 4 (lane / 16) .. + 3]
+    auto load_k = [&](const int (&id)[2]) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, id[b], false);
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) k[b][ks] = __builtin_amdgcn_raw_buffer_load_b128(r, koff, ks * 4 * kBlock * 16, kPolicy);
+        }
+    };
+    auto load_v = [&](const int (&id)[2]) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, id[b], true);
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) v[b][dt] = __builtin_amdgcn_raw_buffer_load_b64(r, voff, dt * 16 * kBlock * 2, kPolicy);
+        }
+    };
+    int id[2] = {__builtin_amdgcn_readlane(ids, 0), __builtin_amdgcn_readlane(ids, 1)};
+    load_k(id);
+    load_v(id);
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        const int tok0 = (part.j0 + 2 * (wave + kShWaves * i)) * kBlock;
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
             for (int b = 0; b < 2; ++b)
-                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[b][ks]), qop[ks], s[b], 0, 0, 0);
+                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[b][ks]), qop[ks], s[b], 0, 0, 0);
+        const int now[2] = {id[0], id[1]};
+        // (Behind the last pair nothing is fetched, but by as many loads.)
+        if ((i + 1) % (kWave / 2) == 0) fetch_ids(i + 1);
+        id[0] = __builtin_amdgcn_readlane(ids, 2 * (i + 1) % kWave);
+        id[1] = __builtin_amdgcn_readlane(ids, (2 * (i + 1) + 1) % kWave);
+        load_k(id);
         float x[2][4];
-        scores_of<kPartial>(s, a.scale_log2, tok0, row_len, which, x);
+        scores_of(s, a.scale_log2, tok0, row_len, (now[0] < 0) | (now[1] < 0) << 1, x);
         if constexpr (kScores) {
-            if (c16 < a.group)
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
-                    if (!kPartial || which[b] >= 0)
-                        *reinterpret_cast<f32x4 *>(a.scores + (((int64_t)which[b] * a.num_kv_heads + part.head) * a.group + c16) * kBlock + 4 * g4) =
-                            f32x4{x[b][0], x[b][1], x[b][2], x[b][3]};
+            for (int b = 0; b < 2; ++b)
+                if (c16 < a.group && now[b] >= 0)
+                    *reinterpret_cast<f32x4 *>(a.scores + (((int64_t)now[b] * a.num_kv_heads + part.head) * a.group + c16) * kBlock + 4 * g4) =
+                        f32x4{x[b][0], x[b][1], x[b][2], x[b][3]};
         }
         const bf16x8 p = st.take(x);
+        if (tok0 + 2 * kBlock > part.longest) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) {
+                    v[b][dt].x = seen_v(v[b][dt].x, tok0 + b * kBlock + 4 * g4, part.longest);
+                    v[b][dt].y = seen_v(v[b][dt].y, tok0 + b * kBlock + 4 * g4 + 2, part.longest);
+                }
+        }
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
-            u32x2 v[2] = {t.v[0][dt], t.v[1][dt]};
-            if constexpr (kPartial)
-                for (int b = 0; b < 2; ++b) v[b] = seen_v(v[b], tok0, b, part.longest, which[b]);
-            const u32x4 va = {v[0].x, v[0].y, v[1].x, v[1].y};
+            const u32x4 va = {v[0][dt].x, v[0][dt].y, v[1][dt].x, v[1][dt].y};
             st.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), p, st.o[dt], 0, 0, 0);
         }
-    };
-    // (A branch around code of its own: as selects in the common code the masks cost as much
-    // as the rest.)
-    auto work = [&](PairRegs<D> &t, const int (&which)[2], int i) {
-        const int tok0 = (part.j0 + 2 * (wave + kShWaves * i)) * kBlock;
-        if (tok0 + 2 * kBlock > part.shortest || which[0] < 0 || which[1] < 0) work_as(t, which, tok0, std::true_type());
-        else work_as(t, which, tok0, std::false_type());
-    };
-    fetch(regs[0], id[0], 0);
-    for (int i = 0; i < mine; i += 2) {
-        fetch(regs[1], id[1], i + 1);
-        work(regs[0], id[0], i);
-        if (i + 1 >= mine) break;
-        fetch(regs[0], id[0], i + 2);
-        work(regs[1], id[1], i + 1);
+        load_v(id);
     }
     st.l = sum_xor_16_32(st.l);
 }
@@ -375,13 +364,11 @@ struct ShSink {
 
 // Adds the waves' states of 16 rows up and writes them.
 template <int D, int kMost>
-__device__ __forceinline__ void merge(ShPlan<kMost> &sm, PairLds<D> &b0, PairLds<D> &b1, const RowState<D> &st, const ShSink &sink) {
+__device__ __forceinline__ void merge(ShPlan<kMost> &sm, PairLds<D> *buf, const RowState<D> &st, const ShSink &sink) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
-    // [wave % 2][D / 16][64] of 16 bytes, waves 0 and 1 in b0
-    auto slot = [&](int w, int dt) {
-        return reinterpret_cast<f32x4 *>(w < 2 ? b0.tile[0] : b1.tile[0]) + (w % 2 * (D / 16) + dt) * kWave + lane;
-    };
-    static_assert(sizeof(PairLds<D>) == 2 * (D / 16) * kWave * sizeof(f32x4), "two waves a buffer");
+    // [wave][D / 16][64] of 16 bytes
+    auto slot = [&](int w, int dt) { return reinterpret_cast<f32x4 *>(buf) + (w * (D / 16) + dt) * kWave + lane; };
+    static_assert(2 * sizeof(PairLds<D>) == kShWaves * (D / 16) * kWave * sizeof(f32x4), "a state per wave");
     if (g4 == 0) {
         sm.m[wave][c16] = st.m;
         sm.l[wave][c16] = st.l;
@@ -419,13 +406,19 @@ __device__ __forceinline__ void merge(ShPlan<kMost> &sm, PairLds<D> &b0, PairLds
 }
 
 // More rows: tiles `wave` and `wave` + 4 of 16 of them are this wave's (count of them),
-// and every pair of the part goes through LDS.
+// and every pair of the part goes through LDS: each wave loads one of its four tiles into
+// registers a pair ahead and stores it beside the pair at work.
 template <int D>
-__device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &part, PairLds<D> &b0, PairLds<D> &b1, PairLds<D> &b2,
-                                          const uint16_t *const (&qrow)[2], const int (&row_len)[2], int count, float *ml, float *acc,
-                                          int rows) {
+__device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &part, PairLds<D> *buf, const uint16_t *const (&qrow)[2],
+                                          const int (&row_len)[2], int count, float *ml, float *acc, int rows) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
     constexpr int kLoads = kBlock * D * 2 / 1024;        // of a tile, a kilobyte each
+    const int pairs = (part.j1 - part.j0 + 1) / 2;
+    int ids = -1;                              // of 64 blocks
+    auto fetch_ids = [&](int i) {
+        ids = part_id(a, part, part.j0 + 2 * i + lane);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+    };
     bf16x8 qop[2][D / 32];
     RowState<D> st[2];
 #pragma unroll
@@ -434,78 +427,73 @@ __device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &par
         for (int ks = 0; ks < D / 32; ++ks) qop[r][ks] = *reinterpret_cast<const bf16x8 *>(qrow[r] + ks * 32 + g4 * 8);
         st[r].clear();
     }
-    const int pairs = (part.j1 - part.j0 + 1) / 2;
-    int ids_load = -1, ids_work = -1;          // of 64 blocks, for the pair being loaded and the one at work
-    // Tile `wave` of pair i: K, K, V, V.  (Behind the last pair nothing is fetched; the loads count all the same.)
-    auto load = [&](PairLds<D> &to, int i) {
-        if (i % (kWave / 2) == 0) ids_load = part_id(a, part, part.j0 + 2 * i + lane);
-        const int id = i < pairs ? __builtin_amdgcn_readlane(ids_load, (2 * i + wave % 2) % kWave) : -1;
-        const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, id, wave >= 2);
+    u32x4 ahead[kLoads];                       // tile `wave` of a pair: K, K, V, V
+    // Requests pair i (behind the last nothing, by as many loads); a bit per block that is absent.
+    auto load = [&](int i) {
+        if (i % (kWave / 2) == 0) fetch_ids(i);
+        const int id0 = __builtin_amdgcn_readlane(ids, 2 * i % kWave), id1 = __builtin_amdgcn_readlane(ids, (2 * i + 1) % kWave);
+        const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, wave % 2 ? id1 : id0, wave >= 2);
 #pragma unroll
-        for (int kb = 0; kb < kLoads; ++kb)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(to.tile[wave] + kb * 1024), 16, lane * 16, kb * 1024, 0, 0);
+        for (int kb = 0; kb < kLoads; ++kb) ahead[kb] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, kb * 1024, 0);
+        return (id0 < 0) | (id1 < 0) << 1;
     };
-    auto barrier = [&]() {
-        __builtin_amdgcn_s_waitcnt(0x0070 | kLoads);     // vmcnt: all but the last pair's; lgkmcnt(0)
+    auto store = [&](int i) {
+        const int tok = (part.j0 + 2 * i + wave % 2) * kBlock;
+        if (wave >= 2 && tok + kBlock > part.longest) {
+            // 16 bytes: eight tokens of a dim
+            const int t = tok + lane % 2 * 8;
+#pragma unroll
+            for (int kb = 0; kb < kLoads; ++kb)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ahead[kb][e] = seen_v(ahead[kb][e], t + 2 * e, part.longest);
+        }
+#pragma unroll
+        for (int kb = 0; kb < kLoads; ++kb) *reinterpret_cast<u32x4 *>(buf[i & 1].tile[wave] + kb * 1024 + lane * 16) = ahead[kb];
+    };
+    int absent = load(0);
+    store(0);
+    int absent_next = load(1);
+#pragma unroll 1
+    for (int i = 0; i < pairs; ++i) {
+        // The stores of pair i are done; loads stay in flight.
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);    // lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-    };
-    auto work_as = [&](PairLds<D> &t, const int (&which)[2], int tok0, auto partial) {
-        constexpr bool kPartial = decltype(partial)::value;
-        f32x4 s[2][2] = {};
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks) {
-                const bf16x8 k = *reinterpret_cast<const bf16x8 *>(t.tile[b] + ks * 1024 + lane * 16);
-#pragma unroll
-                for (int r = 0; r < 2; ++r) s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[r][ks], s[r][b], 0, 0, 0);
-            }
-        bf16x8 p[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float x[2][4];
-            scores_of<kPartial>(s[r], a.scale_log2, tok0, row_len[r], which, x);
-            p[r] = st[r].take(x);
-        }
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) {
-            u32x2 v[2];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                v[b] = *reinterpret_cast<const u32x2 *>(t.tile[2 + b] + (dt * 16 + c16) * kBlock * 2 + g4 * 8);
-                if constexpr (kPartial) v[b] = seen_v(v[b], tok0, b, part.longest, which[b]);
-            }
-            const u32x4 va = {v[0].x, v[0].y, v[1].x, v[1].y};
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                st[r].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), p[r], st[r].o[dt], 0, 0, 0);
-        }
-    };
-    auto stage = [&](int i, PairLds<D> &t, PairLds<D> &ahead) {
-        load(ahead, i + 2);
+        const PairLds<D> &t = buf[i & 1];
+        const int tok0 = (part.j0 + 2 * i) * kBlock;
         if (count) {
-            if (i % (kWave / 2) == 0) ids_work = part_id(a, part, part.j0 + 2 * i + lane);
-            const int which[2] = {__builtin_amdgcn_readlane(ids_work, (2 * i) % kWave), __builtin_amdgcn_readlane(ids_work, (2 * i + 1) % kWave)};
-            const int tok0 = (part.j0 + 2 * i) * kBlock;
-            if (tok0 + 2 * kBlock > part.shortest || which[0] < 0 || which[1] < 0) work_as(t, which, tok0, std::true_type());
-            else work_as(t, which, tok0, std::false_type());
+            f32x4 s[2][2] = {};
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const bf16x8 k = *reinterpret_cast<const bf16x8 *>(t.tile[b] + ks * 1024 + lane * 16);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[r][ks], s[r][b], 0, 0, 0);
+                }
+            bf16x8 p[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float x[2][4];
+                scores_of(s[r], a.scale_log2, tok0, row_len[r], absent, x);
+                p[r] = st[r].take(x);
+            }
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) {
+                const uint8_t *at = t.tile[2] + (dt * 16 + c16) * kBlock * 2 + g4 * 8;
+                const u32x2 v0 = *reinterpret_cast<const u32x2 *>(at), v1 = *reinterpret_cast<const u32x2 *>(at + sizeof t.tile[2]);
+                const u32x4 va = {v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    st[r].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), p[r], st[r].o[dt], 0, 0, 0);
+            }
         }
-        barrier();
-    };
-    load(b0, 0);
-    load(b1, 1);
-    barrier();
-    for (int i = 0;;) {
-        stage(i, b0, b2);
-        if (++i >= pairs) break;
-        stage(i, b1, b0);
-        if (++i >= pairs) break;
-        stage(i, b2, b1);
-        if (++i >= pairs) break;
+        store(i + 1);                          // (the pair before, whose buffer it is, was left at the barrier)
+        absent = absent_next;
+        absent_next = load(i + 2);
     }
-    __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): no load lands in what the next part writes
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int row = (wave + r * kShWaves) * 16 + c16;
@@ -522,51 +510,72 @@ __device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &par
 template <int D, int kMost, bool kWeights>
 __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs a) {
     __shared__ ShPlan<kMost> sm;
-    __shared__ PairLds<D> b0, b1, b2;
-    int32_t *const owner = reinterpret_cast<int32_t *>(b0.tile[0]);       // a session's place among the members, or -1
+    __shared__ PairLds<D> buf[2];
+    int32_t *const owner = reinterpret_cast<int32_t *>(buf[0].tile[0]);   // a session's place among the members, or -1
     static_assert(kShMost * 4 <= sizeof(PairLds<D>), "owners fit a buffer");
     const int tid = threadIdx.x, lane = tid % kWave, c16 = lane % 16;
     const int S = a.num_sessions, G = a.group, H = a.num_kv_heads;
     const bool first_wg = blockIdx.x == 0;
     const int gs = __builtin_ctz(G);           // (G is 1, 2, 4 or 8)
-    // ---- the schedule, made by every workgroup for itself
+    // ---- the schedule, made by every workgroup for itself (its loads all at once)
+    constexpr int kPer = kMost / kShThreads;
+    int32_t *const len = reinterpret_cast<int32_t *>(buf[1].tile[0]);
     int ng = a.num_groups;
     bool bad = false;
-    for (int g = tid; g < ng; g += kShThreads) {
-        const int x = a.starts[g], y = a.starts[g + 1], pb = a.prefix[g];
-        bad = bad || x < 0 || y < x || y > a.num_members || pb < 0 || pb > a.max_blocks || (g == 0 && x != 0) ||
-              (g == ng - 1 && y != a.num_members);
-        sm.start[g] = (uint16_t)x;
-        sm.start[g + 1] = (uint16_t)y;         // (the same value from two threads)
-        sm.prefix[g] = (uint16_t)pb;
-        sm.lead[g] = 0u;
-    }
-    for (int s = tid; s < S; s += kShThreads) {
-        owner[s] = -1;
-        const int raw = a.lens[s];
-        if (first_wg && (raw < 0 || raw > a.max_blocks * kBlock)) flag_error(a.err, LS_DEVERR_LENGTH);
-    }
-    bad = __syncthreads_or(bad);
-    if (ng && !bad) {
-        bool wrong = false;
-        for (int i = tid; i < a.num_members; i += kShThreads) {
-            const int s = a.members[i];
-            if (s < 0 || s >= S) {
-                wrong = true;
-                continue;
+    {
+        int ld_len[kPer], ld_member[kPer], ld_x[kPer], ld_y[kPer], ld_pb[kPer];
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int i = tid + k * kShThreads;
+            ld_len[k] = a.lens[min(i, S - 1)];
+            if (ng) {
+                ld_member[k] = a.members[min(i, a.num_members - 1)];
+                ld_x[k] = a.starts[min(i, ng)];
+                ld_y[k] = a.starts[min(i + 1, ng)];
+                ld_pb[k] = a.prefix[min(i, ng - 1)];
             }
-            const int len = keys_of(a, s);
-            int lo = 0, hi = ng;               // the last group that starts at or before i
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (sm.start[mid] <= i) lo = mid;
-                else hi = mid;
-            }
-            if (atomicExch(&owner[s], i) != -1) wrong = true;
-            sm.gid[s] = (uint16_t)lo;
-            atomicMax(&sm.lead[lo], (uint32_t)len << kRank | (uint32_t)(kShMost - 1 - (i - sm.start[lo])));
         }
-        bad = __syncthreads_or(wrong);
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int i = tid + k * kShThreads;
+            if (i < S) {
+                owner[i] = -1;
+                if (first_wg && (ld_len[k] < 0 || ld_len[k] > a.max_blocks * kBlock)) flag_error(a.err, LS_DEVERR_LENGTH);
+                len[i] = max(min(ld_len[k], a.max_blocks * kBlock), 0);
+            }
+            if (i < ng) {
+                const int x = ld_x[k], y = ld_y[k], pb = ld_pb[k];
+                bad = bad || x < 0 || y < x || y > a.num_members || pb < 0 || pb > a.max_blocks || (i == 0 && x != 0) ||
+                      (i == ng - 1 && y != a.num_members);
+                sm.start[i] = (uint16_t)x;
+                if (i == ng - 1) sm.start[ng] = (uint16_t)y;
+                sm.prefix[i] = (uint16_t)pb;
+                sm.lead[i] = 0u;
+            }
+        }
+        bad = __syncthreads_or(bad);
+        if (ng && !bad) {
+            bool wrong = false;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k) {
+                const int i = tid + k * kShThreads, s = ld_member[k];
+                if (i >= a.num_members) continue;
+                if (s < 0 || s >= S) {
+                    wrong = true;
+                    continue;
+                }
+                int lo = 0, hi = ng;           // the last group that starts at or before i
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (sm.start[mid] <= i) lo = mid;
+                    else hi = mid;
+                }
+                if (atomicExch(&owner[s], i) != -1) wrong = true;
+                sm.gid[s] = (uint16_t)lo;
+                atomicMax(&sm.lead[lo], (uint32_t)len[s] << kRank | (uint32_t)(kShMost - 1 - (i - sm.start[lo])));
+            }
+            bad = __syncthreads_or(wrong);
+        }
     }
     if (bad) {
         // Groups that cannot be: every session is computed on its own.
@@ -603,7 +612,7 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
     {
         const int per = (S + kShThreads - 1) / kShThreads;
         unsigned v[2] = {0, 0}, all[2];
-        auto own = [&](int s, int pb) { return (unsigned)max((keys_of(a, s) + kBlock - 1) / kBlock - pb, 0); };
+        auto own = [&](int s, int pb) { return (unsigned)max((len[s] + kBlock - 1) / kBlock - pb, 0); };
         for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) {
             sm.pb[s] = owner[s] >= 0 ? sm.prefix[sm.gid[s]] : (uint16_t)0;
             v[0] += own(s, sm.pb[s]);
@@ -622,7 +631,7 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             r.own_blocks = (int)(sm.cum[s + 1] - sm.cum[s]);
             r.own_before = sm.cum[s];
             r.own_all = sm.cum[S];
-            r.keys = keys_of(a, s);
+            r.keys = len[s];
             if (owner[s] >= 0) {
                 const int g = sm.gid[s], row = (owner[s] - sm.start[g]) * G;
                 r.prefix_blocks = sm.prefix[g];
@@ -633,54 +642,52 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             a.records[s] = r;
         }
     }
-    __syncthreads();                           // the buffer of the owners is used again
-    const int64_t own_base = (int64_t)H * sm.units[ng];
-    const int64_t units = own_base + (int64_t)H * sm.cum[S] * kCostOwn;
-    int64_t share = (units + gridDim.x - 1) / gridDim.x;
-    if (share < kLeastUnits) share = kLeastUnits;
-    // Consecutive shares on one XCD: the tiles of a group and KV head read the same K and V.
+    __syncthreads();                           // the buffers of owners and lengths are used again
+    // Consecutive shares on one XCD: the tiles of a group and KV head read the same K and V.  Own
+    // shares from the other end, so that where there is little of both it falls to different workgroups.
     const int W = gridDim.x;
-    const int w = W % 8 == 0 ? (int)(blockIdx.x % 8) * (W / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x;
-    const int64_t u0 = (int64_t)w * share, u1 = min(u0 + share, units);
-    // Blocks of the segment at `pos` that are this workgroup's.
-    auto range = [&](int64_t pos, int blocks, int cost, int &j0, int &j1) {
-        j0 = u0 > pos ? (int)((u0 - pos + cost - 1) / cost) : 0;
-        j1 = u1 - pos >= (int64_t)blocks * cost ? blocks : (int)((u1 - pos + cost - 1) / cost);
+    const int wp = W % 8 == 0 ? (int)(blockIdx.x % 8) * (W / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x, wo = W - 1 - wp;
+    // Blocks of the segment at `pos` that are in [u0, u1).
+    auto range = [](int u0, int u1, int pos, int blocks, int cost, int &j0, int &j1) {
+        j0 = u0 > pos ? (u0 - pos + cost - 1) / cost : 0;
+        j1 = u1 - pos >= blocks * cost ? blocks : (u1 - pos + cost - 1) / cost;
     };
-    int64_t at = u0;
-    // ---- prefix tiles
-    if (at < min(u1, own_base)) {
+    auto prefix_tiles = [&]() {
+        const int all = H * (int)sm.units[ng], share = max((all + W - 1) / W, kLeastUnits);
+        if (wp > all / share) return;
+        const int at = wp * share, u1 = min(at + share, all);
+        if (at >= u1) return;
         int g = 0, hi = ng;
         while (hi - g > 1) {
             const int mid = (g + hi) / 2;
-            if ((int64_t)H * sm.units[mid] <= at) g = mid;
+            if (H * (int)sm.units[mid] <= at) g = mid;
             else hi = mid;
         }
-        for (; g < ng && (int64_t)H * sm.units[g] < min(u1, own_base); ++g) {
-            const int64_t stride = sm.units[g + 1] - sm.units[g];
+        for (; g < ng && H * (int)sm.units[g] < u1; ++g) {
+            const int stride = (int)(sm.units[g + 1] - sm.units[g]);
             if (!stride) continue;
             const int pb = sm.prefix[g], first = sm.start[g], rows = (sm.start[g + 1] - first) * G;
             const int tiles = (rows + kTileRows - 1) / kTileRows;
-            const int64_t gpos = (int64_t)H * sm.units[g];
+            const int gpos = H * (int)sm.units[g];
             const int lead_s = a.members[first + kShMost - 1 - (int)(sm.lead[g] & (kShMost - 1))];
-            for (int h = at > gpos ? (int)((at - gpos) / stride) : 0; h < H && gpos + h * stride < u1; ++h) {
-                const int64_t hpos = gpos + h * stride;
-                for (int t = at > hpos ? (int)((at - hpos) / ((int64_t)pb * kCostTile)) : 0; t < tiles; ++t) {
-                    const int64_t pos = hpos + (int64_t)t * pb * kCostTile;
+            for (int h = at > gpos ? (at - gpos) / stride : 0; h < H && gpos + h * stride < u1; ++h) {
+                const int hpos = gpos + h * stride;
+                for (int t = at > hpos ? (at - hpos) / (pb * kCostTile) : 0; t < tiles; ++t) {
+                    const int pos = hpos + t * pb * kCostTile;
                     if (pos >= u1) break;
                     const int n = min(kTileRows, rows - t * kTileRows);
                     ShPart part;
-                    range(pos, pb, tile_cost(n), part.j0, part.j1);
+                    range(at, u1, pos, pb, tile_cost(n), part.j0, part.j1);
                     if (part.j0 >= part.j1) continue;
                     part.table = a.tables + (int64_t)lead_s * a.max_blocks;
                     part.head = h;
                     part.longest = (int)(sm.lead[g] >> kRank);
                     const int seg = H * sm.segs[g] + h * tiles + t;
-                    const int64_t slot = (int64_t)seg + w;
+                    const int64_t slot = (int64_t)seg + wp;
                     float *ml = a.tile_ml + slot * kTileRows * 2, *acc = a.tile_acc + slot * kTileRows * D;
                     if (tid == 0) {
-                        if (part.j0 == 0) a.tile_first[seg] = w;
-                        if (part.j1 == pb) a.tile_last[seg] = w;
+                        if (part.j0 == 0) a.tile_first[seg] = wp;
+                        if (part.j1 == pb) a.tile_last[seg] = wp;
                     }
                     // (lanes of no row take the last one: a load under a condition waits for the one before)
                     auto row_of = [&](int row, const uint16_t *&qrow, int &len) {
@@ -690,70 +697,68 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
                     };
                     if (n <= 16) {
                         const uint16_t *qrow;
-                        int len;
-                        row_of(c16, qrow, len);
-                        part.shortest = len;
-#pragma unroll
-                        for (int off = 1; off < 16; off <<= 1) part.shortest = min(part.shortest, __shfl_xor(part.shortest, off));
-                        part.shortest = __builtin_amdgcn_readfirstlane(part.shortest);
+                        int row_len;
+                        row_of(c16, qrow, row_len);
                         RowState<D> st;
-                        walk<D, false, 0>(a, part, qrow, len, st);
-                        merge<D>(sm, b0, b1, st, ShSink{ml, acc, nullptr, n});
+                        walk<D, false, 0>(a, part, qrow, row_len, st);
+                        merge<D>(sm, buf, st, ShSink{ml, acc, nullptr, n});
                     } else {
                         const int wave = tid / kWave;
                         const uint16_t *qrow[2];
-                        int len[2];
-                        row_of(wave * 16 + c16, qrow[0], len[0]);
-                        row_of((wave + kShWaves) * 16 + c16, qrow[1], len[1]);
-                        part.shortest = min(len[0], len[1]);
-#pragma unroll
-                        for (int off = 1; off < 16; off <<= 1) part.shortest = min(part.shortest, __shfl_xor(part.shortest, off));
-                        part.shortest = __builtin_amdgcn_readfirstlane(part.shortest);
+                        int row_len[2];
+                        row_of(wave * 16 + c16, qrow[0], row_len[0]);
+                        row_of((wave + kShWaves) * 16 + c16, qrow[1], row_len[1]);
                         const int count = (wave * 16 < n) + ((wave + kShWaves) * 16 < n);
-                        tile_walk<D>(a, part, b0, b1, b2, qrow, len, count, ml, acc, n);
+                        tile_walk<D>(a, part, buf, qrow, row_len, count, ml, acc, n);
                     }
                 }
             }
         }
-        at = own_base;
-    }
-    // ---- own keys
-    if (at < u1) {
-        const int64_t rel = (at - own_base) / kCostOwn / H;       // blocks per KV head before
+    };
+    auto own_keys = [&]() {
+        const int all = H * (int)sm.cum[S], share = max((all + W - 1) / W, kLeastOwn);
+        if (wo > all / share) return;
+        const int at = wo * share, u1 = min(at + share, all);
+        if (at >= u1) return;
+        const int rel = at / H;                 // blocks per KV head before
         int s = 0, hi = S;                      // the last session that starts at or before it
         while (hi - s > 1) {
             const int mid = (s + hi) / 2;
-            if ((int64_t)sm.cum[mid] <= rel) s = mid;
+            if ((int)sm.cum[mid] <= rel) s = mid;
             else hi = mid;
         }
         for (; s < S; ++s) {
-            const int64_t spos = own_base + (int64_t)H * sm.cum[s] * kCostOwn;
+            const int spos = H * (int)sm.cum[s];
             if (spos >= u1) break;
             const int nb = (int)(sm.cum[s + 1] - sm.cum[s]);
             if (!nb) continue;
             const int pb = sm.pb[s], L = keys_of(a, s);
-            const int64_t stride = (int64_t)nb * kCostOwn;
-            for (int h = at > spos ? (int)((at - spos) / stride) : 0; h < H; ++h) {
-                const int64_t pos = spos + h * stride;
+            for (int h = at > spos ? (at - spos) / nb : 0; h < H; ++h) {
+                const int pos = spos + h * nb;
                 if (pos >= u1) break;
-                int j0, j1;
-                range(pos, nb, kCostOwn, j0, j1);
+                const int j0 = max(at - pos, 0), j1 = min(u1 - pos, nb);
                 if (j0 >= j1) continue;
-                const ShPart part = {a.tables + (int64_t)s * a.max_blocks, h, pb + j0, pb + j1, L, L};
+                const ShPart part = {a.tables + (int64_t)s * a.max_blocks, h, pb + j0, pb + j1, L};
                 const bool whole = !pb && j0 == 0 && j1 == nb;
                 const int seg = s * H + h;
-                const int64_t slot = (int64_t)seg + w, row0 = (int64_t)seg * G;
+                const int64_t slot = (int64_t)seg + wo, row0 = (int64_t)seg * G;
                 if (tid == 0) {
-                    if (j0 == 0) a.own_first[seg] = w;
-                    if (j1 == nb) a.own_last[seg] = w;
+                    if (j0 == 0) a.own_first[seg] = wo;
+                    if (j1 == nb) a.own_last[seg] = wo;
                 }
                 const ShSink sink = {!whole || kWeights ? a.own_ml + slot * G * 2 : nullptr, whole ? nullptr : a.own_acc + slot * G * D,
                                      a.out + row0 * D, G};
                 RowState<D> st;
                 walk<D, kWeights, kStream>(a, part, a.q + (row0 + min(c16, G - 1)) * D, L, st);
-                merge<D>(sm, b0, b1, st, sink);
+                merge<D>(sm, buf, st, sink);
             }
         }
+    };
+    const bool own_first = blockIdx.x >= gridDim.x / 2;
+#pragma unroll 1
+    for (int phase = 0; phase < 2; ++phase) {
+        if ((phase == 0) == own_first) own_keys();
+        else prefix_tiles();
     }
 }
 
@@ -835,26 +840,26 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
         const uint32_t own_all = a.records[0].own_all;
         if (tid == 0) sm_cum[S] = own_all;
         __syncthreads();
-        const int64_t all = (int64_t)own_all * H, n = gridDim.x - combine, w = blockIdx.x - combine;
-        int64_t per = (all + n - 1) / n;
-        per = max(per, (int64_t)(kShThreads / 4));
-        const int64_t b0 = w * per, b1 = min(b0 + per, all);
+        const int all = (int)own_all * H, n = gridDim.x - combine, w = blockIdx.x - combine;
+        const int per = max((all + n - 1) / n, kShThreads / 4);
+        if (w > all / per) return;
+        const int b0 = w * per, b1 = min(b0 + per, all);
         if (b0 >= b1) return;
         int s = 0, hi = S;
         while (hi - s > 1) {
             const int mid = (s + hi) / 2;
-            if ((int64_t)sm_cum[mid] * H <= b0) s = mid;
+            if ((int)sm_cum[mid] * H <= b0) s = mid;
             else hi = mid;
         }
-        for (; s < S && (int64_t)sm_cum[s] * H < b1; ++s) {
+        for (; s < S && (int)sm_cum[s] * H < b1; ++s) {
             const ShRecord r = a.records[s];
             if (!r.own_blocks) continue;
             const int first = a.first ? a.first[s] : 0;
             const int old = a.reused ? a.reused[s] : INT32_MAX;      // keys from here on are new
             const int begin = a.reused ? (a.begin ? a.begin[s] : old) : 0;
-            const int64_t spos = (int64_t)sm_cum[s] * H;
-            for (int h = b0 > spos ? (int)((b0 - spos) / r.own_blocks) : 0; h < H; ++h) {
-                const int64_t pos = spos + (int64_t)h * r.own_blocks;
+            const int spos = (int)sm_cum[s] * H;
+            for (int h = b0 > spos ? (b0 - spos) / r.own_blocks : 0; h < H; ++h) {
+                const int pos = spos + h * r.own_blocks;
                 if (pos >= b1) break;
                 __syncthreads();                                     // the segment before is done with sm_top
                 if (tid < kWave) {
@@ -882,7 +887,7 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
                     }
                 }
                 __syncthreads();
-                const int j0 = (int)max(b0 - pos, (int64_t)0), j1 = (int)min(b1 - pos, (int64_t)r.own_blocks);
+                const int j0 = max(b0 - pos, 0), j1 = min(b1 - pos, r.own_blocks);
                 for (int j = j0 + tid / 4; j < j1; j += kShThreads / 4) {
                     const int col = r.prefix_blocks + j, t0 = col * kBlock + tid % 4 * 4;
                     const int id = a.tables[(int64_t)s * a.max_blocks + col];
