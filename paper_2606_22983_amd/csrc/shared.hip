@@ -12,9 +12,9 @@
 //
 // Work: segments = (group, KV head, tile of up to 128 rows) over the group's blocks,
 // then (session, KV head) over its own blocks.  A block of a segment costs some units
-// (kCost*).  Workgroups of four waves, two per CU, take equal contiguous shares of the
-// prefix's units and of the own blocks (one of a CU's two begins with the one, the other
-// with the other), so each works on a few parts of segments.  A part with up to 16
+// (kCost*).  Of the workgroups, of four waves, two per CU, as many as the units say are for
+// prefixes and the others for own blocks, on every XCD; each takes an equal contiguous
+// share of the one or the other, so it works on a few parts of segments.  A part with up to 16
 // rows (own keys, small groups): the waves take its pairs of blocks in turn, straight
 // into registers, each with a state of its own, and merge through LDS.  With more rows:
 // the pairs go through LDS, and every wave takes them all, for 16 or 32 rows of its own.
@@ -60,11 +60,13 @@ constexpr int kShFew = 512, kShMost = 2048;
 constexpr int kTileRows = 128;               // rows of a prefix segment: two tiles of 16 per wave
 constexpr int kRank = 11;                    // bits of a member's rank (kShMost of them)
 static_assert(kShMost == 1 << kRank && kShMost == kMaxCacheSessions, "ranks fit");
-// Units of a prefix block: of a tile of up to 16 rows, whose pairs the waves share, and of a
-// larger one.
-constexpr int kCostFew = 1, kCostTile = 3;
-// The least share: of prefix units, and of own blocks (a pair for each wave).
-constexpr int kLeastUnits = 4 * kCostTile, kLeastOwn = 2 * kShWaves;
+// Units: of an own block and a block of a prefix tile of up to 16 rows (whose pairs the
+// waves share), of a block of a larger tile, and of what beginning a part takes (3 us, where
+// an own block of D 128 takes 0.4 and a tile's 1.5: without them, workgroups that got many
+// short segments ended last by far).
+constexpr int kCostFew = 1, kCostTile = 4, kCostPart = 8;
+// The least share.
+constexpr int kLeastTile = kCostPart + 4 * kCostTile, kLeastOwn = kCostPart + 2 * kShWaves;
 constexpr float kNoMax = -1.0e30f;           // running maximum of no key
 // The running maximum moves only when a score passes it by this much (log2), so that
 // probabilities reach 2^8 and most pairs of blocks need no rescaling.
@@ -117,10 +119,11 @@ struct SharedArgs {
 };
 
 __device__ __forceinline__ int tile_cost(int rows) { return rows <= 16 ? kCostFew : kCostTile; }
-// Units per block of all tiles of a group of `rows` rows.
-__device__ __forceinline__ int group_cost(int rows) {
+// Units of all tiles of a group of `rows` rows over `blocks` blocks, per KV head.
+__device__ __forceinline__ int group_cost(int rows, int blocks) {
     const int rest = rows % kTileRows;
-    return rows / kTileRows * kCostTile + (rest ? tile_cost(rest) : 0);
+    if (!blocks) return 0;
+    return rows / kTileRows * (kCostTile * blocks + kCostPart) + (rest ? tile_cost(rest) * blocks + kCostPart : 0);
 }
 // Keys of session s, clipped to its table.
 __device__ __forceinline__ int keys_of(const SharedArgs &a, int s) {
@@ -147,20 +150,23 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_rsrc(const uint16_t *pool
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(t), 0, id < 0 ? 0 : kBlock * D * 2, kRawBuffer);
 }
 
-// A pair of blocks in LDS, as in the pool; in two of them waves merge, and the schedule is made.
+// Two pairs of blocks in LDS, as in the pool; there waves merge, too, and the schedule is made.
 template <int D>
-struct PairLds {
-    __attribute__((aligned(1024))) uint8_t tile[4][kBlock * D * 2];     // K, K, V, V
+struct StageLds {
+    __attribute__((aligned(1024))) uint8_t tile[8][kBlock * D * 2];     // K, K, V, V
 };
 
 template <int kMost>
 struct ShPlan {
     uint32_t cum[kMost + 1];       // own blocks of the sessions before
+    uint32_t cost[kMost + 1];      // and those with what beginning them takes
     uint16_t pb[kMost];            // blocks that the session shares
+    uint8_t pad[kMost];            // slots of its last block without a token
     uint16_t gid[kMost];
     uint16_t start[kMost + 1];     // of the group's members
     uint16_t prefix[kMost];        // blocks of the group
     uint32_t lead[kMost];          // its longest member: length, then lowest rank
+    uint16_t lead_s[kMost];        // that member
     uint32_t units[kMost + 1];     // units per KV head of the groups before
     uint16_t segs[kMost + 1];      // tiles per KV head of the groups before
     unsigned scan[2][kShWaves];
@@ -364,11 +370,11 @@ struct ShSink {
 
 // Adds the waves' states of 16 rows up and writes them.
 template <int D, int kMost>
-__device__ __forceinline__ void merge(ShPlan<kMost> &sm, PairLds<D> *buf, const RowState<D> &st, const ShSink &sink) {
+__device__ __forceinline__ void merge(ShPlan<kMost> &sm, StageLds<D> *buf, const RowState<D> &st, const ShSink &sink) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
     // [wave][D / 16][64] of 16 bytes
     auto slot = [&](int w, int dt) { return reinterpret_cast<f32x4 *>(buf) + (w * (D / 16) + dt) * kWave + lane; };
-    static_assert(2 * sizeof(PairLds<D>) == kShWaves * (D / 16) * kWave * sizeof(f32x4), "a state per wave");
+    static_assert(sizeof(StageLds<D>) == kShWaves * (D / 16) * kWave * sizeof(f32x4), "a state per wave");
     if (g4 == 0) {
         sm.m[wave][c16] = st.m;
         sm.l[wave][c16] = st.l;
@@ -406,102 +412,113 @@ __device__ __forceinline__ void merge(ShPlan<kMost> &sm, PairLds<D> *buf, const 
 }
 
 // More rows: tiles `wave` and `wave` + 4 of 16 of them are this wave's (count of them),
-// and every pair of the part goes through LDS: each wave loads one of its four tiles into
-// registers a pair ahead and stores it beside the pair at work.
+// and every pair of the part goes through LDS, two a stage: each wave loads one of a pair's
+// four tiles into registers a stage ahead and stores it beside the stage at work.
 template <int D>
-__device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &part, PairLds<D> *buf, const uint16_t *const (&qrow)[2],
+__device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &part, StageLds<D> *buf, const uint16_t *const (&qrow)[2],
                                           const int (&row_len)[2], int count, float *ml, float *acc, int rows) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c16 = lane % 16, g4 = lane / 16;
     constexpr int kLoads = kBlock * D * 2 / 1024;        // of a tile, a kilobyte each
-    const int pairs = (part.j1 - part.j0 + 1) / 2;
-    int ids = -1;                              // of 64 blocks
-    auto fetch_ids = [&](int i) {
-        ids = part_id(a, part, part.j0 + 2 * i + lane);
+    const int pairs = (part.j1 - part.j0 + 1) / 2, stages = (pairs + 1) / 2;
+    int ids = -1;                              // of 64 blocks, 16 stages
+    auto fetch_ids = [&](int st) {
+        ids = part_id(a, part, part.j0 + 4 * st + lane);
         __builtin_amdgcn_s_waitcnt(0x0F70);
     };
     bf16x8 qop[2][D / 32];
-    RowState<D> st[2];
+    RowState<D> rs[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks) qop[r][ks] = *reinterpret_cast<const bf16x8 *>(qrow[r] + ks * 32 + g4 * 8);
-        st[r].clear();
+        rs[r].clear();
     }
-    u32x4 ahead[kLoads];                       // tile `wave` of a pair: K, K, V, V
-    // Requests pair i (behind the last nothing, by as many loads); a bit per block that is absent.
-    auto load = [&](int i) {
-        if (i % (kWave / 2) == 0) fetch_ids(i);
-        const int id0 = __builtin_amdgcn_readlane(ids, 2 * i % kWave), id1 = __builtin_amdgcn_readlane(ids, (2 * i + 1) % kWave);
-        const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, wave % 2 ? id1 : id0, wave >= 2);
+    u32x4 ahead[2][kLoads];                    // tile `wave` of each pair: K, K, V, V
+    // Requests a stage (behind the last nothing, by as many loads); a bit per block that is absent.
+    auto load = [&](int st) {
+        if (st % (kWave / 4) == 0) fetch_ids(st);
+        int absent = 0;
 #pragma unroll
-        for (int kb = 0; kb < kLoads; ++kb) ahead[kb] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, kb * 1024, 0);
-        return (id0 < 0) | (id1 < 0) << 1;
+        for (int p = 0; p < 2; ++p) {
+            const int id0 = __builtin_amdgcn_readlane(ids, (4 * st + 2 * p) % kWave), id1 = __builtin_amdgcn_readlane(ids, (4 * st + 2 * p + 1) % kWave);
+            const __amdgpu_buffer_rsrc_t r = tile_rsrc<D>(a.pool, a.num_kv_heads, part.head, wave % 2 ? id1 : id0, wave >= 2);
+#pragma unroll
+            for (int kb = 0; kb < kLoads; ++kb) ahead[p][kb] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, kb * 1024, 0);
+            absent |= (id0 < 0 ? 1 : 0) << (2 * p) | (id1 < 0 ? 2 : 0) << (2 * p);
+        }
+        return absent;
     };
-    auto store = [&](int i) {
-        const int tok = (part.j0 + 2 * i + wave % 2) * kBlock;
-        if (wave >= 2 && tok + kBlock > part.longest) {
-            // 16 bytes: eight tokens of a dim
-            const int t = tok + lane % 2 * 8;
+    auto store = [&](int st) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int tok = (part.j0 + 4 * st + 2 * p + wave % 2) * kBlock;
+            if (wave >= 2 && tok + kBlock > part.longest) {
+                // 16 bytes: eight tokens of a dim
+                const int t = tok + lane % 2 * 8;
+#pragma unroll
+                for (int kb = 0; kb < kLoads; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ahead[p][kb][e] = seen_v(ahead[p][kb][e], t + 2 * e, part.longest);
+            }
 #pragma unroll
             for (int kb = 0; kb < kLoads; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) ahead[kb][e] = seen_v(ahead[kb][e], t + 2 * e, part.longest);
+                *reinterpret_cast<u32x4 *>(buf[st & 1].tile[4 * p + wave] + kb * 1024 + lane * 16) = ahead[p][kb];
         }
-#pragma unroll
-        for (int kb = 0; kb < kLoads; ++kb) *reinterpret_cast<u32x4 *>(buf[i & 1].tile[wave] + kb * 1024 + lane * 16) = ahead[kb];
     };
     int absent = load(0);
     store(0);
     int absent_next = load(1);
 #pragma unroll 1
-    for (int i = 0; i < pairs; ++i) {
-        // The stores of pair i are done; loads stay in flight.
+    for (int st = 0; st < stages; ++st) {
+        // The stage's stores are done; loads stay in flight.
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0xC07F);    // lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        const PairLds<D> &t = buf[i & 1];
-        const int tok0 = (part.j0 + 2 * i) * kBlock;
-        if (count) {
-            f32x4 s[2][2] = {};
+        if (count)
+#pragma unroll 1
+            for (int p = 0; p < min(2, pairs - 2 * st); ++p) {
+                const uint8_t(*t)[kBlock * D * 2] = buf[st & 1].tile + 4 * p;
+                const int tok0 = (part.j0 + 4 * st + 2 * p) * kBlock;
+                f32x4 s[2][2] = {};
 #pragma unroll
-            for (int ks = 0; ks < D / 32; ++ks)
+                for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const bf16x8 k = *reinterpret_cast<const bf16x8 *>(t.tile[b] + ks * 1024 + lane * 16);
+                    for (int b = 0; b < 2; ++b) {
+                        const bf16x8 k = *reinterpret_cast<const bf16x8 *>(t[b] + ks * 1024 + lane * 16);
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[r][ks], s[r][b], 0, 0, 0);
+                        for (int r = 0; r < 2; ++r) s[r][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qop[r][ks], s[r][b], 0, 0, 0);
+                    }
+                bf16x8 pr[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    float x[2][4];
+                    scores_of(s[r], a.scale_log2, tok0, row_len[r], absent >> (2 * p), x);
+                    pr[r] = rs[r].take(x);
                 }
-            bf16x8 p[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float x[2][4];
-                scores_of(s[r], a.scale_log2, tok0, row_len[r], absent, x);
-                p[r] = st[r].take(x);
+                for (int dt = 0; dt < D / 16; ++dt) {
+                    const int at = (dt * 16 + c16) * kBlock * 2 + g4 * 8;
+                    const u32x2 v0 = *reinterpret_cast<const u32x2 *>(t[2] + at), v1 = *reinterpret_cast<const u32x2 *>(t[3] + at);
+                    const u32x4 va = {v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        rs[r].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), pr[r], rs[r].o[dt], 0, 0, 0);
+                }
             }
-#pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) {
-                const uint8_t *at = t.tile[2] + (dt * 16 + c16) * kBlock * 2 + g4 * 8;
-                const u32x2 v0 = *reinterpret_cast<const u32x2 *>(at), v1 = *reinterpret_cast<const u32x2 *>(at + sizeof t.tile[2]);
-                const u32x4 va = {v0.x, v0.y, v1.x, v1.y};
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                    st[r].o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va), p[r], st[r].o[dt], 0, 0, 0);
-            }
-        }
-        store(i + 1);                          // (the pair before, whose buffer it is, was left at the barrier)
+        store(st + 1);                         // (the stage before, whose buffer it is, was left at the barrier)
         absent = absent_next;
-        absent_next = load(i + 2);
+        absent_next = load(st + 2);
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int row = (wave + r * kShWaves) * 16 + c16;
-        const float l = sum_xor_16_32(st[r].l);
+        const float l = sum_xor_16_32(rs[r].l);
         if (row < rows) {
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4 *>(acc + (int64_t)row * D + dt * 16 + 4 * g4) = st[r].o[dt];
-            if (g4 == 0) *reinterpret_cast<float2 *>(ml + 2 * row) = make_float2(st[r].m, l);
+            for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4 *>(acc + (int64_t)row * D + dt * 16 + 4 * g4) = rs[r].o[dt];
+            if (g4 == 0) *reinterpret_cast<float2 *>(ml + 2 * row) = make_float2(rs[r].m, l);
         }
     }
     __syncthreads();
@@ -510,9 +527,9 @@ __device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &par
 template <int D, int kMost, bool kWeights>
 __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs a) {
     __shared__ ShPlan<kMost> sm;
-    __shared__ PairLds<D> buf[2];
+    __shared__ StageLds<D> buf[2];
     int32_t *const owner = reinterpret_cast<int32_t *>(buf[0].tile[0]);   // a session's place among the members, or -1
-    static_assert(kShMost * 4 <= sizeof(PairLds<D>), "owners fit a buffer");
+    static_assert(kShMost * 4 <= sizeof(StageLds<D>), "owners fit a buffer");
     const int tid = threadIdx.x, lane = tid % kWave, c16 = lane % 16;
     const int S = a.num_sessions, G = a.group, H = a.num_kv_heads;
     const bool first_wg = blockIdx.x == 0;
@@ -575,6 +592,14 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
                 atomicMax(&sm.lead[lo], (uint32_t)len[s] << kRank | (uint32_t)(kShMost - 1 - (i - sm.start[lo])));
             }
             bad = __syncthreads_or(wrong);
+            if (!bad)
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    const int i = tid + k * kShThreads, s = ld_member[k];
+                    if (i >= a.num_members) continue;
+                    const int g = sm.gid[s];
+                    if (kShMost - 1 - (i - sm.start[g]) == (int)(sm.lead[g] & (kShMost - 1))) sm.lead_s[g] = (uint16_t)s;
+                }
         }
     }
     if (bad) {
@@ -591,7 +616,7 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             const int rows = (sm.start[g + 1] - sm.start[g]) * G, longest = (int)(sm.lead[g] >> kRank);
             const int pb = min((int)sm.prefix[g], (longest + kBlock - 1) / kBlock);
             sm.prefix[g] = (uint16_t)pb;
-            v[0] += (unsigned)(group_cost(rows) * pb);
+            v[0] += (unsigned)group_cost(rows, pb);
             v[1] += (unsigned)((rows + kTileRows - 1) / kTileRows);
         }
         if (ng) scan2(v, all, sm.scan);
@@ -600,7 +625,7 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             const int rows = (sm.start[g + 1] - sm.start[g]) * G;
             sm.units[g] = v[0];
             sm.segs[g] = (uint16_t)v[1];
-            v[0] += (unsigned)(group_cost(rows) * sm.prefix[g]);
+            v[0] += (unsigned)group_cost(rows, sm.prefix[g]);
             v[1] += (unsigned)((rows + kTileRows - 1) / kTileRows);
         }
         if (tid == 0) {
@@ -615,14 +640,23 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
         auto own = [&](int s, int pb) { return (unsigned)max((len[s] + kBlock - 1) / kBlock - pb, 0); };
         for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) {
             sm.pb[s] = owner[s] >= 0 ? sm.prefix[sm.gid[s]] : (uint16_t)0;
-            v[0] += own(s, sm.pb[s]);
+            sm.pad[s] = (uint8_t)(-len[s] & (kBlock - 1));
+            const unsigned n = own(s, sm.pb[s]);
+            v[0] += n;
+            v[1] += n ? n + kCostPart : 0u;
         }
         scan2(v, all, sm.scan);
         for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) {
+            const unsigned n = own(s, sm.pb[s]);
             sm.cum[s] = v[0];
-            v[0] += own(s, sm.pb[s]);
+            sm.cost[s] = v[1];
+            v[0] += n;
+            v[1] += n ? n + kCostPart : 0u;
         }
-        if (tid == 0) sm.cum[S] = all[0];
+        if (tid == 0) {
+            sm.cum[S] = all[0];
+            sm.cost[S] = all[1];
+        }
     }
     __syncthreads();
     if (first_wg) {
@@ -643,17 +677,22 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
         }
     }
     __syncthreads();                           // the buffers of owners and lengths are used again
-    // Consecutive shares on one XCD: the tiles of a group and KV head read the same K and V.  Own
-    // shares from the other end, so that where there is little of both it falls to different workgroups.
-    const int W = gridDim.x;
-    const int wp = W % 8 == 0 ? (int)(blockIdx.x % 8) * (W / 8) + (int)(blockIdx.x / 8) : (int)blockIdx.x, wo = W - 1 - wp;
+    // Workgroups for prefixes and for own blocks, the same of each on every XCD (8, where workgroup b
+    // runs on b % 8), and consecutive shares on one: the tiles of a group and KV head read the same K and V.
+    const int W = gridDim.x, xcds = W % 8 ? 1 : 8, b = blockIdx.x / xcds, x = blockIdx.x % xcds;
+    const int units_tile = H * (int)sm.units[ng], units_own = H * (int)sm.cost[S];
+    int tile_wgs = units_tile ? (int)((float)(W / xcds) * units_tile / ((float)units_tile + units_own) + 0.5f) : 0;
+    if (units_tile) tile_wgs = max(tile_wgs, 1);
+    if (units_own) tile_wgs = min(tile_wgs, W / xcds - 1);
+    const int own_wgs = W / xcds - tile_wgs;
     // Blocks of the segment at `pos` that are in [u0, u1).
     auto range = [](int u0, int u1, int pos, int blocks, int cost, int &j0, int &j1) {
-        j0 = u0 > pos ? (u0 - pos + cost - 1) / cost : 0;
-        j1 = u1 - pos >= blocks * cost ? blocks : (u1 - pos + cost - 1) / cost;
+        const int from = pos + kCostPart;
+        j0 = u0 > from ? min((u0 - from + cost - 1) / cost, blocks) : 0;
+        j1 = u1 > from ? min((u1 - from + cost - 1) / cost, blocks) : 0;
     };
     auto prefix_tiles = [&]() {
-        const int all = H * (int)sm.units[ng], share = max((all + W - 1) / W, kLeastUnits);
+        const int n = tile_wgs * xcds, wp = x * tile_wgs + b, all = units_tile, share = max((all + n - 1) / n, kLeastTile);
         if (wp > all / share) return;
         const int at = wp * share, u1 = min(at + share, all);
         if (at >= u1) return;
@@ -669,11 +708,11 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             const int pb = sm.prefix[g], first = sm.start[g], rows = (sm.start[g + 1] - first) * G;
             const int tiles = (rows + kTileRows - 1) / kTileRows;
             const int gpos = H * (int)sm.units[g];
-            const int lead_s = a.members[first + kShMost - 1 - (int)(sm.lead[g] & (kShMost - 1))];
+            const int lead_s = sm.lead_s[g];
             for (int h = at > gpos ? (at - gpos) / stride : 0; h < H && gpos + h * stride < u1; ++h) {
                 const int hpos = gpos + h * stride;
-                for (int t = at > hpos ? (at - hpos) / (pb * kCostTile) : 0; t < tiles; ++t) {
-                    const int pos = hpos + t * pb * kCostTile;
+                for (int t = at > hpos ? (at - hpos) / (pb * kCostTile + kCostPart) : 0; t < tiles; ++t) {
+                    const int pos = hpos + t * (pb * kCostTile + kCostPart);
                     if (pos >= u1) break;
                     const int n = min(kTileRows, rows - t * kTileRows);
                     ShPart part;
@@ -716,27 +755,28 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
         }
     };
     auto own_keys = [&]() {
-        const int all = H * (int)sm.cum[S], share = max((all + W - 1) / W, kLeastOwn);
+        const int n = own_wgs * xcds, wo = x * own_wgs + b - tile_wgs, all = units_own, share = max((all + n - 1) / n, kLeastOwn);
         if (wo > all / share) return;
         const int at = wo * share, u1 = min(at + share, all);
         if (at >= u1) return;
-        const int rel = at / H;                 // blocks per KV head before
+        const int rel = at / H;                 // units per KV head before
         int s = 0, hi = S;                      // the last session that starts at or before it
         while (hi - s > 1) {
             const int mid = (s + hi) / 2;
-            if ((int)sm.cum[mid] <= rel) s = mid;
+            if ((int)sm.cost[mid] <= rel) s = mid;
             else hi = mid;
         }
         for (; s < S; ++s) {
-            const int spos = H * (int)sm.cum[s];
+            const int spos = H * (int)sm.cost[s];
             if (spos >= u1) break;
             const int nb = (int)(sm.cum[s + 1] - sm.cum[s]);
             if (!nb) continue;
-            const int pb = sm.pb[s], L = keys_of(a, s);
-            for (int h = at > spos ? (at - spos) / nb : 0; h < H; ++h) {
-                const int pos = spos + h * nb;
+            const int pb = sm.pb[s], L = (pb + nb) * kBlock - sm.pad[s];
+            for (int h = at > spos ? (at - spos) / (nb + kCostPart) : 0; h < H; ++h) {
+                const int pos = spos + h * (nb + kCostPart);
                 if (pos >= u1) break;
-                const int j0 = max(at - pos, 0), j1 = min(u1 - pos, nb);
+                int j0, j1;
+                range(at, u1, pos, nb, 1, j0, j1);
                 if (j0 >= j1) continue;
                 const ShPart part = {a.tables + (int64_t)s * a.max_blocks, h, pb + j0, pb + j1, L};
                 const bool whole = !pb && j0 == 0 && j1 == nb;
@@ -754,12 +794,8 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             }
         }
     };
-    const bool own_first = blockIdx.x >= gridDim.x / 2;
-#pragma unroll 1
-    for (int phase = 0; phase < 2; ++phase) {
-        if ((phase == 0) == own_first) own_keys();
-        else prefix_tiles();
-    }
+    if (b < tile_wgs) prefix_tiles();
+    else own_keys();
 }
 
 // The parts of a row: those of its prefix tile, then its own.
