@@ -10,7 +10,7 @@
 // against K and V tiles that are read once per 64 rows, and each session's own
 // keys are walked for it alone.
 //
-// Work: segments = (group, KV head, tile of up to 128 rows) over the group's blocks,
+// Work: segments = (group, KV head, tile of up to 16 or 128 rows) over the group's blocks,
 // then (session, KV head) over its own blocks.  A block of a segment costs some units
 // (kCost*).  Of the workgroups, of four waves, two per CU, as many as the units say are for
 // prefixes and the others for own blocks, on every XCD; each takes an equal contiguous
@@ -22,7 +22,8 @@
 // instructions for the first time took as long as the work: loops are not unrolled, and
 // masked and whole pairs share their code.  A segment that one workgroup has whole, without a shared
 // prefix, is written out at once; other parts leave their state in the workspace, at slot
-// (segment + workgroup), which no other part has, and a second kernel adds them up.
+// (segment + workgroup), which no other part has (prefix tiles at row 16 places before +
+// 128 workgroup), and a second kernel adds them up.
 //
 // Accumulated weights: the probability of a key is known only once its row's sum
 // is, so the first kernel leaves the scores of the own keys (fp32, 4 bytes a head
@@ -57,7 +58,9 @@ constexpr int kShPerCu = 2;                  // workgroups
 // Sessions, members and groups that a kernel's LDS has room for: with the few, two
 // workgroups fit a CU.
 constexpr int kShFew = 512, kShMost = 2048;
-constexpr int kTileRows = 128;               // rows of a prefix segment: two tiles of 16 per wave
+// Rows of a prefix segment: 128 (two tiles of 16 per wave), but 16 in groups of up to 64,
+// where four parts of 16 cost no more than one of 128 and a wave waits for less.
+constexpr int kTileRows = 128, kFewRows = 16, kFewMost = 64;
 constexpr int kRank = 11;                    // bits of a member's rank (kShMost of them)
 static_assert(kShMost == 1 << kRank && kShMost == kMaxCacheSessions, "ranks fit");
 // Units: of an own block and a block of a prefix tile of up to 16 rows (whose pairs the
@@ -78,8 +81,8 @@ constexpr int kStream = 2;                   // non-temporal: own keys are read 
 struct ShRecord {
     int32_t own_blocks;            // 0: no own key
     int32_t prefix_blocks;         // 0: no prefix
-    int32_t tile_seg;              // prefix segment at KV head 0
-    int32_t tile_seg_stride;       // prefix segments per KV head of its group
+    int32_t tile_seg;              // first 16-row place of its prefix tile at KV head 0
+    int32_t tile_seg_stride;       // places per KV head of its group
     int32_t tile_row;              // its first row in the tile
     int32_t keys;                  // L
     uint32_t own_before;           // own blocks of the sessions before
@@ -102,10 +105,10 @@ struct SharedArgs {
     const int32_t *prefix;         // [num_groups] blocks
     float scale_log2;
     ShRecord *records;             // [S]
-    int32_t *tile_first, *tile_last;     // [prefix segments] workgroups of a segment's first and last part
+    int32_t *tile_first, *tile_last;     // [first place of a prefix tile] workgroups of its first and last part
     int32_t *own_first, *own_last;       // [S][Hkv]
-    float *tile_ml;                // [tile slots][128][2]
-    float *tile_acc;               // [tile slots][128][D]
+    float *tile_ml;                // [16 first places + 128 workgroups][2]
+    float *tile_acc;               // the same [D]
     float *own_ml;                 // [own slots][G][2]
     float *own_acc;                // [own slots][G][D]
     // Accumulated weights
@@ -118,12 +121,18 @@ struct SharedArgs {
     unsigned int *err;
 };
 
-__device__ __forceinline__ int tile_cost(int rows) { return rows <= 16 ? kCostFew : kCostTile; }
+__device__ __forceinline__ int tile_cost(int rows) { return rows <= kFewRows ? kCostFew : kCostTile; }
+__device__ __forceinline__ int tile_size(int rows) { return rows <= kFewMost ? kFewRows : kTileRows; }
+// 16-row places that the tiles of a group take per KV head.
+__device__ __forceinline__ int tile_places(int rows) {
+    const int size = tile_size(rows);
+    return (rows + size - 1) / size * (size / kFewRows);
+}
 // Units of all tiles of a group of `rows` rows over `blocks` blocks, per KV head.
 __device__ __forceinline__ int group_cost(int rows, int blocks) {
-    const int rest = rows % kTileRows;
+    const int size = tile_size(rows), rest = rows % size;
     if (!blocks) return 0;
-    return rows / kTileRows * (kCostTile * blocks + kCostPart) + (rest ? tile_cost(rest) * blocks + kCostPart : 0);
+    return rows / size * (tile_cost(size) * blocks + kCostPart) + (rest ? tile_cost(rest) * blocks + kCostPart : 0);
 }
 // Keys of session s, clipped to its table.
 __device__ __forceinline__ int keys_of(const SharedArgs &a, int s) {
@@ -168,7 +177,7 @@ struct ShPlan {
     uint32_t lead[kMost];          // its longest member: length, then lowest rank
     uint16_t lead_s[kMost];        // that member
     uint32_t units[kMost + 1];     // units per KV head of the groups before
-    uint16_t segs[kMost + 1];      // tiles per KV head of the groups before
+    uint16_t segs[kMost + 1];      // places of their tiles, per KV head
     unsigned scan[2][kShWaves];
     float m[kShWaves][16], l[kShWaves][16];       // the merge of a part's waves
 };
@@ -617,7 +626,7 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             const int pb = min((int)sm.prefix[g], (longest + kBlock - 1) / kBlock);
             sm.prefix[g] = (uint16_t)pb;
             v[0] += (unsigned)group_cost(rows, pb);
-            v[1] += (unsigned)((rows + kTileRows - 1) / kTileRows);
+            v[1] += (unsigned)tile_places(rows);
         }
         if (ng) scan2(v, all, sm.scan);
         else all[0] = all[1] = 0u;
@@ -626,7 +635,7 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             sm.units[g] = v[0];
             sm.segs[g] = (uint16_t)v[1];
             v[0] += (unsigned)group_cost(rows, sm.prefix[g]);
-            v[1] += (unsigned)((rows + kTileRows - 1) / kTileRows);
+            v[1] += (unsigned)tile_places(rows);
         }
         if (tid == 0) {
             sm.units[ng] = all[0];
@@ -667,11 +676,11 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             r.own_all = sm.cum[S];
             r.keys = len[s];
             if (owner[s] >= 0) {
-                const int g = sm.gid[s], row = (owner[s] - sm.start[g]) * G;
+                const int g = sm.gid[s], row = (owner[s] - sm.start[g]) * G, size = tile_size((sm.start[g + 1] - sm.start[g]) * G);
                 r.prefix_blocks = sm.prefix[g];
-                r.tile_seg = H * sm.segs[g] + row / kTileRows;
+                r.tile_seg = H * sm.segs[g] + row / size * (size / kFewRows);
                 r.tile_seg_stride = sm.segs[g + 1] - sm.segs[g];
-                r.tile_row = row % kTileRows;
+                r.tile_row = row % size;
             }
             a.records[s] = r;
         }
@@ -706,31 +715,31 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
             const int stride = (int)(sm.units[g + 1] - sm.units[g]);
             if (!stride) continue;
             const int pb = sm.prefix[g], first = sm.start[g], rows = (sm.start[g + 1] - first) * G;
-            const int tiles = (rows + kTileRows - 1) / kTileRows;
+            const int size = tile_size(rows), tiles = (rows + size - 1) / size, full = pb * tile_cost(size) + kCostPart;
             const int gpos = H * (int)sm.units[g];
             const int lead_s = sm.lead_s[g];
             for (int h = at > gpos ? (at - gpos) / stride : 0; h < H && gpos + h * stride < u1; ++h) {
                 const int hpos = gpos + h * stride;
-                for (int t = at > hpos ? (at - hpos) / (pb * kCostTile + kCostPart) : 0; t < tiles; ++t) {
-                    const int pos = hpos + t * (pb * kCostTile + kCostPart);
+                for (int t = at > hpos ? (at - hpos) / full : 0; t < tiles; ++t) {
+                    const int pos = hpos + t * full;
                     if (pos >= u1) break;
-                    const int n = min(kTileRows, rows - t * kTileRows);
+                    const int n = min(size, rows - t * size);
                     ShPart part;
                     range(at, u1, pos, pb, tile_cost(n), part.j0, part.j1);
                     if (part.j0 >= part.j1) continue;
                     part.table = a.tables + (int64_t)lead_s * a.max_blocks;
                     part.head = h;
                     part.longest = (int)(sm.lead[g] >> kRank);
-                    const int seg = H * sm.segs[g] + h * tiles + t;
-                    const int64_t slot = (int64_t)seg + wp;
-                    float *ml = a.tile_ml + slot * kTileRows * 2, *acc = a.tile_acc + slot * kTileRows * D;
+                    const int seg = H * sm.segs[g] + (h * tiles + t) * (size / kFewRows);
+                    const int64_t row0 = (int64_t)seg * kFewRows + (int64_t)wp * kTileRows;
+                    float *ml = a.tile_ml + row0 * 2, *acc = a.tile_acc + row0 * D;
                     if (tid == 0) {
                         if (part.j0 == 0) a.tile_first[seg] = wp;
                         if (part.j1 == pb) a.tile_last[seg] = wp;
                     }
                     // (lanes of no row take the last one: a load under a condition waits for the one before)
                     auto row_of = [&](int row, const uint16_t *&qrow, int &len) {
-                        const int x = t * kTileRows + min(row, n - 1), s = a.members[first + (x >> gs)];
+                        const int x = t * size + min(row, n - 1), s = a.members[first + (x >> gs)];
                         qrow = a.q + ((int64_t)s * H * G + h * G + (x & (G - 1))) * D;
                         len = keys_of(a, s);
                     };
@@ -809,7 +818,7 @@ __device__ __forceinline__ RowParts parts_of(const SharedArgs &a, const ShRecord
     if (r.prefix_blocks) {
         const int w = a.tile_first[tile];
         p.prefix = a.tile_last[tile] - w + 1;
-        p.prefix_row = ((int64_t)tile + w) * kTileRows + r.tile_row + head;
+        p.prefix_row = (int64_t)tile * kFewRows + (int64_t)w * kTileRows + r.tile_row + head;
     }
     if (r.own_blocks) {
         const int w = a.own_first[seg];
@@ -984,14 +993,15 @@ SharedPlan plan_shared(const PoolGeom &p, int32_t num_sessions, int32_t num_q_he
                        int32_t num_members, bool weights) {
     const int64_t H = p.num_kv_heads, G = num_q_heads / p.num_kv_heads, W = kShPerCu * (p.num_cus > 0 ? p.num_cus : 256);
     SharedPlan s;
-    // (a slot per segment and one per workgroup; a group has a tile that is not full)
-    const size_t tiles = num_groups ? (size_t)(H * ((int64_t)num_members * G / kTileRows + num_groups)) : 0;
-    const size_t tile_slots = num_groups ? tiles + (size_t)W : 0, own_slots = (size_t)(num_sessions * H + W);
+    // (a slot per segment and one per workgroup.  A group's rows round up to 16, those of more than 64 to 128.)
+    const int64_t rows = (int64_t)num_members * G, large = std::min<int64_t>(num_groups, rows / (kFewMost + 1));
+    const size_t tiles = num_groups ? (size_t)(H * (rows / kFewRows + num_groups + (kTileRows / kFewRows - 1) * large)) : 0;
+    const size_t tile_rows = num_groups ? tiles * kFewRows + (size_t)W * kTileRows : 0, own_slots = (size_t)(num_sessions * H + W);
     const size_t sizes[] = {(size_t)num_sessions * sizeof(ShRecord),
                             tiles * 2 * sizeof(int32_t),
                             (size_t)(num_sessions * H) * 2 * sizeof(int32_t),
-                            tile_slots * kTileRows * 2 * sizeof(float),
-                            tile_slots * kTileRows * (size_t)p.head_dim * sizeof(float),
+                            tile_rows * 2 * sizeof(float),
+                            tile_rows * (size_t)p.head_dim * sizeof(float),
                             own_slots * (size_t)G * 2 * sizeof(float),
                             own_slots * (size_t)G * (size_t)p.head_dim * sizeof(float),
                             weights ? (size_t)p.num_blocks * (size_t)num_q_heads * kBlock * sizeof(float) : 0};
