@@ -834,7 +834,6 @@ __device__ __forceinline__ RowParts parts_of(const SharedArgs &a, const ShRecord
 template <int D, bool kWeights>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, int combine) {
     __shared__ uint32_t sm_cum[kWeights ? kShMost + 1 : 1];
-    __shared__ float sm_top[8], sm_inv[8];
     const int tid = threadIdx.x, H = a.num_kv_heads, G = a.group, S = a.num_sessions;
     if ((int)blockIdx.x < combine) {
         constexpr int kLanes = D / 4, kAhead = 8;
@@ -885,8 +884,11 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
         const uint32_t own_all = a.records[0].own_all;
         if (tid == 0) sm_cum[S] = own_all;
         __syncthreads();
-        const int all = (int)own_all * H, n = gridDim.x - combine, w = blockIdx.x - combine;
-        const int per = max((all + n - 1) / n, kShThreads / 4);
+        // Shares are a wave's: with a workgroup's, the second segment of a share waited for the first.
+        constexpr int kQuads = kWave / 4;                            // blocks at a time
+        const int lane = tid % kWave;
+        const int all = (int)own_all * H, n = (gridDim.x - combine) * kShWaves, w = (blockIdx.x - combine) * kShWaves + tid / kWave;
+        const int per = max((all + n - 1) / n, kQuads);
         if (w > all / per) return;
         const int b0 = w * per, b1 = min(b0 + per, all);
         if (b0 >= b1) return;
@@ -906,16 +908,14 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
             for (int h = b0 > spos ? (b0 - spos) / r.own_blocks : 0; h < H; ++h) {
                 const int pos = spos + h * r.own_blocks;
                 if (pos >= b1) break;
-                __syncthreads();                                     // the segment before is done with sm_top
-                if (tid < kWave) {
-                    // lane = (part, query head), eight parts at a time
-                    const int head = tid % 8, lane_part = tid / 8;
-                    const RowParts p = parts_of(a, r, s, h, min(head, G - 1));
-                    float top = kNoMax, sum = 0.f;
-                    for (int i = lane_part; i < p.prefix + p.own; i += kWave / 8) {
+                // The rows' whole sums: lane = (part, query head), eight parts at a time
+                float top = kNoMax, sum = 0.f;
+                {
+                    const RowParts p = parts_of(a, r, s, h, min(lane % 8, G - 1));
+                    for (int i = lane / 8; i < p.prefix + p.own; i += kWave / 8) {
                         const bool tile = i < p.prefix;
-                        const int64_t at = tile ? p.prefix_row + (int64_t)i * kTileRows : p.own_row + (int64_t)(i - p.prefix) * G;
-                        const float2 ml = reinterpret_cast<const float2 *>(tile ? a.tile_ml : a.own_ml)[at];
+                        const int64_t row = tile ? p.prefix_row + (int64_t)i * kTileRows : p.own_row + (int64_t)(i - p.prefix) * G;
+                        const float2 ml = reinterpret_cast<const float2 *>(tile ? a.tile_ml : a.own_ml)[row];
                         const float now = fmaxf(top, ml.x);
                         sum = sum * __builtin_amdgcn_exp2f(top - now) + ml.y * __builtin_amdgcn_exp2f(ml.x - now);
                         top = now;
@@ -926,30 +926,31 @@ __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, 
                         sum = sum * __builtin_amdgcn_exp2f(top - now) + s2 * __builtin_amdgcn_exp2f(t2 - now);
                         top = now;
                     }
-                    if (tid < G) {
-                        sm_top[tid] = top;
-                        sm_inv[tid] = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-                    }
                 }
-                __syncthreads();
+                const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
                 const int j0 = max(b0 - pos, 0), j1 = min(b1 - pos, r.own_blocks);
-                for (int j = j0 + tid / 4; j < j1; j += kShThreads / 4) {
-                    const int col = r.prefix_blocks + j, t0 = col * kBlock + tid % 4 * 4;
-                    const int id = a.tables[(int64_t)s * a.max_blocks + col];
-                    if (id < 0 || id >= a.num_blocks || t0 >= r.keys || t0 + 4 <= first) continue;
-                    const float *x = a.scores + ((int64_t)id * H + h) * G * kBlock + tid % 4 * 4;
-                    const int64_t at = ((int64_t)id * H + h) * kBlock + tid % 4 * 4;
+                for (int j = j0 + lane / 4; j - lane / 4 < j1; j += kQuads) {
+                    const int col = r.prefix_blocks + j, t0 = col * kBlock + lane % 4 * 4;
+                    const int id = j < j1 ? a.tables[(int64_t)s * a.max_blocks + col] : -1;
+                    const bool use = id >= 0 && id < a.num_blocks && t0 < r.keys && t0 + 4 > first;
+                    const int64_t tile = (int64_t)(use ? id : 0) * H + h, at = tile * kBlock + lane % 4 * 4;
+                    const float *x = a.scores + tile * G * kBlock + lane % 4 * 4;
                     const f32x4 was = *reinterpret_cast<const f32x4 *>(a.weights + at);
-                    f32x4 p = {0.f, 0.f, 0.f, 0.f};
-                    f32x4 y[8];
+                    f32x4 p = {0.f, 0.f, 0.f, 0.f}, y[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) y[k] = *reinterpret_cast<const f32x4 *>(x + min(k, G - 1) * kBlock);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < G) {
+                    for (int k = 0; k < 8; ++k) {
+                        const float m = __shfl(top, k), scale = k < G ? __shfl(inv, k) : 0.f;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) p[e] += __builtin_amdgcn_exp2f(y[k][e] - sm_top[k]) * sm_inv[k];
-                        }
+                        for (int e = 0; e < 4; ++e)
+                            if (k < G) p[e] += __builtin_amdgcn_exp2f(y[k][e] - m) * scale;
+                    }
+                    if (!use) continue;
+                    if (t0 >= first && t0 + 4 <= r.keys && t0 + 4 <= old) {
+                        *reinterpret_cast<f32x4 *>(a.weights + at) = was + p;
+                        continue;
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int t = t0 + e;
