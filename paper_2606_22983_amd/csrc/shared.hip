@@ -534,7 +534,7 @@ __device__ __forceinline__ void tile_walk(const SharedArgs &a, const ShPart &par
 }
 
 template <int D, int kMost, bool kWeights>
-__global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs a) {
+__global__ __launch_bounds__(kShThreads, kMost == kShFew ? kShPerCu : 1) void shared_kernel(SharedArgs a) {
     __shared__ ShPlan<kMost> sm;
     __shared__ StageLds<D> buf[2];
     int32_t *const owner = reinterpret_cast<int32_t *>(buf[0].tile[0]);   // a session's place among the members, or -1
@@ -688,7 +688,8 @@ __global__ __launch_bounds__(kShThreads, kShPerCu) void shared_kernel(SharedArgs
     __syncthreads();                           // the buffers of owners and lengths are used again
     // Workgroups for prefixes and for own blocks, the same of each on every XCD (8, where workgroup b
     // runs on b % 8), and consecutive shares on one: the tiles of a group and KV head read the same K and V.
-    const int W = gridDim.x, xcds = W % 8 ? 1 : 8, b = blockIdx.x / xcds, x = blockIdx.x % xcds;
+    // (There are two workgroups at least, so both kinds get one where there is work of both.)
+    const int W = gridDim.x, xcds = W % 8 || W < 16 ? 1 : 8, b = blockIdx.x / xcds, x = blockIdx.x % xcds;
     const int units_tile = H * (int)sm.units[ng], units_own = H * (int)sm.cost[S];
     int tile_wgs = units_tile ? (int)((float)(W / xcds) * units_tile / ((float)units_tile + units_own) + 0.5f) : 0;
     if (units_tile) tile_wgs = max(tile_wgs, 1);

@@ -222,12 +222,14 @@ def test_two_captured_calls_with_their_own_workspaces_and_lengths_that_grow(kv):
     assert kv.ls_device_errors() == 0
 
 
-def test_on_a_stream_of_few_cus(kv):
+@pytest.mark.parametrize("cus", [8, 30])
+def test_on_a_stream_of_few_cus(kv, cus):
+    """Few workgroups: prefixes and own keys each get one at least."""
     from tests.gpu_util import cu_masked_stream, destroy_stream
     rng = np.random.default_rng(14)
     c = Cache(rng, 40 * BLOCK + rng.integers(1, 500, 7), 2, 64, [(list(range(5)), 40)])
     pool, q, out = check(kv, c, 16, "all CUs")
-    made = cu_masked_stream(0, 30)
+    made = cu_masked_stream(0, cus)
     if made is None:
         pytest.skip("no stream with a CU mask")
     stream, handle = made
@@ -235,8 +237,37 @@ def test_on_a_stream_of_few_cus(kv):
     few = run(kv, c, pool, q, stream=stream)
     stream.synchronize()
     destroy_stream(handle)
+    assert kv.ls_device_errors() == 0
     ref, mass, score, _ = decode_reference(c, 0, bits_of(q), 0.125)
-    assert_within(few, ref, mass, score, 64, "30 CUs")
+    assert_within(few, ref, mass, score, 64, "%d CUs" % cus)
+
+
+def test_two_calls_at_once(kv):
+    """On two streams, each with a workspace of its own, over the same pool."""
+    rng = np.random.default_rng(15)
+    c = Cache(rng, 30 * BLOCK + rng.integers(1, 900, 24), 4, 128, [(list(range(4, 24)), 30)])
+    pool = c.device(kv)
+    q = [bf16_dev(W.normal_bf16(rng, (24, 32, 128))) for _ in range(2)]
+    alone = [run(kv, c, pool, x) for x in q]
+    n = kv.decode_shared_workspace_bytes(pool, 24, 32, 1, 20)
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    lens, groups, outs = i32_dev(c.lens), c.group_arrays(), [torch.empty_like(x) for x in q]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, w, o, st in zip(q, ws, outs, streams):
+            kv.paged_attn_decode_shared(pool, 0, x, c.dtables, lens, *groups, 128 ** -0.5, o, w, stream=st)
+    torch.cuda.synchronize()
+    assert kv.ls_device_errors() == 0
+    assert all(torch.equal(a, b) for a, b in zip(alone, outs))
+
+
+def test_half_a_thousand_sessions(kv):
+    """On either side of what the smaller schedule holds."""
+    rng = np.random.default_rng(16)
+    for n in (511, 512, 513):
+        lens = rng.integers(1, 50, n) + 3 * BLOCK
+        check(kv, Cache(rng, lens, 1, 64, [(list(range(i, n, 9)), 3) for i in range(9)]), 8, "%d sessions" % n)
 
 
 def bits_of(t):
