@@ -468,8 +468,8 @@ ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const
  * and not on how often the call is made.  Other arguments as paged_attn_decode.
  *
  * Supported: num_q_heads / num_kv_heads in {1, 2, 4, 8}; at most 2048 sessions, 2048
- * groups and 16384 blocks per session, and fewer than 2^30 sessions x blocks per session
- * x KV heads (LS_EUNSUPPORTED).  Other errors: LS_EINVAL (also
+ * groups, 16384 blocks per session and 4096 KV heads, and fewer than 2^30 sessions x blocks
+ * per session x KV heads (LS_EUNSUPPORTED).  Other errors: LS_EINVAL (also
  * more members than sessions, more groups than members), LS_ENOMEM, LS_EHIP.
  */
 size_t ls_decode_shared_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,

@@ -415,6 +415,9 @@ ls_status check_cache_call(const PoolGeom &p, int32_t layer, int32_t num_session
     if (num_sessions > kMaxCacheSessions || max_blocks > kMaxCacheBlocks || p.num_kv_heads > 4096)
         return fail(LS_EUNSUPPORTED, "%d sessions with %d blocks each and %d KV heads exceed the limits (%d sessions, %d blocks per "
                     "session, 4096 KV heads)", num_sessions, max_blocks, p.num_kv_heads, kMaxCacheSessions, kMaxCacheBlocks);
+    if ((int64_t)num_sessions * max_blocks * p.num_kv_heads >= kMaxCacheUnits)
+        return fail(LS_EUNSUPPORTED, "%d sessions with %d blocks each of %d KV heads: 2^30 in all are too many", num_sessions,
+                    max_blocks, p.num_kv_heads);
     return LS_OK;
 }
 
@@ -450,9 +453,6 @@ ls_status shared_call(ls_kv_pool *pool, int32_t layer, int32_t num_sessions, int
     if (!aligned(c.block_tables, 4) || !aligned(c.context_lens, 4) || !aligned(c.reused_lens, 4) ||
         !aligned(c.first_positions, 4) || !aligned(c.first_lens, 4))
         return fail(LS_EINVAL, "tables, lengths and positions must be 4-byte aligned");
-    if ((int64_t)num_sessions * c.max_blocks * p.num_kv_heads >= kMaxCacheUnits)
-        return fail(LS_EUNSUPPORTED, "%d sessions with %d blocks each of %d KV heads: 2^30 in all are too many", num_sessions,
-                    c.max_blocks, p.num_kv_heads);
     const SharedPlan plan = plan_shared(p, num_sessions, num_q_heads, c.num_groups, c.num_members, weighted);
     if (workspace_bytes < plan.total)
         return fail(LS_ENOMEM, "workspace_bytes (%zu) < required (%zu)", workspace_bytes, plan.total);

@@ -179,7 +179,7 @@ hipError_t launch_prefill(const PoolGeom &p, int layer, int32_t num_sessions, in
 // Most sessions and blocks per session of the decodes with shared prefixes or
 // weights and of a turn's weights.
 constexpr int32_t kMaxCacheSessions = 2048, kMaxCacheBlocks = 16384;
-constexpr int64_t kMaxCacheUnits = 1 << 30;        // sessions x blocks x KV heads of these decodes (32-bit schedule)
+constexpr int64_t kMaxCacheUnits = 1 << 30;        // their product with the KV heads (32-bit schedules and grids)
 constexpr int32_t kMaxEvictSessions = 1 << 20;     // (an eviction's grid)
 
 // Decode with shared prefixes, and with accumulated weights (weights not null).

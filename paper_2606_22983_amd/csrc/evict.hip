@@ -81,13 +81,15 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
         }
         return a.ring ? (unsigned)(blocks_of(L) - blocks_of(keeps(a, s, L))) : 0u;
     };
-    // Exclusive prefix sum over the threads, and the total.
+    // Sums saturate at INT32_MAX, more than any ring has room for.
+    auto add = [](unsigned x, unsigned y) { return min(x + y, (unsigned)INT32_MAX); };
+    // Exclusive prefix sum over the threads, and the total (before: of sums that have not saturated).
     auto scan = [&](unsigned v, unsigned &total) {
         unsigned x = v;
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
             const unsigned y = __shfl_up(x, off);
-            if (lane >= off) x += y;
+            if (lane >= off) x = add(x, y);
         }
         __syncthreads();
         if (lane == kWave - 1) sm_wave[wave] = x;
@@ -96,18 +98,19 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
         total = 0u;
         for (int w = 0; w < kPlanThreads / kWave; ++w) {
             if (w == wave) before = total;
-            total += sm_wave[w];
+            total = add(total, sm_wave[w]);
         }
         return before + x - v;
     };
     unsigned v = 0u, total;
     bool wrong = false;
-    for (int s = tid; s < S; s += kPlanThreads) v += gives(s, wrong);
+    for (int s = tid; s < S; s += kPlanThreads) v = add(v, gives(s, wrong));
     scan(v, total);
     unsigned bad = __syncthreads_or(wrong) ? LS_DEVERR_LENGTH : 0u;
     if (a.ring && !bad) {
         const int64_t avail = given - taken;
-        if (taken < 0 || avail < 0 || avail > a.ring_size || total > a.ring_size - avail) bad = LS_DEVERR_FREE_LIST;
+        if (taken < 0 || avail < 0 || avail > a.ring_size || total == INT32_MAX || total > a.ring_size - avail)
+            bad = LS_DEVERR_FREE_LIST;
     }
     if (tid == 0) {
         if (bad) flag_error(a.err, bad);

@@ -366,7 +366,8 @@ ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_
     const int64_t G = num_q_heads / p.num_kv_heads, pairs = (int64_t)num_sessions * p.num_kv_heads;
     const int64_t cus = p.num_cus > 0 ? p.num_cus : 256;
     ObservePlan o;
-    o.whole_rows = (int32_t)(std::min<int64_t>(rows, max_new_len) * G);
+    // (a turn fits its table)
+    o.whole_rows = (int32_t)(std::min({(int64_t)rows, (int64_t)max_new_len, (int64_t)max_blocks * kBlock}) * G);
     o.row_cap = std::min(o.whole_rows, kObRows);
     // Blocks per wave: as many as leave every CU two workgroups.
     o.blocks = 4;

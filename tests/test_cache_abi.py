@@ -81,6 +81,7 @@ def test_workspace_sizes(lib, pool):  # noqa: F811
     h.restype = SZ
     assert 0 < h(pool, 4, 32, 100, 30, 1, 8) < h(pool, 4, 32, 100, 30, 16, 8) < h(pool, 4, 32, 100, 30, 16, 800)
     assert h(pool, 4, 32, 100, 30, 16, 8) == h(pool, 4, 32, 3000, 30, 16, 8)
+    assert h(pool, 4, 32, 2**31 - 1, 2**31 - 1, 2**31 - 1, 8) == h(pool, 4, 32, 200, 128, 128, 8)      # a turn fits its table
     for bad in ((0, 32, 10, 5, 1, 8), (2049, 32, 10, 5, 1, 8), (4, 30, 10, 5, 1, 8), (4, 32, 10, 11, 1, 8), (4, 32, 10, 0, 1, 8),
                 (4, 32, 10, 5, 0, 8), (4, 32, 10, 5, 1, 0), (4, 32, 10, 5, 1, 16385)):
         assert h(pool, *bad) == 0
@@ -134,6 +135,19 @@ def evict(lib, pool, **kw):  # noqa: F811
 ])
 def test_evict_rejects(lib, pool, kw):  # noqa: F811
     assert evict(lib, pool, **kw) == LS_EINVAL
+
+
+def test_limits_of_the_schedule(lib):  # noqa: F811
+    from tests.test_abi import _desc
+    h = ctypes.c_void_p()
+    for heads, status in ((32, LS_EUNSUPPORTED), (31, LS_ENOMEM)):
+        d = _desc(num_layers=1, num_kv_heads=heads, num_blocks=1, kv_bytes=1 << 30)
+        assert lib.kv_pool_create(ctypes.byref(d), ctypes.byref(h)) == LS_OK
+        big = dict(S=2048, maxb=16384, hq=heads, wsb=1000, M=2048)           # sessions x blocks x KV heads: 2^30, and less
+        assert shared(lib, h, **big) == status
+        assert weights(lib, h, **big) == status
+        assert prompt(lib, h, S=2048, maxb=16384, hq=heads, wsb=1000) == status
+        lib.kv_pool_destroy(h)
 
 
 def test_evict_limits(lib, pool):  # noqa: F811
