@@ -449,8 +449,8 @@ ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const
  *                  no group is computed on its own
  *   prefix_blocks  device int32 [num_groups]: P, 0 .. max_blocks_per_session.  The first P
  *                  blocks of the members' tables hold the same keys; the table row of the
- *                  group's longest member is the one that is read.  A member may be
- *                  shorter than the prefix: it attends to its context_lens[s] keys
+ *                  group's longest member is the one that is read.  A member that is
+ *                  shorter than the prefix is computed on its own
  *   context_lens   device int32 [num_sessions]: keys in the pool, the step's own included.
  *                  0: the session sits the step out, its output row is zeros.  A negative
  *                  length counts as 0 and one past the table as the table's; both are
@@ -462,8 +462,7 @@ ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const
  * outside the batch or twice, a prefix outside the table) are flagged
  * (LS_DEVERR_GROUP), and every session is computed on its own, over its own table.
  * Ids outside the pool are flagged (LS_DEVERR_BLOCK_ID) and their keys left out.
- * V of slots behind the longest member's keys does not reach the output; a NaN or
- * infinite V that one row of a group sees may make the group's other rows NaN.
+ * Slots behind a session's keys may hold anything: neither K nor V of them reaches its row.
  * Results depend on the lengths and on the stream's CUs, by the order of fp32 sums,
  * and not on how often the call is made.  Other arguments as paged_attn_decode.
  *
@@ -500,7 +499,7 @@ ls_status paged_attn_decode_shared(ls_kv_pool *pool, int32_t layer, int32_t num_
  *   first_positions  device int32 [num_sessions] or NULL: the position of the session's first
  *                    new token (NULL: its place in the cache, reused_lens[s])
  *   first_lens       device int32 [num_sessions] or NULL: keys t < first_lens[s] are never
- *                    evicted, and no entry of theirs is read or written.  Blocks that are in
+ *                    evicted, and their entries are not used (kv_evict copies them).  Blocks that are in
  *                    several sessions' tables lie below it (or below a group's prefix)
  *
  * paged_attn_decode_weights — paged_attn_decode_shared that also adds the weights up.
@@ -538,8 +537,7 @@ ls_status paged_attn_decode_weights(ls_kv_pool *pool, int32_t layer, int32_t num
  *                  max_blocks_per_session
  *
  * Ids outside the pool are flagged (LS_DEVERR_BLOCK_ID) and their keys left out.
- * Supported: num_q_heads / num_kv_heads in {1, 2, 4, 8}, at most 2048 sessions and 16384
- * blocks per session (LS_EUNSUPPORTED).  Other errors: LS_EINVAL, LS_ENOMEM, LS_EHIP.
+ * Limits as paged_attn_decode_shared.  Other errors: LS_EINVAL, LS_ENOMEM, LS_EHIP.
  */
 size_t ls_weights_prefill_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
                                           int32_t total_new_tokens, int32_t max_new_len, int32_t rows,

@@ -84,7 +84,7 @@ struct ShRecord {
     int32_t tile_seg;              // first 16-row place of its prefix tile at KV head 0
     int32_t tile_seg_stride;       // places per KV head of its group
     int32_t tile_row;              // its first row in the tile
-    int32_t keys;                  // L
+    int32_t keys;                  // weights are kept of those before this one: L, or 0
     uint32_t own_before;           // own blocks of the sessions before
     uint32_t own_all;              // of all sessions
 };
@@ -220,7 +220,7 @@ struct ShPart {
     const int32_t *table;          // its table row
     int head;                      // KV head
     int j0, j1;
-    int longest;                   // no row sees a key from here on
+    int longest;                   // no row sees a key from here on (and one that sees fewer is not used)
 };
 
 // State of a tile of 16 rows: row lane % 16, dims 16 dt + 4 (lane / 16) + i.
@@ -269,8 +269,8 @@ __device__ __forceinline__ void scores_of(const f32x4 (&s)[2], float scale_log2,
         for (int e = 0; e < 4; ++e) x[b][e] = e < seen ? s[b][e] * scale_log2 : -INFINITY;
     }
 }
-// Eight tokens of V from token t on, or four: zeros from `longest` on.  Slots that no row
-// sees may hold anything (NaN included).
+// Tokens t and t + 1 of V: zeros from `longest` on.  Slots that no row sees may hold anything
+// (NaN included).
 __device__ __forceinline__ uint32_t seen_v(uint32_t two, int t, int longest) {
     return t + 1 < longest ? two : t < longest ? two & 0x0000FFFFu : 0u;
 }
@@ -648,7 +648,14 @@ __global__ __launch_bounds__(kShThreads, kMost == kShFew ? kShPerCu : 1) void sh
         unsigned v[2] = {0, 0}, all[2];
         auto own = [&](int s, int pb) { return (unsigned)max((len[s] + kBlock - 1) / kBlock - pb, 0); };
         for (int s = tid * per; s < min(S, (tid + 1) * per); ++s) {
-            sm.pb[s] = owner[s] >= 0 ? sm.prefix[sm.gid[s]] : (uint16_t)0;
+            // A member that does not see all of the prefix's keys is computed on its own: 0 x V of a key that
+            // the others see is NaN where that V is not finite.
+            int pb = 0;
+            if (owner[s] >= 0) {
+                const int g = sm.gid[s], all_pb = sm.prefix[g], longest = (int)(sm.lead[g] >> kRank);
+                if (len[s] >= min(all_pb * kBlock, longest)) pb = all_pb;
+            }
+            sm.pb[s] = (uint16_t)pb;
             sm.pad[s] = (uint8_t)(-len[s] & (kBlock - 1));
             const unsigned n = own(s, sm.pb[s]);
             v[0] += n;
@@ -677,7 +684,8 @@ __global__ __launch_bounds__(kShThreads, kMost == kShFew ? kShPerCu : 1) void sh
             r.keys = len[s];
             if (owner[s] >= 0) {
                 const int g = sm.gid[s], row = (owner[s] - sm.start[g]) * G, size = tile_size((sm.start[g + 1] - sm.start[g]) * G);
-                r.prefix_blocks = sm.prefix[g];
+                r.prefix_blocks = sm.pb[s];
+                if (!sm.pb[s] && sm.prefix[g]) r.keys = 0;           // (all of them are the prefix's)
                 r.tile_seg = H * sm.segs[g] + row / size * (size / kFewRows);
                 r.tile_seg_stride = sm.segs[g + 1] - sm.segs[g];
                 r.tile_row = row % size;

@@ -85,6 +85,25 @@ def test_lengths_around_the_prefix(kv, lens, prefix):
             assert (out[s] == 0).all()
 
 
+@pytest.mark.parametrize("members", [5, 12, 40])                # rows in a tile of 16, tiles of 16, a tile of 128
+def test_keys_that_a_shorter_member_does_not_see(kv, members):
+    """K and V that are not finite, in shared blocks behind a member's keys: its row does not know."""
+    rng = np.random.default_rng(members)
+    lens = np.full(members, 100)
+    short = [1, 2, members - 1]
+    lens[short] = [60, 0, 37]
+    c = Cache(rng, lens, 2, 128, [(list(range(members)), 5)])
+    pool, q, clean = check(kv, c, 8 if members == 5 else 16, "finite")
+    for k, v in ((np.inf, 1.0), (1.0, np.inf), (np.nan, np.nan)):
+        for t in (60, 79):
+            row = np.ones((1, 2, 128))
+            c.write(0, 0, np.array([t]), W.to_bf16((row * k).astype(np.float32)), W.to_bf16((row * v).astype(np.float32)))
+        out = run(kv, c, c.device(kv), q)
+        assert kv.ls_device_errors() == 0
+        assert torch.equal(out[short], clean[short])
+        assert not torch.isfinite(out[0]).all()
+
+
 @pytest.mark.parametrize("lens", [[1], [2, 31, 32, 33], [5000], [20000, 1, 700], [0, 64, 0]])
 @pytest.mark.parametrize("d,hkv,g", [(128, 4, 8), (64, 1, 1), (128, 8, 2)])
 def test_without_groups(kv, lens, d, hkv, g):
