@@ -48,6 +48,8 @@ struct EvictArgs {
     int32_t ring_size;
     const int64_t *counts;
     int64_t *next_counts;
+    int32_t slices;                // workgroups that share a (session, KV head, layer)
+    bool plans;                    // workgroup 0 plans, and the others check the lengths for themselves
     unsigned int *err;
 };
 
@@ -60,58 +62,67 @@ __device__ __forceinline__ int keeps(const EvictArgs &a, int s, int L) {
     return (int)min((int64_t)L, max((int64_t)a.budget, (int64_t)first + a.recent));
 }
 
+// Blocks that session s gives back; its length may be wrong.
+__device__ __forceinline__ unsigned gives(const EvictArgs &a, int s, bool &wrong) {
+    const int L = a.lens[s];
+    if (L < 0 || L > (int64_t)a.max_blocks * kBlock) {
+        wrong = true;
+        return 0u;
+    }
+    return a.ring ? (unsigned)(blocks_of(L) - blocks_of(keeps(a, s, L))) : 0u;
+}
+// Sums of blocks saturate at INT32_MAX, more than any ring has room for.
+__device__ __forceinline__ unsigned add(unsigned x, unsigned y) { return min(x + y, (unsigned)INT32_MAX); }
+
+// Exclusive prefix sum over the threads, and the total (the former: of sums that have not saturated).
+template <int kThreads>
+__device__ __forceinline__ unsigned scan(unsigned v, unsigned &total, unsigned *sm_wave) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    unsigned x = v;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const unsigned y = __shfl_up(x, off);
+        if (lane >= off) x = add(x, y);
+    }
+    __syncthreads();
+    if (lane == kWave - 1) sm_wave[wave] = x;
+    __syncthreads();
+    unsigned before = 0u;
+    total = 0u;
+    for (int w = 0; w < kThreads / kWave; ++w) {
+        if (w == wave) before = total;
+        total = add(total, sm_wave[w]);
+    }
+    return before + x - v;
+}
+
+// What keeps the whole call from being served (0: nothing), and the blocks that go back.
+template <int kThreads>
+__device__ __forceinline__ unsigned refusal(const EvictArgs &a, int64_t taken, int64_t given, unsigned &total, unsigned *sm_wave) {
+    unsigned v = 0u;
+    bool wrong = false;
+    for (int s = threadIdx.x; s < a.num_sessions; s += kThreads) v = add(v, gives(a, s, wrong));
+    scan<kThreads>(v, total, sm_wave);
+    if (__syncthreads_or(wrong)) return LS_DEVERR_LENGTH;
+    const int64_t avail = given - taken;
+    if (a.ring && (taken < 0 || avail < 0 || avail > a.ring_size || total == INT32_MAX || total > a.ring_size - avail))
+        return LS_DEVERR_FREE_LIST;
+    return 0u;
+}
+
 // Lengths after the call, and the blocks behind them to the ring: one workgroup.  All
 // sessions are served or none.
-__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
-    __shared__ unsigned sm_wave[kPlanThreads / kWave];
-    __shared__ unsigned sm_at[kPlanThreads];
-    __shared__ int sm_col[kPlanThreads];
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, S = a.num_sessions;
-    const int64_t cap = (int64_t)a.max_blocks * kBlock;
+template <int kThreads>
+__device__ __forceinline__ void plan(const EvictArgs &a, unsigned *sm_wave, unsigned *sm_at, int *sm_col) {
+    const int tid = threadIdx.x, S = a.num_sessions;
+    // (before anything is written: the counters may advance in place)
     int64_t taken = 0, given = 0;
     if (a.ring) {
         taken = a.counts[0];
         given = a.counts[1];
     }
-    auto gives = [&](int s, bool &wrong) -> unsigned {
-        const int L = a.lens[s];
-        if (L < 0 || L > cap) {
-            wrong = true;
-            return 0u;
-        }
-        return a.ring ? (unsigned)(blocks_of(L) - blocks_of(keeps(a, s, L))) : 0u;
-    };
-    // Sums saturate at INT32_MAX, more than any ring has room for.
-    auto add = [](unsigned x, unsigned y) { return min(x + y, (unsigned)INT32_MAX); };
-    // Exclusive prefix sum over the threads, and the total (before: of sums that have not saturated).
-    auto scan = [&](unsigned v, unsigned &total) {
-        unsigned x = v;
-#pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const unsigned y = __shfl_up(x, off);
-            if (lane >= off) x = add(x, y);
-        }
-        __syncthreads();
-        if (lane == kWave - 1) sm_wave[wave] = x;
-        __syncthreads();
-        unsigned before = 0u;
-        total = 0u;
-        for (int w = 0; w < kPlanThreads / kWave; ++w) {
-            if (w == wave) before = total;
-            total = add(total, sm_wave[w]);
-        }
-        return before + x - v;
-    };
-    unsigned v = 0u, total;
-    bool wrong = false;
-    for (int s = tid; s < S; s += kPlanThreads) v = add(v, gives(s, wrong));
-    scan(v, total);
-    unsigned bad = __syncthreads_or(wrong) ? LS_DEVERR_LENGTH : 0u;
-    if (a.ring && !bad) {
-        const int64_t avail = given - taken;
-        if (taken < 0 || avail < 0 || avail > a.ring_size || total == INT32_MAX || total > a.ring_size - avail)
-            bad = LS_DEVERR_FREE_LIST;
-    }
+    unsigned total;
+    const unsigned bad = refusal<kThreads>(a, taken, given, total, sm_wave);
     if (tid == 0) {
         if (bad) flag_error(a.err, bad);
         if (a.ring) {
@@ -120,7 +131,7 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
         }
     }
     unsigned carry = 0u;
-    for (int s0 = 0; s0 < S; s0 += kPlanThreads) {
+    for (int s0 = 0; s0 < S; s0 += kThreads) {
         const int s = s0 + tid;
         unsigned n = 0u;
         int m = 0;
@@ -133,14 +144,14 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
             a.next_lens[s] = m;
         }
         unsigned all;
-        sm_at[tid] = scan(n, all);
+        sm_at[tid] = scan<kThreads>(n, all, sm_wave);
         sm_col[tid] = blocks_of(m);
         __syncthreads();
         // thread = block that goes back: the last session whose blocks begin at or before it
-        for (unsigned i = tid; i < all; i += kPlanThreads) {
+        for (unsigned i = tid; i < all; i += kThreads) {
             int e = 0;
 #pragma unroll
-            for (int step = kPlanThreads / 2; step > 0; step >>= 1)
+            for (int step = kThreads / 2; step > 0; step >>= 1)
                 if (sm_at[e + step] <= i) e += step;
             const int id = a.tables[(int64_t)(s0 + e) * a.max_blocks + sm_col[e] + (i - sm_at[e])];
             if (id < 0 || id >= a.num_blocks) flag_error(a.err, LS_DEVERR_BLOCK_ID);
@@ -149,6 +160,12 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
         carry += all;
         __syncthreads();
     }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
+    __shared__ unsigned sm_wave[kPlanThreads / kWave], sm_at[kPlanThreads];
+    __shared__ int sm_col[kPlanThreads];
+    plan<kPlanThreads>(a, sm_wave, sm_at, sm_col);
 }
 
 // Order of two weights as that of two unsigned words: NaN below all, -0 as 0.
@@ -181,9 +198,23 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     __shared__ uint64_t sm_flags[kKeys / 64];
     __shared__ unsigned sm_wave[2][kWaves];
     __shared__ uint32_t sm_digit, sm_rest;
+    static_assert(2 * kThreads <= kBins, "the plan fits the bins");
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int slice = blockIdx.x / a.num_sessions, s = blockIdx.x % a.num_sessions, h = blockIdx.y, la = blockIdx.z;
-    const int H = a.num_kv_heads, slices = gridDim.x / a.num_sessions;
+    const int H = a.num_kv_heads, S = a.num_sessions, slices = a.slices;
+    int x = blockIdx.x, h = blockIdx.y, la = blockIdx.z;
+    unsigned bad = 0u;
+    if (a.plans) {
+        if (x-- == 0) {
+            plan<kThreads>(a, sm_wave[0], sm_bin, reinterpret_cast<int *>(sm_bin) + kThreads);
+            return;
+        }
+        h = x / (S * slices) % H;
+        la = x / (S * slices) / H;
+        x %= S * slices;
+        unsigned total;
+        bad = refusal<kThreads>(a, a.ring ? a.counts[0] : 0, a.ring ? a.counts[1] : 0, total, sm_wave[0]);
+    }
+    const int slice = x / S, s = x % S;
     const int32_t *table = a.tables + (int64_t)s * a.max_blocks;
     const int64_t entries = (int64_t)la * a.num_blocks * H * kBlock;
     const float *weights = a.weights + entries;
@@ -192,7 +223,7 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     int32_t *positions_next = a.positions_next + entries;
     const bool apart = a.weights_next != a.weights;
     const int L = (int)min((int64_t)max(a.lens[s], 0), (int64_t)a.max_blocks * kBlock);
-    const int m = min(max(a.next_lens[s], 0), L);
+    const int m = bad ? L : a.plans ? keeps(a, s, L) : min(max(a.next_lens[s], 0), L);
     const bool cut = m < L;
     if (!cut && (!apart || slice)) return;
     // First entry of a block, or -1: it is not in the pool.
@@ -457,14 +488,20 @@ hipError_t launch_evict(const PoolGeom &p, int32_t layer_begin, int32_t layer_co
     a.counts = c.free_counts;
     a.next_counts = c.next_counts;
     a.err = err;
-    hipLaunchKernelGGL(evict_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (!c.num_sessions) return hipSuccess;
     // With entries apart, and workgroups for a part of the CUs only, several share a (session, KV head,
     // layer)'s moves.
     const int64_t whole = (int64_t)c.num_sessions * p.num_kv_heads * layer_count, cus = stream_cus(p, stream);
-    const int slices = c.weights_next != c.weights ? (int)std::max<int64_t>(1, std::min<int64_t>(kEvSlices, 2 * cus / whole)) : 1;
-    const dim3 grid((unsigned)(c.num_sessions * slices), (unsigned)p.num_kv_heads, (unsigned)layer_count);
+    a.slices = c.weights_next != c.weights && whole ? (int)std::max<int64_t>(1, std::min<int64_t>(kEvSlices, 2 * cus / whole)) : 1;
+    // Up to a thousand sessions, whose lengths a workgroup reads in a microsecond, one launch does all
+    // (but where the plan would write the counters that the others read).
+    a.plans = whole && (!c.free_ring || c.next_counts != c.free_counts) && c.num_sessions <= kPlanThreads && whole * a.slices < INT32_MAX;
+    const dim3 grid = a.plans ? dim3((unsigned)(1 + whole * a.slices))
+                              : dim3((unsigned)(c.num_sessions * a.slices), (unsigned)p.num_kv_heads, (unsigned)layer_count);
+    if (!a.plans) {
+        hipLaunchKernelGGL(evict_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, a);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (!whole) return hipSuccess;
+    }
     const bool narrow = (int64_t)c.max_blocks * kBlock <= kEvKeysShort;
 #define LS_EVICT(D, THREADS, KEYS) hipLaunchKernelGGL((evict_kernel<D, THREADS, KEYS>), grid, dim3(THREADS), 0, stream, a)
     if (p.head_dim == 128) {

@@ -47,7 +47,7 @@ def ring_of(nb, held, start=(1 << 33) + 7):
 
 
 def check(kv, c, budget, limit, recent, what, first=None, next_pos=None, w=None, pos=None, layers=None, apart=False, ring=True,
-          ties=0, seed=3):
+          ties=0, seed=3, in_place=False):
     rng = np.random.default_rng(seed)
     s = len(c.lens)
     firsts = np.zeros(s, dtype=np.int64) if first is None else np.asarray(first)
@@ -64,6 +64,7 @@ def check(kv, c, budget, limit, recent, what, first=None, next_pos=None, w=None,
     held = c.tables[(np.arange(c.tables.shape[1])[None] < -(-c.lens // BLOCK)[:, None])]
     hr, hc = ring_of(c.pool.shape[1], held)
     dring, dcounts, after = dev(hr), dev(hc), torch.empty(2, dtype=torch.int64, device="cuda")
+    after = dcounts if in_place else after
     lens = i32_dev(c.lens)
 
     def call():
@@ -170,7 +171,16 @@ def test_many_sessions(kv):
     check(kv, c, 30, 33, 8, "2500 sessions")
 
 
-def test_refused_as_a_whole(kv):
+@pytest.mark.parametrize("n", [1023, 1024, 1025])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_a_thousand_sessions(kv, n, in_place):
+    """On both sides of what one launch plans and serves; counters that advance in place."""
+    rng = np.random.default_rng(n)
+    check(kv, Cache(rng, rng.integers(0, 50, n), 2, 64), 20, 24, 6, "%d sessions" % n, in_place=in_place)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_refused_as_a_whole(kv, in_place):
     c = Cache(np.random.default_rng(12), [100, 70], 2, 64, extra_cols=0)
     rng = np.random.default_rng(13)
     w, pos = spread(c, rng, c.lens * 2)
@@ -182,6 +192,7 @@ def test_refused_as_a_whole(kv):
         weights, positions = dev(w), dev(pos)
         ring = torch.arange(size, dtype=torch.int32, device="cuda")
         before, after = torch.tensor(counts, device="cuda"), torch.empty(2, dtype=torch.int64, device="cuda")
+        after = before if in_place else after
         nxt = torch.empty(2, dtype=torch.int32, device="cuda")
         kv.kv_evict(pool, i32_dev(lens), c.dtables, 20, 30, 5, i32_dev([300, 300]), weights, positions, nxt, free_ring=ring,
                     free_counts=before, next_counts=after)
