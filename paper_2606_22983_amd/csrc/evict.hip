@@ -189,6 +189,12 @@ struct Quad {
 // equal to it the ones in the highest slots.  Then waves go over their contiguous
 // shares of the slots, 256 at a time (a lane has four consecutive ones, 16 bytes of
 // an entry array), and number the holes below m and the tokens that stay behind it.
+//
+// Bound by the moves' sectors: a token's V values are 2 bytes in each of D rows of 32 bytes.
+// Measured: 64 sessions, about half of them cut to 2048 tokens, 8 layers of 4 heads of
+// 128, 129 us a call, 160 MB written (1.5 TB/s; 95 MB needed in all); 8 prompts of up to
+// 16384 cut to 1024, 4 layers, 150 us, 103 MB written and 323 read.  44 us of either
+// without the moves.  V tiles of blocks with holes, read and written whole: 152 us for 127.
 template <int D, int kThreads, int kKeys>
 __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     constexpr int kWaves = kThreads / kWave;

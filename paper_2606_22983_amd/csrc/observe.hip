@@ -15,7 +15,11 @@
 // read once a launch however many rows there are, and the rows (a few hundred KB)
 // come from L2.  A lane's scores belong to one row (lane % 16): sums over keys end
 // with two lane exchanges, sums over rows stay in the lane until the last row.
-// Bound by the matrix and exponential units when rows are many, by K when few.
+// Bound by the matrix and exponential units when rows are many, by latency when few.
+// Measured: 32 turns, 64 observed rows each over up to 8192 tokens, 32 / 4 heads of 128, 270
+// us a call (rows' launch 153, keys' 140 at best; 761 TFLOP/s of products); one turn, 32 rows
+// over 2090 tokens, 21 us (8.4, 4.4 and 7.0).  Wider waves (8 blocks, 301 us), a persistent
+// grid (368) and four waves a SIMD (289) were slower than the 264 they were compared with.
 #include <algorithm>
 #include <type_traits>
 

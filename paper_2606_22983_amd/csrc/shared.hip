@@ -7,7 +7,7 @@
 // disjoint sets add up by the log-sum-exp rule.  A group's sessions have their
 // first 16 P keys in common: the state over these is computed for all query rows
 // of the group at once, as one matrix of (members x query heads per KV head) rows
-// against K and V tiles that are read once per 64 rows, and each session's own
+// against K and V tiles that are read once per tile of rows, and each session's own
 // keys are walked for it alone.
 //
 // Work: segments = (group, KV head, tile of up to 16 or 128 rows) over the group's blocks,
@@ -37,6 +37,12 @@
 // tokens, in the order that the lanes hold them).  Probabilities are rounded to
 // bf16 there, by half a step (2^-8 of themselves) at most, while sums, maxima and
 // accumulated weights take the fp32 ones.
+//
+// Bound by HBM where own keys are many, else by latency.  Measured (head_dim 128, both
+// kernels, a call): 64 sessions behind 4096 shared tokens, 32 / 4 heads, 51 us, 162 MB read;
+// 256 sessions in 8 groups, 16 / 2 heads, 57 us, 219 MB (4.7 TB/s in the first kernel); 3
+// sessions behind 640 shared tokens 19 us (13.6 and 3.0 on the GPU).  With weights, 64
+// sessions of up to 16384 tokens 173 us, 783 MB needed; the scores' stores take 31 of them.
 #include <algorithm>
 #include <type_traits>
 
@@ -837,9 +843,11 @@ __device__ __forceinline__ RowParts parts_of(const SharedArgs &a, const ShRecord
     return p;
 }
 
-// Workgroups below `combine` add up rows of the output, D / 4 threads a row; the
-// others take equal shares of the own blocks and add their probabilities to the
-// weights, four threads a (block, KV head).
+// Workgroups below `combine` add up rows of the output, D / 4 threads a row; the waves of
+// the others take equal shares of the own blocks and add their probabilities to the
+// weights, four threads a (block, KV head).  Bound by the scores' scattered reads: 64 long
+// sessions 17 us for 70 MB read and written (19 with shares of a workgroup each), one of 1789
+// tokens 3.8.
 template <int D, bool kWeights>
 __global__ __launch_bounds__(kShThreads) void shared_merge_kernel(SharedArgs a, int combine) {
     __shared__ uint32_t sm_cum[kWeights ? kShMost + 1 : 1];
