@@ -499,8 +499,8 @@ hipError_t launch_evict(const PoolGeom &p, int32_t layer_begin, int32_t layer_co
     const int64_t whole = (int64_t)c.num_sessions * p.num_kv_heads * layer_count, cus = stream_cus(p, stream);
     a.slices = c.weights_next != c.weights && whole ? (int)std::max<int64_t>(1, std::min<int64_t>(kEvSlices, 2 * cus / whole)) : 1;
     // Up to a thousand sessions, whose lengths a workgroup reads in a microsecond, one launch does all
-    // (but where the plan would write the counters that the others read).
-    a.plans = whole && (!c.free_ring || c.next_counts != c.free_counts) && c.num_sessions <= kPlanThreads && whole * a.slices < INT32_MAX;
+    // (but where the plan would write the counters that the others read, and in grids of 2^32 threads).
+    a.plans = whole && (!c.free_ring || c.next_counts != c.free_counts) && c.num_sessions <= kPlanThreads && whole * a.slices < 1 << 21;
     const dim3 grid = a.plans ? dim3((unsigned)(1 + whole * a.slices))
                               : dim3((unsigned)(c.num_sessions * a.slices), (unsigned)p.num_kv_heads, (unsigned)layer_count);
     if (!a.plans) {

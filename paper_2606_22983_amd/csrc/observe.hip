@@ -126,8 +126,7 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c16 = lane % 16, g4 = lane / 16;
     const int H = a.num_kv_heads, G = a.group;
     // (A session's chunks are spread over the XCDs: rows are few, and lengths differ.)
-    const uint32_t item = blockIdx.x;
-    const int chunk = item % a.chunks, h = item / a.chunks % H, s = item / a.chunks / H;
+    const int chunk = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
     const Turn t = turn_of(a, s, kKeys && chunk == 0 && h == 0 && a.row0 == 0);
     const int keys = t.c + t.n, col0 = (chunk * kObWaves + wave) * KB;
     if (t.n == 0 || (a.row0 && !t.rows) || chunk * kObWaves * KB * kBlock >= keys) return;
@@ -348,7 +347,7 @@ __global__ __launch_bounds__(kObThreads) void observe_lse_kernel(ObserveArgs a, 
 template <int D, int KB>
 hipError_t launch_observe_t(ObserveArgs a, int32_t whole_rows, hipStream_t stream) {
     constexpr int kChunkTokens = kObWaves * KB * kBlock;
-    const dim3 grid((unsigned)(a.chunks * a.num_kv_heads * a.num_sessions));
+    const dim3 grid((unsigned)a.chunks, (unsigned)a.num_kv_heads, (unsigned)a.num_sessions);
     for (a.row0 = 0; a.row0 < whole_rows; a.row0 += a.row_cap) {
         hipLaunchKernelGGL((observe_kernel<D, KB, false>), grid, dim3(kObThreads), 0, stream, a);
         if (hipError_t e = hipGetLastError()) return e;
