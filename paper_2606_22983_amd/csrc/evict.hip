@@ -175,6 +175,11 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Bits of a ballot below this lane, added to x.
+__device__ __forceinline__ unsigned count_below(uint64_t mask, unsigned x) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, x));
+}
+
 // Weights and positions of four consecutive slots.
 struct Quad {
     f32x4 w;
@@ -203,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t sm_bin[kBins];
     __shared__ uint64_t sm_flags[kKeys / 64];
     __shared__ unsigned sm_wave[2][kWaves];
-    __shared__ uint32_t sm_digit, sm_rest;
+    __shared__ uint32_t sm_digit, sm_rest, sm_ties;
     static_assert(2 * kThreads <= kBins, "the plan fits the bins");
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int H = a.num_kv_heads, S = a.num_sessions, slices = a.slices;
@@ -317,6 +322,7 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
             if (before < rest && rest <= before + own[i]) {
                 sm_digit = (uint32_t)(tid * kPer + i);
                 sm_rest = rest - before;
+                sm_ties = own[i];              // (in the last pass: keys equal to the one found)
             }
             before += own[i];
         }
@@ -327,7 +333,6 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     // ---- numbers of ties, holes and moving tokens
     const int steps = (L + kStep - 1) / kStep, per = (steps + kWaves - 1) / kWaves;
     const int t_begin = min(wave * per, steps) * kStep, t_end = min((wave + 1) * per, steps) * kStep;
-    const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;           // lanes before this one
     // Sums of a wave's value over the waves before, and over all.
     auto wave_sums = [&](unsigned v, int which, unsigned &all) {
         if (lane == 0) sm_wave[which][wave] = v;
@@ -341,22 +346,31 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
         }
         return before;
     };
-    unsigned ties = 0u, all_ties;
-    for (int t0 = t_begin; t0 < t_end; t0 += kStep) {
-        const int t = t0 + lane * 4;
-        const u32x4 k = t < L ? keys(t) : u32x4{0u, 0u, 0u, 0u};
+    const unsigned ties_stay = sm_ties - rest;
+    unsigned seen = 0u;                             // ties before the wave's slots, where some stay and some go
+    if (ties_stay) {
+        unsigned ties = 0u, all_ties;
+        for (int t0 = t_begin; t0 < t_end; t0 += kStep) {
+            const int t = t0 + lane * 4;
+            const u32x4 k = t < L ? keys(t) : u32x4{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ties += __popcll(__ballot(t + i < L && k[i] == prefix));
+            for (int i = 0; i < 4; ++i) ties += __popcll(__ballot(t + i < L && k[i] == prefix));
+        }
+        seen = wave_sums(ties, 1, all_ties);
     }
-    const unsigned ties_before = wave_sums(ties, 1, all_ties), ties_stay = all_ties - rest;
     // Which of the lane's four tokens stay; seen: ties before the step, and after it.
     auto stays = [&](int t, const u32x4 &k, unsigned &seen, bool (&yes)[4]) {
+        if (!ties_stay) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) yes[i] = t + i < L && k[i] > prefix;
+            return;
+        }
         unsigned mine = seen;                       // ties before the lane's first slot
         uint64_t tie[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             tie[i] = __ballot(t + i < L && k[i] == prefix);
-            mine += __popcll(tie[i] & below);
+            mine = count_below(tie[i], mine);
             seen += __popcll(tie[i]);
         }
 #pragma unroll
@@ -368,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     // A bit for each slot whose token stays: four words a step, bit = lane.  Without keys in
     // LDS they take the keys' place; moves in place change what keys are computed from.
     uint64_t *flags = cached ? sm_flags : reinterpret_cast<uint64_t *>(sm_key);
-    unsigned seen = ties_before, holes = 0u, movers = 0u, all_holes, all_movers;
+    unsigned holes = 0u, movers = 0u, all_holes, all_movers;
     for (int t0 = t_begin; t0 < t_end; t0 += kStep) {
         const int t = t0 + lane * 4;
         bool yes[4];
@@ -417,8 +431,8 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
                 const bool yes = (f[i] >> lane) & 1u;
                 come[i] = __ballot(t + i < m && !yes);
                 go[i] = __ballot(t + i >= m && yes);
-                i_hole += __popcll(come[i] & below);
-                i_mover += __popcll(go[i] & below);
+                i_hole = count_below(come[i], i_hole);
+                i_mover = count_below(go[i], i_mover);
                 hole += __popcll(come[i]);
                 mover += __popcll(go[i]);
             }
