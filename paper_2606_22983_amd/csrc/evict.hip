@@ -197,8 +197,8 @@ struct Quad {
 //
 // Bound by the moves' sectors: a token's V values are 2 bytes in each of D rows of 32 bytes.
 // Measured: 64 sessions, about half of them cut to 2048 tokens, 8 layers of 4 heads of
-// 128, 129 us a call, 160 MB written (1.5 TB/s; 95 MB needed in all); 8 prompts of up to
-// 16384 cut to 1024, 4 layers, 150 us, 103 MB written and 323 read.  44 us of either
+// 128, 124-130 us a call, 160 MB written (1.5 TB/s; 95 MB needed in all); 8 prompts of up to
+// 16384 cut to 1024, 4 layers, 144 us, 103 MB written and 323 read.  43 and 42 us
 // without the moves.  V tiles of blocks with holes, read and written whole: 152 us for 127.
 template <int D, int kThreads, int kKeys>
 __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {

@@ -226,8 +226,9 @@ def test_blocks_outside_the_pool(kv):
     c.tables = tables
 
 
-def test_captured_and_replayed(kv):
-    """In place, with counters that advance: every replay cuts what has grown since."""
+@pytest.mark.parametrize("in_place", [True, False])
+def test_captured_and_replayed(kv, in_place):
+    """Entries in place, counters that advance: every replay cuts what has grown since."""
     c = Cache(np.random.default_rng(16), [120, 90, 61], 2, 64)
     rng = np.random.default_rng(17)
     w, pos = spread(c, rng, c.lens * 2)
@@ -236,9 +237,13 @@ def test_captured_and_replayed(kv):
     next_pos = i32_dev(c.lens * 2)
     ring, counts = (dev(x) for x in ring_of(c.pool.shape[1], np.arange(c.pool.shape[1])))
 
+    after = counts if in_place else torch.empty_like(counts)
+
     def call():
         kv.kv_evict(pool, lens, c.dtables, 50, 60, 10, next_pos, weights, positions, nxt, free_ring=ring, free_counts=counts,
-                    next_counts=counts)
+                    next_counts=after)
+        if not in_place:
+            counts.copy_(after)
     graph = torch.cuda.CUDAGraph()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph):
