@@ -505,9 +505,11 @@ ls_status paged_attn_decode_shared(ls_kv_pool *pool, int32_t layer, int32_t num_
  * paged_attn_decode_weights — paged_attn_decode_shared that also adds the weights up.
  * Keys of a group's shared prefix get none.  reused_lens NULL (and first_positions and
  * positions NULL): no key is new.  Every query counts, so a session without a new token
- * sits out with a length of 0.  The workspace (ls_decode_weights_workspace_bytes, which
- * holds the scores of every block of the pool) is 16-byte aligned.  Other arguments,
- * limits and errors as paged_attn_decode_shared.
+ * sits out with a length of 0.  Groups that cannot be (LS_DEVERR_GROUP) do not say which
+ * blocks are shared: out is computed, and weights and positions stay as they are, those of
+ * new keys too.  The workspace (ls_decode_weights_workspace_bytes, which holds the scores of
+ * every block of the pool) is 16-byte aligned.  Other arguments, limits and errors as
+ * paged_attn_decode_shared.
  */
 size_t ls_decode_weights_workspace_bytes(const ls_kv_pool *pool, int32_t num_sessions, int32_t num_q_heads,
                                          int32_t num_groups, int32_t num_members);

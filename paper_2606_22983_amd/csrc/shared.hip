@@ -618,7 +618,7 @@ __global__ __launch_bounds__(kShThreads, kMost == kShFew ? kShPerCu : 1) void sh
         }
     }
     if (bad) {
-        // Groups that cannot be: every session is computed on its own.
+        // Groups that cannot be: every session is computed on its own, and no weight is kept.
         if (first_wg && tid == 0) flag_error(a.err, LS_DEVERR_GROUP);
         ng = 0;
         __syncthreads();
@@ -687,7 +687,8 @@ __global__ __launch_bounds__(kShThreads, kMost == kShFew ? kShPerCu : 1) void sh
             r.own_blocks = (int)(sm.cum[s + 1] - sm.cum[s]);
             r.own_before = sm.cum[s];
             r.own_all = sm.cum[S];
-            r.keys = len[s];
+            // (which blocks are shared is not known of groups that cannot be: their scores and entries are several sessions')
+            r.keys = bad ? 0 : len[s];
             if (owner[s] >= 0) {
                 const int g = sm.gid[s], row = (owner[s] - sm.start[g]) * G, size = tile_size((sm.start[g + 1] - sm.start[g]) * G);
                 r.prefix_blocks = sm.pb[s];
