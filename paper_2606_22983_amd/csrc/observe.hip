@@ -203,21 +203,23 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     auto is_partial = [&](int tile) { return p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent; };
     auto consume = [&](const f32x4 (&of)[KB], float row_lse, int tile, auto partial) {
         const int row = tile * 16 + c16, pos = p0 + ((a.row0 + row) >> gs);
+        auto unseen = [&](int b, int e) {
+            return decltype(partial)::value && (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0);
+        };
         float x[KB][4];
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[b][e] = of[b][e];
-                if constexpr (decltype(partial)::value)
-                    if (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0) x[b][e] = -INFINITY;
-            }
+            for (int e = 0; e < 4; ++e) x[b][e] = unseen(b, e) ? -INFINITY : of[b][e];
         if constexpr (kKeys) {
             if (row >= t.rows) row_lse = INFINITY;             // (no row: no weight)
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[b][e] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -row_lse));
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -row_lse));
+                    sum[b][e] += unseen(b, e) ? 0.f : p;       // (0, but of a row whose sum is no number)
+                }
         } else {
             float m = kNoMax, l = 0.f;
 #pragma unroll
