@@ -227,7 +227,7 @@ struct ObservePlan {
     int32_t row_cap;               // of one round
     int32_t blocks;                // per wave
     int32_t chunks;                // of a table
-    size_t lse_at;
+    size_t whole_at;
     size_t total;
 };
 ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_heads, int32_t max_new_len, int32_t rows,

@@ -8,8 +8,12 @@
 // l is known only after all keys, so the scores are computed twice, from K alone (V is
 // not read), in three launches:
 //   rows    (m, l) of each row over each chunk of keys
-//   lse     their sum over the chunks, as log2(l) + m
-//   keys    e^(x - lse) summed over the rows, added to the weights
+//   sums    their sum over the chunks, as m and 1 / l
+//   keys    e^(x - m) / l summed over the rows, added to the weights
+// The exponential is that of fma(product, scale, -round(m scale)), one operation: what m loses
+// by rounding is in p and in l, and cancels (RowScale).  (With log2(l) + m as one word a score of 2^14
+// put a weight off by 2^-10.  Subtracting products before the scale takes an operation a score more: 283
+// us for the batch below where this takes 272, and the one word took 270.)
 // A wave keeps the K tiles of its blocks in registers, as the A operand of
 // S^T[16 tokens x 16 rows] = K . Q^T, and walks over the rows 16 at a time, so K is
 // read once a launch however many rows there are, and the rows (a few hundred KB)
@@ -54,8 +58,8 @@ struct ObserveArgs {
     int32_t row0;                  // first row of the round
     int32_t row_cap;               // rows of the round, at most
     int32_t chunks;                // chunks of a table, at most
-    float2 *part;                  // [S][Hkv][chunks][row_cap] (m, l)
-    float *lse;                    // [S][Hkv][row_cap]
+    float2 *part;                  // [S][Hkv][chunks][row_cap] (m, l), m before scaling
+    f32x4 *whole;                  // [S][Hkv][row_cap] (round(m scale), scale, 1 / l) over all keys
     float *weights;                // layer base, [num_blocks][Hkv][16]
     int32_t *positions;
     const int32_t *begin;          // [S] or null
@@ -98,6 +102,22 @@ __device__ __forceinline__ float sum_xor_16_32(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The scale (log2) that a row with the largest product m takes, and m scale rounded.  The largest score's
+// exponential is 2^rounding, where it would be 1 with an exact m scale: half a step of m scale.  It stays
+// within 2^64 because a row whose m scale passes 2^31 takes a scale smaller by a power of two, with |m scale|
+// in [2^29, 2^31).  Its fp32 products, where they differ, are then still 2^5 apart, a share of 2^-32 (and
+// twice that or more with the whole scale).
+struct RowScale {
+    float scale, m, rounding;
+    __device__ __forceinline__ RowScale(float product, float scale_log2) {
+        // (exponents apart: the product of the two may be past the largest number.  The biased one of 0 is the least.)
+        const int e = (int)(__float_as_uint(product) >> 23 & 255u) - 126 + __builtin_amdgcn_frexp_expf(scale_log2);
+        scale = __builtin_amdgcn_ldexpf(scale_log2, min(31 - e, 0));
+        m = product * scale;
+        rounding = __builtin_fmaf(product, scale, -m);
+    }
+};
+
 typedef __attribute__((address_space(3))) void lds_void;
 
 // Four tiles of 16 rows, one loaded by each wave: a tile's k-step is a kilobyte, in the
@@ -106,8 +126,8 @@ template <int D>
 struct RowStage {
     __attribute__((aligned(1024))) uint8_t q[kObWaves][D / 32][1024];
 };
-struct LseStage {
-    float lse[kObWaves][kWave];                    // lane: its row's
+struct SumStage {
+    __attribute__((aligned(1024))) f32x4 row[kObWaves][kWave];      // lane: its row's
 };
 
 // One chunk of kObWaves * KB blocks of a (session, KV head); wave w has blocks
@@ -121,7 +141,7 @@ template <int D, int KB, bool kKeys>
 __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     // (arrays of their own: reads of one stage do not wait for the loads of another)
     __shared__ RowStage<D> sq0, sq1;
-    __shared__ LseStage sl0, sl1;
+    __shared__ SumStage sl0, sl1;
     __shared__ float2 sm[3][kObWaves][kObWaves * 16];      // (m, l) of a stage's rows, by wave
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, c16 = lane % 16, g4 = lane / 16;
     const int H = a.num_kv_heads, G = a.group;
@@ -165,15 +185,17 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t *>(a.q + ((int64_t)(t.q0 + t.j0 + (a.row0 >> gs)) * H + h) * G * D), 0, INT32_MAX, kRawBuffer);
     const __amdgpu_buffer_rsrc_t rl =
-        __builtin_amdgcn_make_buffer_rsrc(a.lse + pair * a.row_cap, 0, kKeys ? INT32_MAX : 0, kRawBuffer);
+        __builtin_amdgcn_make_buffer_rsrc(a.whole + pair * a.row_cap, 0, kKeys ? INT32_MAX : 0, kRawBuffer);
     // Lanes of no row, and stages behind the last, read the last row.
-    auto load_stage = [&](RowStage<D> &sq, LseStage &sl, int tile_first) {
+    auto load_stage = [&](RowStage<D> &sq, SumStage &sl, int tile_first) {
         const int row = min((tile_first + wave) * 16 + c16, t.rows - 1);
         const int off = ((row >> gs) * (H * G) + (row & (G - 1))) * (D * 2) + g4 * 16;
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rq, (lds_void *)sq.q[wave][ks], 16, off + ks * 64, 0, 0, 0);
-        if constexpr (kKeys) __builtin_amdgcn_raw_ptr_buffer_load_lds(rl, (lds_void *)sl.lse[wave], 4, row * 4, 0, 0, 0);
+        if constexpr (kKeys) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rl, (lds_void *)sl.row[wave], 16, row * 16, 0, 0, 0);
+        }
     };
     auto stage_barrier = [&]() {
         asm volatile("" ::: "memory");
@@ -185,9 +207,9 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     // ---- products of a tile, and what is made of them (by the rows' launch one tile later, in the
     // same code: the matrix unit has the next tile's while the vector unit has this one's)
     f32x4 acc[2][KB];
-    float lse[2] = {0.f, 0.f};
-    auto products = [&](const RowStage<D> &sq, const LseStage &sl, int i, f32x4 (&to)[KB], float &row_lse) {
-        if constexpr (kKeys) row_lse = sl.lse[i][lane];
+    f32x4 whole = {};
+    auto products = [&](const RowStage<D> &sq, const SumStage &sl, int i, f32x4 (&to)[KB]) {
+        if constexpr (kKeys) whole = sl.row[i][lane];
         bf16x8 q[D / 32];
 #pragma unroll
         for (int ks = 0; ks < D / 32; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(&sq.q[i][ks][lane * 16]);
@@ -201,7 +223,7 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     // Some row of the tile does not see every key of the wave.  (A branch around code of its
     // own: as selects in the common code the masks cost as much as the sums.)
     auto is_partial = [&](int tile) { return p0 + ((a.row0 + tile * 16) >> gs) < wkey0 + KB * kBlock - 1 || absent; };
-    auto consume = [&](const f32x4 (&of)[KB], float row_lse, int tile, auto partial) {
+    auto consume = [&](const f32x4 (&of)[KB], int tile, auto partial) {
         const int row = tile * 16 + c16, pos = p0 + ((a.row0 + row) >> gs);
         auto unseen = [&](int b, int e) {
             return decltype(partial)::value && (wkey0 + b * kBlock + 4 * g4 + e > pos || id[b] < 0);
@@ -212,13 +234,14 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[b][e] = unseen(b, e) ? -INFINITY : of[b][e];
         if constexpr (kKeys) {
-            if (row >= t.rows) row_lse = INFINITY;             // (no row: no weight)
+            const float inv = row < t.rows ? whole.z : 0.f;    // (no row: no weight)
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -row_lse));
-                    sum[b][e] += unseen(b, e) ? 0.f : p;       // (0, but of a row whose sum is no number)
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], whole.y, -whole.x));
+                    // (unseen: 0, also of a row whose sum is no number)
+                    sum[b][e] = unseen(b, e) ? sum[b][e] : __builtin_fmaf(p, inv, sum[b][e]);
                 }
         } else {
             float m = kNoMax, l = 0.f;
@@ -227,11 +250,12 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m = fmaxf(m, x[b][e]);
             // (the scale is positive: the largest product has the largest score)
-            m = fmaxf(max_xor_16_32(m) * a.scale_log2, kNoMax);
+            m = max_xor_16_32(m);
+            const RowScale rs(m, a.scale_log2);
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], a.scale_log2, -m));
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], rs.scale, -rs.m));
             l = sum_xor_16_32(l);
             const int n = tile - tile0;
             if (g4 == 0) sm[n / kObWaves % 3][wave][n % kObWaves * 16 + c16] = make_float2(m, l);
@@ -249,10 +273,13 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
 #pragma unroll
         for (int w = 0; w < kObWaves; ++w) m = fmaxf(m, sm[st % 3][w][lane].x);
 #pragma unroll
-        for (int w = 0; w < kObWaves; ++w) l += __builtin_amdgcn_exp2f(sm[st % 3][w][lane].x - m) * sm[st % 3][w][lane].y;
+        for (int w = 0; w < kObWaves; ++w) {
+            const float2 of = sm[st % 3][w][lane];
+            l += __builtin_amdgcn_exp2f((of.x - m) * a.scale_log2 - RowScale(of.x, a.scale_log2).rounding) * of.y;
+        }
         part[row] = make_float2(m, l);
     };
-    auto stage = [&](int st, RowStage<D> &sq, LseStage &sl, RowStage<D> &ahead_q, LseStage &ahead_l) {
+    auto stage = [&](int st, RowStage<D> &sq, SumStage &sl, RowStage<D> &ahead_q, SumStage &ahead_l) {
         load_stage(ahead_q, ahead_l, tile0 + (st + 1) * kObWaves);
         if (st >= 2) store_rows(st - 2);           // (its last tile was finished in stage st - 1)
 #pragma unroll
@@ -262,17 +289,17 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
             if constexpr (kKeys) {
                 // (at once: the sums take the registers that a tile's products would wait in, and a
                 // third wave per SIMD gives as much: 152 us for the next-turn batch, 174 one later)
-                products(sq, sl, i, acc[0], lse[0]);
-                if (is_partial(tile0 + n)) consume(acc[0], lse[0], tile0 + n, std::true_type());
-                else consume(acc[0], lse[0], tile0 + n, std::false_type());
+                products(sq, sl, i, acc[0]);
+                if (is_partial(tile0 + n)) consume(acc[0], tile0 + n, std::true_type());
+                else consume(acc[0], tile0 + n, std::false_type());
             } else if (n == 0) {
-                products(sq, sl, i, acc[i & 1], lse[i & 1]);
+                products(sq, sl, i, acc[i & 1]);
             } else if (is_partial(tile0 + n - 1)) {
-                products(sq, sl, i, acc[i & 1], lse[i & 1]);
-                consume(acc[(i + 1) & 1], lse[(i + 1) & 1], tile0 + n - 1, std::true_type());
+                products(sq, sl, i, acc[i & 1]);
+                consume(acc[(i + 1) & 1], tile0 + n - 1, std::true_type());
             } else {
-                products(sq, sl, i, acc[i & 1], lse[i & 1]);
-                consume(acc[(i + 1) & 1], lse[(i + 1) & 1], tile0 + n - 1, std::false_type());
+                products(sq, sl, i, acc[i & 1]);
+                consume(acc[(i + 1) & 1], tile0 + n - 1, std::false_type());
             }
         }
         stage_barrier();
@@ -287,8 +314,8 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
             if (++st >= stages) break;
         }
         if constexpr (!kKeys) {
-            if (count & 1) consume(acc[0], lse[0], tiles - 1, std::true_type());
-            else consume(acc[1], lse[1], tiles - 1, std::true_type());
+            if (count & 1) consume(acc[0], tiles - 1, std::true_type());
+            else consume(acc[1], tiles - 1, std::true_type());
             __syncthreads();
             if (stages >= 2) store_rows(stages - 2);
             store_rows(stages - 1);
@@ -319,8 +346,8 @@ __global__ __launch_bounds__(kObThreads, 3) void observe_kernel(ObserveArgs a) {
     }
 }
 
-// log2 of each row's whole sum.
-__global__ __launch_bounds__(kObThreads) void observe_lse_kernel(ObserveArgs a, int chunk_tokens) {
+// What the keys' launch takes of each row.
+__global__ __launch_bounds__(kObThreads) void observe_sum_kernel(ObserveArgs a, int chunk_tokens) {
     const int h = blockIdx.y, s = blockIdx.z, row = blockIdx.x * kObThreads + threadIdx.x;
     const Turn t = turn_of(a, s, false);
     if (row >= t.rows) return;
@@ -336,14 +363,15 @@ __global__ __launch_bounds__(kObThreads) void observe_lse_kernel(ObserveArgs a, 
         for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)min(k0 + i, chunks - 1) * a.row_cap];
 #pragma unroll
         for (int i = 0; i < 8; ++i) now = fmaxf(now, v[i].x);
-        l *= __builtin_amdgcn_exp2f(m - now);
+        l *= __builtin_amdgcn_exp2f((m - now) * a.scale_log2);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (k0 + i < chunks) l += __builtin_amdgcn_exp2f(v[i].x - now) * v[i].y;
+            if (k0 + i < chunks) l += __builtin_amdgcn_exp2f((v[i].x - now) * a.scale_log2) * v[i].y;
         m = now;
     }
     // (a row without a key, all of its blocks absent: no weight)
-    a.lse[pair * a.row_cap + row] = l > 0.f || l != l ? m + __builtin_amdgcn_logf(l) : INFINITY;
+    const RowScale rs(m, a.scale_log2);
+    a.whole[pair * a.row_cap + row] = f32x4{rs.m, rs.scale, l > 0.f || l != l ? __builtin_amdgcn_exp2f(-rs.rounding) / l : 0.f, 0.f};
 }
 
 template <int D, int KB>
@@ -353,7 +381,7 @@ hipError_t launch_observe_t(ObserveArgs a, int32_t whole_rows, hipStream_t strea
     for (a.row0 = 0; a.row0 < whole_rows; a.row0 += a.row_cap) {
         hipLaunchKernelGGL((observe_kernel<D, KB, false>), grid, dim3(kObThreads), 0, stream, a);
         if (hipError_t e = hipGetLastError()) return e;
-        hipLaunchKernelGGL(observe_lse_kernel, dim3((unsigned)((a.row_cap + kObThreads - 1) / kObThreads), (unsigned)a.num_kv_heads, (unsigned)a.num_sessions),
+        hipLaunchKernelGGL(observe_sum_kernel, dim3((unsigned)((a.row_cap + kObThreads - 1) / kObThreads), (unsigned)a.num_kv_heads, (unsigned)a.num_sessions),
                            dim3(kObThreads), 0, stream, a, kChunkTokens);
         if (hipError_t e = hipGetLastError()) return e;
         hipLaunchKernelGGL((observe_kernel<D, KB, true>), grid, dim3(kObThreads), 0, stream, a);
@@ -378,8 +406,8 @@ ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_
     o.blocks = 4;
     while (o.blocks > 1 && pairs * ((max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks)) < 2 * cus) o.blocks /= 2;
     o.chunks = (max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks);
-    o.lse_at = align256((size_t)pairs * (size_t)o.chunks * (size_t)o.row_cap * sizeof(float2));
-    o.total = o.lse_at + align256((size_t)pairs * (size_t)o.row_cap * sizeof(float));
+    o.whole_at = align256((size_t)pairs * (size_t)o.chunks * (size_t)o.row_cap * sizeof(float2));
+    o.total = o.whole_at + align256((size_t)pairs * (size_t)o.row_cap * sizeof(f32x4));
     return o;
 }
 
@@ -405,7 +433,7 @@ hipError_t launch_observe(const PoolGeom &p, int layer, int32_t num_sessions, in
     a.row_cap = plan.row_cap;
     a.chunks = plan.chunks;
     a.part = reinterpret_cast<float2 *>(ws);
-    a.lse = reinterpret_cast<float *>(ws + plan.lse_at);
+    a.whole = reinterpret_cast<f32x4 *>(ws + plan.whole_at);
     a.weights = c.weights + entries;
     a.positions = c.positions + entries;
     a.begin = c.first_positions;
