@@ -40,7 +40,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kObThreads = 256;
 constexpr int kObWaves = kObThreads / kWave;
 constexpr int kObRows = 1024;                // rows of a KV head at a time (the workspace); more take another round
-constexpr float kNoMax = -1.0e30f;
+constexpr float kNoMax = -0x1.fffffep127f;   // maximum of no key: no finite product is below it
 constexpr int kRawBuffer = 0x00020000;
 
 struct ObserveArgs {

@@ -76,7 +76,7 @@ static_assert(kShMost == 1 << kRank && kShMost == kMaxCacheSessions, "ranks fit"
 constexpr int kCostFew = 1, kCostTile = 4, kCostPart = 8;
 // The least share.
 constexpr int kLeastTile = kCostPart + 4 * kCostTile, kLeastOwn = kCostPart + 2 * kShWaves;
-constexpr float kNoMax = -1.0e30f;           // running maximum of no key
+constexpr float kNoMax = -0x1.fffffep127f;   // running maximum of no key: no finite score is below it
 // The running maximum moves only when a score passes it by this much (log2), so that
 // probabilities reach 2^8 and most pairs of blocks need no rescaling.
 constexpr float kMaxSlack = 8.0f;
