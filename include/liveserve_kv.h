@@ -579,11 +579,12 @@ ls_status kv_weights_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
  * kv_tables_update, which then takes next_lens.  All sessions are served or none: a
  * length outside its table is flagged LS_DEVERR_LENGTH, no room in the ring or
  * counters that cannot be LS_DEVERR_FREE_LIST; then next_lens = seq_lens, next_counts =
- * free_counts and nothing moves.  Tokens of a block whose id is outside the pool rank
- * lowest and are not moved (LS_DEVERR_BLOCK_ID).  Apart from shared blocks below
- * first_lens, no block is in two sessions' tables.  Errors: LS_EINVAL (also arrays that
- * overlap and are not said to be the same), LS_EUNSUPPORTED (more than 16384 blocks per
- * session, 2^20 sessions, 65535 layers or KV heads), LS_EHIP.
+ * free_counts and nothing moves.  Nothing is read or written for a block whose id is outside
+ * the pool (LS_DEVERR_BLOCK_ID): its slots below m count as tokens that stay, those behind
+ * are the first to go, and an id that goes back to the ring does so as it is.  Apart from
+ * shared blocks below first_lens, no block is in two sessions' tables.  Errors: LS_EINVAL
+ * (also arrays that overlap and are not said to be the same), LS_EUNSUPPORTED (more than
+ * 16384 blocks per session, 2^20 sessions, 65535 layers or KV heads), LS_EHIP.
  */
 ls_status kv_evict(ls_kv_pool *pool, int32_t layer_begin, int32_t layer_count, int32_t num_sessions,
                    const int32_t *seq_lens, const int32_t *block_tables, int32_t max_blocks_per_session, int32_t budget,

@@ -168,9 +168,9 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan_kernel(EvictArgs a) {
     plan<kPlanThreads>(a, sm_wave, sm_at, sm_col);
 }
 
-// Order of two weights as that of two unsigned words: NaN below all, -0 as 0.
+// Order of two weights as that of two unsigned words: NaN (1) below all, -0 as 0.
 __device__ __forceinline__ uint32_t rank_key(float w) {
-    if (w != w) return 0u;
+    if (w != w) return 1u;
     const uint32_t u = __float_as_uint(w + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -259,12 +259,17 @@ __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     }
     const int first = a.first ? min(max(a.first[s], 0), m) : 0;
     const int64_t late = (int64_t)a.next_pos[s] - a.recent;
-    // Keys of slots t .. t + 3: the largest for first and latest tokens, 0 for absent ones.
+    // Keys of slots t .. t + 3: the largest for first and latest tokens.  Absent ones cannot move or be moved
+    // to: below m the largest (at most t slots come before slot t, so all of these stay), behind it 0 (no more
+    // than L - m, so all of these go).
     auto keys_of = [&](int t, bool &missing) -> u32x4 {
         const int64_t e = block_entry(t / kBlock);
         u32x4 k = {0u, 0u, 0u, 0u};
-        if (e < 0) missing = true;
-        else {
+        if (e < 0) {
+            missing = true;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = t + i < m ? 0xFFFFFFFFu : 0u;
+        } else {
             const Quad x = load(e + t % kBlock);
 #pragma unroll
             for (int i = 0; i < 4; ++i) k[i] = x.p[i] >= late ? 0xFFFFFFFFu : rank_key(x.w[i]);
