@@ -535,6 +535,13 @@ def _group_args(group_starts, group_members, prefix_blocks, dev):
     return n, group_members.shape[0]
 
 
+def _given(**tensors):
+    """Refuse None where a call needs a tensor (raises ValueError)."""
+    for name, t in tensors.items():
+        if t is None:
+            raise ValueError("%s must not be None" % name)
+
+
 def _workspace(t: torch.Tensor, dev):
     if not (t.get_device() == dev and t.is_contiguous()):
         _dev(t, "workspace", dev=dev)
@@ -556,6 +563,7 @@ def paged_attn_decode_shared(pool: KVPool, layer: int, q: torch.Tensor, block_ta
     """paged_attn_decode in which the sessions group_members[group_starts[g]:group_starts[g + 1]] (int32)
     have the first prefix_blocks[g] blocks of their tables in common, read once for the group;
     workspace of decode_shared_workspace_bytes.  A length of 0 gives a row of zeros."""
+    _given(q=q, block_tables=block_tables, context_lens=context_lens, out=out, workspace=workspace)
     if q.dim() != 3:
         raise ValueError("q must be [S][Hq][D]")
     s, hq = q.shape[0], q.shape[1]
@@ -588,6 +596,7 @@ def paged_attn_decode_weights(pool: KVPool, layer: int, q: torch.Tensor, block_t
     KV head, to weights fp32 [layers][blocks][Hkv][16]; of keys t >= reused_lens[s] the weight is set,
     and positions (int32, the same shape) to first_positions[s] + t - reused_lens[s].  Keys below
     first_lens[s] get no weight.  workspace of decode_weights_workspace_bytes."""
+    _given(q=q, block_tables=block_tables, context_lens=context_lens, out=out, weights=weights, workspace=workspace)
     if q.dim() != 3:
         raise ValueError("q must be [S][Hq][D]")
     s, hq = q.shape[0], q.shape[1]
@@ -621,6 +630,8 @@ def kv_weights_prefill(pool: KVPool, layer: int, q: torch.Tensor, cu_new_lens: t
                        stream=None) -> torch.Tensor:
     """Adds what the last `rows` tokens of each turn (q [T][Hq][D], K already in the pool) give to the
     session's keys to weights, as paged_attn_decode_weights; workspace of weights_prefill_workspace_bytes."""
+    _given(q=q, cu_new_lens=cu_new_lens, reused_lens=reused_lens, block_tables=block_tables, weights=weights,
+           positions=positions, workspace=workspace)
     if q.dim() != 3:
         raise ValueError("q must be [T][Hq][D]")
     total, hq, dev = q.shape[0], q.shape[1], pool.device
@@ -656,6 +667,8 @@ def kv_evict(pool: KVPool, seq_lens: torch.Tensor, block_tables: torch.Tensor, b
     first first_lens[s] slots, positions >= next_positions[s] - recent, then the largest weights stay.
     Writes next_lens int32 [S]; weights_next and positions_next (None: in place) get the entries; free_ring
     int32 [R] with free_counts -> next_counts int64 [2] takes the blocks back."""
+    _given(seq_lens=seq_lens, block_tables=block_tables, next_positions=next_positions, weights=weights, positions=positions,
+           next_lens=next_lens)
     s = seq_lens.shape[0] if seq_lens.dim() == 1 else -1
     dev = pool.device
     for t, name, n in ((seq_lens, "seq_lens", s), (next_positions, "next_positions", s), (next_lens, "next_lens", s),
