@@ -466,6 +466,11 @@ ls_status kv_append(ls_kv_pool *pool, int32_t layer, int32_t total_tokens, const
  * Results depend on the lengths and on the stream's CUs, by the order of fp32 sums,
  * and not on how often the call is made.  Other arguments as paged_attn_decode.
  *
+ * paged_attn_decode over the same tables gives the same rows, to rounding, and is faster
+ * where little is shared: this call pays where members x shared tokens x num_kv_heads x
+ * head_dim, summed over the groups, pass some 10^8 (64 members behind 3000 tokens with 4 KV
+ * heads of 128).
+ *
  * Supported: num_q_heads / num_kv_heads in {1, 2, 4, 8}; at most 2048 sessions, 2048
  * groups, 16384 blocks per session and 4096 KV heads, and fewer than 2^30 sessions x blocks
  * per session x KV heads (LS_EUNSUPPORTED).  Other errors: LS_EINVAL (also
@@ -500,7 +505,7 @@ ls_status paged_attn_decode_shared(ls_kv_pool *pool, int32_t layer, int32_t num_
  *                    new token (NULL: its place in the cache, reused_lens[s])
  *   first_lens       device int32 [num_sessions] or NULL: keys t < first_lens[s] are never
  *                    evicted, and their entries are not used (kv_evict copies them).  Blocks that are in
- *                    several sessions' tables lie below it (or below a group's prefix)
+ *                    several sessions' tables lie below it (or, in the decode, below a group's prefix)
  *
  * paged_attn_decode_weights — paged_attn_decode_shared that also adds the weights up.
  * Keys of a group's shared prefix get none.  reused_lens NULL (and first_positions and
@@ -536,7 +541,8 @@ ls_status paged_attn_decode_weights(ls_kv_pool *pool, int32_t layer, int32_t num
  *   rows           >= 1
  *   workspace      device, >= ls_weights_prefill_workspace_bytes(...) bytes, 16-byte
  *                  aligned; its size depends on max_new_len, rows and
- *                  max_blocks_per_session
+ *                  max_blocks_per_session, as does how the work is split: a table much wider
+ *                  than its sessions makes the call slower
  *
  * Ids outside the pool are flagged (LS_DEVERR_BLOCK_ID) and their keys left out.
  * Limits as paged_attn_decode_shared.  Other errors: LS_EINVAL, LS_ENOMEM, LS_EHIP.
@@ -575,7 +581,8 @@ ls_status kv_weights_prefill(ls_kv_pool *pool, int32_t layer, int32_t num_sessio
  *                  Their table entries stay; calls of other layers for the same lengths are
  *                  made without a ring.  NULL, 0, NULL, NULL: none go back
  *
- * Called for all layers at once, after the step's attention and before the next
+ * A table of up to 160 columns takes a kernel that is faster for its sessions than that of
+ * wider ones.  Called for all layers at once, after the step's attention and before the next
  * kv_tables_update, which then takes next_lens.  All sessions are served or none: a
  * length outside its table is flagged LS_DEVERR_LENGTH, no room in the ring or
  * counters that cannot be LS_DEVERR_FREE_LIST; then next_lens = seq_lens, next_counts =

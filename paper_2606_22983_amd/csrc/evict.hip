@@ -20,7 +20,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // Slots whose ranking keys are kept in LDS (a longer session's are computed again for
-// each pass): caches around a budget of a few thousand tokens, and long prompts.
+// each pass): tables of up to 160 columns, and wider ones.
 constexpr int kEvKeysShort = 2560, kEvKeysLong = 16384;
 constexpr int kBins = 2048;                  // of a ranking key's 11 bits
 constexpr int kEvMoves = kBins / 2;          // moves at a time (their slots, where the bins were)
@@ -197,9 +197,10 @@ struct Quad {
 //
 // Bound by the moves' sectors: a token's V values are 2 bytes in each of D rows of 32 bytes.
 // Measured: 64 sessions, about half of them cut to 2048 tokens, 8 layers of 4 heads of
-// 128, 124-130 us a call, 160 MB written (1.5 TB/s; 95 MB needed in all); 8 prompts of up to
+// 128, 125 us a call, 160 MB written (1.5 TB/s; 95 MB needed in all); 8 prompts of up to
 // 16384 cut to 1024, 4 layers, 144 us, 103 MB written and 323 read.  43 and 42 us
-// without the moves.  V tiles of blocks with holes, read and written whole: 152 us for 127.
+// without the moves.  Entries and counters in place: 121 and 189 us.  V tiles of blocks with holes,
+// read and written whole: 152 us for 127.
 template <int D, int kThreads, int kKeys>
 __global__ __launch_bounds__(kThreads) void evict_kernel(EvictArgs a) {
     constexpr int kWaves = kThreads / kWave;
@@ -527,6 +528,9 @@ hipError_t launch_evict(const PoolGeom &p, int32_t layer_begin, int32_t layer_co
         if (hipError_t e = hipGetLastError()) return e;
         if (!whole) return hipSuccess;
     }
+    // By the table's width, as the lengths are on the device: in workgroups of four waves if every
+    // session's keys fit (64 sessions cut to 2048 as above 125 us, cut to 1024 109), else of sixteen (the same
+    // sessions in tables of 1024 columns 153 and 132; cut to 4096 194).
     const bool narrow = (int64_t)c.max_blocks * kBlock <= kEvKeysShort;
 #define LS_EVICT(D, THREADS, KEYS) hipLaunchKernelGGL((evict_kernel<D, THREADS, KEYS>), grid, dim3(THREADS), 0, stream, a)
     if (p.head_dim == 128) {

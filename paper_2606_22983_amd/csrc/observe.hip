@@ -20,10 +20,11 @@
 // come from L2.  A lane's scores belong to one row (lane % 16): sums over keys end
 // with two lane exchanges, sums over rows stay in the lane until the last row.
 // Bound by the matrix and exponential units when rows are many, by latency when few.
-// Measured: 32 turns, 64 observed rows each over up to 8192 tokens, 32 / 4 heads of 128, 270
-// us a call (rows' launch 153, keys' 140 at best; 761 TFLOP/s of products); one turn, 32 rows
-// over 2090 tokens, 21 us (8.4, 4.4 and 7.0).  Wider waves (8 blocks, 301 us), a persistent
-// grid (368) and four waves a SIMD (289) were slower than the 264 they were compared with.
+// Measured: 32 turns, 64 observed rows each over up to 8192 tokens, 32 / 4 heads of 128, 272
+// to 285 us a call, as cards differ (rows' launch 158, keys' 137 at best; 720-755 TFLOP/s of
+// products); one turn, 32 rows over 2090 tokens, 20 us (8.5, 4.5 and 6.5).  Wider waves (8 blocks,
+// 301 us), a persistent grid (368) and four waves a SIMD (289) were slower than the 264 they were
+// compared with.
 #include <algorithm>
 #include <type_traits>
 
@@ -402,7 +403,9 @@ ObservePlan plan_observe(const PoolGeom &p, int32_t num_sessions, int32_t num_q_
     // (a turn fits its table)
     o.whole_rows = (int32_t)(std::min({(int64_t)rows, (int64_t)max_new_len, (int64_t)max_blocks * kBlock}) * G);
     o.row_cap = std::min(o.whole_rows, kObRows);
-    // Blocks per wave: as many as leave every CU two workgroups.
+    // Blocks per wave: as many as leave every CU two workgroups, if the sessions fill their tables (their
+    // lengths are on the device).  In tables of 1024 columns the one turn above takes 26 us for 20, eight first
+    // turns of up to 700 tokens (all rows, 8 heads of 64) 110 for 29, the 32 turns 340 for 281 on one card.
     o.blocks = 4;
     while (o.blocks > 1 && pairs * ((max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks)) < 2 * cus) o.blocks /= 2;
     o.chunks = (max_blocks + kObWaves * o.blocks - 1) / (kObWaves * o.blocks);

@@ -12,7 +12,7 @@
 //
 // Work: segments = (group, KV head, tile of up to 16 or 128 rows) over the group's blocks,
 // then (session, KV head) over its own blocks.  A block of a segment costs some units
-// (kCost*).  Of the workgroups, of four waves, two per CU, as many as the units say are for
+// (kCost*).  Of the workgroups, of four waves, two for each CU, as many as the units say are for
 // prefixes and the others for own blocks, on every XCD; each takes an equal contiguous
 // share of the one or the other, so it works on a few parts of segments.  A part with up to 16
 // rows (own keys, small groups): the waves take its pairs of blocks in turn, straight
@@ -43,6 +43,10 @@
 // 256 sessions in 8 groups, 16 / 2 heads, 57 us, 219 MB (4.7 TB/s in the first kernel); 3
 // sessions behind 640 shared tokens 19 us (13.6 and 3.0 on the GPU).  With weights, 64
 // sessions of up to 16384 tokens 173 us, 783 MB needed; the scores' stores take 31 of them.
+// The decode of each session's own table, one launch with a prefix that stays in the caches,
+// takes 72 (lengths on the host) or 78 us, 57 or 64, and 8 in these three: sharing pays from
+// some 10^8 members x shared tokens x KV heads x D on (4 heads of 128: 128 members behind 1024
+// tokens 33 us for 31, behind 4096 51 for 74; 32 behind 4096 33 for 31, behind 16384 55 for 84).
 #include <algorithm>
 #include <type_traits>
 
@@ -56,13 +60,13 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kShThreads = 256;
 constexpr int kShWaves = kShThreads / kWave;
 constexpr int kShPerCu = 2;                  // workgroups
 // Sessions, members and groups that a kernel's LDS has room for: with the few, two
-// workgroups fit a CU.
+// workgroups fit a CU, with the most one (the other half of the grid follows): 512 sessions of
+// 50 to 500 own tokens, half of them in 8 groups, 16 / 2 heads of 128, take 52 us, 600 78.
 constexpr int kShFew = 512, kShMost = 2048;
 // Rows of a prefix segment: 128 (two tiles of 16 per wave), but 16 in groups of up to 64,
 // where four parts of 16 cost no more than one of 128 and a wave waits for less.
